@@ -376,6 +376,107 @@ int faedkv_decode_attn_static(int n_dft, int n_kv_heads, int n_q_heads, int kv_d
                               const float *coefV, const int32_t *t_len, int batch, float scale,
                               void *out, void *stream, char *err_msg, size_t err_len);
 
+/* ---- the paged 8-bit cache -----------------------------------------------------------------------------
+ * The time-domain side of a cache: where tokens live before faedkv_compress_prefill() / faedkv_prefill_windowed()
+ * takes them to the frequency domain, or instead of it.  A page holds page_size tokens of every kv head:
+ *   k_pages, v_pages  e4m3 codes [n_pages][n_kv_heads][page_size][head_dim]
+ *   k_scale, v_scale  float32 [n_pages][n_kv_heads];  value = code * scale
+ *   table             int32 [batch][max_pages]: the pages of each sequence in order; entries behind its last page are
+ *                     not read
+ *   kv_len            int32 [batch], cached tokens of each sequence
+ * The pages, scales, tables and lengths are the caller's; the handle holds the configuration and one status word.
+ * New tokens of a step lie one sequence after the other in token tensors [n_tokens][heads][head_dim]; sequence b owns
+ * rows q_start[b] .. q_start[b + 1) - 1 (int32 [batch + 1]).  Rows behind q_start[batch] are padding: their slot is -1,
+ * and output rows there are left as they were.
+ *
+ * Calls run on the handle's device, whatever the current one is, enqueue on `stream` (a stream of that device) and
+ * neither allocate nor synchronise, but for create, destroy and device_status.  Code and scale tensors, q, out and the workspace are
+ * 16-byte aligned, int32 tensors 4-byte aligned.  No call keeps anything between calls, so calls on one handle may
+ * overlap on the GPU as long as they do not write the same tensors; as with a context, a handle must not be used from
+ * two host threads at once.  An index that comes from device memory and lies outside what it indexes (a table entry, a
+ * slot, a length) is not followed: the kernel skips that token and leaves a code in the status word. */
+typedef struct faedkv_pages faedkv_pages; /* opaque */
+
+typedef struct {
+    int n_kv_heads; /* 1 .. 4096                                                                   */
+    int n_q_heads;  /* 1 to 8 query heads per kv head, any value                                   */
+    int head_dim;   /* must be 128                                                                 */
+    int page_size;  /* tokens of a page: 16, 32, 64 or 128                                         */
+    int n_pages;    /* pages of the pool; n_pages * n_kv_heads * page_size < 2^31                  */
+    int max_pages;  /* width of the block tables; max_pages * page_size <= 2^30                    */
+    int max_batch;  /* 1 .. 65535                                                                  */
+    int kv_dtype;   /* faedkv_dtype of the new tokens, of q and out, and of rows read back         */
+} faedkv_pages_config;
+
+/* Create a handle on the CURRENT device.  host: cfg, out. */
+int faedkv_pages_create(const faedkv_pages_config *cfg, faedkv_pages **out);
+
+/* Free the handle.  NULL is allowed. */
+void faedkv_pages_destroy(faedkv_pages *pg);
+
+/* Text of the last error on this handle ("" if none). */
+const char *faedkv_pages_last_error(const faedkv_pages *pg);
+
+/* Bytes of ONE code tensor (K or V). */
+size_t faedkv_pages_bytes(const faedkv_pages *pg);
+
+/* One step's block tables and slots, from the lengths of its requests.  n_new[b] > 0: that many tokens arrive for request
+ * b; 0: none; < 0: the request has finished and gives its pages back.  Free pages are a stack, free_pages[0 .. *n_free)
+ * with the top at the end (int32 [n_pages], int32 [1]).
+ *   finished requests   their ceil(t_len / page_size) pages are pushed in request order; kv_len[b] = 0;
+ *   arriving tokens     served in request order, each new page popped from the top; kv_len[b] = t_len[b] + n_new[b], and
+ *                       the new entries of table row b are written.  A request that does not fit gets nothing: kv_len[b]
+ *                       = t_len[b] and the slots of its tokens are -1.  It does not fit when its tokens exceed the table
+ *                       row or n_tokens, or when the stack does not hold its pages and those of the requests before
+ *                       it; in the last case every later request that needs a page waits too.
+ * q_start[b] counts the tokens before request b (finished ones count none), slots[i] = page * page_size + row of token
+ * i < n_tokens, -1 where it has none.  *n_free_out is the new height of the stack.  ws: int32 [batch + 1], overwritten.
+ * kv_len may be t_len itself, n_free_out may be n_free. */
+int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, int32_t *table,
+                        int32_t *free_pages, const int32_t *n_free, int n_tokens, int32_t *q_start, int32_t *kv_len,
+                        int32_t *slots, int32_t *n_free_out, int32_t *ws, void *stream);
+
+/* Quantise new tokens into their slots.  k_new, v_new: [n_tokens][n_kv_heads][head_dim] (kv_dtype), token rows ld_new
+ * elements apart (ld_new >= n_kv_heads * head_dim, a multiple of 16 bytes: slices of a fused projection's output are
+ * taken as they are).  Each (page, head) keeps the smallest power of two s with every finite magnitude <= 448 s (at
+ * least 2^-126); when a later token needs a larger s, the page's older rows are rounded again.  Codes are rounded to
+ * nearest even (relative error at most 2^-4, absolute at most 2^-10 s below 2^-6 s); infinities become +-448 s, NaN stays
+ * NaN, and neither sets a scale.  A token at row 0 of a page starts the page afresh.  The tokens of one page must be consecutive in
+ * the call with slots ascending by one, and a slot may occur once (what faedkv_pages_tables writes is so); slots < 0 are
+ * skipped.  Pages that no slot names, and rows behind a page's last token, are left as they were. */
+int faedkv_pages_store(faedkv_pages *pg, const void *k_new, const void *v_new, long long ld_new, const int32_t *slots,
+                       int n_tokens, void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *stream);
+
+/* Workspace bytes of faedkv_pages_attn() at this batch and token count (0 for arguments that it would refuse). */
+size_t faedkv_pages_attn_bytes(const faedkv_pages *pg, int batch, int n_tokens);
+
+/* Attention of the newest tokens over the cache:
+ *   out[i] = softmax_n( scale * q[i] . K[n] ) V[n],   n < kv_len[b] - n_new + (i - q_start[b]) + 1
+ * for the n_new = q_start[b + 1] - q_start[b] newest tokens of every sequence b: causal among themselves, and each sees
+ * itself (store first).  q_start = NULL: one token per sequence, n_tokens = batch (a decode step).  q: token rows ld_q
+ * elements apart (as ld_new), [n_q_heads][head_dim] each; out: contiguous [n_tokens][n_q_heads][head_dim]; both kv_dtype.
+ * scale = 0 means 1/sqrt(head_dim).  A token that sees nothing (kv_len[b] = 0) gets a row of zeros.  Scales need not be
+ * powers of two.  ws: faedkv_pages_attn_bytes(), overwritten; calls that overlap need one each. */
+int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
+                      const int32_t *kv_len, const int32_t *table, const void *k_pages, const void *v_pages,
+                      const float *k_scale, const float *v_scale, float scale, void *out, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* The cached tokens as rows: K_out, V_out [batch][n_kv_heads][L][head_dim] (kv_dtype), zero from row kv_len[b] on, in the
+ * layout that faedkv_compress_prefill() and faedkv_prefill_windowed() take.  A sequence longer than L is cut.  Either of
+ * (k_pages, k_scale, K_out) or (v_pages, v_scale, V_out) may be all NULL. */
+int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *table, int batch, int L, const void *k_pages,
+                      const void *v_pages, const float *k_scale, const float *v_scale, void *K_out, void *V_out,
+                      void *stream);
+
+/* Status word (host read; synchronises `stream`): 0, or the code of the first index that was not followed (0x101 a page,
+ * 0x102 a slot, 0x103 a length, 0x104 the free stack, 0x105 a start) or of a bounded wait that gave up (0x4x). */
+int faedkv_pages_device_status(faedkv_pages *pg, void *stream);
+int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream);
+
+/* Kernels enqueued through this handle so far. */
+unsigned long long faedkv_pages_launch_count(const faedkv_pages *pg);
+
 /* Number of kernels this context has enqueued since it was created (host
  * counter; the benchmark reports its difference over the timed region). */
 unsigned long long faedkv_launch_count(const faedkv_ctx *ctx);

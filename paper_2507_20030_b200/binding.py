@@ -34,6 +34,9 @@ EXPORTS = [
     "faedkv_reconstruct_windowed",
     "faedkv_device_status", "faedkv_launch_count", "faedkv_decode_attn_static",
     "faedkv_reset_device_status", "faedkv_test_hooks", "faedkv_debug_build", "faedkv_debug_word",
+    "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables",
+    "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
+    "faedkv_pages_reset_device_status", "faedkv_pages_launch_count",
 ]
 
 STATIC_SCRATCH_BYTES = 8 << 20
@@ -49,6 +52,11 @@ class Config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in (
         "n_layers", "n_kv_heads", "n_q_heads", "head_dim", "n_dft", "max_batch", "kv_dtype",
         "prefill_mode", "twiddle_terms", "decode_mode", "n_sink", "n_recent", "n_defer", "recon_engine")]
+
+
+class PagesConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in (
+        "n_kv_heads", "n_q_heads", "head_dim", "page_size", "n_pages", "max_pages", "max_batch", "kv_dtype")]
 
 
 _lib = None
@@ -127,6 +135,32 @@ def load() -> ctypes.CDLL:
     lib.faedkv_debug_build.restype = _int
     lib.faedkv_debug_word.argtypes = [_vp, _vp]
     lib.faedkv_debug_word.restype = ctypes.c_longlong
+    _ll = ctypes.c_longlong
+    lib.faedkv_pages_create.argtypes = [ctypes.POINTER(PagesConfig), ctypes.POINTER(_vp)]
+    lib.faedkv_pages_create.restype = _int
+    lib.faedkv_pages_destroy.argtypes = [_vp]
+    lib.faedkv_pages_destroy.restype = None
+    lib.faedkv_pages_last_error.argtypes = [_vp]
+    lib.faedkv_pages_last_error.restype = ctypes.c_char_p
+    lib.faedkv_pages_bytes.argtypes = [_vp]
+    lib.faedkv_pages_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_tables.argtypes = [_vp, _vp, _vp, _int, _vp, _vp, _vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.faedkv_pages_tables.restype = _int
+    lib.faedkv_pages_store.argtypes = [_vp, _vp, _vp, _ll, _vp, _int, _vp, _vp, _vp, _vp, _vp]
+    lib.faedkv_pages_store.restype = _int
+    lib.faedkv_pages_attn_bytes.argtypes = [_vp, _int, _int]
+    lib.faedkv_pages_attn_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_attn.argtypes = [_vp, _vp, _ll, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
+                                      ctypes.c_size_t, _vp]
+    lib.faedkv_pages_attn.restype = _int
+    lib.faedkv_pages_load.argtypes = [_vp, _vp, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.faedkv_pages_load.restype = _int
+    lib.faedkv_pages_device_status.argtypes = [_vp, _vp]
+    lib.faedkv_pages_device_status.restype = _int
+    lib.faedkv_pages_reset_device_status.argtypes = [_vp, _vp]
+    lib.faedkv_pages_reset_device_status.restype = _int
+    lib.faedkv_pages_launch_count.argtypes = [_vp]
+    lib.faedkv_pages_launch_count.restype = ctypes.c_ulonglong
     _lib = lib
     return lib
 
@@ -381,3 +415,164 @@ class Context:
     def test_hooks(self, wait_limit_ns: int = 0, withhold_step: int = 0):
         """faedkv_test_hooks: wait limit of the tensor-core prefill's bounded waits and the withheld-signal test."""
         self._check(self._lib.faedkv_test_hooks(self._h, int(wait_limit_ns), int(withhold_step)))
+
+
+@dataclass
+class Pages:
+    """The paged 8-bit cache (faedkv_pages): methods carry the names of the C calls without the prefix.
+
+    Shapes are checked here, since a wrong one would read or write past a tensor: a ValueError names the tensor.  Workspaces
+    that a call needs are taken from PyTorch's allocator on the call's stream unless the caller passes one."""
+    n_kv_heads: int
+    n_q_heads: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+    max_batch: int
+    kv_dtype: int = BF16
+    head_dim: int = 128
+
+    def __post_init__(self):
+        self._lib = load()
+        cfg = PagesConfig(self.n_kv_heads, self.n_q_heads, self.head_dim, self.page_size, self.n_pages, self.max_pages,
+                          self.max_batch, self.kv_dtype)
+        h = _vp()
+        rc = self._lib.faedkv_pages_create(ctypes.byref(cfg), ctypes.byref(h))
+        if rc != 0:
+            raise FaedkvError(rc, "faedkv_pages_create failed")
+        self._h = h
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    # -- lifetime
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.faedkv_pages_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc: int):
+        if rc != 0:
+            raise FaedkvError(rc, self._lib.faedkv_pages_last_error(self._h).decode())
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.kv_dtype == BF16 else torch.float32
+
+    def _need(self, name, t, dtype, shape=None, size=None):
+        """A contiguous tensor of this dtype on the handle's device, of this shape or at least this many elements."""
+        if t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {self.device}, got {t.dtype} on {t.device}")
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+        if size is not None and t.numel() < size:
+            raise ValueError(f"{name} must hold at least {size} elements, got {t.numel()}")
+        return t.data_ptr()
+
+    def _rows(self, name, t, heads):
+        """Token rows [n_tokens, heads, head_dim], contiguous from the head on: pointer, tokens, row stride in elements."""
+        if t.dtype != self.torch_dtype or t.device != self.device:
+            raise ValueError(f"{name} must be {self.torch_dtype} on {self.device}, got {t.dtype} on {t.device}")
+        if t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.head_dim):
+            raise ValueError(f"{name} must have shape [n_tokens, {heads}, {self.head_dim}], got {tuple(t.shape)}")
+        n = t.shape[0]
+        row = heads * self.head_dim
+        if n and ((heads > 1 and t.stride(1) != self.head_dim) or t.stride(2) != 1 or (n > 1 and t.stride(0) < row)):
+            raise ValueError(f"{name}: heads and channels must be contiguous within a token row, strides {t.stride()}")
+        return t.data_ptr(), n, (t.stride(0) if n > 1 else row)
+
+    def _cache(self, k_pages, v_pages, k_scale, v_scale):
+        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        return (self._need("k_pages", k_pages, torch.float8_e4m3fn, shape), self._need("v_pages", v_pages, torch.float8_e4m3fn, shape),
+                self._need("k_scale", k_scale, torch.float32, shape[:2]), self._need("v_scale", v_scale, torch.float32, shape[:2]))
+
+    def _workspace(self, ws, nbytes, stream):
+        if ws is not None:
+            if not ws.is_contiguous() or ws.device != self.device:
+                raise ValueError(f"ws must be a contiguous tensor on {self.device}")
+            return ws, ws.numel() * ws.element_size()
+        if stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+        s = torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
+        with torch.cuda.stream(s):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+
+    def _on(self, stream):
+        """The stream's handle; by default the current stream of the handle's device."""
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
+    def alloc(self):
+        """k_pages, v_pages (torch.float8_e4m3fn [n_pages, n_kv_heads, page_size, head_dim]), k_scale, v_scale (float32
+        [n_pages, n_kv_heads]), all uninitialised."""
+        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        codes = [torch.empty(shape, dtype=torch.float8_e4m3fn, device=self.device) for _ in range(2)]
+        scales = [torch.empty(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2)]
+        return (*codes, *scales)
+
+    # -- the calls
+    def tables(self, t_len, n_new, table, free_pages, n_free, q_start, kv_len, slots, n_free_out, ws=None, stream=None):
+        batch, i32 = t_len.shape[0], torch.int32
+        need = self._need
+        args = (need("t_len", t_len, i32, (batch,)), need("n_new", n_new, i32, (batch,)), batch,
+                need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, (self.n_pages,)),
+                need("n_free", n_free, i32, size=1), slots.numel(), need("q_start", q_start, i32, size=batch + 1),
+                need("kv_len", kv_len, i32, (batch,)), need("slots", slots, i32), need("n_free_out", n_free_out, i32, size=1))
+        w, nbytes = self._workspace(ws, 4 * (batch + 1), stream)
+        if nbytes < 4 * (batch + 1):
+            raise ValueError(f"ws must hold {4 * (batch + 1)} bytes")
+        self._check(self._lib.faedkv_pages_tables(self._h, *args, w.data_ptr(), self._on(stream)))
+
+    def store(self, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None):
+        k, n, ld = self._rows("k_new", k_new, self.n_kv_heads)
+        v, nv, ldv = self._rows("v_new", v_new, self.n_kv_heads)
+        if nv != n or ldv != ld:
+            raise ValueError(f"k_new and v_new must have the same tokens and row stride, got {n}, {nv} tokens, strides {ld}, {ldv}")
+        s = self._need("slots", slots, torch.int32, (n,))
+        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
+        self._check(self._lib.faedkv_pages_store(self._h, k, v, ld, s, n, kp, vp, ks, vs, self._on(stream)))
+
+    def attn_bytes(self, batch: int, n_tokens: int) -> int:
+        return int(self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens))
+
+    def attn(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, out, q_start=None, scale: float = 0.0, ws=None, stream=None):
+        batch = kv_len.shape[0]
+        qp, n, ld = self._rows("q", q, self.n_q_heads)
+        o = self._need("out", out, self.torch_dtype, (n, self.n_q_heads, self.head_dim))
+        st = None if q_start is None else self._need("q_start", q_start, torch.int32, size=batch + 1)
+        kv = self._need("kv_len", kv_len, torch.int32, (batch,))
+        tb = self._need("table", table, torch.int32, (batch, self.max_pages))
+        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
+        w, nbytes = self._workspace(ws, self.attn_bytes(batch, n), stream)
+        self._check(self._lib.faedkv_pages_attn(self._h, qp, ld, st, n, batch, kv, tb, kp, vp, ks, vs, float(scale), o, w.data_ptr(),
+                                                nbytes, self._on(stream)))
+
+    def load(self, kv_len, table, k_pages, v_pages, k_scale, v_scale, L: int, K_out=None, V_out=None, stream=None):
+        """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end."""
+        batch = kv_len.shape[0]
+        shape = (batch, self.n_kv_heads, L, self.head_dim)
+        if K_out is None:
+            K_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+        if V_out is None:
+            V_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+        kv = self._need("kv_len", kv_len, torch.int32, (batch,))
+        tb = self._need("table", table, torch.int32, (batch, self.max_pages))
+        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
+        self._check(self._lib.faedkv_pages_load(
+            self._h, kv, tb, batch, L, kp, vp, ks, vs, self._need("K_out", K_out, self.torch_dtype, shape),
+            self._need("V_out", V_out, self.torch_dtype, shape), self._on(stream)))
+        return K_out, V_out
+
+    def launch_count(self) -> int:
+        return int(self._lib.faedkv_pages_launch_count(self._h))
+
+    def device_status(self, stream=None) -> int:
+        return int(self._lib.faedkv_pages_device_status(self._h, self._on(stream)))
+
+    def reset_device_status(self, stream=None):
+        self._check(self._lib.faedkv_pages_reset_device_status(self._h, self._on(stream)))

@@ -1,0 +1,422 @@
+// The paged 8-bit cache: block tables and slots from request lengths, quantised writes, rows read back.
+//
+// A page holds `page` tokens of every kv head as e4m3 codes [n_pages][H][page][128]; one float32 scale per (page, head):
+// value = code * scale.  The writes here choose scales that are powers of two: e4m3 is a floating-point format, so a
+// power of two loses nothing of its relative precision (half a step is 2^-4 of the value), dividing by it is exact, and
+// re-rounding older rows when a page's scale grows changes only codes that fall into e4m3's subnormal range.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+
+namespace faedkv {
+namespace pages {
+
+// Device status word: codes of indices that came from device memory and lie outside what they index.  The access is
+// skipped (the token is not stored / not attended to / reads as zero) and the kernel carries on.
+constexpr unsigned int kBadPage = 0x101, kBadSlot = 0x102, kBadLength = 0x103, kBadFreeList = 0x104, kBadStart = 0x105;
+
+__device__ __forceinline__ void flag(unsigned int *status, unsigned int code) { atomicCAS(status, 0u, code); }
+
+// ---- tables -------------------------------------------------------------------------------------------
+
+struct TablesArgs {
+    const int32_t *t_len, *n_new, *n_free;
+    int32_t *table, *free_pages, *q_start, *kv_len, *slots, *n_free_out, *ws;   // ws[b]: first new page in the running order, -1 denied; ws[B]: stack height before the grants
+    int B, W, page_shift, n_pages, n_tokens;
+    unsigned int *status;
+};
+
+constexpr int kPlanThreads = 1024;
+
+// Inclusive sum over the block's threads; *total receives the block's sum.  Two barriers.
+__device__ __forceinline__ long long block_scan(long long v, long long *warp_sums, long long *total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, v, s);
+        if (lane >= s) v += o;
+    }
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    long long w = warp_sums[lane];                       // 32 warps: one sum per lane
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, w, s);
+        if (lane >= s) w += o;
+    }
+    *total = __shfl_sync(0xffffffffu, w, 31);
+    const long long before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+    __syncthreads();
+    return v + (warp > 0 ? before : 0);
+}
+
+// Last b with start[b] <= i, for i < start[B].
+__device__ __forceinline__ int find_sequence(const int32_t *start, int B, int i) {
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start[mid] <= i) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Slot of new token i, and the table entry when the token opens a page.
+__device__ __forceinline__ void place_token(const TablesArgs &a, int i) {
+    int slot = -1;
+    if (i < a.q_start[a.B]) {
+        const int b = find_sequence(a.q_start, a.B, i);
+        const int base = a.ws[b];
+        if (base >= 0) {
+            const int first = a.q_start[b], n = a.q_start[b + 1] - first;
+            const int t = a.kv_len[b] - n, pos = t + (i - first);
+            const int p = pos >> a.page_shift, old = (t + (1 << a.page_shift) - 1) >> a.page_shift;
+            int id;
+            if (p < old) {
+                id = a.table[(size_t)b * a.W + p];
+            } else {
+                id = a.free_pages[a.ws[a.B] - 1 - (base + p - old)];
+                if ((pos & ((1 << a.page_shift) - 1)) == 0) a.table[(size_t)b * a.W + p] = id;
+            }
+            if (id >= 0 && id < a.n_pages) slot = (id << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+            else flag(a.status, kBadPage);
+        }
+    }
+    a.slots[i] = slot;
+}
+
+// One CTA: pushes the pages of finished requests, grants pages in request order (three block-wide sums per 1024
+// requests), writes lengths and starts; with PLACE also the slots.  Every input of a request is read before an output
+// of the same request is written, and n_free before n_free_out, so outputs may be the inputs' own buffers.
+// Bound by latency: a chain of three scans, about 3 us for up to 1024 requests.
+template <bool PLACE>
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan(const TablesArgs a) {
+    __shared__ long long warp_sums[32];
+    __shared__ int rel_base[kPlanThreads], rel_n[kPlanThreads];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int page = 1 << a.page_shift;
+    const long long cap = (long long)a.W * page;
+    long long height = *a.n_free;
+    if (height < 0 || height > a.n_pages) {
+        if (tid == 0) flag(a.status, kBadFreeList);
+        height = height < 0 ? 0 : a.n_pages;
+    }
+    // finished requests: pages onto the stack, in request order
+    for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+        const int b = b0 + tid;
+        long long held = 0;
+        if (b < a.B && a.n_new[b] < 0) {
+            const long long t = a.t_len[b];
+            if (t < 0 || t > cap) flag(a.status, kBadLength);
+            held = t <= 0 ? 0 : ((t < cap ? t : cap) + page - 1) >> a.page_shift;
+        }
+        if (!__syncthreads_or(held > 0)) continue;
+        long long total;
+        const long long upto = block_scan(held, warp_sums, &total);
+        rel_base[tid] = (int)min(height + upto - held, (long long)a.n_pages);
+        rel_n[tid] = (int)held;
+        __syncthreads();
+        for (int r = warp; r < kPlanThreads; r += kPlanThreads / 32) {
+            const int n = rel_n[r], base = rel_base[r];
+            for (int j = lane; j < n; j += 32) {
+                if (base + j < a.n_pages) a.free_pages[base + j] = a.table[(size_t)(b0 + r) * a.W + j];
+                else flag(a.status, kBadFreeList);
+            }
+        }
+        height = min(height + total, (long long)a.n_pages);
+        __syncthreads();
+    }
+    // arriving tokens and the pages they need
+    long long tok_before = 0, need_before = 0, taken = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+        const int b = b0 + tid;
+        long long t = 0, n = 0;
+        bool done = true, valid = false;
+        if (b < a.B) {
+            t = a.t_len[b];
+            n = a.n_new[b];
+            done = n < 0;
+            if (done) n = 0;
+        }
+        long long tok_total, need_total;
+        const long long tok_end = tok_before + block_scan(n, warp_sums, &tok_total);
+        if (b < a.B && !done) {
+            if (t < 0 || t > cap) flag(a.status, kBadLength);
+            valid = t >= 0 && t + n <= cap && tok_end <= a.n_tokens;
+        }
+        const long long old = (t + page - 1) >> a.page_shift;
+        const long long need = valid ? ((t + n + page - 1) >> a.page_shift) - old : 0;
+        const long long need_end = need_before + block_scan(need, warp_sums, &need_total);
+        const bool ok = valid && (need == 0 || need_end <= height);
+        long long took_total;
+        block_scan(ok ? need : 0, warp_sums, &took_total);
+        if (b < a.B) {
+            a.q_start[b] = (int)min(tok_end - n, 0x7fffffffLL);
+            if (b == a.B - 1) a.q_start[a.B] = (int)min(tok_end, 0x7fffffffLL);
+            a.kv_len[b] = done ? 0 : (ok ? (int)(t + n) : (int)t);
+            a.ws[b] = ok ? (int)min(need_end - need, (long long)a.n_pages) : -1;
+        }
+        tok_before += tok_total;
+        need_before += need_total;
+        taken += took_total;
+    }
+    if (tid == 0) {
+        a.ws[a.B] = (int)height;
+        *a.n_free_out = (int)(height - taken);
+    }
+    if (PLACE) {
+        __syncthreads();
+        for (int i = tid; i < a.n_tokens; i += kPlanThreads) place_token(a, i);
+    }
+}
+
+__global__ void __launch_bounds__(256) k_page_slots(const TablesArgs a) {
+    pdl_wait();
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < a.n_tokens) place_token(a, i);
+}
+
+// ---- store --------------------------------------------------------------------------------------------
+
+// The smallest power of two s >= 2^-126 with amax / s <= 448 (amax finite, >= 0): 448 = 1.75 * 2^8.
+__device__ __forceinline__ float scale_for(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    if (e < 1) e = 1;
+    return __uint_as_float((uint32_t)e << 23);
+}
+// |x| of a finite x as bits (ordered like the values), 0 for infinities and NaN: they do not set a page's scale.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+}
+// Two e4m3 codes, round to nearest even, |x| > 448 and infinities to 448, NaN to NaN.
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ uint2 to_e4m3x8(const float (&x)[8], float mul) {
+    uint2 r;
+    r.x = to_e4m3x2(x[0] * mul, x[1] * mul) | to_e4m3x2(x[2] * mul, x[3] * mul) << 16;
+    r.y = to_e4m3x2(x[4] * mul, x[5] * mul) | to_e4m3x2(x[6] * mul, x[7] * mul) << 16;
+    return r;
+}
+// The values of two codes (exact: e4m3 is a subset of f16).
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t codes) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3);
+    return __half22float2(__half2(h));
+}
+__device__ __forceinline__ void from_e4m3x4(uint32_t codes, float (&x)[4]) {
+    const float2 a = from_e4m3x2(codes), b = from_e4m3x2(codes >> 16);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+}
+
+template <typename T> struct Raw8;                        // 8 consecutive elements, as they lie in memory
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = __ldcs(reinterpret_cast<const float4 *>(p));
+        b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+};
+
+constexpr int kStoreThreads = 256;
+
+struct StoreArgs {
+    const void *x[2];                                     // k_new, v_new: token rows `ld` elements apart, heads 128 apart
+    uint8_t *codes[2];
+    float *scale[2];
+    const int32_t *slots;
+    long long ld;
+    int n_tokens, tile, H, n_pages;
+    unsigned int *status;
+};
+
+// Grid (tiles of consecutive tokens, 2 H).  The tokens of one page are a run of consecutive tokens with ascending slots;
+// a CTA owns the runs that START in its tile, one (tensor, head) of them: 16 threads per row of 128, 8 elements a thread.
+// It reads a run once into registers, takes the largest finite magnitude, settles the page's scale, re-rounds the page's
+// older rows if the scale grew, and writes the new codes: the data is read once and written once.
+template <typename T, int PAGE>
+__global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a) {
+    constexpr int kRows = kStoreThreads / 16, kIter = (PAGE + kRows - 1) / kRows;
+    __shared__ int slot_s[2 * PAGE + 1];                  // [0]: the token before the tile
+    __shared__ uint32_t start_s[(2 * PAGE + 31) / 32];    // bit j: token j of the tile starts a run
+    __shared__ uint32_t max_s[kStoreThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int which = blockIdx.y & 1, h = blockIdx.y >> 1;
+    const long long i0 = (long long)blockIdx.x * a.tile;
+    const long long limit = (long long)a.n_pages * PAGE;
+    const int n_here = (int)min((long long)a.tile + PAGE, a.n_tokens - i0);   // tokens looked at: a run may end behind the tile
+    for (int j = tid; j <= n_here; j += kStoreThreads) slot_s[j] = i0 + j == 0 ? -2 : a.slots[i0 + j - 1];
+    __syncthreads();
+    for (int j0 = warp * 32; j0 < n_here; j0 += kStoreThreads) {
+        const int j = j0 + lane;
+        bool st = true;
+        if (j < n_here) {
+            const int s = slot_s[j + 1];
+            st = s < 0 || s % PAGE == 0 || s != slot_s[j] + 1;
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, st);
+        if (lane == 0) start_s[j0 >> 5] = m;
+    }
+    __syncthreads();
+    const T *x = static_cast<const T *>(a.x[which]) + (size_t)h * kHeadDim;
+    uint8_t *codes = a.codes[which];
+    float *scales = a.scale[which];
+    const int c8 = (tid & 15) * 8, row_t = tid >> 4;
+    const int n_tile = min(a.tile, n_here);
+    for (int j = 0; j < n_tile; ++j) {
+        if (!((start_s[j >> 5] >> (j & 31)) & 1u)) continue;
+        const int slot = slot_s[j + 1];
+        if (slot < 0) continue;
+        if (slot >= limit) {
+            if (tid == 0) flag(a.status, kBadSlot);
+            continue;
+        }
+        int n = 1;                                        // run length: up to the next start
+        const int r0 = slot % PAGE;
+        while (j + n < n_here && n < PAGE - r0 && !((start_s[(j + n) >> 5] >> ((j + n) & 31)) & 1u)) ++n;
+        const int pg = slot / PAGE;
+        const T *src = x + (size_t)(i0 + j) * a.ld;
+        Raw8<T> raw[kIter];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int k = 0; k < kIter; ++k) {
+            const int r = row_t + k * kRows;
+            if (r < n) raw[k].load(src + (size_t)r * a.ld + c8);
+        }
+#pragma unroll
+        for (int k = 0; k < kIter; ++k) {
+            if (row_t + k * kRows < n) {
+                float v[8];
+                raw[k].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(v[e]));
+            }
+        }
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        if (lane == 0) max_s[warp] = amax;
+        const size_t ph = (size_t)pg * a.H + h;
+        const float s_old = r0 > 0 ? scales[ph] : 0.f;
+        __syncthreads();
+        amax = max_s[lane & (kStoreThreads / 32 - 1)];
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        float s = scale_for(__uint_as_float(amax));
+        uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim);
+        if (r0 > 0) {
+            if (s > s_old) {                              // the page's older rows, rounded again at the larger scale
+                const float mul = s_old * __uint_as_float((254u << 23) - __float_as_uint(s));
+                for (int r = row_t; r < r0; r += kRows) {
+                    uint2 *p = reinterpret_cast<uint2 *>(dst + r * kHeadDim + c8);
+                    const uint2 c = *p;
+                    float v[8], q[4];
+                    from_e4m3x4(c.x, q);
+                    v[0] = q[0]; v[1] = q[1]; v[2] = q[2]; v[3] = q[3];
+                    from_e4m3x4(c.y, q);
+                    v[4] = q[0]; v[5] = q[1]; v[6] = q[2]; v[7] = q[3];
+                    *p = to_e4m3x8(v, mul);
+                }
+            } else {
+                s = s_old;
+            }
+        }
+        // 1 / s: exact for the powers of two that this kernel writes; a scale of another origin is divided by
+        const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0u;
+        const float inv = pow2 ? __uint_as_float((254u << 23) - __float_as_uint(s)) : __fdiv_rn(1.0f, s);
+#pragma unroll
+        for (int k = 0; k < kIter; ++k) {
+            const int r = row_t + k * kRows;
+            if (r < n) {
+                float v[8];
+                raw[k].get(v);
+                *reinterpret_cast<uint2 *>(dst + (size_t)(r0 + r) * kHeadDim + c8) = to_e4m3x8(v, inv);
+            }
+        }
+        if (tid == 0) scales[ph] = s;
+        __syncthreads();                                  // max_s, and the scale if the next run is of the same page
+    }
+}
+
+// ---- load ---------------------------------------------------------------------------------------------
+
+struct LoadArgs {
+    const uint8_t *codes[2];
+    const float *scale[2];
+    void *out[2];
+    const int32_t *kv_len, *table;
+    int H, L, W, n_pages, page_shift;
+    unsigned int *status;
+};
+
+__device__ __forceinline__ void put8(__nv_bfloat16 *p, const float (&x)[8]) {
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<uint4 *>(h));
+}
+__device__ __forceinline__ void put8(float *p, const float (&x)[8]) {
+    __stcs(reinterpret_cast<float4 *>(p), make_float4(x[0], x[1], x[2], x[3]));
+    __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
+}
+
+// Grid (pages of the longest row, H, sequences); a CTA turns one page of one head, K and V, into rows.
+// Rounding: to the tensor type, once (code * scale is exact in float32 but for underflow).
+template <typename T>
+__global__ void __launch_bounds__(256) k_page_load(const LoadArgs a) {
+    const int b = blockIdx.z, h = blockIdx.y, page = 1 << a.page_shift;
+    const int n0 = blockIdx.x << a.page_shift;
+    long long live = a.kv_len[b];
+    const long long cap = (long long)a.W << a.page_shift;
+    if (live < 0 || live > cap) {
+        if (threadIdx.x == 0) flag(a.status, kBadLength);
+        live = live < 0 ? 0 : cap;
+    }
+    int id = -1;
+    if (n0 < live) {
+        id = a.table[(size_t)b * a.W + blockIdx.x];
+        if (id < 0 || id >= a.n_pages) {
+            if (threadIdx.x == 0) flag(a.status, kBadPage);
+            id = -1;
+        }
+    }
+    const int c8 = (threadIdx.x & 15) * 8;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        if (a.out[t] == nullptr) continue;
+        const size_t ph = (size_t)(id < 0 ? 0 : id) * a.H + h;
+        const float s = id < 0 ? 0.f : a.scale[t][ph];
+        const uint8_t *src = a.codes[t] + (ph << a.page_shift) * kHeadDim + c8;
+        T *dst = static_cast<T *>(a.out[t]) + (((size_t)b * a.H + h) * a.L + n0) * kHeadDim + c8;
+        for (int r = threadIdx.x >> 4; r < page && n0 + r < a.L; r += 16) {
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (id >= 0 && n0 + r < live) {
+                const uint2 c = __ldcs(reinterpret_cast<const uint2 *>(src + (size_t)r * kHeadDim));
+                float q[4];
+                from_e4m3x4(c.x, q);
+                x[0] = q[0] * s; x[1] = q[1] * s; x[2] = q[2] * s; x[3] = q[3] * s;
+                from_e4m3x4(c.y, q);
+                x[4] = q[0] * s; x[5] = q[1] * s; x[6] = q[2] * s; x[7] = q[3] * s;
+            }
+            put8(dst + (size_t)r * kHeadDim, x);
+        }
+    }
+}
+
+}  // namespace pages
+}  // namespace faedkv
