@@ -18,6 +18,8 @@ struct faedkv_pages {
     faedkv_pages_config cfg;
     int device = 0, n_sm = 1, page_shift = 0, gq = 1;
     unsigned int *dev_status = nullptr;
+    unsigned int attr_set = 0;                 // attention instances already opted in to large shared memory
+    void *encode = nullptr;                    // cuTensorMapEncodeTiled
     unsigned long long launches = 0;
     char err[512] = {0};
 };
@@ -118,18 +120,70 @@ void launch_store(const pages::StoreArgs &a, int page, dim3 grid, cudaStream_t s
     }
 }
 
-template <typename T>
-void launch_attn_simple(const pages::AttnArgs &a, dim3 grid, cudaStream_t st) {
-    switch (a.G) {
-        case 1: pages::k_page_attn_simple<T, 1><<<grid, 256, 0, st>>>(a); break;
-        case 2: pages::k_page_attn_simple<T, 2><<<grid, 256, 0, st>>>(a); break;
-        case 3: pages::k_page_attn_simple<T, 3><<<grid, 256, 0, st>>>(a); break;
-        case 4: pages::k_page_attn_simple<T, 4><<<grid, 256, 0, st>>>(a); break;
-        case 5: pages::k_page_attn_simple<T, 5><<<grid, 256, 0, st>>>(a); break;
-        case 6: pages::k_page_attn_simple<T, 6><<<grid, 256, 0, st>>>(a); break;
-        case 7: pages::k_page_attn_simple<T, 7><<<grid, 256, 0, st>>>(a); break;
-        default: pages::k_page_attn_simple<T, 8><<<grid, 256, 0, st>>>(a); break;
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// All rows of a code tensor, [n_pages * H * page][128] bytes; a box is one head's page.
+int make_map(faedkv_pages *pg, CUtensorMap *map, const void *codes) {
+    const faedkv_pages_config &c = pg->cfg;
+    const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)c.n_pages * c.n_kv_heads * c.page_size};
+    const cuuint64_t strides[1] = {(cuuint64_t)kHeadDim};
+    const cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)c.page_size}, step[2] = {1, 1};
+    const CUresult r = reinterpret_cast<EncodeTiled>(pg->encode)(
+        map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(pg, FAEDKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return FAEDKV_OK;
+}
+
+//                                            type            columns, terms of q and w, chained, stages, weight buffers, CTAs per SM
+using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 2, 3, false, 5, 2, 1>;
+using DecodeF32 = pages::AttnCfg<float, 8, 6, 6, false, 5, 2, 1>;
+using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 64, 2, 2, true, 2, 1, 2>;
+
+// How a call is cut up.
+struct AttnPlan {
+    bool wide;               // 64 columns a unit instead of 8
+    int qc, blocks, splits;  // MODE 1: blocks of new tokens, splits of the cached ones
+    int ctas;                // MODE 0
+    size_t bytes0, bytes1;   // workspace of the two modes
+};
+
+AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
+    const faedkv_pages_config &c = pg->cfg;
+    AttnPlan p{};
+    const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
+    // more query columns per sequence than 8: a block of 64 columns reads the cache once for all of them
+    p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
+    p.qc = p.wide ? ChunkBf16::QC : 8;
+    p.blocks = n_tokens / (p.qc / pg->gq) + batch;
+    const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : 1);
+    long long splits = units > 0 ? room / units : 1;
+    if (splits > (max_tiles + 1) / 2) splits = (max_tiles + 1) / 2;
+    p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+    p.bytes1 = p.splits > 1 ? (size_t)units * p.splits * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
+    const long long all_tiles = max_tiles * batch * c.n_kv_heads;
+    p.ctas = (int)(all_tiles < pg->n_sm ? all_tiles : pg->n_sm);
+    p.bytes0 = 16 + sizeof(pages::UnitMeta) * (size_t)batch * c.n_kv_heads + (size_t)p.ctas * 2 * pages::attn_slot_floats(8) * sizeof(float);
+    return p;
+}
+
+template <typename C, int MODE>
+int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int attr_bit,
+                cudaStream_t st) {
+    auto kernel = pages::k_page_attn<C, MODE>;
+    if (!(pg->attr_set & (1u << attr_bit))) {
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes));
+        pg->attr_set |= 1u << attr_bit;
     }
+    const dim3 grid = MODE == 0 ? dim3(p.ctas) : dim3(p.blocks, a.H, p.splits);
+    kernel<<<grid, pages::kAttnThreads, C::kSmemBytes, st>>>(mk, mv, a);
+    if (int r = launch_check(pg, "k_page_attn")) return r;
+    if (MODE == 1 && p.splits == 1) return FAEDKV_OK;
+    const dim3 jgrid = MODE == 0 ? dim3((unsigned)(a.B * a.H), a.G) : dim3((unsigned)(p.blocks * a.H), C::QC / a.G * a.G);
+    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim), 0, st, a, (int)C::QC));
+    return launch_check(pg, "k_page_attn_join");
 }
 
 }  // namespace
@@ -154,7 +208,10 @@ int faedkv_pages_create(const faedkv_pages_config *cfg, faedkv_pages **out) {
     pg->cfg = c;
     pg->gq = c.n_q_heads / c.n_kv_heads;
     while ((1 << pg->page_shift) < c.page_size) ++pg->page_shift;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
     if (cudaGetDevice(&pg->device) != cudaSuccess ||
+        cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &pg->encode, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess || pg->encode == nullptr ||
         cudaDeviceGetAttribute(&pg->n_sm, cudaDevAttrMultiProcessorCount, pg->device) != cudaSuccess ||
         cudaMalloc(&pg->dev_status, sizeof(unsigned int)) != cudaSuccess ||
         cudaMemset(pg->dev_status, 0, sizeof(unsigned int)) != cudaSuccess) {
@@ -239,7 +296,9 @@ int faedkv_pages_store(faedkv_pages *pg, const void *k_new, const void *v_new, l
 
 size_t faedkv_pages_attn_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
     if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_tokens < 0) return 0;
-    return 16;
+    if ((long long)n_tokens + batch > (1LL << 30)) return 0;
+    const AttnPlan p = plan_attn(pg, batch, n_tokens);
+    return n_tokens == batch && p.bytes0 > p.bytes1 ? p.bytes0 : p.bytes1;
 }
 
 int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
@@ -249,7 +308,8 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     const CallRange nvtx_range("faedkv_pages_attn");
     if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
     if (int r = check_batch(pg, batch)) return r;
-    if (n_tokens < 0) return fail(pg, FAEDKV_ERR_SHAPE, "n_tokens = %d is negative", n_tokens);
+    if (n_tokens < 0 || (long long)n_tokens + batch > (1LL << 30))
+        return fail(pg, FAEDKV_ERR_SHAPE, "n_tokens = %d outside [0, 2^30 - batch]", n_tokens);
     if (q_start == nullptr && n_tokens != batch)
         return fail(pg, FAEDKV_ERR_SHAPE, "without q_start there is one token per sequence: n_tokens = %d, batch = %d", n_tokens, batch);
     if (!(scale >= 0.0f) || std::isinf(scale)) return fail(pg, FAEDKV_ERR_INVALID_ARG, "scale must be >= 0 and finite");
@@ -266,13 +326,17 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     const DeviceGuard guard(pg);
     if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const pages::AttnArgs a{q, out, q_start, kv_len, table, static_cast<const uint8_t *>(k_pages), static_cast<const uint8_t *>(v_pages),
-                            k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq, c.max_pages, c.n_pages, pg->page_shift,
-                            scale, pg->dev_status};
-    const dim3 grid(n_tokens, c.n_kv_heads);
-    if (c.kv_dtype == FAEDKV_BF16) launch_attn_simple<__nv_bfloat16>(a, grid, st);
-    else launch_attn_simple<float>(a, grid, st);
-    return launch_check(pg, "k_page_attn_simple");
+    CUtensorMap mk, mv;
+    if (int r = make_map(pg, &mk, k_pages)) return r;
+    if (int r = make_map(pg, &mv, v_pages)) return r;
+    const AttnPlan p = plan_attn(pg, batch, n_tokens);
+    const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
+                            c.max_pages, c.n_pages, pg->page_shift, p.splits, scale * 1.44269504088896341f,
+                            static_cast<unsigned char *>(ws), pg->dev_status};
+    if (c.kv_dtype == FAEDKV_F32)
+        return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st) : launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st);
+    if (q_start == nullptr) return launch_attn<DecodeBf16, 0>(pg, mk, mv, a, p, 2, st);
+    return p.wide ? launch_attn<ChunkBf16, 1>(pg, mk, mv, a, p, 3, st) : launch_attn<DecodeBf16, 1>(pg, mk, mv, a, p, 4, st);
 }
 
 int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *table, int batch, int L, const void *k_pages,
