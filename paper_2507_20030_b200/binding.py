@@ -417,6 +417,10 @@ class Context:
         self._check(self._lib.faedkv_test_hooks(self._h, int(wait_limit_ns), int(withhold_step)))
 
 
+# the current stream's handle without building a Stream object (1 us a call)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 @dataclass
 class Pages:
     """The paged 8-bit cache (faedkv_pages): methods carry the names of the C calls without the prefix.
@@ -442,6 +446,7 @@ class Pages:
             raise FaedkvError(rc, "faedkv_pages_create failed")
         self._h = h
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._shapes()
 
     # -- lifetime
     def close(self):
@@ -463,69 +468,76 @@ class Pages:
     def torch_dtype(self):
         return torch.bfloat16 if self.kv_dtype == BF16 else torch.float32
 
-    def _need(self, name, t, dtype, shape=None, size=None):
-        """A contiguous tensor of this dtype on the handle's device, of this shape or at least this many elements."""
-        if t.dtype != dtype or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {self.device}, got {t.dtype} on {t.device}")
-        if shape is not None and tuple(t.shape) != shape:
-            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-        if size is not None and t.numel() < size:
-            raise ValueError(f"{name} must hold at least {size} elements, got {t.numel()}")
+    def _shapes(self):
+        """What the checks compare with, worked out once: a decode step's calls are short enough for it to show."""
+        self._index = -1 if self.device.type == "cpu" else self.device.index
+        self._dtype = torch.bfloat16 if self.kv_dtype == BF16 else torch.float32
+        self._scale_shape = (self.n_pages, self.n_kv_heads)
+        self._code_shape = (*self._scale_shape, self.page_size, self.head_dim)
+        self._pool_shape = (self.n_pages,)
+
+    def _refuse(self, name, t, dtype, shape):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
+                         f"with strides {t.stride()} on {t.device}")
+
+    def _need(self, name, t, dtype, shape):
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
+            self._refuse(name, t, dtype, shape)
         return t.data_ptr()
 
     def _rows(self, name, t, heads):
         """Token rows [n_tokens, heads, head_dim], contiguous from the head on: pointer, tokens, row stride in elements."""
-        if t.dtype != self.torch_dtype or t.device != self.device:
-            raise ValueError(f"{name} must be {self.torch_dtype} on {self.device}, got {t.dtype} on {t.device}")
-        if t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.head_dim):
-            raise ValueError(f"{name} must have shape [n_tokens, {heads}, {self.head_dim}], got {tuple(t.shape)}")
-        n = t.shape[0]
-        row = heads * self.head_dim
-        if n and ((heads > 1 and t.stride(1) != self.head_dim) or t.stride(2) != 1 or (n > 1 and t.stride(0) < row)):
-            raise ValueError(f"{name}: heads and channels must be contiguous within a token row, strides {t.stride()}")
-        return t.data_ptr(), n, (t.stride(0) if n > 1 else row)
+        if t.dtype is not self._dtype or t.get_device() != self._index:
+            raise ValueError(f"{name} must be {self._dtype} on {self.device}, got {t.dtype} on {t.device}")
+        shape = t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim:
+            raise ValueError(f"{name} must have shape [n_tokens, {heads}, {self.head_dim}], got {tuple(shape)}")
+        n, row = shape[0], heads * self.head_dim
+        if t.is_contiguous():
+            return t.data_ptr(), n, row
+        st = t.stride()
+        if (heads > 1 and st[1] != self.head_dim) or st[2] != 1 or (n > 1 and st[0] < row):
+            raise ValueError(f"{name}: heads and channels must be contiguous within a token row, strides {st}")
+        return t.data_ptr(), n, (st[0] if n > 1 else row)
 
     def _cache(self, k_pages, v_pages, k_scale, v_scale):
-        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
-        return (self._need("k_pages", k_pages, torch.float8_e4m3fn, shape), self._need("v_pages", v_pages, torch.float8_e4m3fn, shape),
-                self._need("k_scale", k_scale, torch.float32, shape[:2]), self._need("v_scale", v_scale, torch.float32, shape[:2]))
+        need, f8, f32 = self._need, torch.float8_e4m3fn, torch.float32
+        return (need("k_pages", k_pages, f8, self._code_shape), need("v_pages", v_pages, f8, self._code_shape),
+                need("k_scale", k_scale, f32, self._scale_shape), need("v_scale", v_scale, f32, self._scale_shape))
 
     def _workspace(self, ws, nbytes, stream):
         if ws is not None:
-            if not ws.is_contiguous() or ws.device != self.device:
-                raise ValueError(f"ws must be a contiguous tensor on {self.device}")
-            return ws, ws.numel() * ws.element_size()
+            if not ws.is_contiguous() or ws.get_device() != self._index or ws.numel() * ws.element_size() < nbytes:
+                raise ValueError(f"ws must be a contiguous tensor of at least {nbytes} bytes on {self.device}")
+            return ws
         if stream is None:
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         s = torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
         with torch.cuda.stream(s):
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def _on(self, stream):
         """The stream's handle; by default the current stream of the handle's device."""
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return _current_raw_stream(self._index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def alloc(self):
         """k_pages, v_pages (torch.float8_e4m3fn [n_pages, n_kv_heads, page_size, head_dim]), k_scale, v_scale (float32
         [n_pages, n_kv_heads]), all uninitialised."""
-        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
-        codes = [torch.empty(shape, dtype=torch.float8_e4m3fn, device=self.device) for _ in range(2)]
-        scales = [torch.empty(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2)]
+        codes = [torch.empty(self._code_shape, dtype=torch.float8_e4m3fn, device=self.device) for _ in range(2)]
+        scales = [torch.empty(self._scale_shape, dtype=torch.float32, device=self.device) for _ in range(2)]
         return (*codes, *scales)
 
     # -- the calls
     def tables(self, t_len, n_new, table, free_pages, n_free, q_start, kv_len, slots, n_free_out, ws=None, stream=None):
-        batch, i32 = t_len.shape[0], torch.int32
-        need = self._need
-        args = (need("t_len", t_len, i32, (batch,)), need("n_new", n_new, i32, (batch,)), batch,
-                need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, (self.n_pages,)),
-                need("n_free", n_free, i32, size=1), slots.numel(), need("q_start", q_start, i32, size=batch + 1),
-                need("kv_len", kv_len, i32, (batch,)), need("slots", slots, i32), need("n_free_out", n_free_out, i32, size=1))
-        w, nbytes = self._workspace(ws, 4 * (batch + 1), stream)
-        if nbytes < 4 * (batch + 1):
-            raise ValueError(f"ws must hold {4 * (batch + 1)} bytes")
+        batch, i32, need = t_len.shape[0], torch.int32, self._need
+        per_seq, one, n_tokens = (batch,), (1,), slots.numel()
+        args = (need("t_len", t_len, i32, per_seq), need("n_new", n_new, i32, per_seq), batch,
+                need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, self._pool_shape),
+                need("n_free", n_free, i32, one), n_tokens, need("q_start", q_start, i32, (batch + 1,)),
+                need("kv_len", kv_len, i32, per_seq), need("slots", slots, i32, (n_tokens,)), need("n_free_out", n_free_out, i32, one))
+        w = self._workspace(ws, 4 * (batch + 1), stream)
         self._check(self._lib.faedkv_pages_tables(self._h, *args, w.data_ptr(), self._on(stream)))
 
     def store(self, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None):
@@ -534,23 +546,24 @@ class Pages:
         if nv != n or ldv != ld:
             raise ValueError(f"k_new and v_new must have the same tokens and row stride, got {n}, {nv} tokens, strides {ld}, {ldv}")
         s = self._need("slots", slots, torch.int32, (n,))
-        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
-        self._check(self._lib.faedkv_pages_store(self._h, k, v, ld, s, n, kp, vp, ks, vs, self._on(stream)))
+        self._check(self._lib.faedkv_pages_store(self._h, k, v, ld, s, n, *self._cache(k_pages, v_pages, k_scale, v_scale),
+                                                 self._on(stream)))
 
     def attn_bytes(self, batch: int, n_tokens: int) -> int:
-        return int(self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens))
+        return self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens)
 
     def attn(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, out, q_start=None, scale: float = 0.0, ws=None, stream=None):
-        batch = kv_len.shape[0]
+        batch, i32, need = kv_len.shape[0], torch.int32, self._need
         qp, n, ld = self._rows("q", q, self.n_q_heads)
-        o = self._need("out", out, self.torch_dtype, (n, self.n_q_heads, self.head_dim))
-        st = None if q_start is None else self._need("q_start", q_start, torch.int32, size=batch + 1)
-        kv = self._need("kv_len", kv_len, torch.int32, (batch,))
-        tb = self._need("table", table, torch.int32, (batch, self.max_pages))
-        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
-        w, nbytes = self._workspace(ws, self.attn_bytes(batch, n), stream)
-        self._check(self._lib.faedkv_pages_attn(self._h, qp, ld, st, n, batch, kv, tb, kp, vp, ks, vs, float(scale), o, w.data_ptr(),
-                                                nbytes, self._on(stream)))
+        o = need("out", out, self._dtype, (n, self.n_q_heads, self.head_dim))
+        st = None if q_start is None else need("q_start", q_start, i32, (batch + 1,))
+        kv = need("kv_len", kv_len, i32, (batch,))
+        tb = need("table", table, i32, (batch, self.max_pages))
+        cache = self._cache(k_pages, v_pages, k_scale, v_scale)
+        nbytes = self.attn_bytes(batch, n)
+        w = self._workspace(ws, nbytes, stream)
+        self._check(self._lib.faedkv_pages_attn(self._h, qp, ld, st, n, batch, kv, tb, *cache, scale, o, w.data_ptr(), nbytes,
+                                                self._on(stream)))
 
     def load(self, kv_len, table, k_pages, v_pages, k_scale, v_scale, L: int, K_out=None, V_out=None, stream=None):
         """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end."""
@@ -560,12 +573,12 @@ class Pages:
             K_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
         if V_out is None:
             V_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
-        kv = self._need("kv_len", kv_len, torch.int32, (batch,))
-        tb = self._need("table", table, torch.int32, (batch, self.max_pages))
-        kp, vp, ks, vs = self._cache(k_pages, v_pages, k_scale, v_scale)
+        need = self._need
+        kv = need("kv_len", kv_len, torch.int32, (batch,))
+        tb = need("table", table, torch.int32, (batch, self.max_pages))
         self._check(self._lib.faedkv_pages_load(
-            self._h, kv, tb, batch, L, kp, vp, ks, vs, self._need("K_out", K_out, self.torch_dtype, shape),
-            self._need("V_out", V_out, self.torch_dtype, shape), self._on(stream)))
+            self._h, kv, tb, batch, L, *self._cache(k_pages, v_pages, k_scale, v_scale), need("K_out", K_out, self._dtype, shape),
+            need("V_out", V_out, self._dtype, shape), self._on(stream)))
         return K_out, V_out
 
     def launch_count(self) -> int:

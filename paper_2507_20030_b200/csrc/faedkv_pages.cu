@@ -137,14 +137,16 @@ int make_map(faedkv_pages *pg, CUtensorMap *map, const void *codes) {
     return FAEDKV_OK;
 }
 
-//                                            type            columns, terms of q and w, chained, stages, weight buffers, CTAs per SM
-using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 2, 3, false, 5, 2, 1>;
-using DecodeF32 = pages::AttnCfg<float, 8, 6, 6, false, 5, 2, 1>;
-using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 64, 2, 2, true, 2, 1, 2>;
+//                                  type           columns, warpgroups, terms of q and w, chained, stages, weight buffers, CTAs per SM
+using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 3, false, 3, 2, 2>;
+using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 6, false, 2, 2, 2>;
+using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 128, 2, 2, 2, true, 3, 2, 1>;
+constexpr int kDecodeCtas = DecodeBf16::CTAS;
+static_assert(kDecodeCtas == DecodeF32::CTAS && DecodeF32::QC == 8 && DecodeBf16::QC == 8, "one plan for both types");
 
 // How a call is cut up.
 struct AttnPlan {
-    bool wide;               // 64 columns a unit instead of 8
+    bool wide;               // 128 columns a unit instead of 8
     int qc, blocks, splits;  // MODE 1: blocks of new tokens, splits of the cached ones
     int ctas;                // MODE 0
     size_t bytes0, bytes1;   // workspace of the two modes
@@ -154,17 +156,18 @@ AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     const faedkv_pages_config &c = pg->cfg;
     AttnPlan p{};
     const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
-    // more query columns per sequence than 8: a block of 64 columns reads the cache once for all of them
+    // more query columns per sequence than 8: a block of 128 columns reads the cache once for all of them
     p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;
-    const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : 1);
+    const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : kDecodeCtas);
     long long splits = units > 0 ? room / units : 1;
     if (splits > (max_tiles + 1) / 2) splits = (max_tiles + 1) / 2;
     p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
     p.bytes1 = p.splits > 1 ? (size_t)units * p.splits * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
     const long long all_tiles = max_tiles * batch * c.n_kv_heads;
-    p.ctas = (int)(all_tiles < pg->n_sm ? all_tiles : pg->n_sm);
+    const long long most = (long long)pg->n_sm * kDecodeCtas;
+    p.ctas = (int)(all_tiles < most ? all_tiles : most);
     p.bytes0 = 16 + sizeof(pages::UnitMeta) * (size_t)batch * c.n_kv_heads + (size_t)p.ctas * 2 * pages::attn_slot_floats(8) * sizeof(float);
     return p;
 }
@@ -178,7 +181,7 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
         pg->attr_set |= 1u << attr_bit;
     }
     const dim3 grid = MODE == 0 ? dim3(p.ctas) : dim3(p.blocks, a.H, p.splits);
-    kernel<<<grid, pages::kAttnThreads, C::kSmemBytes, st>>>(mk, mv, a);
+    kernel<<<grid, C::kThreads, C::kSmemBytes, st>>>(mk, mv, a);
     if (int r = launch_check(pg, "k_page_attn")) return r;
     if (MODE == 1 && p.splits == 1) return FAEDKV_OK;
     const dim3 jgrid = MODE == 0 ? dim3((unsigned)(a.B * a.H), a.G) : dim3((unsigned)(p.blocks * a.H), C::QC / a.G * a.G);
@@ -288,7 +291,9 @@ int faedkv_pages_store(faedkv_pages *pg, const void *k_new, const void *v_new, l
     if (tile > c.page_size) tile = c.page_size;
     const pages::StoreArgs a{{k_new, v_new}, {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
                              slots, ld_new, n_tokens, (int)tile, c.n_kv_heads, c.n_pages, pg->dev_status};
-    const dim3 grid((unsigned)((n_tokens + tile - 1) / tile), 2 * c.n_kv_heads);
+    const long long ctas = (n_tokens + tile - 1) / tile * 2 * c.n_kv_heads;
+    if (ctas >= (1LL << 31)) return fail(pg, FAEDKV_ERR_SHAPE, "n_tokens = %d is too many for one call", n_tokens);
+    const dim3 grid((unsigned)ctas);
     if (c.kv_dtype == FAEDKV_BF16) launch_store<__nv_bfloat16>(a, c.page_size, grid, st);
     else launch_store<float>(a, c.page_size, grid, st);
     return launch_check(pg, "k_page_store");

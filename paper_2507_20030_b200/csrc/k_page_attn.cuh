@@ -19,7 +19,8 @@
 // some x exceeds it by 8, and then to 6 below the maximum, so weights stay in e4m3's range and most tiles exchange one
 // vote instead of a maximum per column.  O stays in TMEM over all tiles of a segment.
 //
-// A CTA: warps 0-3 softmax (thread = token row of S, channel row of O), warp 4 TMA, warp 5 MMA.
+// A CTA: one or two softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
+// columns), a TMA warp, an MMA warp.
 #pragma once
 #include "common.cuh"
 #include "k_pages.cuh"
@@ -30,26 +31,32 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr int kAttnThreads = 192;
 constexpr float kLagMax = 8.0f, kLagTo = 6.0f;            // weights stay <= 2^8; after a raise the largest is 2^6
-constexpr float kMuNone = -3e38f;
+constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
 
-// Instances: QC query columns, QT / PT terms of q / of the weights, the terms side by side as further columns of one
-// product (CHAIN = false: few columns, one pass over the tile) or added up in the same accumulator (CHAIN = true).
-template <typename T_, int QC_, int QT_, int PT_, bool CHAIN_, int STAGES_, int PBUFS_, int CTAS_> struct AttnCfg {
+// Instances: QC query columns over WGS softmax warpgroups, QT / PT terms of q / of the weights, the terms side by side as
+// further columns of one product (CHAIN = false: few columns, one pass over the tile) or added up in the same accumulator
+// (CHAIN = true).
+template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int STAGES_, int PBUFS_, int CTAS_> struct AttnCfg {
     using T = T_;
-    static constexpr int QC = QC_, QT = QT_, PT = PT_, STAGES = STAGES_, PBUFS = PBUFS_, CTAS = CTAS_;
+    static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, STAGES = STAGES_, PBUFS = PBUFS_, CTAS = CTAS_;
     static constexpr bool CHAIN = CHAIN_;
+    static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
+    static constexpr int kThreads = 128 * WGS + 64;
     static constexpr int NS = CHAIN ? QC : (QC * QT + 15) / 16 * 16;          // columns of S, of O
     static constexpr int NO = CHAIN ? QC : (QC * PT + 15) / 16 * 16;
     static constexpr int kTmemUsed = 2 * NS + NO;
     static constexpr uint32_t kTmemCols = kTmemUsed <= 32 ? 32 : kTmemUsed <= 64 ? 64 : kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
+    static constexpr uint32_t PW = NO <= 32 ? 32 : NO <= 64 ? 64 : 128;       // bytes of a token's weights (one term's, if CHAIN)
+    static constexpr uint32_t kPBytes = (CHAIN ? PT : 1) * kTile * PW;
     static constexpr uint32_t kQBytes = (CHAIN ? QT * QC : NS) * 128;
     static constexpr uint32_t kOffQ = STAGES * 2 * kTileBytes;
     static constexpr uint32_t kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
-    static constexpr uint32_t kOffMisc = kOffP + PBUFS * kTileBytes;
-    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (4 * QC + 4 * QC + STAGES * 32 + 64) + 1024 + 1024;
+    static constexpr uint32_t kOffMisc = kOffP + PBUFS * kPBytes;
+    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (10 * QC + STAGES * 32) + 256 + 1024;
+    static_assert(!CHAIN || PW == NO, "a chained term fills its rows");
+    static_assert(WGS == 1 || CHAIN, "two warpgroups share chained columns");
 };
 
 struct AttnArgs {
@@ -78,15 +85,55 @@ __device__ __forceinline__ float warp_max(float v) {
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ bool softmax_any(bool v) {     // over the four softmax warps; a barrier
+// Barriers over `threads` softmax threads, the first with a vote.
+__device__ __forceinline__ bool softmax_any(bool v, int id, int threads) {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p, q;\n\t"
                  "setp.ne.u32 q, %1, 0;\n\t"
-                 "barrier.cta.red.or.pred p, 1, 128, q;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(r) : "r"((uint32_t)v) : "memory");
+                 "barrier.cta.red.or.pred p, %2, %3, q;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(r) : "r"((uint32_t)v), "r"(id), "r"(threads) : "memory");
     return r != 0;
 }
-__device__ __forceinline__ void softmax_bar() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void softmax_bar(int id, int threads) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Two float32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// MN-major operand: rows of `row` bytes (32, 64 or 128) along MN, one row per K index, swizzled over their own width;
+// eight rows to a group, groups back to back.
+template <uint32_t row>
+__device__ __forceinline__ uint64_t desc_mn_rows(uint32_t saddr) {
+    constexpr uint64_t layout = row == 128 ? 2 : row == 64 ? 4 : 6;
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((8 * row) >> 4) << 16) | ((uint64_t)((8 * row) >> 4) << 32) |
+           ((uint64_t)1 << 46) | (layout << 61);
+}
+// Where 16-byte chunk k of row r of such an operand lies.
+template <uint32_t row>
+__device__ __forceinline__ uint32_t mn_chunk(uint32_t r, uint32_t k) {
+    return r * row + ((k ^ (row == 128 ? r & 7u : row == 64 ? (r >> 1) & 3u : (r >> 2) & 1u)) << 4);
+}
 
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -105,6 +152,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
         : "r"(taddr) : "memory");
 #pragma unroll
     for (int i = 0; i < 16; ++i) r[i] = __uint_as_float(u[i]);
+}
+// N columns (a multiple of 16) of this warp's lanes; completed by tmem_ld_wait().
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&r)[N]) {
+#pragma unroll
+    for (int c = 0; c < N; c += 16) tmem_ld16(taddr + c, *reinterpret_cast<float(*)[16]>(r + c));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&r)[16]) {
     uint32_t u[16];
@@ -209,23 +262,25 @@ template <> struct Work<1> {
 };
 
 template <typename C, int MODE>
-__global__ void __launch_bounds__(kAttnThreads, C::CTAS)
+__global__ void __launch_bounds__(C::kThreads, C::CTAS)
 k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a) {
     using namespace umma;
     using T = typename C::T;
-    constexpr int QC = C::QC, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, STAGES = C::STAGES, PB = C::PBUFS;
+    constexpr int QC = C::QC, QW = C::QW, WGS = C::WGS, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, STAGES = C::STAGES, PB = C::PBUFS;
+    constexpr int kSoftmax = 128 * WGS, kWarpTma = 4 * WGS, kWarpMma = 4 * WGS + 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
     auto k_tile = [&](int s) { return base + (uint32_t)s * 2 * kTileBytes; };
     auto v_tile = [&](int s) { return base + (uint32_t)s * 2 * kTileBytes + kTileBytes; };
     const uint32_t q_base = base + C::kOffQ;
-    auto p_tile = [&](int p) { return base + C::kOffP + (uint32_t)p * kTileBytes; };
-    float *col_cs = reinterpret_cast<float *>(gbase + C::kOffMisc);          // [QC] factor of a column's raw score
-    float *col_mu = col_cs + QC;                                             // [QC] Mu
-    float *col_f = col_mu + QC;                                              // [QC] rescale factor / 1 / l
+    auto p_tile = [&](int p) { return base + C::kOffP + (uint32_t)p * C::kPBytes; };
+    float *col = reinterpret_cast<float *>(gbase + C::kOffMisc);             // per pair of columns: factors of the raw scores, -Mu
+    float *col_d = col + 2 * QC;                                             // [QC] last raise of Mu
+    float *col_f = col_d + QC;                                               // [QC] 2^-raise
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
-    float *red = reinterpret_cast<float *>(col_lim + QC);                    // [4][QC]
+    int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
+    float *red = reinterpret_cast<float *>(col_set + QC);                    // [4][QC]
     float *stage_ks = red + 4 * QC;                                          // [STAGES][32]: 8 k_scale, 8 log2 v_scale, 8 1 / v_scale, pages mask
     uint64_t *bars = reinterpret_cast<uint64_t *>(stage_ks + STAGES * 32);
     const uint32_t bar0 = smem_u32(bars);
@@ -298,12 +353,12 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(kfull(s), 1); mbar_init(vfull(s), 1); mbar_init(empty(s), 1); }
         for (int i = 0; i < 2; ++i) mbar_init(sfull(i), 1);
-        for (int i = 0; i < PB; ++i) { mbar_init(pfull(i), 4); mbar_init(pdone(i), 1); }
-        mbar_init(qfull, 4);
+        for (int i = 0; i < PB; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
+        mbar_init(qfull, 4 * WGS);
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 5) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
+    if (warp == kWarpMma) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -312,7 +367,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 
     bool dead = false;                                    // a bounded wait gave up: no further waits, run out
     auto wait = [&](uint32_t bar, uint32_t parity, unsigned int code) {
-        if (dead) return;
+        if (dead || mbar_try_wait(bar, parity)) return;
         if (*abort_flag || !mbar_wait(bar, parity)) {
             if (!*abort_flag) atomicExch(a.status, code);
             *abort_flag = 1;
@@ -320,7 +375,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         }
     };
 
-    if (warp == 4) {
+    if (warp == kWarpTma) {
         // ------------------------------------------------------------------------ producer: pages by TMA, scales
         const int lg_ppt = 7 - a.page_shift, ppt = 1 << lg_ppt;               // pages of a tile
         const int tiles_batch = 32 >> lg_ppt;                                 // a lane looks after one page of the next 32
@@ -386,7 +441,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 mbar_wait(kfull(i % STAGES), (uint32_t)(i / STAGES) & 1u);
                 mbar_wait(vfull(i % STAGES), (uint32_t)(i / STAGES) & 1u);
             }
-    } else if (warp == 5) {
+    } else if (warp == kWarpMma) {
         // ------------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
             constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO);
@@ -420,7 +475,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             mma_f8(tmem_o, desc_mnmajor_sw128(v_tile(st) + k * 4096, kTileBytes),
-                                   desc_mnmajor_sw128(p_tile(pb) + term * QC + k * 4096, kTileBytes), kIdescO,
+                                   desc_mn_rows<C::PW>(p_tile(pb) + (term * kTile + k * 32) * C::PW), kIdescO,
                                    (!first || term || k) ? 1u : 0u);
                     mma_commit(empty(st));
                     mma_commit(pdone(pb));
@@ -439,16 +494,17 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         }
     } else {
         // ------------------------------------------------------------------------ softmax
-        const uint32_t lane_addr = (uint32_t)(warp * 32) << 16;
-        const uint32_t sw = (uint32_t)(tid & 7);
+        const int wg = warp >> 2, row = tid & 127, c_wg = wg * QW;            // this thread's token / channel, its first column
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
+        const float2 *col2 = reinterpret_cast<const float2 *>(col);           // [2 p] factors, [2 p + 1] -Mu of columns 2 p, 2 p + 1
         Work<MODE> w = w0;
         Segment s;
         int it = 0;
         while (w.next(a, QC, s)) {
             const int n_cols = s.n_tok * a.G;
             // -- the query columns as e4m3 terms, each column with a power of two of its own
-            for (int c = warp; c < QC; c += 4) {
+            for (int c = warp; c < QC; c += 4 * WGS) {
                 float x[4] = {0.f, 0.f, 0.f, 0.f};
                 float qs = 1.f;
                 if (c < n_cols) {
@@ -464,9 +520,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
                 }
                 if (lane == 0) {
-                    col_cs[c] = qs * a.scale_log2;
-                    col_mu[c] = kMuNone;
-                    col_lim[c] = s.see0 + c / a.G;
+                    col[(c >> 1) * 4 + (c & 1)] = qs * a.scale_log2;
+                    col[(c >> 1) * 4 + 2 + (c & 1)] = 0.f;
+                    col_lim[c] = c < n_cols ? s.see0 + c / a.G : 0;
+                    col_set[c] = c < n_cols ? 0 : 1;
                 }
 #pragma unroll
                 for (int i = 0; i < QT; ++i) {
@@ -482,124 +539,158 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                     }
                     const uint32_t codes = to_e4m3x2(t[0], t[1]) | to_e4m3x2(t[2], t[3]) << 16;
-                    const uint32_t row = (uint32_t)(i * QC + c);
-                    *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + row * 128 + ((((uint32_t)lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4) = codes;
+                    const uint32_t r = (uint32_t)(i * QC + c);
+                    *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + mn_chunk<128>(r, (uint32_t)lane >> 2) + (lane & 3) * 4) = codes;
                 }
             }
             if constexpr (!C::CHAIN && NS > QC * QT)
                 for (int r = QC * QT + warp; r < NS; r += 4)
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + r * 128 + lane * 4) = 0u;
             fence_proxy_async();
-            softmax_bar();                                 // col_* are read by all four warps
+            softmax_bar(3, kSoftmax);                      // the col arrays are read by all warps
             if (lane == 0) mbar_arrive(qfull);
 
-            float l[QC];
+            float2 l[QW / 2];
 #pragma unroll
-            for (int c = 0; c < QC; ++c) l[c] = 0.f;
-            unsigned long long poison = 0;                 // columns whose channel `tid` met a NaN value
+            for (int p = 0; p < QW / 2; ++p) l[p] = make_float2(0.f, 0.f);
+            unsigned long long poison = 0;                 // columns (of the warpgroup) whose channel `row` met a NaN value
+            bool raise = true;                             // some column's Mu does not stand for a maximum yet
 
             for (int t = s.t0; t < s.t1; ++t, ++it) {
                 const int st = it % STAGES, pb = it % PB;
                 wait(vfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnSoftmax);
                 const float *sc = stage_ks + st * 32;
-                const int pg = tid >> a.page_shift;
+                const int pg = row >> a.page_shift;
                 const float ks = sc[pg], lvs = sc[8 + pg];
                 float ivs = sc[16 + pg];
                 const uint32_t have = reinterpret_cast<const uint32_t *>(sc)[24];
-                const int tok = t * kTile + tid;
+                const int tok = t * kTile + row;
                 // columns may see a different number of this tile's tokens, or pages may be missing
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
                 wait(sfull(it & 1), (uint32_t)(it >> 1) & 1u, kErrAttnSoftmax);
                 tc_fence_after();
-                float x[QC];
+                float2 y[QW / 2];                          // x - Mu
+                float excess = -INFINITY;
                 {
-                    const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr;
-                    float raw[NS];
+                    const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
+                    const float2 ks2 = make_float2(ks, ks), lvs2 = make_float2(lvs, lvs), term2 = make_float2(kTerm, kTerm);
+                    constexpr int kLoad = C::CHAIN ? (QW < 32 ? QW : 32) : NS;   // columns in registers at a time
+                    constexpr int kPart = C::CHAIN ? kLoad : QW;
 #pragma unroll
-                    for (int c0 = 0; c0 < NS; c0 += 16) tmem_ld16(ts + c0, *reinterpret_cast<float(*)[16]>(raw + c0));
-                    tmem_ld_wait();
+                    for (int c0 = 0; c0 < QW; c0 += kPart) {
+                        float raw[kLoad];
+                        tmem_ld<kLoad>(ts + c0, raw);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < QC; ++c) {
-                        if (C::CHAIN) {
-                            x[c] = raw[c];
-                        } else {
-                            float v = raw[(QT - 1) * QC + c];
+                        for (int p = 0; p < kPart / 2; ++p) {
+                            float2 v;
+                            if constexpr (C::CHAIN) {
+                                v = make_float2(raw[2 * p], raw[2 * p + 1]);
+                            } else {
+                                v = make_float2(raw[(QT - 1) * QC + 2 * p], raw[(QT - 1) * QC + 2 * p + 1]);
 #pragma unroll
-                            for (int i = QT - 2; i >= 0; --i) v = fmaf(v, kTerm, raw[i * QC + c]);
-                            x[c] = v;
+                                for (int i = QT - 2; i >= 0; --i)
+                                    v = fma2(v, term2, make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
+                            }
+                            const int pc = (c_wg + c0) / 2 + p;
+                            v = fma2(v, mul2(ks2, col2[2 * pc]), add2(lvs2, col2[2 * pc + 1]));
+                            if (!masked) excess = max3(excess, v.x, v.y);
+                            y[c0 / 2 + p] = v;
                         }
                     }
                 }
-                float excess = -INFINITY;
+                if (masked) {
 #pragma unroll
-                for (int c = 0; c < QC; ++c) {
-                    x[c] = fmaf(x[c], ks * col_cs[c], lvs);
-                    if (masked) x[c] = valid && tok < col_lim[c] && c < n_cols ? x[c] : -INFINITY;
-                    excess = fmaxf(excess, x[c] - col_mu[c]);
+                    for (int p = 0; p < QW / 2; ++p) {
+                        if (!(valid && tok < col_lim[c_wg + 2 * p])) y[p].x = -INFINITY;
+                        if (!(valid && tok < col_lim[c_wg + 2 * p + 1])) y[p].y = -INFINITY;
+                        excess = max3(excess, y[p].x, y[p].y);
+                    }
+                    if (!valid) ivs = 0.f;
                 }
-                if (masked && !valid) ivs = 0.f;
-                if (softmax_any(excess > kLagMax)) {
-                    // raise Mu to 6 below the column maxima, rescale what has been summed
+                if (softmax_any(excess > kLagMax || raise, 1 + wg, 128)) {
+                    // Mu to 6 below the column maxima, and what has been summed rescaled
                     if (t > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
 #pragma unroll
-                    for (int c = 0; c < QC; ++c) {
-                        const float m = warp_max(x[c]);
-                        if (lane == 0) red[warp * QC + c] = m;
+                    for (int p = 0; p < QW / 2; ++p) {
+                        const float m0 = warp_max(y[p].x), m1 = warp_max(y[p].y);
+                        if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + 2 * p) = make_float2(m0, m1);
                     }
-                    softmax_bar();
-                    for (int c = tid; c < QC; c += 128) {
+                    softmax_bar(1 + wg, 128);
+                    bool unset = false;
+                    if (row < QW) {
+                        const int c = c_wg + row;
                         const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - kLagTo;
-                        const float old = col_mu[c], mu = m > old ? m : old;
-                        col_mu[c] = mu;
-                        col_f[c] = ex2(old - mu);
+                        const bool first = col_set[c] == 0, seen = m > -INFINITY;
+                        const float d = seen && (first || m > 0.f) ? m : 0.f;
+                        col[(c >> 1) * 4 + 2 + (c & 1)] -= d;
+                        col_d[c] = d;
+                        col_f[c] = first ? 1.f : ex2(-d);  // nothing has been summed yet
+                        if (seen) col_set[c] = 1;
+                        unset = first && !seen;
                     }
-                    softmax_bar();
+                    raise = softmax_any(unset, 1 + wg, 128);
 #pragma unroll
-                    for (int c = 0; c < QC; ++c) l[c] *= col_f[c];
+                    for (int p = 0; p < QW / 2; ++p) {
+                        const float2 d = *reinterpret_cast<const float2 *>(col_d + c_wg + 2 * p);
+                        y[p].x -= d.x; y[p].y -= d.y;
+                        l[p] = mul2(l[p], *reinterpret_cast<const float2 *>(col_f + c_wg + 2 * p));
+                    }
                     if (t > s.t0) {
                         tc_fence_after();
+                        constexpr int kCols = C::CHAIN ? QW : NO;
 #pragma unroll 1
-                        for (int c0 = 0; c0 < NO; c0 += 16) {
+                        for (int c0 = 0; c0 < kCols; c0 += 16) {
                             float o[16];
-                            tmem_ld16(tmem_o + lane_addr + c0, o);
+                            tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] *= col_f[(c0 + e) % QC];
-                            tmem_st16(tmem_o + lane_addr + c0, o);
+                            for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC];
+                            tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
                         }
                         tmem_st_wait();
                     }
                 }
                 // weights, their sum, their e4m3 terms
+                const float2 ivs2 = make_float2(ivs, ivs);
 #pragma unroll
-                for (int c = 0; c < QC; ++c) {
-                    x[c] = ex2(x[c] - col_mu[c]);
-                    l[c] = fmaf(x[c], ivs, l[c]);
+                for (int p = 0; p < QW / 2; ++p) {
+                    y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
+                    l[p] = fma2(y[p], ivs2, l[p]);
                 }
-                // PV(it - PB) has read this weight buffer
+                // the product that read this weight buffer is done
                 if (it >= PB) wait(pdone(pb), (uint32_t)((it - PB) / PB) & 1u, kErrAttnSoftmax);
-                uint8_t *prow = gbase + C::kOffP + pb * kTileBytes + tid * 128;
+                uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
+                const float2 minus = make_float2(-1.f, -1.f);
                 if constexpr (C::CHAIN) {
+                    // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not make up
+                    // for it: an error below 2^-10 beside a largest weight of 2^6 and more
 #pragma unroll
                     for (int i = 0; i < PT; ++i)
 #pragma unroll
-                        for (int c0 = 0; c0 < QC; c0 += 16) {
+                        for (int c0 = 0; c0 < QW; c0 += 16) {
                             uint32_t u[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                float y[4];
+                                uint32_t half[2];
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const int c = c0 + 4 * k + e;
-                                    y[e] = i < PT - 1 ? lead4(x[c]) : x[c];
-                                    x[c] -= y[e];
+                                for (int e = 0; e < 2; ++e) {
+                                    float2 &v = y[c0 / 2 + 2 * k + e];
+                                    float2 h = v;
+                                    if (i < PT - 1) {
+                                        h.x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
+                                        h.y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
+                                        v = fma2(h, minus, v);
+                                    }
+                                    half[e] = to_e4m3x2(h.x, h.y);
                                 }
-                                u[k] = to_e4m3x2(y[0], y[1]) | to_e4m3x2(y[2], y[3]) << 16;
+                                u[k] = __byte_perm(half[0], half[1], 0x5410);
                             }
-                            *reinterpret_cast<uint4 *>(prow + ((((uint32_t)(i * QC + c0) >> 4) ^ sw) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+                            *reinterpret_cast<uint4 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)(c_wg + c0) >> 4)) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
                 } else {
+                    const float2 sixteen = make_float2(16.f, 16.f);
                     uint32_t u[NO / 4];
 #pragma unroll
                     for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
@@ -607,51 +698,53 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     for (int i = 0; i < PT; ++i)
 #pragma unroll
                         for (int c0 = 0; c0 < QC; c0 += 4) {
-                            float y[4];
+                            uint32_t half[2];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int c = c0 + e;
-                                y[e] = i < PT - 1 ? lead4(x[c]) : x[c];
-                                x[c] = (x[c] - y[e]) * 16.0f;
+                            for (int e = 0; e < 2; ++e) {
+                                float2 &v = y[c0 / 2 + e];
+                                float2 h = v;
+                                if (i < PT - 1) {
+                                    h = make_float2(lead4(v.x), lead4(v.y));
+                                    v = mul2(fma2(h, minus, v), sixteen);
+                                }
+                                half[e] = to_e4m3x2(h.x, h.y);
                             }
-                            u[(i * QC + c0) / 4] = to_e4m3x2(y[0], y[1]) | to_e4m3x2(y[2], y[3]) << 16;
+                            u[(i * QC + c0) / 4] = __byte_perm(half[0], half[1], 0x5410);
                         }
 #pragma unroll
                     for (int k = 0; k < NO / 16; ++k)
-                        *reinterpret_cast<uint4 *>(prow + (((uint32_t)k ^ sw) << 4)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+                        *reinterpret_cast<uint4 *>(prow + mn_chunk<C::PW>(row, k)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
                 }
-                if (masked) {
-                    uint8_t *vrow = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes + tid * 128;
-                    if (!valid) {                          // 0 * NaN is not 0: values behind the end must not reach the product
+                uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
+                if (masked && !valid && wg == 0) {         // 0 * NaN is not 0: values behind the end must not reach the product
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vrow)[k] = make_uint4(0u, 0u, 0u, 0u);
-                    }
+                    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vtile + row * 128)[k] = make_uint4(0u, 0u, 0u, 0u);
                 }
                 if (MODE == 1 && s.n_tok > 1 && (t + 1) * kTile > s.see0) {
                     // a NaN value of a token that some columns see and others do not: taken out of the product, and noted
                     // for the columns that see it
-                    uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
                     bool nan = false;
-                    if (valid) {
+                    if (valid && wg == 0) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
-                            const uint4 v = reinterpret_cast<const uint4 *>(vtile + tid * 128)[k];
+                            const uint4 v = reinterpret_cast<const uint4 *>(vtile + row * 128)[k];
                             const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) nan |= __vcmpeq4(u[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
                         }
                     }
-                    if (softmax_any(nan)) {
-                        for (int r = 0; r < kTile; ++r) {
-                            const int pos = t * kTile + r;
-                            if (pos >= s.live) break;
-                            uint8_t *cell = vtile + r * 128 + ((((uint32_t)tid >> 4) ^ (r & 7)) << 4) + (tid & 15);
-                            if ((*cell & 0x7f) == 0x7f) {
-                                const int c = max(0, pos + 1 - s.see0) * a.G;          // first column that sees it
+                    if (softmax_any(nan, 3, kSoftmax)) {
+                        const int n = min(kTile, s.live - t * kTile);
+                        auto cell = [&](int r) { return vtile + mn_chunk<128>(r, (uint32_t)row >> 4) + (row & 15); };
+                        for (int r = 0; r < n; ++r)
+                            if ((*cell(r) & 0x7f) == 0x7f) {
+                                const int c = max(0, max(0, t * kTile + r + 1 - s.see0) * a.G - c_wg);   // first column that sees it
                                 if (c < 64) poison |= ~0ull << c;
-                                *cell = 0;
                             }
-                        }
+                        softmax_bar(3, kSoftmax);
+                        if (wg == 0)
+                            for (int r = 0; r < n; ++r)
+                                if ((*cell(r) & 0x7f) == 0x7f) *cell(r) = 0;
                     }
                 }
                 fence_proxy_async();
@@ -662,23 +755,27 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 
             // -- the segment's end: sums over the 128 token rows, then this thread's channel of every column
 #pragma unroll
-            for (int c = 0; c < QC; ++c) {
-                float v = l[c];
+            for (int p = 0; p < QW / 2; ++p) {
+                float2 v = l[p];
 #pragma unroll
-                for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (lane == 0) red[warp * QC + c] = v;
+                for (int o = 16; o; o >>= 1) {
+                    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+                    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+                }
+                if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + 2 * p) = v;
             }
             if (s.t1 > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
             tc_fence_after();
-            softmax_bar();
+            softmax_bar(3, kSoftmax);
             const bool whole = MODE == 0 ? s.t0 == 0 && s.t1 == s.tiles : a.splits == 1;
             float *slot = nullptr;
             if (!whole) {
                 const size_t head = MODE == 0 ? 16 + sizeof(UnitMeta) * (size_t)a.B * a.H : 0;
                 slot = reinterpret_cast<float *>(a.ws + head) + (size_t)s.slot * attn_slot_floats(QC);
-                for (int c = tid; c < n_cols; c += 128) {
-                    slot[c] = col_mu[c];
-                    slot[QC + c] = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                for (int c = tid; c < n_cols; c += kSoftmax) {
+                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                    slot[c] = sum == 0.f ? kMuNone : -col[(c >> 1) * 4 + 2 + (c & 1)];
+                    slot[QC + c] = sum;
                 }
             }
             if constexpr (MODE == 0)
@@ -687,40 +784,47 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     m->first = w.pos - (s.t1 - s.t0);
                     m->tiles = s.tiles;
                 }
-            float raw[NO];
+            auto put = [&](int c, float v) {
+                if (c >= n_cols) return;
+                if (s.t1 == s.t0) v = 0.f;                 // an empty split
+                if (MODE == 1 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
+                if (whole) {
+                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                    const float o = sum == 0.f ? 0.f : __fdiv_rn(v, sum);
+                    store1(static_cast<T *>(a.out) + ((size_t)(s.tok0 + c / a.G) * a.H * a.G + (size_t)s.h * a.G + c % a.G) * kHeadDim + row, o);
+                } else {
+                    slot[2 * QC + (size_t)c * kHeadDim + row] = v;
+                }
+            };
+            if constexpr (C::CHAIN) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < QW; c0 += 16) {
+                    float o[16];
+                    tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
+                    tmem_ld_wait();
 #pragma unroll
-            for (int c0 = 0; c0 < NO; c0 += 16) tmem_ld16(tmem_o + lane_addr + c0, *reinterpret_cast<float(*)[16]>(raw + c0));
-            tmem_ld_wait();
+                    for (int e = 0; e < 16; ++e) put(c_wg + c0 + e, o[e]);
+                }
+            } else {
+                float o[NO];
+                tmem_ld<NO>(tmem_o + lane_addr, o);
+                tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < QC; ++c) {
-                if (c < n_cols) {
-                    float v;
-                    if (C::CHAIN) {
-                        v = raw[c];
-                    } else {
-                        v = raw[(PT - 1) * QC + c];
+                for (int c = 0; c < QC; ++c) {
+                    float v = o[(PT - 1) * QC + c];
 #pragma unroll
-                        for (int i = PT - 2; i >= 0; --i) v = fmaf(v, kTerm, raw[i * QC + c]);
-                    }
-                    if (s.t1 == s.t0) v = 0.f;             // an empty split
-                    if (MODE == 1 && c < 64 && ((poison >> c) & 1ull)) v = __uint_as_float(0x7fffffffu);
-                    if (whole) {
-                        const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
-                        const float y = sum == 0.f ? 0.f : __fdiv_rn(v, sum);
-                        store1(static_cast<T *>(a.out) + ((size_t)(s.tok0 + c / a.G) * a.H * a.G + (size_t)s.h * a.G + c % a.G) * kHeadDim + tid, y);
-                    } else {
-                        slot[2 * QC + (size_t)c * kHeadDim + tid] = v;
-                    }
+                    for (int i = PT - 2; i >= 0; --i) v = fmaf(v, kTerm, o[i * QC + c]);
+                    put(c, v);
                 }
             }
             tc_fence_before();
-            softmax_bar();                                 // red and col_* are free for the next segment
+            softmax_bar(3, kSoftmax);                      // red and the col arrays are free for the next segment
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == kWarpMma) {
         tc_fence_after();
         tmem_dealloc(tmem, C::kTmemCols);
     }
@@ -766,14 +870,34 @@ __global__ void __launch_bounds__(kHeadDim) k_page_attn_join(const AttnArgs a, c
         const long long at = MODE == 0 ? (i == 0 ? first_slot + first_odd : first_slot + 2LL * i) : first_slot + i;
         return slots + (size_t)at * attn_slot_floats(qc);
     };
-    float mu = kMuNone;
-    for (int i = 0; i < n; ++i) mu = fmaxf(mu, slot(i)[c]);
-    float sum = 0.f, o = 0.f;
-    for (int i = 0; i < n; ++i) {
-        const float *p = slot(i);
-        const float f = ex2(p[c] - mu);
-        sum = fmaf(p[qc + c], f, sum);
-        o = fmaf(p[2 * qc + (size_t)c * kHeadDim + d], f, o);
+    // 128 parts at a time: their Mu and sums by one thread each, then every thread adds up its channel
+    __shared__ float f_s[kHeadDim], red_s[2][4];
+    float mu = kMuNone, sum = 0.f, o = 0.f;
+    for (int i0 = 0; i0 < n; i0 += kHeadDim) {
+        const int k = min(kHeadDim, n - i0);
+        float m = kMuNone, l = 0.f;
+        if (d < k) {
+            const float *p = slot(i0 + d);
+            m = p[c];
+            l = p[qc + c];
+        }
+        const float wm = warp_max(m);
+        if ((d & 31) == 0) red_s[0][d >> 5] = wm;
+        __syncthreads();
+        const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
+        const float f = ex2(m - top), back = ex2(mu - top);
+        f_s[d] = f;
+        l *= f;
+#pragma unroll
+        for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+        if ((d & 31) == 0) red_s[1][d >> 5] = l;
+        __syncthreads();
+        sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
+        o *= back;
+        mu = top;
+#pragma unroll 8
+        for (int i = 0; i < k; ++i) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);
+        __syncthreads();
     }
     store1(static_cast<T *>(a.out) + out_row * kHeadDim + d, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
 }

@@ -215,6 +215,15 @@ template <typename T> struct Raw8;                        // 8 consecutive eleme
 template <> struct Raw8<__nv_bfloat16> {
     uint4 v;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
+    // the largest magnitude so far, as bits: two bf16 maxima side by side until to_float_bits()
+    __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+        m = __vmaxu2(m, v.x & 0x7fff7fffu);
+        m = __vmaxu2(m, v.y & 0x7fff7fffu);
+        m = __vmaxu2(m, v.z & 0x7fff7fffu);
+        return __vmaxu2(m, v.w & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ uint32_t to_float_bits(uint32_t m) const { return max(m << 16, m & 0xffff0000u); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -230,6 +239,14 @@ template <> struct Raw8<float> {
         a = __ldcs(reinterpret_cast<const float4 *>(p));
         b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
     }
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ uint32_t to_float_bits(uint32_t m) const { return m; }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
         x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -248,8 +265,9 @@ struct StoreArgs {
     unsigned int *status;
 };
 
-// Grid (tiles of consecutive tokens, 2 H).  The tokens of one page are a run of consecutive tokens with ascending slots;
-// a CTA owns the runs that START in its tile, one (tensor, head) of them: 16 threads per row of 128, 8 elements a thread.
+// Grid: 2 H CTAs for each tile of consecutive tokens, one (tensor, head) each and next to one another, so that a token's
+// row is read from memory while it is open.  The tokens of one page are a run of consecutive tokens with ascending slots;
+// a CTA owns the runs that START in its tile: 16 threads per row of 128, 8 elements a thread.
 // It reads a run once into registers, takes the largest finite magnitude, settles the page's scale, re-rounds the page's
 // older rows if the scale grew, and writes the new codes: the data is read once and written once.
 template <typename T, int PAGE>
@@ -259,8 +277,8 @@ __global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a)
     __shared__ uint32_t start_s[(2 * PAGE + 31) / 32];    // bit j: token j of the tile starts a run
     __shared__ uint32_t max_s[kStoreThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int which = blockIdx.y & 1, h = blockIdx.y >> 1;
-    const long long i0 = (long long)blockIdx.x * a.tile;
+    const int unit = blockIdx.x % (2 * a.H), which = unit & 1, h = unit >> 1;
+    const long long i0 = (long long)(blockIdx.x / (2 * a.H)) * a.tile;
     const long long limit = (long long)a.n_pages * PAGE;
     const int n_here = (int)min((long long)a.tile + PAGE, a.n_tokens - i0);   // tokens looked at: a run may end behind the tile
     for (int j = tid; j <= n_here; j += kStoreThreads) slot_s[j] = i0 + j == 0 ? -2 : a.slots[i0 + j - 1];
@@ -281,17 +299,23 @@ __global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a)
     float *scales = a.scale[which];
     const int c8 = (tid & 15) * 8, row_t = tid >> 4;
     const int n_tile = min(a.tile, n_here);
-    for (int j = 0; j < n_tile; ++j) {
-        if (!((start_s[j >> 5] >> (j & 31)) & 1u)) continue;
+    auto next_start = [&](int j) {                        // the first run that starts at or behind j
+        int k = j >> 5;
+        const int words = (n_here + 31) >> 5;
+        if (k >= words) return n_here;
+        uint32_t m = start_s[k] & (~0u << (j & 31));
+        while (m == 0u && ++k < words) m = start_s[k];
+        return m == 0u ? n_here : min(n_here, 32 * k + __ffs(m) - 1);
+    };
+    for (int j = next_start(0), j_next; j < n_tile; j = j_next) {
+        j_next = next_start(j + 1);
         const int slot = slot_s[j + 1];
         if (slot < 0) continue;
         if (slot >= limit) {
             if (tid == 0) flag(a.status, kBadSlot);
             continue;
         }
-        int n = 1;                                        // run length: up to the next start
-        const int r0 = slot % PAGE;
-        while (j + n < n_here && n < PAGE - r0 && !((start_s[(j + n) >> 5] >> ((j + n) & 31)) & 1u)) ++n;
+        const int r0 = slot % PAGE, n = min(j_next - j, PAGE - r0);
         const int pg = slot / PAGE;
         const T *src = x + (size_t)(i0 + j) * a.ld;
         Raw8<T> raw[kIter];
@@ -300,14 +324,17 @@ __global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a)
         for (int k = 0; k < kIter; ++k) {
             const int r = row_t + k * kRows;
             if (r < n) raw[k].load(src + (size_t)r * a.ld + c8);
+            else raw[k].zero();
         }
 #pragma unroll
-        for (int k = 0; k < kIter; ++k) {
-            if (row_t + k * kRows < n) {
-                float v[8];
-                raw[k].get(v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(v[e]));
+        for (int k = 0; k < kIter; ++k) amax = raw[k].max_bits(amax);
+        amax = raw[0].to_float_bits(amax);
+        if (amax >= 0x7f800000u) {                        // an infinity or NaN among them: again, without those
+            amax = 0;
+#pragma unroll 1
+            for (int k = 0; k < kIter; ++k) {
+                const int r = row_t + k * kRows;
+                for (int e = 0; r < n && e < 8; ++e) amax = max(amax, finite_bits(load1(src + (size_t)r * a.ld + c8 + e)));
             }
         }
         amax = __reduce_max_sync(0xffffffffu, amax);

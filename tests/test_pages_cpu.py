@@ -48,6 +48,7 @@ def _bare(fk, **kw):
     pg = object.__new__(fk.Pages)
     pg.__dict__.update(dict(n_kv_heads=2, n_q_heads=4, page_size=16, n_pages=3, max_pages=4, max_batch=2, kv_dtype=fk.BF16, head_dim=128,
                             device=torch.device("cpu"), _h=None), **kw)
+    pg._shapes()
     return pg
 
 
