@@ -19,7 +19,7 @@
 // some x exceeds it by 8, and then to 6 below the maximum, so weights stay in e4m3's range and most tiles exchange one
 // vote instead of a maximum per column.  O stays in TMEM over all tiles of a segment.
 //
-// A CTA: one or two softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
+// A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.
 #pragma once
 #include "common.cuh"
@@ -56,7 +56,7 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int STA
     static constexpr uint32_t kOffMisc = kOffP + PBUFS * kPBytes;
     static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (10 * QC + STAGES * 32) + 256 + 1024;
     static_assert(!CHAIN || PW == NO, "a chained term fills its rows");
-    static_assert(WGS == 1 || CHAIN, "two warpgroups share chained columns");
+    static_assert(WGS == 1 || CHAIN, "warpgroups share chained columns");
 };
 
 struct AttnArgs {
@@ -497,7 +497,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const int wg = warp >> 2, row = tid & 127, c_wg = wg * QW;            // this thread's token / channel, its first column
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
-        const float2 *col2 = reinterpret_cast<const float2 *>(col);           // [2 p] factors, [2 p + 1] -Mu of columns 2 p, 2 p + 1
+        const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
         Work<MODE> w = w0;
         Segment s;
         int it = 0;
@@ -538,7 +538,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             t[e] = x[e];
                         }
                     }
-                    const uint32_t codes = to_e4m3x2(t[0], t[1]) | to_e4m3x2(t[2], t[3]) << 16;
+                    const uint32_t codes = to_e4m3x4(t[0], t[1], t[2], t[3]);
                     const uint32_t r = (uint32_t)(i * QC + c);
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + mn_chunk<128>(r, (uint32_t)lane >> 2) + (lane & 3) * 4) = codes;
                 }
@@ -547,7 +547,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 for (int r = QC * QT + warp; r < NS; r += 4)
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + r * 128 + lane * 4) = 0u;
             fence_proxy_async();
-            softmax_bar(3, kSoftmax);                      // the col arrays are read by all warps
+            softmax_bar(1, kSoftmax);                      // the col arrays are read by all warps
             if (lane == 0) mbar_arrive(qfull);
 
             float2 l[QW / 2];
@@ -594,7 +594,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                     v = fma2(v, term2, make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
                             }
                             const int pc = (c_wg + c0) / 2 + p;
-                            v = fma2(v, mul2(ks2, col2[2 * pc]), add2(lvs2, col2[2 * pc + 1]));
+                            const float4 fm = col4[pc];
+                            v = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), add2(lvs2, make_float2(fm.z, fm.w)));
                             if (!masked) excess = max3(excess, v.x, v.y);
                             y[c0 / 2 + p] = v;
                         }
@@ -609,7 +610,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                     if (!valid) ivs = 0.f;
                 }
-                if (softmax_any(excess > kLagMax || raise, 1 + wg, 128)) {
+                if (softmax_any(excess > kLagMax || raise, 2 + wg, 128)) {
                     // Mu to 6 below the column maxima, and what has been summed rescaled
                     if (t > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
 #pragma unroll
@@ -617,7 +618,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         const float m0 = warp_max(y[p].x), m1 = warp_max(y[p].y);
                         if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + 2 * p) = make_float2(m0, m1);
                     }
-                    softmax_bar(1 + wg, 128);
+                    softmax_bar(2 + wg, 128);
                     bool unset = false;
                     if (row < QW) {
                         const int c = c_wg + row;
@@ -630,7 +631,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         if (seen) col_set[c] = 1;
                         unset = first && !seen;
                     }
-                    raise = softmax_any(unset, 1 + wg, 128);
+                    raise = softmax_any(unset, 2 + wg, 128);
 #pragma unroll
                     for (int p = 0; p < QW / 2; ++p) {
                         const float2 d = *reinterpret_cast<const float2 *>(col_d + c_wg + 2 * p);
@@ -673,19 +674,18 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             uint32_t u[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                uint32_t half[2];
+                                float2 h[2];
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
                                     float2 &v = y[c0 / 2 + 2 * k + e];
-                                    float2 h = v;
+                                    h[e] = v;
                                     if (i < PT - 1) {
-                                        h.x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
-                                        h.y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                        v = fma2(h, minus, v);
+                                        h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
+                                        h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
+                                        v = fma2(h[e], minus, v);
                                     }
-                                    half[e] = to_e4m3x2(h.x, h.y);
                                 }
-                                u[k] = __byte_perm(half[0], half[1], 0x5410);
+                                u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
                             }
                             *reinterpret_cast<uint4 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)(c_wg + c0) >> 4)) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
@@ -698,18 +698,17 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     for (int i = 0; i < PT; ++i)
 #pragma unroll
                         for (int c0 = 0; c0 < QC; c0 += 4) {
-                            uint32_t half[2];
+                            float2 h[2];
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float2 &v = y[c0 / 2 + e];
-                                float2 h = v;
+                                h[e] = v;
                                 if (i < PT - 1) {
-                                    h = make_float2(lead4(v.x), lead4(v.y));
-                                    v = mul2(fma2(h, minus, v), sixteen);
+                                    h[e] = make_float2(lead4(v.x), lead4(v.y));
+                                    v = mul2(fma2(h[e], minus, v), sixteen);
                                 }
-                                half[e] = to_e4m3x2(h.x, h.y);
                             }
-                            u[(i * QC + c0) / 4] = __byte_perm(half[0], half[1], 0x5410);
+                            u[(i * QC + c0) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
                         }
 #pragma unroll
                     for (int k = 0; k < NO / 16; ++k)
@@ -733,7 +732,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             for (int e = 0; e < 4; ++e) nan |= __vcmpeq4(u[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
                         }
                     }
-                    if (softmax_any(nan, 3, kSoftmax)) {
+                    if (softmax_any(nan, 1, kSoftmax)) {
                         const int n = min(kTile, s.live - t * kTile);
                         auto cell = [&](int r) { return vtile + mn_chunk<128>(r, (uint32_t)row >> 4) + (row & 15); };
                         for (int r = 0; r < n; ++r)
@@ -741,7 +740,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 const int c = max(0, max(0, t * kTile + r + 1 - s.see0) * a.G - c_wg);   // first column that sees it
                                 if (c < 64) poison |= ~0ull << c;
                             }
-                        softmax_bar(3, kSoftmax);
+                        softmax_bar(1, kSoftmax);
                         if (wg == 0)
                             for (int r = 0; r < n; ++r)
                                 if ((*cell(r) & 0x7f) == 0x7f) *cell(r) = 0;
@@ -766,7 +765,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
             if (s.t1 > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
             tc_fence_after();
-            softmax_bar(3, kSoftmax);
+            softmax_bar(1, kSoftmax);
             const bool whole = MODE == 0 ? s.t0 == 0 && s.t1 == s.tiles : a.splits == 1;
             float *slot = nullptr;
             if (!whole) {
@@ -818,7 +817,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
             }
             tc_fence_before();
-            softmax_bar(3, kSoftmax);                      // red and the col arrays are free for the next segment
+            softmax_bar(1, kSoftmax);                      // red and the col arrays are free for the next segment
         }
     }
     __syncwarp();

@@ -191,14 +191,19 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
     const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
     return u < 0x7f800000u ? u : 0u;
 }
-// Two e4m3 codes, round to nearest even, |x| > 448 and infinities to 448, NaN to NaN.
-__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
-    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+// e4m3 codes, round to nearest even, |x| > 448 and infinities to 448, NaN to NaN; the first in the lowest byte.
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
 }
 __device__ __forceinline__ uint2 to_e4m3x8(const float (&x)[8], float mul) {
     uint2 r;
-    r.x = to_e4m3x2(x[0] * mul, x[1] * mul) | to_e4m3x2(x[2] * mul, x[3] * mul) << 16;
-    r.y = to_e4m3x2(x[4] * mul, x[5] * mul) | to_e4m3x2(x[6] * mul, x[7] * mul) << 16;
+    r.x = to_e4m3x4(x[0] * mul, x[1] * mul, x[2] * mul, x[3] * mul);
+    r.y = to_e4m3x4(x[4] * mul, x[5] * mul, x[6] * mul, x[7] * mul);
     return r;
 }
 // The values of two codes (exact: e4m3 is a subset of f16).
