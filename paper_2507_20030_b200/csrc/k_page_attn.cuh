@@ -16,7 +16,7 @@
 //
 // Softmax runs in base 2 with the page scales inside: x = s * (k_scale * scale * log2 e) + log2(v_scale), weights
 // w = 2^(x - Mu), sum l += w / v_scale.  Mu follows the column maximum lazily: it is raised (and O, l rescaled) only when
-// some x exceeds it by 8, and then to 6 below the maximum, so weights stay in e4m3's range and most tiles exchange one
+// some x exceeds it by 8, and then to 2 below the maximum, so weights stay in e4m3's range and most tiles exchange one
 // vote instead of a maximum per column.  O stays in TMEM over all tiles of a segment.
 //
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
@@ -31,7 +31,7 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr float kLagMax = 8.0f, kLagTo = 6.0f;            // weights stay <= 2^8; after a raise the largest is 2^6
+constexpr float kLagMax = 8.0f, kLagTo = 2.0f;            // weights stay <= 2^8; after a raise the largest is 2^2
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
 
@@ -54,7 +54,7 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int STA
     static constexpr uint32_t kOffQ = STAGES * 2 * kTileBytes;
     static constexpr uint32_t kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
     static constexpr uint32_t kOffMisc = kOffP + PBUFS * kPBytes;
-    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (10 * QC + STAGES * 32) + 256 + 1024;
+    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + STAGES * 32) + 256 + 1024;
     static_assert(!CHAIN || PW == NO, "a chained term fills its rows");
     static_assert(WGS == 1 || CHAIN, "warpgroups share chained columns");
 };
@@ -276,8 +276,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const uint32_t q_base = base + C::kOffQ;
     auto p_tile = [&](int p) { return base + C::kOffP + (uint32_t)p * C::kPBytes; };
     float *col = reinterpret_cast<float *>(gbase + C::kOffMisc);             // per pair of columns: factors of the raw scores, -Mu
-    float *col_d = col + 2 * QC;                                             // [QC] last raise of Mu
-    float *col_f = col_d + QC;                                               // [QC] 2^-raise
+    float *col_f = col + 2 * QC;                                             // [QC] 2^-raise
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
     int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
     float *red = reinterpret_cast<float *>(col_set + QC);                    // [4][QC]
@@ -498,6 +497,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
         const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
+        constexpr int kPart = C::CHAIN ? 16 : QW, kLoad = C::CHAIN ? 16 : NS;  // columns at a time, raw scores of them
         Work<MODE> w = w0;
         Segment s;
         int it = 0;
@@ -558,6 +558,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 
             for (int t = s.t0; t < s.t1; ++t, ++it) {
                 const int st = it % STAGES, pb = it % PB;
+                bool done_max = false;                     // Mu has been set by this tile's maxima
                 wait(vfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnSoftmax);
                 const float *sc = stage_ks + st * 32;
                 const int pg = row >> a.page_shift;
@@ -568,151 +569,166 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 // columns may see a different number of this tile's tokens, or pages may be missing
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
+                if (masked && !valid) ivs = 0.f;
+                const float2 ks2 = make_float2(ks, ks), lvs2 = make_float2(lvs, lvs), ivs2 = make_float2(ivs, ivs);
+                const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
+                // y = x - Mu of the columns c_wg + c0 .. from their raw scores
+                auto exponents = [&](const float(&raw)[kLoad], int c0, float2(&y)[kPart / 2]) {
+#pragma unroll
+                    for (int p = 0; p < kPart / 2; ++p) {
+                        float2 v;
+                        if constexpr (C::CHAIN) {
+                            v = make_float2(raw[2 * p], raw[2 * p + 1]);
+                        } else {
+                            v = make_float2(raw[(QT - 1) * QC + 2 * p], raw[(QT - 1) * QC + 2 * p + 1]);
+#pragma unroll
+                            for (int i = QT - 2; i >= 0; --i)
+                                v = fma2(v, make_float2(kTerm, kTerm), make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
+                        }
+                        const float4 fm = col4[(c_wg + c0) / 2 + p];
+                        y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), add2(lvs2, make_float2(fm.z, fm.w)));
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int p = 0; p < kPart / 2; ++p) {
+                            const int2 lim = *reinterpret_cast<const int2 *>(col_lim + c_wg + c0 + 2 * p);
+                            if (!(valid && tok < lim.x)) y[p].x = -INFINITY;
+                            if (!(valid && tok < lim.y)) y[p].y = -INFINITY;
+                        }
+                    }
+                };
                 wait(sfull(it & 1), (uint32_t)(it >> 1) & 1u, kErrAttnSoftmax);
+                // the product that read this weight buffer is done
+                if (it >= PB) wait(pdone(pb), (uint32_t)((it - PB) / PB) & 1u, kErrAttnSoftmax);
                 tc_fence_after();
-                float2 y[QW / 2];                          // x - Mu
-                float excess = -INFINITY;
-                {
-                    const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
-                    const float2 ks2 = make_float2(ks, ks), lvs2 = make_float2(lvs, lvs), term2 = make_float2(kTerm, kTerm);
-                    constexpr int kLoad = C::CHAIN ? (QW < 32 ? QW : 32) : NS;   // columns in registers at a time
-                    constexpr int kPart = C::CHAIN ? kLoad : QW;
+                uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
+                bool again = false;
+                for (;;) {
+                    if (raise) {
+                        // Mu to 2 below the column maxima, and what has been summed rescaled
+                        if (t > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
+#pragma unroll 1
+                        for (int c0 = 0; c0 < QW; c0 += kPart) {
+                            float raw[kLoad];
+                            float2 y[kPart / 2];
+                            tmem_ld<kLoad>(ts + c0, raw);
+                            tmem_ld_wait();
+                            exponents(raw, c0, y);
+#pragma unroll
+                            for (int p = 0; p < kPart / 2; ++p) {
+                                const float m0 = warp_max(y[p].x), m1 = warp_max(y[p].y);
+                                if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + c0 + 2 * p) = make_float2(m0, m1);
+                            }
+                        }
+                        softmax_bar(2 + wg, 128);
+                        bool unset = false;
+                        if (row < QW) {
+                            const int c = c_wg + row;
+                            const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - kLagTo;
+                            const bool first = col_set[c] == 0, seen = m > -INFINITY;
+                            const float d = seen && (first || m > 0.f) ? m : 0.f;
+                            col[(c >> 1) * 4 + 2 + (c & 1)] -= d;
+                            // 1: nothing has been summed yet; 0: what has been is beyond float32's reach
+                            col_f[c] = first ? 1.f : d > 64.f ? 0.f : ex2(-d);
+                            if (seen) col_set[c] = 1;
+                            unset = first && !seen;
+                        }
+                        raise = softmax_any(unset, 2 + wg, 128);
+#pragma unroll
+                        for (int p = 0; p < QW / 2; ++p) l[p] = mul2(l[p], *reinterpret_cast<const float2 *>(col_f + c_wg + 2 * p));
+                        if (t > s.t0) {
+                            tc_fence_after();
+                            constexpr int kCols = C::CHAIN ? QW : NO;
+#pragma unroll 1
+                            for (int c0 = 0; c0 < kCols; c0 += 16) {
+                                float o[16];
+                                tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC];
+                                tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
+                            }
+                            tmem_st_wait();
+                        }
+                        done_max = true;
+                    }
+                    // weights, their sum, their e4m3 terms
+                    float excess = -INFINITY;
 #pragma unroll
                     for (int c0 = 0; c0 < QW; c0 += kPart) {
                         float raw[kLoad];
+                        float2 y[kPart / 2];
                         tmem_ld<kLoad>(ts + c0, raw);
                         tmem_ld_wait();
+                        exponents(raw, c0, y);
 #pragma unroll
                         for (int p = 0; p < kPart / 2; ++p) {
-                            float2 v;
-                            if constexpr (C::CHAIN) {
-                                v = make_float2(raw[2 * p], raw[2 * p + 1]);
-                            } else {
-                                v = make_float2(raw[(QT - 1) * QC + 2 * p], raw[(QT - 1) * QC + 2 * p + 1]);
-#pragma unroll
-                                for (int i = QT - 2; i >= 0; --i)
-                                    v = fma2(v, term2, make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
+                            excess = max3(excess, y[p].x, y[p].y);
+                            y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
+                            float2 &sum = l[c0 / 2 + p];
+                            if (!again) {
+                                sum = fma2(y[p], ivs2, sum);
+                            } else {                       // this tile is in the sum already, unless that was dropped
+                                const float2 f = *reinterpret_cast<const float2 *>(col_f + c_wg + c0 + 2 * p);
+                                if (f.x == 0.f) sum.x = y[p].x * ivs;
+                                if (f.y == 0.f) sum.y = y[p].y * ivs;
                             }
-                            const int pc = (c_wg + c0) / 2 + p;
-                            const float4 fm = col4[pc];
-                            v = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), add2(lvs2, make_float2(fm.z, fm.w)));
-                            if (!masked) excess = max3(excess, v.x, v.y);
-                            y[c0 / 2 + p] = v;
                         }
-                    }
-                }
-                if (masked) {
+                        const float2 minus = make_float2(-1.f, -1.f);
+                        if constexpr (C::CHAIN) {
+                            // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
+                            // make up for it: an error below 2^-10 beside a largest weight of 2^2 and more
 #pragma unroll
-                    for (int p = 0; p < QW / 2; ++p) {
-                        if (!(valid && tok < col_lim[c_wg + 2 * p])) y[p].x = -INFINITY;
-                        if (!(valid && tok < col_lim[c_wg + 2 * p + 1])) y[p].y = -INFINITY;
-                        excess = max3(excess, y[p].x, y[p].y);
-                    }
-                    if (!valid) ivs = 0.f;
-                }
-                if (softmax_any(excess > kLagMax || raise, 2 + wg, 128)) {
-                    // Mu to 6 below the column maxima, and what has been summed rescaled
-                    if (t > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
+                            for (int i = 0; i < PT; ++i)
 #pragma unroll
-                    for (int p = 0; p < QW / 2; ++p) {
-                        const float m0 = warp_max(y[p].x), m1 = warp_max(y[p].y);
-                        if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + 2 * p) = make_float2(m0, m1);
-                    }
-                    softmax_bar(2 + wg, 128);
-                    bool unset = false;
-                    if (row < QW) {
-                        const int c = c_wg + row;
-                        const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - kLagTo;
-                        const bool first = col_set[c] == 0, seen = m > -INFINITY;
-                        const float d = seen && (first || m > 0.f) ? m : 0.f;
-                        col[(c >> 1) * 4 + 2 + (c & 1)] -= d;
-                        col_d[c] = d;
-                        col_f[c] = first ? 1.f : ex2(-d);  // nothing has been summed yet
-                        if (seen) col_set[c] = 1;
-                        unset = first && !seen;
-                    }
-                    raise = softmax_any(unset, 2 + wg, 128);
+                                for (int j = 0; j < kPart; j += 16) {
+                                    uint32_t u[4];
 #pragma unroll
-                    for (int p = 0; p < QW / 2; ++p) {
-                        const float2 d = *reinterpret_cast<const float2 *>(col_d + c_wg + 2 * p);
-                        y[p].x -= d.x; y[p].y -= d.y;
-                        l[p] = mul2(l[p], *reinterpret_cast<const float2 *>(col_f + c_wg + 2 * p));
-                    }
-                    if (t > s.t0) {
-                        tc_fence_after();
-                        constexpr int kCols = C::CHAIN ? QW : NO;
-#pragma unroll 1
-                        for (int c0 = 0; c0 < kCols; c0 += 16) {
-                            float o[16];
-                            tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
-                            tmem_ld_wait();
+                                    for (int k = 0; k < 4; ++k) {
+                                        float2 h[2];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC];
-                            tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
-                        }
-                        tmem_st_wait();
-                    }
-                }
-                // weights, their sum, their e4m3 terms
-                const float2 ivs2 = make_float2(ivs, ivs);
-#pragma unroll
-                for (int p = 0; p < QW / 2; ++p) {
-                    y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
-                    l[p] = fma2(y[p], ivs2, l[p]);
-                }
-                // the product that read this weight buffer is done
-                if (it >= PB) wait(pdone(pb), (uint32_t)((it - PB) / PB) & 1u, kErrAttnSoftmax);
-                uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
-                const float2 minus = make_float2(-1.f, -1.f);
-                if constexpr (C::CHAIN) {
-                    // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not make up
-                    // for it: an error below 2^-10 beside a largest weight of 2^6 and more
-#pragma unroll
-                    for (int i = 0; i < PT; ++i)
-#pragma unroll
-                        for (int c0 = 0; c0 < QW; c0 += 16) {
-                            uint32_t u[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                float2 h[2];
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    float2 &v = y[c0 / 2 + 2 * k + e];
-                                    h[e] = v;
-                                    if (i < PT - 1) {
-                                        h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
-                                        h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                        v = fma2(h[e], minus, v);
+                                        for (int e = 0; e < 2; ++e) {
+                                            float2 &v = y[j / 2 + 2 * k + e];
+                                            h[e] = v;
+                                            if (i < PT - 1) {
+                                                h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
+                                                h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
+                                                v = fma2(h[e], minus, v);
+                                            }
+                                        }
+                                        u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
                                     }
+                                    *reinterpret_cast<uint4 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)(c_wg + c0 + j) >> 4)) = make_uint4(u[0], u[1], u[2], u[3]);
                                 }
-                                u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
-                            }
-                            *reinterpret_cast<uint4 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)(c_wg + c0) >> 4)) = make_uint4(u[0], u[1], u[2], u[3]);
-                        }
-                } else {
-                    const float2 sixteen = make_float2(16.f, 16.f);
-                    uint32_t u[NO / 4];
+                        } else {
+                            const float2 sixteen = make_float2(16.f, 16.f);
+                            uint32_t u[NO / 4];
 #pragma unroll
-                    for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
+                            for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
 #pragma unroll
-                    for (int i = 0; i < PT; ++i)
+                            for (int i = 0; i < PT; ++i)
 #pragma unroll
-                        for (int c0 = 0; c0 < QC; c0 += 4) {
-                            float2 h[2];
+                                for (int j = 0; j < QC; j += 4) {
+                                    float2 h[2];
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float2 &v = y[c0 / 2 + e];
-                                h[e] = v;
-                                if (i < PT - 1) {
-                                    h[e] = make_float2(lead4(v.x), lead4(v.y));
-                                    v = mul2(fma2(h[e], minus, v), sixteen);
+                                    for (int e = 0; e < 2; ++e) {
+                                        float2 &v = y[j / 2 + e];
+                                        h[e] = v;
+                                        if (i < PT - 1) {
+                                            h[e] = make_float2(lead4(v.x), lead4(v.y));
+                                            v = mul2(fma2(h[e], minus, v), sixteen);
+                                        }
+                                    }
+                                    u[(i * QC + j) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
                                 }
-                            }
-                            u[(i * QC + c0) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
-                        }
 #pragma unroll
-                    for (int k = 0; k < NO / 16; ++k)
-                        *reinterpret_cast<uint4 *>(prow + mn_chunk<C::PW>(row, k)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+                            for (int k = 0; k < NO / 16; ++k)
+                                *reinterpret_cast<uint4 *>(prow + mn_chunk<C::PW>(row, k)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+                        }
+                    }
+                    // a weight beyond 2^8 does not fit its terms: raise Mu, and the weights once more
+                    if (done_max || !softmax_any(excess > kLagMax, 2 + wg, 128)) break;
+                    raise = again = true;
                 }
                 uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
                 if (masked && !valid && wg == 0) {         // 0 * NaN is not 0: values behind the end must not reach the product
