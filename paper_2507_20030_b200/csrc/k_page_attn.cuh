@@ -22,6 +22,8 @@
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.
 #pragma once
+#include <type_traits>
+
 #include "common.cuh"
 #include "k_pages.cuh"
 #include "umma_common.cuh"
@@ -38,9 +40,9 @@ constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax =
 // Instances: QC query columns over WGS softmax warpgroups, QT / PT terms of q / of the weights, the terms side by side as
 // further columns of one product (CHAIN = false: few columns, one pass over the tile) or added up in the same accumulator
 // (CHAIN = true).
-template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int STAGES_, int PBUFS_, int CTAS_> struct AttnCfg {
+template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int PART_, int STAGES_, int CTAS_> struct AttnCfg {
     using T = T_;
-    static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, STAGES = STAGES_, PBUFS = PBUFS_, CTAS = CTAS_;
+    static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, PART = PART_, STAGES = STAGES_, CTAS = CTAS_;
     static constexpr bool CHAIN = CHAIN_;
     static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
     static constexpr int kThreads = 128 * WGS + 64;
@@ -53,9 +55,10 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int STA
     static constexpr uint32_t kQBytes = (CHAIN ? QT * QC : NS) * 128;
     static constexpr uint32_t kOffQ = STAGES * 2 * kTileBytes;
     static constexpr uint32_t kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
-    static constexpr uint32_t kOffMisc = kOffP + PBUFS * kPBytes;
+    static constexpr uint32_t kOffMisc = kOffP + 2 * kPBytes;
     static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + STAGES * 32) + 256 + 1024;
-    static_assert(!CHAIN || PW == NO, "a chained term fills its rows");
+    static_assert(!CHAIN || PW >= NO, "a chained term fits its rows");
+    static_assert(!CHAIN || (PART % 8 == 0 && QW % PART == 0), "whole parts");
     static_assert(WGS == 1 || CHAIN, "warpgroups share chained columns");
 };
 
@@ -143,21 +146,36 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
-    uint32_t u[16];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
-          "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-        : "r"(taddr) : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = __uint_as_float(u[i]);
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+        : "r"(taddr));
 }
-// N columns (a multiple of 16) of this warp's lanes; completed by tmem_ld_wait().
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(taddr));
+}
+// N columns (a multiple of 8) of this warp's lanes; completed by tmem_ld_done(), which names the registers, so that other
+// work may be scheduled between the two.
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&r)[N]) {
 #pragma unroll
-    for (int c = 0; c < N; c += 16) tmem_ld16(taddr + c, *reinterpret_cast<float(*)[16]>(r + c));
+    for (int c = 0; c + 16 <= N; c += 16) tmem_ld16(taddr + c, *reinterpret_cast<float(*)[16]>(r + c));
+    if (N % 16 != 0) tmem_ld8(taddr + N - 8, r + N - 8);
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld_done(float (&r)[N]) {
+#pragma unroll
+    for (int c = 0; c < N; c += 8) {
+        float *f = r + c;
+        if (c == 0)
+            asm volatile("tcgen05.wait::ld.sync.aligned;"
+                         : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]));
+        else
+            asm volatile("" : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]));
+    }
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&r)[16]) {
     uint32_t u[16];
@@ -266,7 +284,7 @@ __global__ void __launch_bounds__(C::kThreads, C::CTAS)
 k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a) {
     using namespace umma;
     using T = typename C::T;
-    constexpr int QC = C::QC, QW = C::QW, WGS = C::WGS, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, STAGES = C::STAGES, PB = C::PBUFS;
+    constexpr int QC = C::QC, QW = C::QW, WGS = C::WGS, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, STAGES = C::STAGES;
     constexpr int kSoftmax = 128 * WGS, kWarpTma = 4 * WGS, kWarpMma = 4 * WGS + 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -288,11 +306,11 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     auto empty = [&](int s) { return bar0 + 8 * (2 * STAGES + s); };
     auto sfull = [&](int i) { return bar0 + 8 * (3 * STAGES + i); };
     auto pfull = [&](int i) { return bar0 + 8 * (3 * STAGES + 2 + i); };
-    auto pdone = [&](int i) { return bar0 + 8 * (3 * STAGES + 2 + PB + i); };
-    const uint32_t qfull = bar0 + 8 * (3 * STAGES + 2 + 2 * PB);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 3 * STAGES + 3 + 2 * PB);
+    auto pdone = [&](int i) { return bar0 + 8 * (3 * STAGES + 4 + i); };
+    const uint32_t qfull = bar0 + 8 * (3 * STAGES + 6);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 3 * STAGES + 7);
     volatile uint32_t *abort_flag = tmem_slot + 1;
-    static_assert(8 * (3 * STAGES + 4 + 2 * PB) <= 256, "barriers fit the room behind the stages");
+    static_assert(8 * (3 * STAGES + 8) <= 256, "barriers fit the room behind the stages");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int page = 1 << a.page_shift;
@@ -352,7 +370,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(kfull(s), 1); mbar_init(vfull(s), 1); mbar_init(empty(s), 1); }
         for (int i = 0; i < 2; ++i) mbar_init(sfull(i), 1);
-        for (int i = 0; i < PB; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
         mbar_init(qfull, 4 * WGS);
         *abort_flag = 0;
         fence_barrier_init();
@@ -413,14 +431,6 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     const uint32_t bytes = (uint32_t)__popc(have) * (uint32_t)(page * kHeadDim);
                     dead = __any_sync(0xffffffffu, dead);
                     if (dead) continue;
-                    if (lane == 0) mbar_expect_tx(kfull(st), bytes);
-                    __syncwarp();
-                    if (mine && id >= 0) {
-                        const int y = (id * a.H + s.h) << a.page_shift;
-                        const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
-                        tma_load_2d(k_tile(st) + off, &map_k, kfull(st), 0, y);
-                        tma_load_2d(v_tile(st) + off, &map_v, vfull(st), 0, y);
-                    }
                     float *sc = stage_ks + st * 32;
                     if (mine) {
                         sc[k] = ks;
@@ -429,7 +439,17 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                     if (lane == 0) reinterpret_cast<uint32_t *>(sc)[24] = have;
                     __syncwarp();
-                    if (lane == 0) mbar_expect_tx(vfull(st), bytes);
+                    if (lane == 0) {
+                        mbar_expect_tx(kfull(st), bytes);
+                        mbar_expect_tx(vfull(st), bytes);
+                    }
+                    __syncwarp();
+                    if (mine && id >= 0) {
+                        const int y = (id * a.H + s.h) << a.page_shift;
+                        const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
+                        tma_load_2d(k_tile(st) + off, &map_k, kfull(st), 0, y);
+                        tma_load_2d(v_tile(st) + off, &map_v, vfull(st), 0, y);
+                    }
                     issued = it + 1;
                 }
                 id = id_next; ks = ks_next; vs = vs_next;
@@ -464,8 +484,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 ++it;
             };
             auto output = [&](int i, bool first) {
-                const int st = i % STAGES, pb = i % PB;
-                wait(pfull(pb), (uint32_t)(i / PB) & 1u, kErrAttnMma);
+                const int st = i % STAGES, pb = i & 1;
+                wait(pfull(pb), (uint32_t)(i >> 1) & 1u, kErrAttnMma);
                 wait(vfull(st), (uint32_t)(i / STAGES) & 1u, kErrAttnMma);
                 if (!dead) {
                     tc_fence_after();
@@ -497,7 +517,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
         const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
-        constexpr int kPart = C::CHAIN ? 16 : QW, kLoad = C::CHAIN ? 16 : NS;  // columns at a time, raw scores of them
+        constexpr int kPart = C::CHAIN ? C::PART : QW, kLoad = C::CHAIN ? C::PART : NS;  // columns at a time, raw scores of them
         Work<MODE> w = w0;
         Segment s;
         int it = 0;
@@ -557,9 +577,12 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             bool raise = true;                             // some column's Mu does not stand for a maximum yet
 
             for (int t = s.t0; t < s.t1; ++t, ++it) {
-                const int st = it % STAGES, pb = it % PB;
+                const int st = it % STAGES, pb = it & 1;
                 bool done_max = false;                     // Mu has been set by this tile's maxima
-                wait(vfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnSoftmax);
+                // the scores of this tile are complete: so are its K copy, behind which the scales were written, and the
+                // output product of two tiles ago, issued before these scores, which read this tile's weight buffer
+                wait(sfull(it & 1), (uint32_t)(it >> 1) & 1u, kErrAttnSoftmax);
+                tc_fence_after();
                 const float *sc = stage_ks + st * 32;
                 const int pg = row >> a.page_shift;
                 const float ks = sc[pg], lvs = sc[8 + pg];
@@ -597,22 +620,99 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                     }
                 };
-                wait(sfull(it & 1), (uint32_t)(it >> 1) & 1u, kErrAttnSoftmax);
-                // the product that read this weight buffer is done
-                if (it >= PB) wait(pdone(pb), (uint32_t)((it - PB) / PB) & 1u, kErrAttnSoftmax);
-                tc_fence_after();
                 uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
+                // weights, their sum, their e4m3 terms; returns the largest exponent
+                auto weights = [&](auto repeat) {
+                    float excess = -INFINITY;
+                    float raw[2][kLoad];
+                    tmem_ld<kLoad>(ts, raw[0]);
+                    tmem_ld_done<kLoad>(raw[0]);
+#pragma unroll
+                    for (int c0 = 0; c0 < QW; c0 += kPart) {
+                        float2 y[kPart / 2];
+                        float(&now)[kLoad] = raw[c0 / kPart & 1], (&next)[kLoad] = raw[(c0 / kPart + 1) & 1];
+                        if (c0 + kPart < QW) tmem_ld<kLoad>(ts + c0 + kPart, next);   // the next columns' scores on their way
+                        exponents(now, c0, y);
+#pragma unroll
+                        for (int p = 0; p < kPart / 2; ++p) {
+                            excess = max3(excess, y[p].x, y[p].y);
+                            y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
+                            float2 &sum = l[c0 / 2 + p];
+                            if (!decltype(repeat)::value) {
+                                sum = fma2(y[p], ivs2, sum);
+                            } else {                       // this tile is in the sum already, unless that was dropped
+                                const float2 f = *reinterpret_cast<const float2 *>(col_f + c_wg + c0 + 2 * p);
+                                if (f.x == 0.f) sum.x = y[p].x * ivs;
+                                if (f.y == 0.f) sum.y = y[p].y * ivs;
+                            }
+                        }
+                        const float2 minus = make_float2(-1.f, -1.f);
+                        if constexpr (C::CHAIN) {
+                            // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
+                            // make up for it: an error below 2^-10 beside a largest weight of 2^2 and more
+#pragma unroll
+                            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                                for (int j = 0; j < kPart; j += 8) {
+                                    uint32_t u[2];
+#pragma unroll
+                                    for (int k = 0; k < 2; ++k) {
+                                        float2 h[2];
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            float2 &v = y[j / 2 + 2 * k + e];
+                                            h[e] = v;
+                                            if (i < PT - 1) {
+                                                h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
+                                                h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
+                                                v = fma2(h[e], minus, v);
+                                            }
+                                        }
+                                        u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
+                                    }
+                                    const int c = c_wg + c0 + j;
+                                    *reinterpret_cast<uint2 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)c >> 4) + (c & 8)) = make_uint2(u[0], u[1]);
+                                }
+                        } else {
+                            const float2 sixteen = make_float2(16.f, 16.f);
+                            uint32_t u[NO / 4];
+#pragma unroll
+                            for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
+#pragma unroll
+                            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                                for (int j = 0; j < QC; j += 4) {
+                                    float2 h[2];
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        float2 &v = y[j / 2 + e];
+                                        h[e] = v;
+                                        if (i < PT - 1) {
+                                            h[e] = make_float2(lead4(v.x), lead4(v.y));
+                                            v = mul2(fma2(h[e], minus, v), sixteen);
+                                        }
+                                    }
+                                    u[(i * QC + j) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
+                                }
+#pragma unroll
+                            for (int k = 0; k < NO / 16; ++k)
+                                *reinterpret_cast<uint4 *>(prow + mn_chunk<C::PW>(row, k)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+                        }
+                        if (c0 + kPart < QW) tmem_ld_done<kLoad>(next);
+                    }
+                    return excess;
+                };
                 bool again = false;
                 for (;;) {
                     if (raise) {
                         // Mu to 2 below the column maxima, and what has been summed rescaled
-                        if (t > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
+                        if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
 #pragma unroll 1
                         for (int c0 = 0; c0 < QW; c0 += kPart) {
                             float raw[kLoad];
                             float2 y[kPart / 2];
                             tmem_ld<kLoad>(ts + c0, raw);
-                            tmem_ld_wait();
+                            tmem_ld_done<kLoad>(raw);
                             exponents(raw, c0, y);
 #pragma unroll
                             for (int p = 0; p < kPart / 2; ++p) {
@@ -642,8 +742,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll 1
                             for (int c0 = 0; c0 < kCols; c0 += 16) {
                                 float o[16];
-                                tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
-                                tmem_ld_wait();
+                                tmem_ld<16>(tmem_o + lane_addr + c_wg + c0, o);
+                                tmem_ld_done<16>(o);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC];
                                 tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
@@ -652,85 +752,13 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                         done_max = true;
                     }
-                    // weights, their sum, their e4m3 terms
-                    float excess = -INFINITY;
-#pragma unroll
-                    for (int c0 = 0; c0 < QW; c0 += kPart) {
-                        float raw[kLoad];
-                        float2 y[kPart / 2];
-                        tmem_ld<kLoad>(ts + c0, raw);
-                        tmem_ld_wait();
-                        exponents(raw, c0, y);
-#pragma unroll
-                        for (int p = 0; p < kPart / 2; ++p) {
-                            excess = max3(excess, y[p].x, y[p].y);
-                            y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
-                            float2 &sum = l[c0 / 2 + p];
-                            if (!again) {
-                                sum = fma2(y[p], ivs2, sum);
-                            } else {                       // this tile is in the sum already, unless that was dropped
-                                const float2 f = *reinterpret_cast<const float2 *>(col_f + c_wg + c0 + 2 * p);
-                                if (f.x == 0.f) sum.x = y[p].x * ivs;
-                                if (f.y == 0.f) sum.y = y[p].y * ivs;
-                            }
-                        }
-                        const float2 minus = make_float2(-1.f, -1.f);
-                        if constexpr (C::CHAIN) {
-                            // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
-                            // make up for it: an error below 2^-10 beside a largest weight of 2^2 and more
-#pragma unroll
-                            for (int i = 0; i < PT; ++i)
-#pragma unroll
-                                for (int j = 0; j < kPart; j += 16) {
-                                    uint32_t u[4];
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) {
-                                        float2 h[2];
-#pragma unroll
-                                        for (int e = 0; e < 2; ++e) {
-                                            float2 &v = y[j / 2 + 2 * k + e];
-                                            h[e] = v;
-                                            if (i < PT - 1) {
-                                                h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
-                                                h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                                v = fma2(h[e], minus, v);
-                                            }
-                                        }
-                                        u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
-                                    }
-                                    *reinterpret_cast<uint4 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)(c_wg + c0 + j) >> 4)) = make_uint4(u[0], u[1], u[2], u[3]);
-                                }
-                        } else {
-                            const float2 sixteen = make_float2(16.f, 16.f);
-                            uint32_t u[NO / 4];
-#pragma unroll
-                            for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
-#pragma unroll
-                            for (int i = 0; i < PT; ++i)
-#pragma unroll
-                                for (int j = 0; j < QC; j += 4) {
-                                    float2 h[2];
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        float2 &v = y[j / 2 + e];
-                                        h[e] = v;
-                                        if (i < PT - 1) {
-                                            h[e] = make_float2(lead4(v.x), lead4(v.y));
-                                            v = mul2(fma2(h[e], minus, v), sixteen);
-                                        }
-                                    }
-                                    u[(i * QC + j) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
-                                }
-#pragma unroll
-                            for (int k = 0; k < NO / 16; ++k)
-                                *reinterpret_cast<uint4 *>(prow + mn_chunk<C::PW>(row, k)) = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
-                        }
-                    }
+                    const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
                     // a weight beyond 2^8 does not fit its terms: raise Mu, and the weights once more
                     if (done_max || !softmax_any(excess > kLagMax, 2 + wg, 128)) break;
                     raise = again = true;
                 }
                 uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
+                if (masked) wait(vfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnSoftmax);   // it is read and written below
                 if (masked && !valid && wg == 0) {         // 0 * NaN is not 0: values behind the end must not reach the product
 #pragma unroll
                     for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vtile + row * 128)[k] = make_uint4(0u, 0u, 0u, 0u);
@@ -779,7 +807,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
                 if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + 2 * p) = v;
             }
-            if (s.t1 > s.t0) wait(pdone((it - 1) % PB), (uint32_t)((it - 1) / PB) & 1u, kErrAttnSoftmax);
+            if (s.t1 > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
             tc_fence_after();
             softmax_bar(1, kSoftmax);
             const bool whole = MODE == 0 ? s.t0 == 0 && s.t1 == s.tiles : a.splits == 1;
@@ -815,15 +843,15 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll 1
                 for (int c0 = 0; c0 < QW; c0 += 16) {
                     float o[16];
-                    tmem_ld16(tmem_o + lane_addr + c_wg + c0, o);
-                    tmem_ld_wait();
+                    tmem_ld<16>(tmem_o + lane_addr + c_wg + c0, o);
+                    tmem_ld_done<16>(o);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) put(c_wg + c0 + e, o[e]);
                 }
             } else {
                 float o[NO];
                 tmem_ld<NO>(tmem_o + lane_addr, o);
-                tmem_ld_wait();
+                tmem_ld_done<NO>(o);
 #pragma unroll
                 for (int c = 0; c < QC; ++c) {
                     float v = o[(PT - 1) * QC + c];
