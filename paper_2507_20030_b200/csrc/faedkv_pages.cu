@@ -140,8 +140,9 @@ int make_map(faedkv_pages *pg, CUtensorMap *map, const void *codes) {
 //                                  type           columns, warpgroups, terms of q and w, chained, columns at a time, stages, CTAs per SM
 using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 3, false, 8, 3, 2>;
 using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 6, false, 8, 2, 2>;
-#ifndef CHUNK
-#define CHUNK 96, 3, 2, 2, true, 16, 3, 1
+#define CHUNK 128, 4, 2, 2, true, 8, 3, 1
+#ifndef RND
+#define RND 8
 #endif
 using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, CHUNK>;
 constexpr int kDecodeCtas = DecodeBf16::CTAS;
@@ -164,8 +165,11 @@ AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;
     const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : kDecodeCtas);
-    long long splits = units > 0 ? room / units : 1;
-    if (splits > (max_tiles + 1) / 2) splits = (max_tiles + 1) / 2;
+    // fewer units than the SMs hold: the cached tokens are split until they are full.  More: they are split too, so that the
+    // last round of CTAs is a small part of the whole, as long as a split is not shorter than 16 tiles.
+    long long splits = units < room ? room / units : (RND * room + units - 1) / units;
+    const long long cap = units < room ? (max_tiles + 1) / 2 : max_tiles / 16;
+    if (splits > cap) splits = cap;
     p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
     p.bytes1 = p.splits > 1 ? (size_t)units * p.splits * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
     const long long all_tiles = max_tiles * batch * c.n_kv_heads;
@@ -339,7 +343,8 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const AttnPlan p = plan_attn(pg, batch, n_tokens);
     const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
-                            c.max_pages, c.n_pages, pg->page_shift, p.splits, scale * 1.44269504088896341f,
+                            c.max_pages, c.n_pages, pg->page_shift, p.splits,
+                            65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status};
     if (c.kv_dtype == FAEDKV_F32)
         return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st) : launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st);

@@ -69,6 +69,7 @@ struct AttnArgs {
     const float *ks, *vs;
     long long ld_q;
     int n_tokens, B, H, G, W, n_pages, page_shift, splits;
+    uint32_t inv_g;                                       // c * inv_g >> 16 = c / G for the columns c < 128
     float scale_log2;                                     // scale * log2(e)
     unsigned char *ws;
     unsigned int *status;
@@ -524,25 +525,29 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         while (w.next(a, QC, s)) {
             const int n_cols = s.n_tok * a.G;
             // -- the query columns as e4m3 terms, each column with a power of two of its own
-            for (int c = warp; c < QC; c += 4 * WGS) {
-                float x[4] = {0.f, 0.f, 0.f, 0.f};
-                float qs = 1.f;
-                if (c < n_cols) {
-                    const int tok = s.tok0 + c / a.G, hq = s.h * a.G + c % a.G;
-                    const float4 v = load4(static_cast<const T *>(a.q) + (size_t)tok * a.ld_q + (size_t)hq * kHeadDim + lane * 4);
-                    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-                    uint32_t m = 0;
+            constexpr int kEach = QC / (4 * WGS);          // columns of a warp: their loads first, then the work
+            const T *q_row = static_cast<const T *>(a.q) + (size_t)s.tok0 * a.ld_q + (size_t)s.h * a.G * kHeadDim + lane * 4;
+            float4 q_in[kEach];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
-                    qs = 2.0f * scale_for(__uint_as_float(__reduce_max_sync(0xffffffffu, m)));
-                    const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
+            for (int j = 0; j < kEach; ++j) {
+                const int c = warp + 4 * WGS * j, tok = c * a.inv_g >> 16;
+                q_in[j] = c < n_cols ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
-                }
+            for (int j = 0; j < kEach; ++j) {
+                const int c = warp + 4 * WGS * j;
+                float x[4] = {q_in[j].x, q_in[j].y, q_in[j].z, q_in[j].w};
+                uint32_t m = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
+                const float qs = 2.0f * scale_for(__uint_as_float(__reduce_max_sync(0xffffffffu, m)));
+                const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
                 if (lane == 0) {
                     col[(c >> 1) * 4 + (c & 1)] = qs * a.scale_log2;
                     col[(c >> 1) * 4 + 2 + (c & 1)] = 0.f;
-                    col_lim[c] = c < n_cols ? s.see0 + c / a.G : 0;
+                    col_lim[c] = c < n_cols ? s.see0 + (int)(c * a.inv_g >> 16) : 0;
                     col_set[c] = c < n_cols ? 0 : 1;
                 }
 #pragma unroll
@@ -827,14 +832,22 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     m->first = w.pos - (s.t1 - s.t0);
                     m->tiles = s.tiles;
                 }
+            if (whole) {
+                for (int c = tid; c < QC; c += kSoftmax) {
+                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                    col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
+                }
+                softmax_bar(1, kSoftmax);
+            }
+            T *out_row = static_cast<T *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
+            const size_t out_tok = (size_t)a.H * a.G * kHeadDim;
             auto put = [&](int c, float v) {
                 if (c >= n_cols) return;
                 if (s.t1 == s.t0) v = 0.f;                 // an empty split
                 if (MODE == 1 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
                 if (whole) {
-                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
-                    const float o = sum == 0.f ? 0.f : __fdiv_rn(v, sum);
-                    store1(static_cast<T *>(a.out) + ((size_t)(s.tok0 + c / a.G) * a.H * a.G + (size_t)s.h * a.G + c % a.G) * kHeadDim + row, o);
+                    const int tok = c * a.inv_g >> 16;
+                    store1(out_row + tok * out_tok + (c - tok * a.G) * kHeadDim, col_f[c] == 0.f ? 0.f : v * col_f[c]);
                 } else {
                     slot[2 * QC + (size_t)c * kHeadDim + row] = v;
                 }
