@@ -430,8 +430,9 @@ size_t faedkv_pages_bytes(const faedkv_pages *pg);
  *                       row or n_tokens, or when the stack does not hold its pages and those of the requests before
  *                       it; in the last case every later request that needs a page waits too.
  * q_start[b] counts the tokens before request b (finished ones count none), slots[i] = page * page_size + row of token
- * i < n_tokens, -1 where it has none.  *n_free_out is the new height of the stack.  ws: int32 [batch + 1], overwritten.
- * kv_len may be t_len itself, n_free_out may be n_free. */
+ * i < n_tokens, -1 where it has none.  *n_free_out is the new height of the stack.  ws: faedkv_pages_tables_bytes(),
+ * overwritten, 4-byte aligned (NULL where that is 0).  kv_len may be t_len itself, n_free_out may be n_free. */
+size_t faedkv_pages_tables_bytes(const faedkv_pages *pg, int batch, int n_tokens);
 int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, int32_t *table,
                         int32_t *free_pages, const int32_t *n_free, int n_tokens, int32_t *q_start, int32_t *kv_len,
                         int32_t *slots, int32_t *n_free_out, int32_t *ws, void *stream);

@@ -34,7 +34,7 @@ EXPORTS = [
     "faedkv_reconstruct_windowed",
     "faedkv_device_status", "faedkv_launch_count", "faedkv_decode_attn_static",
     "faedkv_reset_device_status", "faedkv_test_hooks", "faedkv_debug_build", "faedkv_debug_word",
-    "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables",
+    "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables_bytes", "faedkv_pages_tables",
     "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
     "faedkv_pages_reset_device_status", "faedkv_pages_launch_count",
 ]
@@ -144,6 +144,8 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_last_error.restype = ctypes.c_char_p
     lib.faedkv_pages_bytes.argtypes = [_vp]
     lib.faedkv_pages_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_tables_bytes.argtypes = [_vp, _int, _int]
+    lib.faedkv_pages_tables_bytes.restype = ctypes.c_size_t
     lib.faedkv_pages_tables.argtypes = [_vp, _vp, _vp, _int, _vp, _vp, _vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.faedkv_pages_tables.restype = _int
     lib.faedkv_pages_store.argtypes = [_vp, _vp, _vp, _ll, _vp, _int, _vp, _vp, _vp, _vp, _vp]
@@ -537,8 +539,9 @@ class Pages:
                 need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, self._pool_shape),
                 need("n_free", n_free, i32, one), n_tokens, need("q_start", q_start, i32, (batch + 1,)),
                 need("kv_len", kv_len, i32, per_seq), need("slots", slots, i32, (n_tokens,)), need("n_free_out", n_free_out, i32, one))
-        w = self._workspace(ws, 4 * (batch + 1), stream)
-        self._check(self._lib.faedkv_pages_tables(self._h, *args, w.data_ptr(), self._on(stream)))
+        nbytes = self._lib.faedkv_pages_tables_bytes(self._h, batch, n_tokens)
+        w = self._workspace(ws, nbytes, stream) if nbytes else None
+        self._check(self._lib.faedkv_pages_tables(self._h, *args, None if w is None else w.data_ptr(), self._on(stream)))
 
     def store(self, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None):
         k, n, ld = self._rows("k_new", k_new, self.n_kv_heads)

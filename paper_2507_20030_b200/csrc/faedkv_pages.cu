@@ -140,11 +140,7 @@ int make_map(faedkv_pages *pg, CUtensorMap *map, const void *codes) {
 //                                  type           columns, warpgroups, terms of q and w, chained, columns at a time, stages, CTAs per SM
 using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 3, false, 8, 3, 2>;
 using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 6, false, 8, 2, 2>;
-#define CHUNK 128, 4, 2, 2, true, 8, 3, 1
-#ifndef RND
-#define RND 8
-#endif
-using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, CHUNK>;
+using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 128, 4, 2, 2, true, 8, 3, 1>;
 constexpr int kDecodeCtas = DecodeBf16::CTAS;
 static_assert(kDecodeCtas == DecodeF32::CTAS && DecodeF32::QC == 8 && DecodeBf16::QC == 8, "one plan for both types");
 
@@ -153,23 +149,23 @@ struct AttnPlan {
     bool wide;               // 128 columns a unit instead of 8
     int qc, blocks, splits;  // MODE 1: blocks of new tokens, splits of the cached ones
     int ctas;                // MODE 0
+    long long max_tiles;     // of a table row
     size_t bytes0, bytes1;   // workspace of the two modes
 };
 
 AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     const faedkv_pages_config &c = pg->cfg;
     AttnPlan p{};
-    const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
+    const long long max_tiles = p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
     // more query columns per sequence than 8: a block of 128 columns reads the cache once for all of them
     p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;
     const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : kDecodeCtas);
-    // fewer units than the SMs hold: the cached tokens are split until they are full.  More: they are split too, so that the
-    // last round of CTAs is a small part of the whole, as long as a split is not shorter than 16 tiles.
-    long long splits = units < room ? room / units : (RND * room + units - 1) / units;
-    const long long cap = units < room ? (max_tiles + 1) / 2 : max_tiles / 16;
-    if (splits > cap) splits = cap;
+    // fewer units than the SMs hold: the cached tokens are split until they are full.  (Splitting more units too, for a
+    // shorter last round, was slower: 2 splits 1011 us, 1 split 935 us at 2048 new tokens over 18432.)
+    long long splits = room / (units > 0 ? units : 1);
+    if (splits > (max_tiles + 1) / 2) splits = (max_tiles + 1) / 2;
     p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
     p.bytes1 = p.splits > 1 ? (size_t)units * p.splits * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
     const long long all_tiles = max_tiles * batch * c.n_kv_heads;
@@ -190,9 +186,11 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
     const dim3 grid = MODE == 0 ? dim3(p.ctas) : dim3(p.blocks, a.H, p.splits);
     kernel<<<grid, C::kThreads, C::kSmemBytes, st>>>(mk, mv, a);
     if (int r = launch_check(pg, "k_page_attn")) return r;
-    if (MODE == 1 && p.splits == 1) return FAEDKV_OK;
-    const dim3 jgrid = MODE == 0 ? dim3((unsigned)(a.B * a.H), a.G) : dim3((unsigned)(p.blocks * a.H), C::QC / a.G * a.G);
-    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim), 0, st, a, (int)C::QC));
+    if (MODE == 0 ? p.max_tiles == 1 : p.splits == 1) return FAEDKV_OK;      // no unit is ever in parts
+    // few units: a block per column; many, with few parts each: a block joins 16 columns
+    const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 || p.splits > 8 ? 1 : 16;
+    const dim3 jgrid((unsigned)((MODE == 0 ? a.B : p.blocks) * a.H), (cols + each - 1) / each);
+    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC, each));
     return launch_check(pg, "k_page_attn_join");
 }
 
@@ -249,6 +247,15 @@ size_t faedkv_pages_bytes(const faedkv_pages *pg) {
     return pg ? (size_t)pg->cfg.n_pages * pg->cfg.n_kv_heads * pg->cfg.page_size * kHeadDim : 0;
 }
 
+// Up to this many tokens and requests one CTA places the tokens itself; above, a second launch over all SMs is faster
+// (32768 tokens: 40 us in one CTA) and the numbers between the two lie in the workspace.
+static bool pages_in_one(int batch, int n_tokens) { return n_tokens <= 2048 && batch <= pages::kPlaceBatch; }
+
+size_t faedkv_pages_tables_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
+    if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_tokens < 0 || pages_in_one(batch, n_tokens)) return 0;
+    return sizeof(int32_t) * ((size_t)batch + 1);
+}
+
 int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, int32_t *table,
                         int32_t *free_pages, const int32_t *n_free, int n_tokens, int32_t *q_start, int32_t *kv_len,
                         int32_t *slots, int32_t *n_free_out, int32_t *ws, void *stream) {
@@ -257,7 +264,7 @@ int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n
     if (int r = check_batch(pg, batch)) return r;
     if (n_tokens < 0) return fail(pg, FAEDKV_ERR_SHAPE, "n_tokens = %d is negative", n_tokens);
     if (t_len == nullptr || n_new == nullptr || table == nullptr || free_pages == nullptr || n_free == nullptr ||
-        q_start == nullptr || kv_len == nullptr || (slots == nullptr && n_tokens > 0) || n_free_out == nullptr || ws == nullptr)
+        q_start == nullptr || kv_len == nullptr || (slots == nullptr && n_tokens > 0) || n_free_out == nullptr)
         return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_tables");
     if (int r = check_align(pg, {}, {t_len, n_new, table, free_pages, n_free, q_start, kv_len, slots, n_free_out, ws})) return r;
     const DeviceGuard guard(pg);
@@ -265,12 +272,11 @@ int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const pages::TablesArgs a{t_len, n_new, n_free, table, free_pages, q_start, kv_len, slots, n_free_out, ws, batch,
                               pg->cfg.max_pages, pg->page_shift, pg->cfg.n_pages, n_tokens, pg->dev_status};
-    // up to this many tokens one CTA places them itself; above, a second launch over all SMs is the faster way
-    constexpr int kPlaceInPlan = 2048;
-    if (n_tokens <= kPlaceInPlan) {
+    if (pages_in_one(batch, n_tokens)) {
         pages::k_page_plan<true><<<1, pages::kPlanThreads, 0, st>>>(a);
         return launch_check(pg, "k_page_plan");
     }
+    if (ws == nullptr) return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL workspace passed to faedkv_pages_tables");
     pages::k_page_plan<false><<<1, pages::kPlanThreads, 0, st>>>(a);
     if (int r = launch_check(pg, "k_page_plan")) return r;
     CUDA_TRY(pg, launch_pdl(pages::k_page_slots, dim3((n_tokens + 255) / 256), dim3(256), 0, st, a));

@@ -886,19 +886,21 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
 }
 
-// Joins the partial results of a unit: rescaled to the largest Mu, summed in order, divided.  Grid (units, columns of a
-// unit), a thread per channel.  MODE 0: a unit's parts lie in the slots of the consecutive CTAs that shared it.  MODE 1:
+// Joins the partial results of a unit: rescaled to the largest Mu, summed in order, divided.  Grid (units, groups of `each`
+// columns), four threads per channel that share the parts.  MODE 0: a unit's parts lie in the slots of the consecutive CTAs that shared it.  MODE 1:
 // one slot per split.
+constexpr int kJoinGroups = 4;
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kHeadDim) k_page_attn_join(const AttnArgs a, const int qc) {
+__global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const AttnArgs a, const int qc, const int each) {
     pdl_wait();
-    const int c = blockIdx.y, d = threadIdx.x;
+    const int d = threadIdx.x;
     long long first_slot = 0;
-    int n = 0, first_odd = 0;
-    size_t out_row = 0;
+    int n = 0, first_odd = 0, h, tok0, n_cols;
     const float *slots;
     if constexpr (MODE == 0) {
-        const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
+        tok0 = blockIdx.x / a.H;
+        h = blockIdx.x % a.H;
+        n_cols = a.G;
         const UnitMeta m = reinterpret_cast<const UnitMeta *>(a.ws + 16)[blockIdx.x];
         const long long share = *reinterpret_cast<const long long *>(a.ws);
         const long long cta0 = m.first / share, cta1 = (m.first + m.tiles - 1) / share;
@@ -906,56 +908,73 @@ __global__ void __launch_bounds__(kHeadDim) k_page_attn_join(const AttnArgs a, c
         n = (int)(cta1 - cta0) + 1;
         first_slot = cta0 * 2;
         first_odd = m.first % share != 0 ? 1 : 0;
-        out_row = (size_t)b * a.H * a.G + (size_t)h * a.G + c;
         slots = reinterpret_cast<const float *>(a.ws + 16 + sizeof(UnitMeta) * (size_t)a.B * a.H);
     } else {
-        const int tq = qc / a.G, v = blockIdx.x / a.H, h = blockIdx.x % a.H;
+        const int tq = qc / a.G, v = blockIdx.x / a.H;
+        h = blockIdx.x % a.H;
         int lo = 0, hi = a.B - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (a.q_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
         }
         const int first = a.q_start[lo], nn = a.q_start[lo + 1] - first, j = v - (first / tq + lo);
-        if (first < 0 || nn < 0 || first > a.n_tokens - nn || j < 0 || (long long)j * tq + c / a.G >= nn) return;
+        if (first < 0 || nn < 0 || first > a.n_tokens - nn || j < 0 || (long long)j * tq >= nn) return;
         n = a.splits;
         first_slot = (long long)blockIdx.x * a.splits;
-        out_row = (size_t)(first + j * tq + c / a.G) * a.H * a.G + (size_t)h * a.G + c % a.G;
+        tok0 = first + j * tq;
+        n_cols = min(tq, nn - j * tq) * a.G;
         slots = reinterpret_cast<const float *>(a.ws);
     }
     auto slot = [&](int i) {
         const long long at = MODE == 0 ? (i == 0 ? first_slot + first_odd : first_slot + 2LL * i) : first_slot + i;
         return slots + (size_t)at * attn_slot_floats(qc);
     };
-    // 128 parts at a time: their Mu and sums by one thread each, then every thread adds up its channel
-    __shared__ float f_s[kHeadDim], red_s[2][4];
-    float mu = kMuNone, sum = 0.f, o = 0.f;
-    for (int i0 = 0; i0 < n; i0 += kHeadDim) {
-        const int k = min(kHeadDim, n - i0);
-        float m = kMuNone, l = 0.f;
-        if (d < k) {
-            const float *p = slot(i0 + d);
-            m = p[c];
-            l = p[qc + c];
-        }
-        const float wm = warp_max(m);
-        if ((d & 31) == 0) red_s[0][d >> 5] = wm;
-        __syncthreads();
-        const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
-        const float f = ex2(m - top), back = ex2(mu - top);
-        f_s[d] = f;
-        l *= f;
+    // 128 parts at a time: their Mu and sums by one thread each, then a thread adds up its channel of every fourth part
+    __shared__ float f_s[kHeadDim], red_s[2][4], o_s[kJoinGroups][kHeadDim];
+    const int grp = threadIdx.y;
+    const int c_end = min((int)(blockIdx.y + 1) * each, n_cols);
+    for (int c = blockIdx.y * each; c < c_end; ++c) {
+        float mu = kMuNone, sum = 0.f, o = 0.f;
+        for (int i0 = 0; i0 < n; i0 += kHeadDim) {
+            const int k = min(kHeadDim, n - i0);
+            float m = kMuNone, l = 0.f;
+            if (grp == 0) {
+                if (d < k) {
+                    const float *p = slot(i0 + d);
+                    m = p[c];
+                    l = p[qc + c];
+                }
+                const float wm = warp_max(m);
+                if ((d & 31) == 0) red_s[0][d >> 5] = wm;
+            }
+            __syncthreads();
+            const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
+            const float back = ex2(mu - top);
+            if (grp == 0) {
+                const float f = ex2(m - top);
+                f_s[d] = f;
+                l *= f;
 #pragma unroll
-        for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-        if ((d & 31) == 0) red_s[1][d >> 5] = l;
-        __syncthreads();
-        sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
-        o *= back;
-        mu = top;
+                for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+                if ((d & 31) == 0) red_s[1][d >> 5] = l;
+            }
+            __syncthreads();
+            sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
+            o *= back;
+            mu = top;
 #pragma unroll 8
-        for (int i = 0; i < k; ++i) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);
+            for (int i = grp; i < k; i += kJoinGroups) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);
+            __syncthreads();
+        }
+        o_s[grp][d] = o;
+        __syncthreads();
+        if (grp == 0) {
+            const int tok = c / a.G;
+            o = (o_s[0][d] + o_s[1][d]) + (o_s[2][d] + o_s[3][d]);
+            store1(static_cast<T *>(a.out) + (((size_t)(tok0 + tok) * a.H + h) * a.G + (c - tok * a.G)) * kHeadDim + d, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
+        }
         __syncthreads();
     }
-    store1(static_cast<T *>(a.out) + out_row * kHeadDim + d, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
 }
 
 }  // namespace pages

@@ -62,21 +62,21 @@ __device__ __forceinline__ int find_sequence(const int32_t *start, int B, int i)
     return lo;
 }
 
-// Slot of new token i, and the table entry when the token opens a page.
-__device__ __forceinline__ void place_token(const TablesArgs &a, int i) {
+// Slot of new token i, and the table entry when the token opens a page.  start: q_start; base: ws.
+__device__ __forceinline__ void place_token(const TablesArgs &a, int i, const int32_t *start, const int32_t *base) {
     int slot = -1;
-    if (i < a.q_start[a.B]) {
-        const int b = find_sequence(a.q_start, a.B, i);
-        const int base = a.ws[b];
-        if (base >= 0) {
-            const int first = a.q_start[b], n = a.q_start[b + 1] - first;
+    if (i < start[a.B]) {
+        const int b = find_sequence(start, a.B, i);
+        const int page0 = base[b];
+        if (page0 >= 0) {
+            const int first = start[b], n = start[b + 1] - first;
             const int t = a.kv_len[b] - n, pos = t + (i - first);
             const int p = pos >> a.page_shift, old = (t + (1 << a.page_shift) - 1) >> a.page_shift;
             int id;
             if (p < old) {
                 id = a.table[(size_t)b * a.W + p];
             } else {
-                id = a.free_pages[a.ws[a.B] - 1 - (base + p - old)];
+                id = a.free_pages[base[a.B] - 1 - (page0 + p - old)];
                 if ((pos & ((1 << a.page_shift) - 1)) == 0) a.table[(size_t)b * a.W + p] = id;
             }
             if (id >= 0 && id < a.n_pages) slot = (id << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
@@ -86,14 +86,17 @@ __device__ __forceinline__ void place_token(const TablesArgs &a, int i) {
     a.slots[i] = slot;
 }
 
+constexpr int kPlaceBatch = kPlanThreads;                 // requests that the one-launch form holds in shared memory
+
 // One CTA: pushes the pages of finished requests, grants pages in request order (three block-wide sums per 1024
-// requests), writes lengths and starts; with PLACE also the slots.  Every input of a request is read before an output
-// of the same request is written, and n_free before n_free_out, so outputs may be the inputs' own buffers.
-// Bound by latency: a chain of three scans, about 3 us for up to 1024 requests.
+// requests), writes lengths and starts; with PLACE also the slots, from starts and page numbers kept in shared memory.
+// Every input of a request is read before an output of the same request is written, and n_free before n_free_out, so
+// outputs may be the inputs' own buffers.  Bound by latency: a chain of loads and three sums.
 template <bool PLACE>
 __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const TablesArgs a) {
     __shared__ long long warp_sums[32];
     __shared__ int rel_base[kPlanThreads], rel_n[kPlanThreads];
+    __shared__ int32_t start_s[PLACE ? kPlaceBatch + 1 : 1], base_s[PLACE ? kPlaceBatch + 1 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int page = 1 << a.page_shift;
     const long long cap = (long long)a.W * page;
@@ -117,11 +120,19 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const TablesArgs a) 
         rel_base[tid] = (int)min(height + upto - held, (long long)a.n_pages);
         rel_n[tid] = (int)held;
         __syncthreads();
-        for (int r = warp; r < kPlanThreads; r += kPlanThreads / 32) {
+        for (int r = warp; r < min(kPlanThreads, a.B - b0); r += kPlanThreads / 32) {
             const int n = rel_n[r], base = rel_base[r];
-            for (int j = lane; j < n; j += 32) {
-                if (base + j < a.n_pages) a.free_pages[base + j] = a.table[(size_t)(b0 + r) * a.W + j];
-                else flag(a.status, kBadFreeList);
+            const int32_t *row = a.table + (size_t)(b0 + r) * a.W;
+            for (int j0 = lane; j0 < n; j0 += 256) {       // eight entries a lane in flight
+                int id[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) id[k] = j0 + 32 * k < n ? row[j0 + 32 * k] : 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int j = j0 + 32 * k;
+                    if (j < n && base + j < a.n_pages) a.free_pages[base + j] = id[k];
+                    else if (j < n) flag(a.status, kBadFreeList);
+                }
             }
         }
         height = min(height + total, (long long)a.n_pages);
@@ -152,29 +163,45 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const TablesArgs a) 
         long long took_total;
         block_scan(ok ? need : 0, warp_sums, &took_total);
         if (b < a.B) {
-            a.q_start[b] = (int)min(tok_end - n, 0x7fffffffLL);
-            if (b == a.B - 1) a.q_start[a.B] = (int)min(tok_end, 0x7fffffffLL);
+            const int start = (int)min(tok_end - n, 0x7fffffffLL), end = (int)min(tok_end, 0x7fffffffLL);
+            const int base = ok ? (int)min(need_end - need, (long long)a.n_pages) : -1;
+            a.q_start[b] = start;
+            if (b == a.B - 1) a.q_start[a.B] = end;
             a.kv_len[b] = done ? 0 : (ok ? (int)(t + n) : (int)t);
-            a.ws[b] = ok ? (int)min(need_end - need, (long long)a.n_pages) : -1;
+            if (PLACE) {
+                start_s[b] = start;
+                if (b == a.B - 1) start_s[a.B] = end;
+                base_s[b] = base;
+            } else {
+                a.ws[b] = base;
+            }
         }
         tok_before += tok_total;
         need_before += need_total;
         taken += took_total;
     }
     if (tid == 0) {
-        a.ws[a.B] = (int)height;
+        (PLACE ? base_s : a.ws)[a.B] = (int)height;
         *a.n_free_out = (int)(height - taken);
     }
     if (PLACE) {
         __syncthreads();
-        for (int i = tid; i < a.n_tokens; i += kPlanThreads) place_token(a, i);
+        for (int i = tid; i < a.n_tokens; i += kPlanThreads) place_token(a, i, start_s, base_s);
     }
 }
 
+// The slots of many tokens.  The search for a token's request is a chain of loads: in shared memory while it fits.
+constexpr int kSlotsBatch = 4096;
 __global__ void __launch_bounds__(256) k_page_slots(const TablesArgs a) {
+    __shared__ int32_t start_s[kSlotsBatch + 1];
     pdl_wait();
+    const bool fits = a.B <= kSlotsBatch;
+    if (fits) {
+        for (int b = threadIdx.x; b <= a.B; b += 256) start_s[b] = a.q_start[b];
+        __syncthreads();
+    }
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < a.n_tokens) place_token(a, i);
+    if (i < a.n_tokens) place_token(a, i, fits ? start_s : a.q_start, a.ws);
 }
 
 // ---- store --------------------------------------------------------------------------------------------
