@@ -184,7 +184,7 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
         pg->attr_set |= 1u << attr_bit;
     }
     const dim3 grid = MODE == 0 ? dim3(p.ctas) : dim3(p.blocks, a.H, p.splits);
-    kernel<<<grid, C::kThreads, C::kSmemBytes, st>>>(mk, mv, a);
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), C::kSmemBytes, st, mk, mv, a));
     if (int r = launch_check(pg, "k_page_attn")) return r;
     if (MODE == 0 ? p.max_tiles == 1 : p.splits == 1) return FAEDKV_OK;      // no unit is ever in parts
     // few units: a block per column; many, with few parts each: a block joins 16 columns

@@ -316,6 +316,19 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int page = 1 << a.page_shift;
 
+    // ---- what needs nothing of the call's inputs, while the stream's previous kernel drains
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(kfull(s), 1); mbar_init(vfull(s), 1); mbar_init(empty(s), 1); }
+        for (int i = 0; i < 2; ++i) mbar_init(sfull(i), 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
+        mbar_init(qfull, 4 * WGS);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == kWarpMma) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
+    pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the join may be placed as SMs fall free
+
     // ---- this CTA's work
     Work<MODE> w0;
     if constexpr (MODE == 0) {
@@ -338,45 +351,35 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         __syncthreads();
         const long long w_sum[4] = {found[0], found[1], found[2], found[3]};
         const long long total = (w_sum[0] + w_sum[1] + w_sum[2] + w_sum[3]) * a.H;
-        const long long share = (total + gridDim.x - 1) / gridDim.x;
+        // (a 32-bit division where that will do: a 64-bit one takes 0.3 us here)
+        const long long share = total < (1LL << 31) ? (long long)(((uint32_t)total + gridDim.x - 1) / gridDim.x) : (total + gridDim.x - 1) / gridDim.x;
         w0.pos = share * blockIdx.x;
         w0.end = min(total, w0.pos + share);
-        if (w0.pos >= w0.end) return;                     // the whole CTA
         w0.at_start = true;
         if (tid == 0 && blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
-        // the run that holds sequence tile pos / H ... then the sequence, one after the other
-        int lo = 0, hi = 127;
-        auto before = [&](int i) { return run_sum[i] + (i >= 32 ? w_sum[0] : 0) + (i >= 64 ? w_sum[1] : 0) + (i >= 96 ? w_sum[2] : 0); };
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (mid * run < a.B && before(mid) * a.H <= w0.pos) lo = mid; else hi = mid - 1;
+        if (w0.pos < w0.end) {
+            // the run that holds sequence tile pos / H ... then the sequence, one after the other
+            int lo = 0, hi = 127;
+            auto before = [&](int i) { return run_sum[i] + (i >= 32 ? w_sum[0] : 0) + (i >= 64 ? w_sum[1] : 0) + (i >= 96 ? w_sum[2] : 0); };
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (mid * run < a.B && before(mid) * a.H <= w0.pos) lo = mid; else hi = mid - 1;
+            }
+            long long at = before(lo) * a.H;
+            int b = lo * run, n = tiles_of(clamp_len(a, b, false));
+            while (at + (long long)n * a.H <= w0.pos) {
+                at += (long long)n * a.H;
+                n = tiles_of(clamp_len(a, ++b, false));
+            }
+            const long long in = w0.pos - at;              // < n * H
+            w0.b = b;
+            w0.h = in < (1LL << 31) ? (int)((uint32_t)in / (uint32_t)n) : (int)(in / n);
+            w0.t = (int)(in - (long long)w0.h * n);
+            w0.tiles = n;
         }
-        long long at = before(lo) * a.H;
-        int b = lo * run, n = tiles_of(clamp_len(a, b, false));
-        while (at + (long long)n * a.H <= w0.pos) {
-            at += (long long)n * a.H;
-            n = tiles_of(clamp_len(a, ++b, false));
-        }
-        w0.b = b;
-        w0.h = (int)((w0.pos - at) / n);
-        w0.t = (int)((w0.pos - at) % n);
-        w0.tiles = n;
     } else {
         w0.done = false;
-        Work<MODE> probe = w0;
-        Segment s;
-        if (!probe.next(a, QC, s)) return;                // no such block (the whole CTA)
     }
-
-    if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(kfull(s), 1); mbar_init(vfull(s), 1); mbar_init(empty(s), 1); }
-        for (int i = 0; i < 2; ++i) mbar_init(sfull(i), 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
-        mbar_init(qfull, 4 * WGS);
-        *abort_flag = 0;
-        fence_barrier_init();
-    }
-    if (warp == kWarpMma) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -413,7 +416,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     } else {
                         const size_t ph = (size_t)id * a.H + s.h;
                         ks = a.ks[ph];
-                        vs = fmaxf(a.vs[ph], 1.17549435e-38f);
+                        vs = a.vs[ph];
                     }
                 }
             };
@@ -432,24 +435,25 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     const uint32_t bytes = (uint32_t)__popc(have) * (uint32_t)(page * kHeadDim);
                     dead = __any_sync(0xffffffffu, dead);
                     if (dead) continue;
+                    if (mine && id >= 0) {
+                        const int y = (id * a.H + s.h) << a.page_shift;
+                        const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
+                        tma_load_2d(k_tile(st) + off, &map_k, kfull(st), 0, y);
+                        tma_load_2d(v_tile(st) + off, &map_v, vfull(st), 0, y);
+                    }
+                    // the scales (their loads may still be on their way) before the barrier's own arrival
                     float *sc = stage_ks + st * 32;
                     if (mine) {
+                        const float v = fmaxf(vs, 1.17549435e-38f);
                         sc[k] = ks;
-                        sc[8 + k] = __log2f(vs);
-                        sc[16 + k] = __frcp_rn(vs);
+                        sc[8 + k] = __log2f(v);
+                        sc[16 + k] = __frcp_rn(v);
                     }
                     if (lane == 0) reinterpret_cast<uint32_t *>(sc)[24] = have;
                     __syncwarp();
                     if (lane == 0) {
                         mbar_expect_tx(kfull(st), bytes);
                         mbar_expect_tx(vfull(st), bytes);
-                    }
-                    __syncwarp();
-                    if (mine && id >= 0) {
-                        const int y = (id * a.H + s.h) << a.page_shift;
-                        const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
-                        tma_load_2d(k_tile(st) + off, &map_k, kfull(st), 0, y);
-                        tma_load_2d(v_tile(st) + off, &map_v, vfull(st), 0, y);
                     }
                     issued = it + 1;
                 }
