@@ -301,88 +301,93 @@ struct StoreArgs {
 // row is read from memory while it is open.  The tokens of one page are a run of consecutive tokens with ascending slots;
 // a CTA owns the runs that START in its tile: 16 threads per row of 128, 8 elements a thread.
 // It reads a run once into registers, takes the largest finite magnitude, settles the page's scale, re-rounds the page's
-// older rows if the scale grew, and writes the new codes: the data is read once and written once.
+// older rows if the scale grew, and writes the new codes: the data is read once and written once.  What it takes is a chain
+// of dependent loads (slots, rows) and one barrier, so every warp finds the runs by itself and registers are kept few, for
+// CTAs enough to cover it.
 template <typename T, int PAGE>
-__global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a) {
-    constexpr int kRows = kStoreThreads / 16, kIter = (PAGE + kRows - 1) / kRows;
-    __shared__ int slot_s[2 * PAGE + 1];                  // [0]: the token before the tile
-    __shared__ uint32_t start_s[(2 * PAGE + 31) / 32];    // bit j: token j of the tile starts a run
-    __shared__ uint32_t max_s[kStoreThreads / 32];
+__global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 6 : 4) : (PAGE < 64 ? 6 : PAGE < 128 ? 4 : 2)) k_page_store(const StoreArgs a) {
+    constexpr int kRows = kStoreThreads / 16, kIter = (PAGE + kRows - 1) / kRows, kWords = (PAGE + 31) / 32;
+    __shared__ uint32_t max_s[2][kStoreThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int unit = blockIdx.x % (2 * a.H), which = unit & 1, h = unit >> 1;
-    const long long i0 = (long long)(blockIdx.x / (2 * a.H)) * a.tile;
-    const long long limit = (long long)a.n_pages * PAGE;
-    const int n_here = (int)min((long long)a.tile + PAGE, a.n_tokens - i0);   // tokens looked at: a run may end behind the tile
-    for (int j = tid; j <= n_here; j += kStoreThreads) slot_s[j] = i0 + j == 0 ? -2 : a.slots[i0 + j - 1];
-    __syncthreads();
-    for (int j0 = warp * 32; j0 < n_here; j0 += kStoreThreads) {
-        const int j = j0 + lane;
-        bool st = true;
-        if (j < n_here) {
-            const int s = slot_s[j + 1];
-            st = s < 0 || s % PAGE == 0 || s != slot_s[j] + 1;
+    const unsigned int units = 2 * a.H, part = blockIdx.x / units, unit = blockIdx.x - part * units;
+    const int which = unit & 1, h = unit >> 1;
+    const long long i0 = (long long)part * a.tile;
+    const int n_rest = (int)min((long long)a.n_tokens - i0, (long long)(2 * PAGE)), n_tile = min(a.tile, n_rest);
+    const int limit = a.n_pages * PAGE;                   // < 2^31
+    const int32_t *slots = a.slots + i0;
+    // the first token of the tile that starts a run; every later run of the tile follows the one before it
+    int j = n_tile;
+    for (int base = 0; base < n_tile; base += 32) {
+        const int i = base + lane;
+        bool starts = false;
+        if (i < n_tile) {
+            const int s = slots[i], before = i0 + i > 0 ? slots[i - 1] : -2;
+            starts = s < 0 || s % PAGE == 0 || s != before + 1;
         }
-        const uint32_t m = __ballot_sync(0xffffffffu, st);
-        if (lane == 0) start_s[j0 >> 5] = m;
+        const uint32_t m = __ballot_sync(0xffffffffu, starts);
+        if (m != 0u) { j = base + __ffs(m) - 1; break; }
     }
-    __syncthreads();
-    const T *x = static_cast<const T *>(a.x[which]) + (size_t)h * kHeadDim;
-    uint8_t *codes = a.codes[which];
-    float *scales = a.scale[which];
+    const T *x = static_cast<const T *>(which == 0 ? a.x[0] : a.x[1]) + (size_t)i0 * a.ld + (size_t)h * kHeadDim;
+    uint8_t *codes = which == 0 ? a.codes[0] : a.codes[1];    // (indexing the arguments would copy them to local memory)
+    float *scales = which == 0 ? a.scale[0] : a.scale[1];
     const int c8 = (tid & 15) * 8, row_t = tid >> 4;
-    const int n_tile = min(a.tile, n_here);
-    auto next_start = [&](int j) {                        // the first run that starts at or behind j
-        int k = j >> 5;
-        const int words = (n_here + 31) >> 5;
-        if (k >= words) return n_here;
-        uint32_t m = start_s[k] & (~0u << (j & 31));
-        while (m == 0u && ++k < words) m = start_s[k];
-        return m == 0u ? n_here : min(n_here, 32 * k + __ffs(m) - 1);
-    };
-    for (int j = next_start(0), j_next; j < n_tile; j = j_next) {
-        j_next = next_start(j + 1);
-        const int slot = slot_s[j + 1];
+    for (int turn = 0; j < n_tile; ++turn) {
+        const int slot = slots[j];
+        const int r0 = slot & (PAGE - 1), cap = min(PAGE - r0, n_rest - j);
+        // run length: up to the first token whose slot does not follow
+        int n = cap;
+        if (slot < 0) {
+            n = 1;
+        } else {
+            int follows[kWords];
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) follows[w] = 32 * w + lane < cap ? slots[j + 32 * w + lane] : -1;
+#pragma unroll
+            for (int w = kWords - 1; w >= 0; --w) {
+                const uint32_t m = __ballot_sync(0xffffffffu, follows[w] != slot + 32 * w + lane);
+                if (m != 0u) n = min(cap, 32 * w + __ffs(m) - 1);
+            }
+        }
+        const int at = j;
+        j += n;
         if (slot < 0) continue;
         if (slot >= limit) {
             if (tid == 0) flag(a.status, kBadSlot);
             continue;
         }
-        const int r0 = slot % PAGE, n = min(j_next - j, PAGE - r0);
         const int pg = slot / PAGE;
-        const T *src = x + (size_t)(i0 + j) * a.ld;
+        const T *src = x + (size_t)at * a.ld + c8;
         Raw8<T> raw[kIter];
         uint32_t amax = 0;
 #pragma unroll
         for (int k = 0; k < kIter; ++k) {
             const int r = row_t + k * kRows;
-            if (r < n) raw[k].load(src + (size_t)r * a.ld + c8);
+            if (r < n) raw[k].load(src + (size_t)r * a.ld);
             else raw[k].zero();
         }
+        const size_t ph = (size_t)pg * a.H + h;
+        const float s_old = r0 > 0 ? scales[ph] : 0.f;
 #pragma unroll
         for (int k = 0; k < kIter; ++k) amax = raw[k].max_bits(amax);
         amax = raw[0].to_float_bits(amax);
         if (amax >= 0x7f800000u) {                        // an infinity or NaN among them: again, without those
             amax = 0;
 #pragma unroll 1
-            for (int k = 0; k < kIter; ++k) {
-                const int r = row_t + k * kRows;
-                for (int e = 0; r < n && e < 8; ++e) amax = max(amax, finite_bits(load1(src + (size_t)r * a.ld + c8 + e)));
-            }
+            for (int r = row_t; r < n; r += kRows)
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(load1(src + (size_t)r * a.ld + e)));
         }
         amax = __reduce_max_sync(0xffffffffu, amax);
-        if (lane == 0) max_s[warp] = amax;
-        const size_t ph = (size_t)pg * a.H + h;
-        const float s_old = r0 > 0 ? scales[ph] : 0.f;
+        if (lane == 0) max_s[turn & 1][warp] = amax;
         __syncthreads();
-        amax = max_s[lane & (kStoreThreads / 32 - 1)];
-        amax = __reduce_max_sync(0xffffffffu, amax);
+        amax = __reduce_max_sync(0xffffffffu, max_s[turn & 1][lane & (kStoreThreads / 32 - 1)]);
         float s = scale_for(__uint_as_float(amax));
-        uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim);
+        uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim) + c8;
         if (r0 > 0) {
             if (s > s_old) {                              // the page's older rows, rounded again at the larger scale
                 const float mul = s_old * __uint_as_float((254u << 23) - __float_as_uint(s));
                 for (int r = row_t; r < r0; r += kRows) {
-                    uint2 *p = reinterpret_cast<uint2 *>(dst + r * kHeadDim + c8);
+                    uint2 *p = reinterpret_cast<uint2 *>(dst + r * kHeadDim);
                     const uint2 c = *p;
                     float v[8], q[4];
                     from_e4m3x4(c.x, q);
@@ -404,11 +409,10 @@ __global__ void __launch_bounds__(kStoreThreads) k_page_store(const StoreArgs a)
             if (r < n) {
                 float v[8];
                 raw[k].get(v);
-                *reinterpret_cast<uint2 *>(dst + (size_t)(r0 + r) * kHeadDim + c8) = to_e4m3x8(v, inv);
+                *reinterpret_cast<uint2 *>(dst + (r0 + r) * kHeadDim) = to_e4m3x8(v, inv);
             }
         }
         if (tid == 0) scales[ph] = s;
-        __syncthreads();                                  // max_s, and the scale if the next run is of the same page
     }
 }
 
