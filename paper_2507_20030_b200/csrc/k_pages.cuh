@@ -427,56 +427,77 @@ struct LoadArgs {
     unsigned int *status;
 };
 
-__device__ __forceinline__ void put8(__nv_bfloat16 *p, const float (&x)[8]) {
-    __nv_bfloat162 h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<uint4 *>(h));
-}
-__device__ __forceinline__ void put8(float *p, const float (&x)[8]) {
-    __stcs(reinterpret_cast<float4 *>(p), make_float4(x[0], x[1], x[2], x[3]));
-    __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
-}
+// Rows of a thread: 16 bytes of output each, so that a warp's store is contiguous.
+template <typename T> struct RowPart;
+template <> struct RowPart<__nv_bfloat16> {
+    static constexpr int kElems = 8;
+    uint2 c;
+    __device__ __forceinline__ void load(const uint8_t *p) { c = __ldcs(reinterpret_cast<const uint2 *>(p)); }
+    __device__ __forceinline__ void put(__nv_bfloat16 *p, float s) const {
+        float q[4], r[4];
+        from_e4m3x4(c.x, q);
+        from_e4m3x4(c.y, r);
+        __nv_bfloat162 h[4] = {__floats2bfloat162_rn(q[0] * s, q[1] * s), __floats2bfloat162_rn(q[2] * s, q[3] * s),
+                               __floats2bfloat162_rn(r[0] * s, r[1] * s), __floats2bfloat162_rn(r[2] * s, r[3] * s)};
+        __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<uint4 *>(h));
+    }
+    static __device__ __forceinline__ void zero(__nv_bfloat16 *p) { __stcs(reinterpret_cast<uint4 *>(p), make_uint4(0u, 0u, 0u, 0u)); }
+};
+template <> struct RowPart<float> {
+    static constexpr int kElems = 4;
+    uint32_t c;
+    __device__ __forceinline__ void load(const uint8_t *p) { c = __ldcs(reinterpret_cast<const uint32_t *>(p)); }
+    __device__ __forceinline__ void put(float *p, float s) const {
+        float q[4];
+        from_e4m3x4(c, q);
+        __stcs(reinterpret_cast<float4 *>(p), make_float4(q[0] * s, q[1] * s, q[2] * s, q[3] * s));
+    }
+    static __device__ __forceinline__ void zero(float *p) { __stcs(reinterpret_cast<float4 *>(p), make_float4(0.f, 0.f, 0.f, 0.f)); }
+};
 
-// Grid (pages of the longest row, H, sequences); a CTA turns one page of one head, K and V, into rows.
-// Rounding: to the tensor type, once (code * scale is exact in float32 but for underflow).
+// Grid (pages of the longest row, H, sequences); a CTA turns one page of one head, K and V, into rows, four rows a thread in
+// flight.  Rounding: to the tensor type, once (code * scale is exact in float32 for a power of two, else rounded there too).
 template <typename T>
 __global__ void __launch_bounds__(256) k_page_load(const LoadArgs a) {
+    using Part = RowPart<T>;
+    constexpr int kPerRow = kHeadDim / Part::kElems, kRows = 256 / kPerRow;      // threads of a row, rows at a time
     const int b = blockIdx.z, h = blockIdx.y, page = 1 << a.page_shift;
     const int n0 = blockIdx.x << a.page_shift;
     long long live = a.kv_len[b];
+    int id = blockIdx.x < a.W ? a.table[(size_t)b * a.W + blockIdx.x] : -1;      // may lie behind the sequence's end
     const long long cap = (long long)a.W << a.page_shift;
     if (live < 0 || live > cap) {
         if (threadIdx.x == 0) flag(a.status, kBadLength);
         live = live < 0 ? 0 : cap;
     }
-    int id = -1;
-    if (n0 < live) {
-        id = a.table[(size_t)b * a.W + blockIdx.x];
-        if (id < 0 || id >= a.n_pages) {
-            if (threadIdx.x == 0) flag(a.status, kBadPage);
-            id = -1;
-        }
+    if (n0 >= live) {
+        id = -1;
+    } else if (id < 0 || id >= a.n_pages) {
+        if (threadIdx.x == 0) flag(a.status, kBadPage);
+        id = -1;
     }
-    const int c8 = (threadIdx.x & 15) * 8;
+    const int n_out = min(page, a.L - n0), n_in = id < 0 ? 0 : (int)min((long long)n_out, live - n0);
+    const int row = threadIdx.x / kPerRow, el = threadIdx.x % kPerRow * Part::kElems;
+    const size_t ph = (size_t)(id < 0 ? 0 : id) * a.H + h;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         if (a.out[t] == nullptr) continue;
-        const size_t ph = (size_t)(id < 0 ? 0 : id) * a.H + h;
-        const float s = id < 0 ? 0.f : a.scale[t][ph];
-        const uint8_t *src = a.codes[t] + (ph << a.page_shift) * kHeadDim + c8;
-        T *dst = static_cast<T *>(a.out[t]) + (((size_t)b * a.H + h) * a.L + n0) * kHeadDim + c8;
-        for (int r = threadIdx.x >> 4; r < page && n0 + r < a.L; r += 16) {
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (id >= 0 && n0 + r < live) {
-                const uint2 c = __ldcs(reinterpret_cast<const uint2 *>(src + (size_t)r * kHeadDim));
-                float q[4];
-                from_e4m3x4(c.x, q);
-                x[0] = q[0] * s; x[1] = q[1] * s; x[2] = q[2] * s; x[3] = q[3] * s;
-                from_e4m3x4(c.y, q);
-                x[4] = q[0] * s; x[5] = q[1] * s; x[6] = q[2] * s; x[7] = q[3] * s;
+        const float s = n_in > 0 ? a.scale[t][ph] : 0.f;
+        const uint8_t *src = a.codes[t] + (ph << a.page_shift) * kHeadDim + el;
+        T *dst = static_cast<T *>(a.out[t]) + (((size_t)b * a.H + h) * a.L + n0) * kHeadDim + el;
+        for (int r0 = row; r0 < n_out; r0 += 4 * kRows) {
+            Part p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + k * kRows;
+                if (r < n_in) p[k].load(src + r * kHeadDim);
             }
-            put8(dst + (size_t)r * kHeadDim, x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + k * kRows;
+                if (r < n_in) p[k].put(dst + (size_t)r * kHeadDim, s);
+                else if (r < n_out) Part::zero(dst + (size_t)r * kHeadDim);
+            }
         }
     }
 }
