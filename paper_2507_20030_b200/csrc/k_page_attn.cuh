@@ -14,10 +14,11 @@
 // lost is only what the last term rounds off (bf16 q: two terms, exact; bf16 weights: three terms, 2^-13 of a weight, or
 // two, 2^-9, where many columns share a tile; float32: six terms, 2^-25).
 //
-// Softmax runs in base 2 with the page scales inside: x = s * (k_scale * scale * log2 e) + log2(v_scale), weights
-// w = 2^(x - Mu), sum l += w / v_scale.  Mu follows the column maximum lazily: it is raised (and O, l rescaled) only when
-// some x exceeds it by 8, and then to 2 below the maximum, so weights stay in e4m3's range and most tiles exchange one
-// vote instead of a maximum per column.  O stays in TMEM over all tiles of a segment.
+// Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
+// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8, and then to 2 below the
+// maximum, so weights stay in e4m3's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
+// power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
+// segment.
 //
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.
@@ -299,7 +300,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
     int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
     float *red = reinterpret_cast<float *>(col_set + QC);                    // [4][QC]
-    float *stage_ks = red + 4 * QC;                                          // [STAGES][32]: 8 k_scale, 8 log2 v_scale, 8 1 / v_scale, pages mask
+    float *stage_ks = red + 4 * QC;                                          // [STAGES][32]: 8 k_scale, 8 v_scale, the largest |v_scale|, at 24 the pages that are there
     uint64_t *bars = reinterpret_cast<uint64_t *>(stage_ks + STAGES * 32);
     const uint32_t bar0 = smem_u32(bars);
     auto kfull = [&](int s) { return bar0 + 8 * s; };
@@ -407,7 +408,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             const int32_t *row = a.table + (size_t)s.b * a.W;
             auto fetch = [&](int t_first, int &id, float &ks, float &vs) {
                 const long long p = ((long long)t_first << lg_ppt) + lane;
-                id = -1; ks = 0.f; vs = 1.f;
+                id = -1; ks = 0.f; vs = 0.f;
                 if ((p << a.page_shift) < s.live && t_first + (lane >> lg_ppt) < s.t1) {
                     id = row[p];
                     if (id < 0 || id >= a.n_pages) {
@@ -443,13 +444,15 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                     // the scales (their loads may still be on their way) before the barrier's own arrival
                     float *sc = stage_ks + st * 32;
+                    const float v_max = warp_max(mine ? fabsf(vs) : 0.f);
                     if (mine) {
-                        const float v = fmaxf(vs, 1.17549435e-38f);
                         sc[k] = ks;
-                        sc[8 + k] = __log2f(v);
-                        sc[16 + k] = __frcp_rn(v);
+                        sc[8 + k] = vs;
                     }
-                    if (lane == 0) reinterpret_cast<uint32_t *>(sc)[24] = have;
+                    if (lane == 0) {
+                        sc[16] = v_max;
+                        reinterpret_cast<uint32_t *>(sc)[24] = have;
+                    }
                     __syncwarp();
                     if (lane == 0) {
                         mbar_expect_tx(kfull(st), bytes);
@@ -583,7 +586,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
             for (int p = 0; p < QW / 2; ++p) l[p] = make_float2(0.f, 0.f);
             unsigned long long poison = 0;                 // columns (of the warpgroup) whose channel `row` met a NaN value
-            bool raise = true;                             // some column's Mu does not stand for a maximum yet
+            bool unset_any = true;                         // some column's Mu does not stand for a maximum yet
+            float v_ref = 0.f, v_inv = 0.f;
 
             for (int t = s.t0; t < s.t1; ++t, ++it) {
                 const int st = it % STAGES, pb = it & 1;
@@ -594,17 +598,25 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 tc_fence_after();
                 const float *sc = stage_ks + st * 32;
                 const int pg = row >> a.page_shift;
-                const float ks = sc[pg], lvs = sc[8 + pg];
-                float ivs = sc[16 + pg];
+                const float ks = sc[pg], vs = sc[8 + pg], v_max = sc[16];
                 const uint32_t have = reinterpret_cast<const uint32_t *>(sc)[24];
                 const int tok = t * kTile + row;
                 // columns may see a different number of this tile's tokens, or pages may be missing
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
-                if (masked && !valid) ivs = 0.f;
-                const float2 ks2 = make_float2(ks, ks), lvs2 = make_float2(lvs, lvs), ivs2 = make_float2(ivs, ivs);
+                const float2 ks2 = make_float2(ks, ks);
+                // a larger v_scale than any before, or a column without a maximum: raised before the weights are taken
+                bool raise = __any_sync(0xffffffffu, unset_any || v_max > v_ref);
+                float o_factor = 1.f;
+                if (raise && !(v_max <= v_ref)) {
+                    const float up = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
+                    if (v_ref > 0.f) o_factor = v_ref / up;
+                    v_ref = up;
+                    v_inv = __fdiv_rn(1.f, up);
+                }
+                const float2 r2 = make_float2(vs * v_inv, vs * v_inv);
                 const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
-                // y = x - Mu of the columns c_wg + c0 .. from their raw scores
+                // y of the columns c_wg + c0 .. from their raw scores
                 auto exponents = [&](const float(&raw)[kLoad], int c0, float2(&y)[kPart / 2]) {
 #pragma unroll
                     for (int p = 0; p < kPart / 2; ++p) {
@@ -618,7 +630,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 v = fma2(v, make_float2(kTerm, kTerm), make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
                         }
                         const float4 fm = col4[(c_wg + c0) / 2 + p];
-                        y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), add2(lvs2, make_float2(fm.z, fm.w)));
+                        y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), make_float2(fm.z, fm.w));
                     }
                     if (masked) {
 #pragma unroll
@@ -648,12 +660,13 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             y[p] = make_float2(ex2(y[p].x), ex2(y[p].y));
                             float2 &sum = l[c0 / 2 + p];
                             if (!decltype(repeat)::value) {
-                                sum = fma2(y[p], ivs2, sum);
+                                sum = add2(sum, y[p]);
                             } else {                       // this tile is in the sum already, unless that was dropped
                                 const float2 f = *reinterpret_cast<const float2 *>(col_f + c_wg + c0 + 2 * p);
-                                if (f.x == 0.f) sum.x = y[p].x * ivs;
-                                if (f.y == 0.f) sum.y = y[p].y * ivs;
+                                if (f.x == 0.f) sum.x = y[p].x;
+                                if (f.y == 0.f) sum.y = y[p].y;
                             }
+                            y[p] = mul2(y[p], r2);
                         }
                         const float2 minus = make_float2(-1.f, -1.f);
                         if constexpr (C::CHAIN) {
@@ -742,7 +755,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             if (seen) col_set[c] = 1;
                             unset = first && !seen;
                         }
-                        raise = softmax_any(unset, 2 + wg, 128);
+                        unset_any = softmax_any(unset, 2 + wg, 128);
+                        raise = false;
 #pragma unroll
                         for (int p = 0; p < QW / 2; ++p) l[p] = mul2(l[p], *reinterpret_cast<const float2 *>(col_f + c_wg + 2 * p));
                         if (t > s.t0) {
@@ -754,11 +768,12 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 tmem_ld<16>(tmem_o + lane_addr + c_wg + c0, o);
                                 tmem_ld_done<16>(o);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC];
+                                for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC] * o_factor;
                                 tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
                             }
                             tmem_st_wait();
                         }
+                        o_factor = 1.f;
                         done_max = true;
                     }
                     const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
@@ -830,28 +845,26 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     slot[QC + c] = sum;
                 }
             }
+            for (int c = tid; c < QC; c += kSoftmax) {
+                const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
+            }
+            softmax_bar(1, kSoftmax);
             if constexpr (MODE == 0)
                 if (s.t0 == 0 && tid == 0) {               // first tile of the unit: where the join finds its parts
                     UnitMeta *m = reinterpret_cast<UnitMeta *>(a.ws + 16) + (size_t)s.b * a.H + s.h;
                     m->first = w.pos - (s.t1 - s.t0);
                     m->tiles = s.tiles;
                 }
-            if (whole) {
-                for (int c = tid; c < QC; c += kSoftmax) {
-                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
-                    col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
-                }
-                softmax_bar(1, kSoftmax);
-            }
             T *out_row = static_cast<T *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
             const size_t out_tok = (size_t)a.H * a.G * kHeadDim;
             auto put = [&](int c, float v) {
                 if (c >= n_cols) return;
-                if (s.t1 == s.t0) v = 0.f;                 // an empty split
+                v = col_f[c] == 0.f ? 0.f : v * col_f[c] * v_ref;     // no token, or an empty split: zero
                 if (MODE == 1 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
                 if (whole) {
                     const int tok = c * a.inv_g >> 16;
-                    store1(out_row + tok * out_tok + (c - tok * a.G) * kHeadDim, col_f[c] == 0.f ? 0.f : v * col_f[c]);
+                    store1(out_row + tok * out_tok + (c - tok * a.G) * kHeadDim, v);
                 } else {
                     slot[2 * QC + (size_t)c * kHeadDim + row] = v;
                 }
@@ -956,8 +969,8 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
             const float back = ex2(mu - top);
             if (grp == 0) {
                 const float f = ex2(m - top);
-                f_s[d] = f;
-                l *= f;
+                l *= f;                                    // a part's output is divided by its sum already
+                f_s[d] = l;
 #pragma unroll
                 for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
                 if ((d & 31) == 0) red_s[1][d >> 5] = l;
