@@ -524,6 +524,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const int wg = warp >> 2, row = tid & 127, c_wg = wg * QW;            // this thread's token / channel, its first column
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
+        auto mu_at = [&](int c) -> float & { return C::CHAIN ? col[c] : col[(c >> 1) * 4 + 2 + (c & 1)]; };   // -Mu of column c
+        const float2 *col_mu = reinterpret_cast<const float2 *>(col);
         const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
         constexpr int kPart = C::CHAIN ? C::PART : QW, kLoad = C::CHAIN ? C::PART : NS;  // columns at a time, raw scores of them
         Work<MODE> w = w0;
@@ -540,20 +542,40 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const int c = warp + 4 * WGS * j, tok = c * a.inv_g >> 16;
                 q_in[j] = c < n_cols ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+            // one power of two for all columns where they are many (it stays out of the softmax's inner loop): an element is
+            // then off by at most 2^-16 of the largest of them; one for each column otherwise
+            float unit_top = 0.f;
+            if constexpr (C::CHAIN) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    m = max(max(m, max(finite_bits(q_in[j].x), finite_bits(q_in[j].y))), max(finite_bits(q_in[j].z), finite_bits(q_in[j].w)));
+                m = __reduce_max_sync(0xffffffffu, m);
+                if (lane == 0) red[warp] = __uint_as_float(m);
+                softmax_bar(1, kSoftmax);
+#pragma unroll
+                for (int i = 0; i < 4 * WGS; ++i) unit_top = fmaxf(unit_top, red[i]);
+                softmax_bar(1, kSoftmax);
+            }
+            float unit_cs = 0.f;
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const int c = warp + 4 * WGS * j;
                 float x[4] = {q_in[j].x, q_in[j].y, q_in[j].z, q_in[j].w};
-                uint32_t m = 0;
+                uint32_t m = __float_as_uint(unit_top);
+                if constexpr (!C::CHAIN) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
-                const float qs = 2.0f * scale_for(__uint_as_float(__reduce_max_sync(0xffffffffu, m)));
+                    for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
+                    m = __reduce_max_sync(0xffffffffu, m);
+                }
+                const float qs = 2.0f * scale_for(__uint_as_float(m));
+                unit_cs = qs * a.scale_log2;
                 const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
                 if (lane == 0) {
-                    col[(c >> 1) * 4 + (c & 1)] = qs * a.scale_log2;
-                    col[(c >> 1) * 4 + 2 + (c & 1)] = 0.f;
+                    if (!C::CHAIN) col[(c >> 1) * 4 + (c & 1)] = unit_cs;
+                    mu_at(c) = 0.f;
                     col_lim[c] = c < n_cols ? s.see0 + (int)(c * a.inv_g >> 16) : 0;
                     col_set[c] = c < n_cols ? 0 : 1;
                 }
@@ -604,7 +626,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 // columns may see a different number of this tile's tokens, or pages may be missing
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
-                const float2 ks2 = make_float2(ks, ks);
+                const float kf = C::CHAIN ? ks * unit_cs : ks;
+                const float2 ks2 = make_float2(kf, kf);
                 // a larger v_scale than any before, or a column without a maximum: raised before the weights are taken
                 bool raise = __any_sync(0xffffffffu, unset_any || v_max > v_ref);
                 float o_factor = 1.f;
@@ -629,8 +652,12 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             for (int i = QT - 2; i >= 0; --i)
                                 v = fma2(v, make_float2(kTerm, kTerm), make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
                         }
-                        const float4 fm = col4[(c_wg + c0) / 2 + p];
-                        y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), make_float2(fm.z, fm.w));
+                        if constexpr (C::CHAIN) {
+                            y[p] = fma2(v, ks2, col_mu[(c_wg + c0) / 2 + p]);
+                        } else {
+                            const float4 fm = col4[(c_wg + c0) / 2 + p];
+                            y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), make_float2(fm.z, fm.w));
+                        }
                     }
                     if (masked) {
 #pragma unroll
@@ -749,7 +776,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - kLagTo;
                             const bool first = col_set[c] == 0, seen = m > -INFINITY;
                             const float d = seen && (first || m > 0.f) ? m : 0.f;
-                            col[(c >> 1) * 4 + 2 + (c & 1)] -= d;
+                            mu_at(c) -= d;
                             // 1: nothing has been summed yet; 0: what has been is beyond float32's reach
                             col_f[c] = first ? 1.f : d > 64.f ? 0.f : ex2(-d);
                             if (seen) col_set[c] = 1;
@@ -841,7 +868,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 slot = reinterpret_cast<float *>(a.ws + head) + (size_t)s.slot * attn_slot_floats(QC);
                 for (int c = tid; c < n_cols; c += kSoftmax) {
                     const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
-                    slot[c] = sum == 0.f ? kMuNone : -col[(c >> 1) * 4 + 2 + (c & 1)];
+                    slot[c] = sum == 0.f ? kMuNone : -mu_at(c);
                     slot[QC + c] = sum;
                 }
             }
