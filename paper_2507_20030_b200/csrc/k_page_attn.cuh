@@ -121,6 +121,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
     return d;
 }
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) {
+    float2 d;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -608,6 +614,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
             for (int p = 0; p < QW / 2; ++p) l[p] = make_float2(0.f, 0.f);
             unsigned long long poison = 0;                 // columns (of the warpgroup) whose channel `row` met a NaN value
+            static_assert(!C::CHAIN || QW == 32, "one pair of chunks a warpgroup");
+            const uint32_t p_off = mn_chunk<C::PW>(row, (uint32_t)c_wg >> 4);
             bool unset_any = true;                         // some column's Mu does not stand for a maximum yet
             float v_ref = 0.f, v_inv = 0.f;
 
@@ -669,6 +677,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                 };
                 uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
+                uint8_t *prow0 = prow + p_off, *prow1 = prow + (p_off ^ 16u);
                 // weights, their sum, their e4m3 terms; returns the largest exponent
                 auto weights = [&](auto repeat) {
                     float excess = -INFINITY;
@@ -693,9 +702,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 if (f.x == 0.f) sum.x = y[p].x;
                                 if (f.y == 0.f) sum.y = y[p].y;
                             }
-                            y[p] = mul2(y[p], r2);
+                            y[p].x *= r2.x; y[p].y *= r2.x;
                         }
-                        const float2 minus = make_float2(-1.f, -1.f);
                         if constexpr (C::CHAIN) {
                             // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
                             // make up for it: an error below 2^-10 beside a largest weight of 2^2 and more
@@ -714,13 +722,15 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                             if (i < PT - 1) {
                                                 h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
                                                 h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                                v = fma2(h[e], minus, v);
+                                                v = sub2(v, h[e]);
                                             }
                                         }
                                         u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
                                     }
-                                    const int c = c_wg + c0 + j;
-                                    *reinterpret_cast<uint2 *>(prow + i * kTile * C::PW + mn_chunk<C::PW>(row, (uint32_t)c >> 4) + (c & 8)) = make_uint2(u[0], u[1]);
+                                    // (16-byte chunks k and k + 1 of a row, k even, differ in address bit 4 alone)
+                                    const int c = c0 + j;
+                                    uint8_t *at = (c & 16) ? prow1 : prow0;
+                                    *reinterpret_cast<uint2 *>(at + i * kTile * C::PW + ((c & ~31) >> 4) * 16 + (c & 8)) = make_uint2(u[0], u[1]);
                                 }
                         } else {
                             const float2 sixteen = make_float2(16.f, 16.f);
@@ -738,7 +748,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                         h[e] = v;
                                         if (i < PT - 1) {
                                             h[e] = make_float2(lead4(v.x), lead4(v.y));
-                                            v = mul2(fma2(h[e], minus, v), sixteen);
+                                            v = mul2(sub2(v, h[e]), sixteen);
                                         }
                                     }
                                     u[(i * QC + j) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
