@@ -147,31 +147,32 @@ static_assert(kDecodeCtas == DecodeF32::CTAS && DecodeF32::QC == 8 && DecodeBf16
 // How a call is cut up.
 struct AttnPlan {
     bool wide;               // 128 columns a unit instead of 8
-    int qc, blocks, splits;  // MODE 1: blocks of new tokens, splits of the cached ones
-    int ctas;                // MODE 0
+    int qc, blocks;          // columns of a unit; blocks of new tokens, at most
+    bool shared;             // blocks few enough for their tiles to be shared out evenly (MODE 1); else a CTA each (MODE 2)
     long long max_tiles;     // of a table row
-    size_t bytes0, bytes1;   // workspace of the two modes
+    int ctas0, ctas1;        // MODE 0 and 1
+    size_t bytes0, bytes1;   // workspace of MODE 0, of the others
 };
 
 AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     const faedkv_pages_config &c = pg->cfg;
     AttnPlan p{};
-    const long long max_tiles = p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
+    p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
     // more query columns per sequence than 8: a block of 128 columns reads the cache once for all of them
     p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;
-    const long long units = (long long)p.blocks * c.n_kv_heads, room = (long long)pg->n_sm * (p.wide ? ChunkBf16::CTAS : kDecodeCtas);
-    // fewer units than the SMs hold: the cached tokens are split until they are full.  (Splitting more units too, for a
-    // shorter last round, was slower: 2 splits 1011 us, 1 split 935 us at 2048 new tokens over 18432.)
-    long long splits = room / (units > 0 ? units : 1);
-    if (splits > (max_tiles + 1) / 2) splits = (max_tiles + 1) / 2;
-    p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
-    p.bytes1 = p.splits > 1 ? (size_t)units * p.splits * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
-    const long long all_tiles = max_tiles * batch * c.n_kv_heads;
-    const long long most = (long long)pg->n_sm * kDecodeCtas;
-    p.ctas = (int)(all_tiles < most ? all_tiles : most);
-    p.bytes0 = 16 + sizeof(pages::UnitMeta) * (size_t)batch * c.n_kv_heads + (size_t)p.ctas * 2 * pages::attn_slot_floats(8) * sizeof(float);
+    p.shared = p.blocks <= pages::kMaxBlocks;
+    auto ctas = [&](long long units, int per_sm) {
+        const long long most = (long long)pg->n_sm * per_sm, tiles = p.max_tiles * units;
+        return (int)(tiles < most ? tiles : most);
+    };
+    auto slots = [&](int n_ctas, int qc) { return (size_t)n_ctas * 2 * pages::attn_slot_floats(qc) * sizeof(float); };
+    const long long units0 = (long long)batch * c.n_kv_heads, units1 = (long long)p.blocks * c.n_kv_heads;
+    p.ctas0 = ctas(units0, kDecodeCtas);
+    p.ctas1 = ctas(units1, p.wide ? ChunkBf16::CTAS : kDecodeCtas);
+    p.bytes0 = pages::attn_meta_bytes(0, (size_t)units0, 0) + slots(p.ctas0, 8);
+    p.bytes1 = p.shared ? pages::attn_meta_bytes(1, 0, (size_t)p.ctas1) + slots(p.ctas1, p.qc) : 16;
     return p;
 }
 
@@ -179,19 +180,23 @@ template <typename C, int MODE>
 int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int attr_bit,
                 cudaStream_t st) {
     auto kernel = pages::k_page_attn<C, MODE>;
+    constexpr uint32_t smem = C::kSmemBytes + (MODE == 1 ? C::kSmemBlocks : 0);
     if (!(pg->attr_set & (1u << attr_bit))) {
-        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes));
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         pg->attr_set |= 1u << attr_bit;
     }
-    const dim3 grid = MODE == 0 ? dim3(p.ctas) : dim3(p.blocks, a.H, p.splits);
-    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), C::kSmemBytes, st, mk, mv, a));
+    const dim3 grid = MODE == 0 ? dim3(p.ctas0) : MODE == 1 ? dim3(p.ctas1) : dim3(p.blocks, a.H);
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
     if (int r = launch_check(pg, "k_page_attn")) return r;
-    if (MODE == 0 ? p.max_tiles == 1 : p.splits == 1) return FAEDKV_OK;      // no unit is ever in parts
-    // few units: a block per column; many, with few parts each: a block joins 16 columns
-    const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 || p.splits > 8 ? 1 : 16;
-    const dim3 jgrid((unsigned)((MODE == 0 ? a.B : p.blocks) * a.H), (cols + each - 1) / each);
-    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC, each));
-    return launch_check(pg, "k_page_attn_join");
+    if (MODE == 2 || p.max_tiles == 1) return FAEDKV_OK;                     // no unit is ever in parts
+    if constexpr (MODE != 2) {
+        const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 4;
+        const dim3 jgrid((unsigned)(MODE == 0 ? a.B * a.H : p.ctas1), (cols + each - 1) / each);
+        CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC,
+                                each, MODE == 0 ? p.ctas0 : p.ctas1));
+        return launch_check(pg, "k_page_attn_join");
+    }
+    return FAEDKV_OK;
 }
 
 }  // namespace
@@ -349,13 +354,17 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const AttnPlan p = plan_attn(pg, batch, n_tokens);
     const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
-                            c.max_pages, c.n_pages, pg->page_shift, p.splits,
+                            c.max_pages, c.n_pages, pg->page_shift, p.blocks,
                             65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status};
     if (c.kv_dtype == FAEDKV_F32)
-        return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st) : launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st);
-    if (q_start == nullptr) return launch_attn<DecodeBf16, 0>(pg, mk, mv, a, p, 2, st);
-    return p.wide ? launch_attn<ChunkBf16, 1>(pg, mk, mv, a, p, 3, st) : launch_attn<DecodeBf16, 1>(pg, mk, mv, a, p, 4, st);
+        return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st)
+               : p.shared         ? launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st)
+                                  : launch_attn<DecodeF32, 2>(pg, mk, mv, a, p, 2, st);
+    if (q_start == nullptr) return launch_attn<DecodeBf16, 0>(pg, mk, mv, a, p, 3, st);
+    if (p.wide)
+        return p.shared ? launch_attn<ChunkBf16, 1>(pg, mk, mv, a, p, 4, st) : launch_attn<ChunkBf16, 2>(pg, mk, mv, a, p, 5, st);
+    return p.shared ? launch_attn<DecodeBf16, 1>(pg, mk, mv, a, p, 6, st) : launch_attn<DecodeBf16, 2>(pg, mk, mv, a, p, 7, st);
 }
 
 int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *table, int batch, int L, const void *k_pages,

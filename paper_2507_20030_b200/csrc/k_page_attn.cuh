@@ -15,7 +15,7 @@
 // two, 2^-9, where many columns share a tile; float32: six terms, 2^-25).
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
-// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8, and then to 2 below the
+// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 2 below the
 // maximum, so weights stay in e4m3's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
 // power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
 // segment.
@@ -34,8 +34,9 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr float kLagMax = 8.0f, kLagTo = 2.0f;            // weights stay <= 2^8; after a raise the largest is 2^2
+constexpr float kLagTo = 2.0f;                            // after a raise of Mu the largest weight is 2^2
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
+constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
 
 // Instances: QC query columns over WGS softmax warpgroups, QT / PT terms of q / of the weights, the terms side by side as
@@ -47,6 +48,8 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int PAR
     static constexpr bool CHAIN = CHAIN_;
     static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
     static constexpr int kThreads = 128 * WGS + 64;
+    // the largest weight: e4m3 ends at 448, and a second term that is scaled by 16 needs the first one's step to be 16
+    static constexpr float kLagMax = CHAIN ? 8.75f : 8.0f;
     static constexpr int NS = CHAIN ? QC : (QC * QT + 15) / 16 * 16;          // columns of S, of O
     static constexpr int NO = CHAIN ? QC : (QC * PT + 15) / 16 * 16;
     static constexpr int kTmemUsed = 2 * NS + NO;
@@ -58,6 +61,7 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int PAR
     static constexpr uint32_t kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
     static constexpr uint32_t kOffMisc = kOffP + 2 * kPBytes;
     static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + STAGES * 32) + 256 + 1024;
+    static constexpr uint32_t kSmemBlocks = 4 * (kMaxBlocks + 1);             // MODE 1 appends its prefix sums
     static_assert(!CHAIN || PW >= NO, "a chained term fits its rows");
     static_assert(!CHAIN || (PART % 8 == 0 && QW % PART == 0), "whole parts");
     static_assert(WGS == 1 || CHAIN, "warpgroups share chained columns");
@@ -69,15 +73,19 @@ struct AttnArgs {
     const int32_t *q_start, *kv_len, *table;              // q_start may be NULL: one token per sequence
     const float *ks, *vs;
     long long ld_q;
-    int n_tokens, B, H, G, W, n_pages, page_shift, splits;
+    int n_tokens, B, H, G, W, n_pages, page_shift, blocks;
     uint32_t inv_g;                                       // c * inv_g >> 16 = c / G for the columns c < 128
     float scale_log2;                                     // scale * log2(e)
     unsigned char *ws;
     unsigned int *status;
 };
 
-// Workspace of a decode step (MODE 0): header, one record per (sequence, kv head), two partial results per CTA.
-struct UnitMeta { long long first; int tiles, pad; };
+// Workspace of MODE 0 and 1: header, records, two partial results per CTA (of the unit it goes on with, of the one it leaves).
+struct UnitMeta { long long first; int tiles, pad; };                             // MODE 0, by unit
+struct CtaMeta { long long first; int tiles, tok0, n_cols, h; };                  // MODE 1, by CTA: the unit that a CTA goes on with (tiles = 0: none)
+__host__ __device__ constexpr size_t attn_meta_bytes(int mode, size_t units, size_t ctas) {
+    return 16 + (mode == 0 ? sizeof(UnitMeta) * units : (sizeof(CtaMeta) * ctas + 15) / 16 * 16);
+}
 __host__ __device__ constexpr size_t attn_slot_floats(int qc) { return (size_t)qc * (kHeadDim + 2); }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -213,7 +221,7 @@ struct Segment {
     int see0;                    // tokens that the first query token sees (its column limit); the i-th sees see0 + i
     int live;                    // tokens that the last one sees, >= 0
     int t0, t1, tiles;           // tiles of the segment, of the unit
-    long long slot;              // where a partial result goes
+    long long first;             // position of the unit's first tile among all
 };
 
 __device__ __forceinline__ long long clamp_len(const AttnArgs &a, int b, bool report) {
@@ -227,14 +235,40 @@ __device__ __forceinline__ long long clamp_len(const AttnArgs &a, int b, bool re
 }
 __device__ __forceinline__ int tiles_of(long long live) { return live <= 0 ? 1 : (int)((live + kTile - 1) / kTile); }
 
+// Which new tokens block v of a call with blocks of tq holds: block v - (q_start[b] / tq + b) of sequence b, since sequences
+// begin at distinct numbers of that form.  Not every v is a block.
+struct Block { int b, tok0, n_tok, see0, live; };
+__device__ __forceinline__ bool find_block(const AttnArgs &a, int tq, int v, bool report, Block &k) {
+    int lo = 0, hi = a.B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.q_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
+    }
+    const int first = a.q_start[lo], n = a.q_start[lo + 1] - first;
+    if (first < 0 || n < 0 || first > a.n_tokens - n) {
+        if (report) flag(a.status, kBadStart);
+        return false;
+    }
+    const int j = v - (first / tq + lo);
+    if (j < 0 || (long long)j * tq >= n) return false;
+    k.b = lo;
+    k.tok0 = first + j * tq;
+    k.n_tok = min(tq, n - j * tq);
+    k.see0 = (int)clamp_len(a, lo, report) - n + j * tq + 1;
+    k.live = max(0, k.see0 + k.n_tok - 1);
+    return true;
+}
+
 // MODE 0, a decode step: the tiles of all (sequence, head) units in a row are cut into equal shares, one per CTA; a share
-// begins and ends anywhere inside a unit.  MODE 1, blocks of new tokens: CTA (v, h, s) is split s of one unit.
+// begins and ends anywhere inside a unit.  MODE 1, blocks of new tokens: the same over (head, block) units, whose sizes stand
+// as prefix sums in shared memory; a unit counts for kUnitCost positions more than it has tiles, which is what its queries,
+// its first maxima and its output take.  MODE 2, more blocks than MODE 1 takes: a CTA per unit.
+constexpr int kUnitCost = 8;
 template <int MODE> struct Work;
 
 template <> struct Work<0> {
     int b, h, t, tiles;
     long long pos, end;
-    bool at_start;
     __device__ __forceinline__ bool next(const AttnArgs &a, int, Segment &s) {
         if (pos >= end) return false;
         s.b = b; s.h = h; s.tok0 = b; s.n_tok = 1;
@@ -242,10 +276,9 @@ template <> struct Work<0> {
         s.see0 = s.live;
         tiles = tiles_of(s.live);
         s.tiles = tiles; s.t0 = t;
+        s.first = pos - t;
         const long long left = end - pos;
         s.t1 = left < tiles - t ? t + (int)left : tiles;
-        s.slot = (long long)blockIdx.x * 2 + (at_start ? 0 : 1);
-        at_start = false;
         pos += s.t1 - s.t0;
         t = 0;
         if (++h == a.H) { h = 0; ++b; }
@@ -254,35 +287,44 @@ template <> struct Work<0> {
 };
 
 template <> struct Work<1> {
+    int v, h, per_head;
+    long long pos, end;
+    const int32_t *before;                                // [blocks + 1]: positions of one head's blocks before block v
+    __device__ __forceinline__ bool next(const AttnArgs &a, int qc, Segment &s) {
+        while (pos < end) {
+            while (before[v + 1] == before[v])            // not a block
+                if (++v == a.blocks) { v = 0; ++h; }
+            const long long u0 = (long long)h * per_head + before[v];
+            const int size = before[v + 1] - before[v], to = (int)min((long long)size, end - u0);
+            s.t0 = max(0, (int)(pos - u0) - kUnitCost);
+            s.t1 = max(0, to - kUnitCost);
+            s.h = h;
+            const int block = v;
+            pos = u0 + to;
+            if (++v == a.blocks) { v = 0; ++h; }
+            if (s.t1 <= s.t0) continue;                   // the share ended before the unit's first tile
+            Block k;
+            if (!find_block(a, qc / a.G, block, false, k)) return false;
+            s.b = k.b; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live;
+            s.tiles = size - kUnitCost;
+            s.first = u0 + kUnitCost;
+            return true;
+        }
+        return false;
+    }
+};
+
+template <> struct Work<2> {
     bool done;
     __device__ __forceinline__ bool next(const AttnArgs &a, int qc, Segment &s) {
         if (done) return false;
         done = true;
-        const int tq = qc / a.G;
-        const int v = (int)(gridDim.x - 1 - blockIdx.x);   // the blocks that see most first
-        // block v of the call is block v - (q_start[b] / tq + b) of sequence b: sequences begin at distinct numbers
-        int lo = 0, hi = a.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.q_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
-        }
-        const int first = a.q_start[lo];
-        int n = a.q_start[lo + 1] - first;
-        if (first < 0 || n < 0 || first > a.n_tokens - n) {
-            if (threadIdx.x == 0) flag(a.status, kBadStart);
-            return false;
-        }
-        const int j = v - (first / tq + lo);
-        if (j < 0 || (long long)j * tq >= n) return false;
-        s.b = lo; s.h = blockIdx.y; s.tok0 = first + j * tq;
-        s.n_tok = min(tq, n - j * tq);
-        const int kv = (int)clamp_len(a, lo, threadIdx.x == 0);
-        s.see0 = kv - n + j * tq + 1;
-        s.live = max(0, s.see0 + s.n_tok - 1);
+        Block k;
+        // the blocks that see most first
+        if (!find_block(a, qc / a.G, (int)(gridDim.x - 1 - blockIdx.x), threadIdx.x == 0, k)) return false;
+        s.b = k.b; s.h = blockIdx.y; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live;
         s.tiles = tiles_of(s.live);
-        s.t0 = (int)((long long)s.tiles * blockIdx.z / a.splits);
-        s.t1 = (int)((long long)s.tiles * (blockIdx.z + 1) / a.splits);
-        s.slot = ((long long)v * a.H + s.h) * a.splits + blockIdx.z;
+        s.t0 = 0; s.t1 = s.tiles; s.first = 0;
         return true;
     }
 };
@@ -362,7 +404,6 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const long long share = total < (1LL << 31) ? (long long)(((uint32_t)total + gridDim.x - 1) / gridDim.x) : (total + gridDim.x - 1) / gridDim.x;
         w0.pos = share * blockIdx.x;
         w0.end = min(total, w0.pos + share);
-        w0.at_start = true;
         if (tid == 0 && blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
         if (w0.pos < w0.end) {
             // the run that holds sequence tile pos / H ... then the sequence, one after the other
@@ -383,6 +424,45 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             w0.h = in < (1LL << 31) ? (int)((uint32_t)in / (uint32_t)n) : (int)(in / n);
             w0.t = (int)(in - (long long)w0.h * n);
             w0.tiles = n;
+        }
+    } else if constexpr (MODE == 1) {
+        int32_t *before = reinterpret_cast<int32_t *>(gbase + C::kOffMisc + (C::kSmemBytes - 1024 - C::kOffMisc));
+        for (int v = tid; v < a.blocks; v += C::kThreads) {
+            Block k;
+            before[v + 1] = find_block(a, QC / a.G, v, blockIdx.x == 0, k) ? kUnitCost + tiles_of(k.live) : 0;
+        }
+        if (tid == 0) before[0] = 0;
+        __syncthreads();
+        if (warp == 0)
+            for (int v0 = 0, carry = 0; v0 < a.blocks; v0 += 32) {
+                int n = v0 + lane < a.blocks ? before[v0 + lane + 1] : 0;
+#pragma unroll
+                for (int s = 1; s < 32; s <<= 1) {
+                    const int o = __shfl_up_sync(0xffffffffu, n, s);
+                    if (lane >= s) n += o;
+                }
+                n += carry;
+                if (v0 + lane < a.blocks) before[v0 + lane + 1] = n;
+                carry = __shfl_sync(0xffffffffu, n, 31);
+            }
+        __syncthreads();
+        const int per_head = before[a.blocks];
+        const long long total = (long long)per_head * a.H, share = (total + gridDim.x - 1) / gridDim.x;
+        w0.before = before;
+        w0.pos = share * blockIdx.x;
+        w0.end = min(total, w0.pos + share);
+        w0.per_head = per_head;
+        if (tid == 0 && blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
+        if (tid == 0) reinterpret_cast<CtaMeta *>(a.ws + 16)[blockIdx.x].tiles = 0;
+        if (w0.pos < w0.end) {
+            w0.h = (int)(w0.pos / per_head);
+            const int in = (int)(w0.pos - (long long)w0.h * per_head);
+            int lo = 0, hi = a.blocks - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (before[mid] <= in) lo = mid; else hi = mid - 1;
+            }
+            w0.v = lo;
         }
     } else {
         w0.done = false;
@@ -636,10 +716,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
                 const float kf = C::CHAIN ? ks * unit_cs : ks;
                 const float2 ks2 = make_float2(kf, kf);
-                // a larger v_scale than any before, or a column without a maximum: raised before the weights are taken
-                bool raise = __any_sync(0xffffffffu, unset_any || v_max > v_ref);
+                // a column without a maximum: Mu is settled before the weights are taken; a larger v_scale than any before: Vref
+                bool raise = unset_any;
                 float o_factor = 1.f;
-                if (raise && !(v_max <= v_ref)) {
+                if (v_max > v_ref) {
                     const float up = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
                     if (v_ref > 0.f) o_factor = v_ref / up;
                     v_ref = up;
@@ -793,29 +873,32 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             unset = first && !seen;
                         }
                         unset_any = softmax_any(unset, 2 + wg, 128);
-                        raise = false;
 #pragma unroll
                         for (int p = 0; p < QW / 2; ++p) l[p] = mul2(l[p], *reinterpret_cast<const float2 *>(col_f + c_wg + 2 * p));
-                        if (t > s.t0) {
-                            tc_fence_after();
-                            constexpr int kCols = C::CHAIN ? QW : NO;
+                    }
+                    if (t > s.t0 && (raise || o_factor != 1.f)) {
+                        if (!raise) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
+                        tc_fence_after();
+                        constexpr int kCols = C::CHAIN ? QW : NO;
 #pragma unroll 1
-                            for (int c0 = 0; c0 < kCols; c0 += 16) {
-                                float o[16];
-                                tmem_ld<16>(tmem_o + lane_addr + c_wg + c0, o);
-                                tmem_ld_done<16>(o);
+                        for (int c0 = 0; c0 < kCols; c0 += 16) {
+                            float o[16];
+                            tmem_ld<16>(tmem_o + lane_addr + c_wg + c0, o);
+                            tmem_ld_done<16>(o);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] *= col_f[(c_wg + c0 + e) % QC] * o_factor;
-                                tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
-                            }
-                            tmem_st_wait();
+                            for (int e = 0; e < 16; ++e) o[e] *= (raise ? col_f[(c_wg + c0 + e) % QC] : 1.f) * o_factor;
+                            tmem_st16(tmem_o + lane_addr + c_wg + c0, o);
                         }
-                        o_factor = 1.f;
+                        tmem_st_wait();
+                    }
+                    o_factor = 1.f;
+                    if (raise) {
                         done_max = true;
+                        raise = false;
                     }
                     const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
                     // a weight beyond 2^8 does not fit its terms: raise Mu, and the weights once more
-                    if (done_max || !softmax_any(excess > kLagMax, 2 + wg, 128)) break;
+                    if (done_max || !softmax_any(excess > C::kLagMax, 2 + wg, 128)) break;
                     raise = again = true;
                 }
                 uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
@@ -824,7 +907,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                     for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vtile + row * 128)[k] = make_uint4(0u, 0u, 0u, 0u);
                 }
-                if (MODE == 1 && s.n_tok > 1 && (t + 1) * kTile > s.see0) {
+                if (MODE != 0 && s.n_tok > 1 && (t + 1) * kTile > s.see0) {
                     // a NaN value of a token that some columns see and others do not: taken out of the product, and noted
                     // for the columns that see it
                     bool nan = false;
@@ -871,40 +954,42 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             if (s.t1 > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
             tc_fence_after();
             softmax_bar(1, kSoftmax);
-            const bool whole = MODE == 0 ? s.t0 == 0 && s.t1 == s.tiles : a.splits == 1;
+            const bool whole = MODE == 2 || (s.t0 == 0 && s.t1 == s.tiles);
             float *slot = nullptr;
             if (!whole) {
-                const size_t head = MODE == 0 ? 16 + sizeof(UnitMeta) * (size_t)a.B * a.H : 0;
-                slot = reinterpret_cast<float *>(a.ws + head) + (size_t)s.slot * attn_slot_floats(QC);
+                const size_t head = attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
+                slot = reinterpret_cast<float *>(a.ws + head) + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(QC);
                 for (int c = tid; c < n_cols; c += kSoftmax) {
                     const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
                     slot[c] = sum == 0.f ? kMuNone : -mu_at(c);
                     slot[QC + c] = sum;
                 }
             }
+            if (MODE == 0 && s.t0 == 0 && tid == 0) {      // where the join finds the unit's parts
+                UnitMeta *m = reinterpret_cast<UnitMeta *>(a.ws + 16) + (size_t)s.b * a.H + s.h;
+                m->first = s.first;
+                m->tiles = s.tiles;
+            }
+            if (MODE == 1 && s.t0 > 0 && tid == 0) reinterpret_cast<CtaMeta *>(a.ws + 16)[blockIdx.x] = CtaMeta{s.first, s.tiles, s.tok0, n_cols, s.h};
+            // where a column's results go: the token's row of the output, or the column of the slot
+            for (int c = tid; c < QC; c += kSoftmax) {
+                const int k = c * a.inv_g >> 16;
+                col_lim[c] = whole ? (k * a.H * a.G + (c - k * a.G)) * kHeadDim : c * kHeadDim;
+            }
             for (int c = tid; c < QC; c += kSoftmax) {
                 const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
                 col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
             }
             softmax_bar(1, kSoftmax);
-            if constexpr (MODE == 0)
-                if (s.t0 == 0 && tid == 0) {               // first tile of the unit: where the join finds its parts
-                    UnitMeta *m = reinterpret_cast<UnitMeta *>(a.ws + 16) + (size_t)s.b * a.H + s.h;
-                    m->first = w.pos - (s.t1 - s.t0);
-                    m->tiles = s.tiles;
-                }
             T *out_row = static_cast<T *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
-            const size_t out_tok = (size_t)a.H * a.G * kHeadDim;
+            float *part_row = whole ? nullptr : slot + 2 * QC + row;
             auto put = [&](int c, float v) {
                 if (c >= n_cols) return;
-                v = col_f[c] == 0.f ? 0.f : v * col_f[c] * v_ref;     // no token, or an empty split: zero
-                if (MODE == 1 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
-                if (whole) {
-                    const int tok = c * a.inv_g >> 16;
-                    store1(out_row + tok * out_tok + (c - tok * a.G) * kHeadDim, v);
-                } else {
-                    slot[2 * QC + (size_t)c * kHeadDim + row] = v;
-                }
+                const float f = col_f[c];
+                v = f == 0.f ? 0.f : v * f * v_ref;        // no token: zero
+                if (MODE != 0 && poison != 0 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
+                if (whole) store1(out_row + col_lim[c], v);
+                else part_row[col_lim[c]] = v;
             };
             if constexpr (C::CHAIN) {
 #pragma unroll 1
@@ -940,53 +1025,59 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
 }
 
-// Joins the partial results of a unit: rescaled to the largest Mu, summed in order, divided.  Grid (units, groups of `each`
-// columns), four threads per channel that share the parts.  MODE 0: a unit's parts lie in the slots of the consecutive CTAs that shared it.  MODE 1:
-// one slot per split.
+// Joins the partial results of a unit: rescaled to the largest Mu, summed in order, divided.  They lie in the slots of the
+// consecutive CTAs that shared the unit, the first one in its second slot (a part that begins a unit), the others in their
+// first.  Grid: MODE 0 (units, columns); MODE 1 (CTAs, groups of `each` columns), where the second CTA of a shared unit is the
+// one that looks after it.  Four threads per channel share the parts or the columns.
 constexpr int kJoinGroups = 4;
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const AttnArgs a, const int qc, const int each) {
+__global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const AttnArgs a, const int qc, const int each, const int ctas) {
     pdl_wait();
-    const int d = threadIdx.x;
-    long long first_slot = 0;
-    int n = 0, first_odd = 0, h, tok0, n_cols;
-    const float *slots;
+    const int d = threadIdx.x, grp = threadIdx.y;
+    const uint32_t share = (uint32_t)min(*reinterpret_cast<const long long *>(a.ws), 0x7fffffffLL);
+    long long first;
+    int tiles, tok0, n_cols, h;
     if constexpr (MODE == 0) {
-        tok0 = blockIdx.x / a.H;
-        h = blockIdx.x % a.H;
-        n_cols = a.G;
         const UnitMeta m = reinterpret_cast<const UnitMeta *>(a.ws + 16)[blockIdx.x];
-        const long long share = *reinterpret_cast<const long long *>(a.ws);
-        const long long cta0 = m.first / share, cta1 = (m.first + m.tiles - 1) / share;
-        if (cta0 == cta1) return;                          // one CTA had it all and wrote the result
-        n = (int)(cta1 - cta0) + 1;
-        first_slot = cta0 * 2;
-        first_odd = m.first % share != 0 ? 1 : 0;
-        slots = reinterpret_cast<const float *>(a.ws + 16 + sizeof(UnitMeta) * (size_t)a.B * a.H);
+        first = m.first; tiles = m.tiles;
+        h = blockIdx.x % a.H; tok0 = blockIdx.x / a.H; n_cols = a.G;
     } else {
-        const int tq = qc / a.G, v = blockIdx.x / a.H;
-        h = blockIdx.x % a.H;
-        int lo = 0, hi = a.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.q_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
-        }
-        const int first = a.q_start[lo], nn = a.q_start[lo + 1] - first, j = v - (first / tq + lo);
-        if (first < 0 || nn < 0 || first > a.n_tokens - nn || j < 0 || (long long)j * tq >= nn) return;
-        n = a.splits;
-        first_slot = (long long)blockIdx.x * a.splits;
-        tok0 = first + j * tq;
-        n_cols = min(tq, nn - j * tq) * a.G;
-        slots = reinterpret_cast<const float *>(a.ws);
+        const CtaMeta m = reinterpret_cast<const CtaMeta *>(a.ws + 16)[blockIdx.x];
+        first = m.first; tiles = m.tiles;
+        h = m.h; tok0 = m.tok0; n_cols = m.n_cols;
+        if (tiles == 0) return;                            // this CTA began with a unit of its own
     }
-    auto slot = [&](int i) {
-        const long long at = MODE == 0 ? (i == 0 ? first_slot + first_odd : first_slot + 2LL * i) : first_slot + i;
-        return slots + (size_t)at * attn_slot_floats(qc);
+    // (positions beyond 2^31 only in calls that no memory holds: the 64-bit division is there for them)
+    const uint32_t cta0 = first < 0x7fffffffLL ? (uint32_t)first / share : (uint32_t)(first / share);
+    const uint32_t cta1 = first + tiles < 0x7fffffffLL ? (uint32_t)(first + tiles - 1) / share : (uint32_t)((first + tiles - 1) / share);
+    if (MODE == 0 ? cta0 == cta1 : cta0 + 1 != blockIdx.x) return;
+    const int n = (int)(cta1 - cta0) + 1;
+    const float *slots = reinterpret_cast<const float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, ctas));
+    auto slot = [&](int i) { return slots + (size_t)(2 * (cta0 + i) + (i == 0 ? 1 : 0)) * attn_slot_floats(qc); };
+    auto store = [&](int c, float o) {
+        const int tok = c / a.G;
+        store1(static_cast<T *>(a.out) + (((size_t)(tok0 + tok) * a.H + h) * a.G + (c - tok * a.G)) * kHeadDim + d, o);
     };
+    const int c_end = min((int)(blockIdx.y + 1) * each, n_cols);
+    if constexpr (MODE == 1) {
+        // a column per group at a time; few parts: every thread takes the factors itself
+        for (int c = blockIdx.y * each + grp; c < c_end; c += kJoinGroups) {
+            float mu = kMuNone, sum = 0.f, o = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) mu = fmaxf(mu, slot(i)[c]);
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const float *p = slot(i);
+                const float l = p[qc + c] * ex2(p[c] - mu);                    // a part's output is divided by its sum already
+                sum += l;
+                o = fmaf(p[2 * qc + (size_t)c * kHeadDim + d], l, o);
+            }
+            store(c, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
+        }
+        return;
+    }
     // 128 parts at a time: their Mu and sums by one thread each, then a thread adds up its channel of every fourth part
     __shared__ float f_s[kHeadDim], red_s[2][4], o_s[kJoinGroups][kHeadDim];
-    const int grp = threadIdx.y;
-    const int c_end = min((int)(blockIdx.y + 1) * each, n_cols);
     for (int c = blockIdx.y * each; c < c_end; ++c) {
         float mu = kMuNone, sum = 0.f, o = 0.f;
         for (int i0 = 0; i0 < n; i0 += kHeadDim) {
@@ -1005,8 +1096,7 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
             const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
             const float back = ex2(mu - top);
             if (grp == 0) {
-                const float f = ex2(m - top);
-                l *= f;                                    // a part's output is divided by its sum already
+                l *= ex2(m - top);
                 f_s[d] = l;
 #pragma unroll
                 for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
@@ -1022,11 +1112,7 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
         }
         o_s[grp][d] = o;
         __syncthreads();
-        if (grp == 0) {
-            const int tok = c / a.G;
-            o = (o_s[0][d] + o_s[1][d]) + (o_s[2][d] + o_s[3][d]);
-            store1(static_cast<T *>(a.out) + (((size_t)(tok0 + tok) * a.H + h) * a.G + (c - tok * a.G)) * kHeadDim + d, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
-        }
+        if (grp == 0) store(c, sum == 0.f ? 0.f : __fdiv_rn((o_s[0][d] + o_s[1][d]) + (o_s[2][d] + o_s[3][d]), sum));
         __syncthreads();
     }
 }
