@@ -267,14 +267,14 @@ constexpr int kUnitCost = 8;
 template <int MODE> struct Work;
 
 template <> struct Work<0> {
-    int b, h, t, tiles;
+    int b, h, t;
     long long pos, end;
     __device__ __forceinline__ bool next(const AttnArgs &a, int, Segment &s) {
         if (pos >= end) return false;
         s.b = b; s.h = h; s.tok0 = b; s.n_tok = 1;
         s.live = (int)clamp_len(a, b, false);
         s.see0 = s.live;
-        tiles = tiles_of(s.live);
+        const int tiles = tiles_of(s.live);
         s.tiles = tiles; s.t0 = t;
         s.first = pos - t;
         const long long left = end - pos;
@@ -381,50 +381,52 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     // ---- this CTA's work
     Work<MODE> w0;
     if constexpr (MODE == 0) {
-        // prefix sums of the sequences' tiles: 128 runs of consecutive sequences, one per thread
-        __shared__ long long run_sum[128];
-        __shared__ long long found[4];
+        // prefix sums of the sequences' tiles: 128 runs of consecutive sequences, one per thread.  The thread whose run holds
+        // the CTA's first position finds the place in it for all.
+        __shared__ long long warp_sum[4];
+        __shared__ Work<MODE> place;
         const int run = (a.B + 127) / 128;
+        long long n = 0, upto = 0;
         if (tid < 128) {
-            long long n = 0;
             for (int b = tid * run; b < min(a.B, (tid + 1) * run); ++b) n += tiles_of(clamp_len(a, b, blockIdx.x == 0));
-            const long long own = n;
+            upto = n;
 #pragma unroll
             for (int s = 1; s < 32; s <<= 1) {
-                const long long o = __shfl_up_sync(0xffffffffu, n, s);
-                if (lane >= s) n += o;
+                const long long o = __shfl_up_sync(0xffffffffu, upto, s);
+                if (lane >= s) upto += o;
             }
-            run_sum[tid] = n - own;                       // within the warp, exclusive
-            if (lane == 31) found[warp] = n;
+            if (lane == 31) warp_sum[warp] = upto;
         }
         __syncthreads();
-        const long long w_sum[4] = {found[0], found[1], found[2], found[3]};
+        const long long w_sum[4] = {warp_sum[0], warp_sum[1], warp_sum[2], warp_sum[3]};
         const long long total = (w_sum[0] + w_sum[1] + w_sum[2] + w_sum[3]) * a.H;
         // (a 32-bit division where that will do: a 64-bit one takes 0.3 us here)
         const long long share = total < (1LL << 31) ? (long long)(((uint32_t)total + gridDim.x - 1) / gridDim.x) : (total + gridDim.x - 1) / gridDim.x;
-        w0.pos = share * blockIdx.x;
-        w0.end = min(total, w0.pos + share);
-        if (tid == 0 && blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
-        if (w0.pos < w0.end) {
-            // the run that holds sequence tile pos / H ... then the sequence, one after the other
-            int lo = 0, hi = 127;
-            auto before = [&](int i) { return run_sum[i] + (i >= 32 ? w_sum[0] : 0) + (i >= 64 ? w_sum[1] : 0) + (i >= 96 ? w_sum[2] : 0); };
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (mid * run < a.B && before(mid) * a.H <= w0.pos) lo = mid; else hi = mid - 1;
-            }
-            long long at = before(lo) * a.H;
-            int b = lo * run, n = tiles_of(clamp_len(a, b, false));
-            while (at + (long long)n * a.H <= w0.pos) {
-                at += (long long)n * a.H;
-                n = tiles_of(clamp_len(a, ++b, false));
-            }
-            const long long in = w0.pos - at;              // < n * H
-            w0.b = b;
-            w0.h = in < (1LL << 31) ? (int)((uint32_t)in / (uint32_t)n) : (int)(in / n);
-            w0.t = (int)(in - (long long)w0.h * n);
-            w0.tiles = n;
+        const long long pos = share * blockIdx.x, end = min(total, pos + share);
+        if (tid == 0) {
+            if (blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
+            if (pos >= end) place.pos = place.end = 0;
         }
+        if (tid < 128) {
+            upto += (warp > 0 ? w_sum[0] : 0) + (warp > 1 ? w_sum[1] : 0) + (warp > 2 ? w_sum[2] : 0);
+            if (pos < end && (upto - n) * a.H <= pos && pos < upto * a.H) {
+                long long at = (upto - n) * a.H;
+                int b = tid * run, tiles = tiles_of(clamp_len(a, b, false));
+                while (at + (long long)tiles * a.H <= pos) {
+                    at += (long long)tiles * a.H;
+                    tiles = tiles_of(clamp_len(a, ++b, false));
+                }
+                const long long in = pos - at;             // < tiles * H
+                place.b = b;
+                place.h = in < (1LL << 31) ? (int)((uint32_t)in / (uint32_t)tiles) : (int)(in / tiles);
+                place.t = (int)(in - (long long)place.h * tiles);
+                place.pos = pos;
+                place.end = end;
+            }
+        }
+        tc_fence_before();
+        __syncthreads();
+        w0 = place;
     } else if constexpr (MODE == 1) {
         int32_t *before = reinterpret_cast<int32_t *>(gbase + C::kOffMisc + (C::kSmemBytes - 1024 - C::kOffMisc));
         for (int v = tid; v < a.blocks; v += C::kThreads) {
@@ -467,8 +469,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     } else {
         w0.done = false;
     }
-    tc_fence_before();
-    __syncthreads();
+    if constexpr (MODE != 0) {                             // (MODE 0 has just met)
+        tc_fence_before();
+        __syncthreads();
+    }
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tmem_slot);
     const uint32_t tmem_s = tmem, tmem_o = tmem + 2 * NS;
@@ -782,7 +786,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 if (f.x == 0.f) sum.x = y[p].x;
                                 if (f.y == 0.f) sum.y = y[p].y;
                             }
-                            y[p].x *= r2.x; y[p].y *= r2.x;
+                            y[p] = mul2(y[p], r2);
                         }
                         if constexpr (C::CHAIN) {
                             // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
@@ -1074,46 +1078,46 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
             }
             store(c, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
         }
-        return;
-    }
-    // 128 parts at a time: their Mu and sums by one thread each, then a thread adds up its channel of every fourth part
-    __shared__ float f_s[kHeadDim], red_s[2][4], o_s[kJoinGroups][kHeadDim];
-    for (int c = blockIdx.y * each; c < c_end; ++c) {
-        float mu = kMuNone, sum = 0.f, o = 0.f;
-        for (int i0 = 0; i0 < n; i0 += kHeadDim) {
-            const int k = min(kHeadDim, n - i0);
-            float m = kMuNone, l = 0.f;
-            if (grp == 0) {
-                if (d < k) {
-                    const float *p = slot(i0 + d);
-                    m = p[c];
-                    l = p[qc + c];
+    } else {
+        // 128 parts at a time: their Mu and sums by one thread each, then a thread adds up its channel of every fourth part
+        __shared__ float f_s[kHeadDim], red_s[2][4], o_s[kJoinGroups][kHeadDim];
+        for (int c = blockIdx.y * each; c < c_end; ++c) {
+            float mu = kMuNone, sum = 0.f, o = 0.f;
+            for (int i0 = 0; i0 < n; i0 += kHeadDim) {
+                const int k = min(kHeadDim, n - i0);
+                float m = kMuNone, l = 0.f;
+                if (grp == 0) {
+                    if (d < k) {
+                        const float *p = slot(i0 + d);
+                        m = p[c];
+                        l = p[qc + c];
+                    }
+                    const float wm = warp_max(m);
+                    if ((d & 31) == 0) red_s[0][d >> 5] = wm;
                 }
-                const float wm = warp_max(m);
-                if ((d & 31) == 0) red_s[0][d >> 5] = wm;
-            }
-            __syncthreads();
-            const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
-            const float back = ex2(mu - top);
-            if (grp == 0) {
-                l *= ex2(m - top);
-                f_s[d] = l;
+                __syncthreads();
+                const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
+                const float back = ex2(mu - top);
+                if (grp == 0) {
+                    l *= ex2(m - top);
+                    f_s[d] = l;
 #pragma unroll
-                for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-                if ((d & 31) == 0) red_s[1][d >> 5] = l;
-            }
-            __syncthreads();
-            sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
-            o *= back;
-            mu = top;
+                    for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+                    if ((d & 31) == 0) red_s[1][d >> 5] = l;
+                }
+                __syncthreads();
+                sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
+                o *= back;
+                mu = top;
 #pragma unroll 8
-            for (int i = grp; i < k; i += kJoinGroups) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);
+                for (int i = grp; i < k; i += kJoinGroups) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);
+                __syncthreads();
+            }
+            o_s[grp][d] = o;
+            __syncthreads();
+            if (grp == 0) store(c, sum == 0.f ? 0.f : __fdiv_rn((o_s[0][d] + o_s[1][d]) + (o_s[2][d] + o_s[3][d]), sum));
             __syncthreads();
         }
-        o_s[grp][d] = o;
-        __syncthreads();
-        if (grp == 0) store(c, sum == 0.f ? 0.f : __fdiv_rn((o_s[0][d] + o_s[1][d]) + (o_s[2][d] + o_s[3][d]), sum));
-        __syncthreads();
     }
 }
 
