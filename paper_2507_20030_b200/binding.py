@@ -477,6 +477,7 @@ class Pages:
         self._scale_shape = (self.n_pages, self.n_kv_heads)
         self._code_shape = (*self._scale_shape, self.page_size, self.head_dim)
         self._pool_shape = (self.n_pages,)
+        self._attn_bytes = {}
 
     def _refuse(self, name, t, dtype, shape):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
@@ -553,7 +554,14 @@ class Pages:
                                                  self._on(stream)))
 
     def attn_bytes(self, batch: int, n_tokens: int) -> int:
-        return self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens)
+        """Workspace of attn(): a function of the handle's configuration and the two counts alone, so it is asked for once."""
+        key = (batch, n_tokens)
+        n = self._attn_bytes.get(key)
+        if n is None:
+            if len(self._attn_bytes) > 4096:
+                self._attn_bytes.clear()
+            n = self._attn_bytes[key] = self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens)
+        return n
 
     def attn(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, out, q_start=None, scale: float = 0.0, ws=None, stream=None):
         batch, i32, need = kv_len.shape[0], torch.int32, self._need
