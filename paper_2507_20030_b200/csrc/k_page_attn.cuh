@@ -15,7 +15,7 @@
 // two, 2^-9, where many columns share a tile; float32: six terms, 2^-25).
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
-// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 2 below the
+// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 3 below the
 // maximum, so weights stay in e4m3's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
 // power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
 // segment.
@@ -34,7 +34,7 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr float kLagTo = 2.0f;                            // after a raise of Mu the largest weight is 2^2
+constexpr float kLagTo = 3.0f;                            // after a raise of Mu the largest weight is 2^3
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
@@ -789,7 +789,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                         if constexpr (C::CHAIN) {
                             // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
-                            // make up for it: an error below 2^-10 beside a largest weight of 2^2 and more
+                            // make up for it: an error below 2^-10 beside a largest weight of 2^3 and more
 #pragma unroll
                             for (int i = 0; i < PT; ++i)
 #pragma unroll
@@ -847,7 +847,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 bool again = false;
                 for (;;) {
                     if (raise) {
-                        // Mu to 2 below the column maxima, and what has been summed rescaled
+                        // Mu to 3 below the column maxima, and what has been summed rescaled
                         if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
 #pragma unroll 1
                         for (int c0 = 0; c0 < QW; c0 += kPart) {
