@@ -162,7 +162,7 @@ AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;
-    p.shared = p.blocks <= pages::kMaxBlocks;
+    p.shared = p.blocks <= pages::kMaxBlocks && p.blocks * (p.max_tiles + pages::kUnitCost) < (1LL << 31);   // (32-bit positions)
     auto ctas = [&](long long units, int per_sm) {
         const long long most = (long long)pg->n_sm * per_sm, tiles = p.max_tiles * units;
         return (int)(tiles < most ? tiles : most);
@@ -190,7 +190,7 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
     if (int r = launch_check(pg, "k_page_attn")) return r;
     if (MODE == 2 || p.max_tiles == 1) return FAEDKV_OK;                     // no unit is ever in parts
     if constexpr (MODE != 2) {
-        const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 4;
+        const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 16;
         const dim3 jgrid((unsigned)(MODE == 0 ? a.B * a.H : p.ctas1), (cols + each - 1) / each);
         CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC,
                                 each, MODE == 0 ? p.ctas0 : p.ctas1));

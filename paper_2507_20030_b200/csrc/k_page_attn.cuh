@@ -1037,7 +1037,7 @@ template <typename T, int MODE>
 __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const AttnArgs a, const int qc, const int each, const int ctas) {
     pdl_wait();
     const int d = threadIdx.x, grp = threadIdx.y;
-    const uint32_t share = (uint32_t)min(*reinterpret_cast<const long long *>(a.ws), 0x7fffffffLL);
+    const long long share = *reinterpret_cast<const long long *>(a.ws);
     long long first;
     int tiles, tok0, n_cols, h;
     if constexpr (MODE == 0) {
@@ -1050,11 +1050,10 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
         h = m.h; tok0 = m.tok0; n_cols = m.n_cols;
         if (tiles == 0) return;                            // this CTA began with a unit of its own
     }
-    // (positions beyond 2^31 only in calls that no memory holds: the 64-bit division is there for them)
-    const uint32_t cta0 = first < 0x7fffffffLL ? (uint32_t)first / share : (uint32_t)(first / share);
-    const uint32_t cta1 = first + tiles < 0x7fffffffLL ? (uint32_t)(first + tiles - 1) / share : (uint32_t)((first + tiles - 1) / share);
-    if (MODE == 0 ? cta0 == cta1 : cta0 + 1 != blockIdx.x) return;
-    const int n = (int)(cta1 - cta0) + 1;
+    auto cta_of = [&](long long pos) { return pos < (1LL << 31) && share < (1LL << 31) ? (int)((uint32_t)pos / (uint32_t)share) : (int)(pos / share); };
+    const int cta0 = cta_of(first), cta1 = cta_of(first + tiles - 1);
+    if (MODE == 0 ? cta0 == cta1 : cta0 + 1 != (int)blockIdx.x) return;       // one CTA had it all; another one's join
+    const int n = cta1 - cta0 + 1;
     const float *slots = reinterpret_cast<const float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, ctas));
     auto slot = [&](int i) { return slots + (size_t)(2 * (cta0 + i) + (i == 0 ? 1 : 0)) * attn_slot_floats(qc); };
     auto store = [&](int c, float o) {
@@ -1063,19 +1062,34 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
     };
     const int c_end = min((int)(blockIdx.y + 1) * each, n_cols);
     if constexpr (MODE == 1) {
-        // a column per group at a time; few parts: every thread takes the factors itself
-        for (int c = blockIdx.y * each + grp; c < c_end; c += kJoinGroups) {
-            float mu = kMuNone, sum = 0.f, o = 0.f;
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) mu = fmaxf(mu, slot(i)[c]);
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) {
-                const float *p = slot(i);
-                const float l = p[qc + c] * ex2(p[c] - mu);                    // a part's output is divided by its sum already
-                sum += l;
-                o = fmaf(p[2 * qc + (size_t)c * kHeadDim + d], l, o);
+        // four columns a thread (c, c + 4, ...: `each` is 16), so that their loads are on the way together
+        const int c0 = blockIdx.y * each + grp;
+        float mu[4], sum[4], o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { mu[k] = kMuNone; sum[k] = 0.f; o[k] = 0.f; }
+#pragma unroll 2
+        for (int i = 0; i < n; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = c0 + kJoinGroups * k;
+                if (c < c_end) mu[k] = fmaxf(mu[k], slot(i)[c]);
             }
-            store(c, sum == 0.f ? 0.f : __fdiv_rn(o, sum));
+#pragma unroll 2
+        for (int i = 0; i < n; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = c0 + kJoinGroups * k;
+                if (c < c_end) {
+                    const float *p = slot(i);
+                    const float l = p[qc + c] * ex2(p[c] - mu[k]);             // a part's output is divided by its sum already
+                    sum[k] += l;
+                    o[k] = fmaf(p[2 * qc + (size_t)c * kHeadDim + d], l, o[k]);
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = c0 + kJoinGroups * k;
+            if (c < c_end) store(c, sum[k] == 0.f ? 0.f : __fdiv_rn(o[k], sum[k]));
         }
     } else {
         // 128 parts at a time: their Mu and sums by one thread each, then a thread adds up its channel of every fourth part

@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 
             }
         }
         // 1 / s: exact for the powers of two that this kernel writes; a scale of another origin is divided by
-        const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0u;
+        const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0u && __float_as_uint(s) - 1u < (254u << 23) - 1u;
         const float inv = pow2 ? __uint_as_float((254u << 23) - __float_as_uint(s)) : __fdiv_rn(1.0f, s);
 #pragma unroll
         for (int k = 0; k < kIter; ++k) {

@@ -296,6 +296,21 @@ def test_attention_scale_and_sharp_scores(fk, dtype):
     _attn_case(fk, dtype, 64, 1, 4, [700], [300], qmul=8.0)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attention_of_many_sequences(fk, dtype):
+    """More sequences than the decode step's scan has threads, more blocks of new tokens than are shared out evenly, more kv
+    heads than warps."""
+    rng = np.random.default_rng(8)
+    lens = rng.integers(0, 40, 300).tolist()
+    _attn_case(fk, dtype, 16, 1, 2, lens, None)
+    _attn_case(fk, dtype, 16, 40, 1, [140, 3], None)
+    _attn_case(fk, dtype, 16, 20, 2, [140, 3], [130, 2])
+    lens = rng.integers(1, 20, 1100).tolist()
+    _attn_case(fk, dtype, 16, 1, 1, lens, [min(n, 1 + i % 3) for i, n in enumerate(lens)])      # 8 columns a block
+    lens = [n + 2 for n in lens]
+    _attn_case(fk, dtype, 16, 1, 4, lens, [3] * len(lens), pad=1)                                # 128 (bf16)
+
+
 def _cache_from_rows(K, V, page, n_pages, table, lens):
     """Codes and scales of float64 rows [B][H, n, 128], stored as the reference stores them."""
     H = K[0].shape[0]
