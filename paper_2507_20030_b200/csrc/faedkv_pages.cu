@@ -113,10 +113,10 @@ cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t s
 template <typename T>
 void launch_store(const pages::StoreArgs &a, int page, dim3 grid, cudaStream_t st) {
     switch (page) {
-        case 16: pages::k_page_store<T, 16><<<grid, pages::kStoreThreads, 0, st>>>(a); break;
-        case 32: pages::k_page_store<T, 32><<<grid, pages::kStoreThreads, 0, st>>>(a); break;
-        case 64: pages::k_page_store<T, 64><<<grid, pages::kStoreThreads, 0, st>>>(a); break;
-        default: pages::k_page_store<T, 128><<<grid, pages::kStoreThreads, 0, st>>>(a); break;
+        case 16: pages::k_page_store<T, 16><<<grid, pages::kStoreThreads<T, 16>, 0, st>>>(a); break;
+        case 32: pages::k_page_store<T, 32><<<grid, pages::kStoreThreads<T, 32>, 0, st>>>(a); break;
+        case 64: pages::k_page_store<T, 64><<<grid, pages::kStoreThreads<T, 64>, 0, st>>>(a); break;
+        default: pages::k_page_store<T, 128><<<grid, pages::kStoreThreads<T, 128>, 0, st>>>(a); break;
     }
 }
 

@@ -284,7 +284,9 @@ template <> struct Raw8<float> {
     }
 };
 
-constexpr int kStoreThreads = 256;
+// Threads of a store CTA: few, since finding a run costs each warp about as much as 16 KB of its rows, but no more than 32
+// registers of rows a thread.
+template <typename T, int PAGE> constexpr int kStoreThreads = PAGE * sizeof(T) <= 128 ? 128 : 256;
 
 struct StoreArgs {
     const void *x[2];                                     // k_new, v_new: token rows `ld` elements apart, heads 128 apart
@@ -305,9 +307,10 @@ struct StoreArgs {
 // CTAs enough to cover it.  Measured: 32768 tokens x 8 heads, bf16, 40.5 us (5.0 TB/s; the ALU pipe is at 67 %), 2.8 us for 16
 // tokens.
 template <typename T, int PAGE>
-__global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 6 : 4) : (PAGE < 64 ? 6 : PAGE < 128 ? 4 : 2)) k_page_store(const StoreArgs a) {
-    constexpr int kRows = kStoreThreads / 16, kIter = (PAGE + kRows - 1) / kRows, kWords = (PAGE + 31) / 32;
-    __shared__ uint32_t max_s[2][kStoreThreads / 32];
+__global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 128 ? 8 : PAGE * sizeof(T) <= 256 ? 4 : 2) k_page_store(const StoreArgs a) {
+    constexpr int kRows = kStoreThreads<T, PAGE> / 16, kIter = (PAGE + kRows - 1) / kRows, kWords = (PAGE + 31) / 32;
+    constexpr int kWarps = kStoreThreads<T, PAGE> / 32;
+    __shared__ uint32_t max_s[2][kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned int units = 2 * a.H, part = blockIdx.x / units, unit = blockIdx.x - part * units;
     const int which = unit & 1, h = unit >> 1;
@@ -331,6 +334,7 @@ __global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 
     uint8_t *codes = which == 0 ? a.codes[0] : a.codes[1];    // (indexing the arguments would copy them to local memory)
     float *scales = which == 0 ? a.scale[0] : a.scale[1];
     const int c8 = (tid & 15) * 8, row_t = tid >> 4;
+    const size_t step = (size_t)kRows * a.ld;
     for (int turn = 0; j < n_tile; ++turn) {
         const int slot = slots[j];
         const int r0 = slot & (PAGE - 1), cap = min(PAGE - r0, n_rest - j);
@@ -356,14 +360,16 @@ __global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 
             continue;
         }
         const int pg = slot / PAGE;
-        const T *src = x + (size_t)at * a.ld + c8;
+        const T *src = x + (size_t)(at + row_t) * a.ld + c8;
         Raw8<T> raw[kIter];
         uint32_t amax = 0;
+        {
+            const T *from = src;
 #pragma unroll
-        for (int k = 0; k < kIter; ++k) {
-            const int r = row_t + k * kRows;
-            if (r < n) raw[k].load(src + (size_t)r * a.ld);
-            else raw[k].zero();
+            for (int k = 0; k < kIter; ++k, from += step) {
+                if (row_t + k * kRows < n) raw[k].load(from);
+                else raw[k].zero();
+            }
         }
         const size_t ph = (size_t)pg * a.H + h;
         const float s_old = r0 > 0 ? scales[ph] : 0.f;
@@ -373,20 +379,20 @@ __global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 
         if (amax >= 0x7f800000u) {                        // an infinity or NaN among them: again, without those
             amax = 0;
 #pragma unroll 1
-            for (int r = row_t; r < n; r += kRows)
+            for (int k = 0; row_t + k * kRows < n; ++k)
 #pragma unroll 1
-                for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(load1(src + (size_t)r * a.ld + e)));
+                for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(load1(src + k * step + e)));
         }
         amax = __reduce_max_sync(0xffffffffu, amax);
         if (lane == 0) max_s[turn & 1][warp] = amax;
         __syncthreads();
-        amax = __reduce_max_sync(0xffffffffu, max_s[turn & 1][lane & (kStoreThreads / 32 - 1)]);
+        amax = __reduce_max_sync(0xffffffffu, max_s[turn & 1][lane & (kWarps - 1)]);
         float s = scale_for(__uint_as_float(amax));
-        uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim) + c8;
+        uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim) + row_t * kHeadDim + c8;
         if (r0 > 0) {
             if (s > s_old) {                              // the page's older rows, rounded again at the larger scale
                 const float mul = s_old * __uint_as_float((254u << 23) - __float_as_uint(s));
-                for (int r = row_t; r < r0; r += kRows) {
+                for (int r = 0; row_t + r < r0; r += kRows) {
                     uint2 *p = reinterpret_cast<uint2 *>(dst + r * kHeadDim);
                     const uint2 c = *p;
                     float v[8], q[4];
@@ -403,13 +409,13 @@ __global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? (PAGE < 128 ? 
         // 1 / s: exact for the powers of two that this kernel writes; a scale of another origin is divided by
         const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0u && __float_as_uint(s) - 1u < (254u << 23) - 1u;
         const float inv = pow2 ? __uint_as_float((254u << 23) - __float_as_uint(s)) : __fdiv_rn(1.0f, s);
+        dst += r0 * kHeadDim;
 #pragma unroll
         for (int k = 0; k < kIter; ++k) {
-            const int r = row_t + k * kRows;
-            if (r < n) {
+            if (row_t + k * kRows < n) {
                 float v[8];
                 raw[k].get(v);
-                *reinterpret_cast<uint2 *>(dst + (r0 + r) * kHeadDim) = to_e4m3x8(v, inv);
+                *reinterpret_cast<uint2 *>(dst + k * kRows * kHeadDim) = to_e4m3x8(v, inv);
             }
         }
         if (tid == 0) scales[ph] = s;
