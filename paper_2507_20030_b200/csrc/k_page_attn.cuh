@@ -208,6 +208,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&r)[16]) 
         ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
           "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]) : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
@@ -722,7 +726,32 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 // columns may see a different number of this tile's tokens, or pages may be missing
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
-                const float kf = C::CHAIN ? ks * unit_cs : ks;
+                const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
+                float kf = C::CHAIN ? ks * unit_cs : ks;
+                if (masked) {
+                    // a pass of its own over the scores, which leaves them multiplied by kf, or minus infinity: the loop below
+                    // need not know of masks
+#pragma unroll 1
+                    for (int c0 = 0; c0 < QW; c0 += 8) {
+                        constexpr int kTerms = C::CHAIN ? 1 : QT;
+                        float v[8 * kTerms];
+#pragma unroll
+                        for (int i = 0; i < kTerms; ++i) tmem_ld8(ts + i * QC + c0, v + 8 * i);
+                        tmem_ld_done<8 * kTerms>(v);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                            for (int i = kTerms - 2; i >= 0; --i) v[8 * i + e] = fmaf(v[8 * (i + 1) + e], kTerm, v[8 * i + e]);
+                            v[e] = valid && tok < col_lim[c_wg + c0 + e] ? v[e] * kf : -INFINITY;
+#pragma unroll
+                            for (int i = 1; i < kTerms; ++i) v[8 * i + e] = 0.f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < kTerms; ++i) tmem_st8(ts + i * QC + c0, v + 8 * i);
+                    }
+                    tmem_st_wait();
+                    kf = 1.f;
+                }
                 const float2 ks2 = make_float2(kf, kf);
                 // a column without a maximum: Mu is settled before the weights are taken; a larger v_scale than any before: Vref
                 bool raise = unset_any;
@@ -734,7 +763,6 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     v_inv = __fdiv_rn(1.f, up);
                 }
                 const float2 r2 = make_float2(vs * v_inv, vs * v_inv);
-                const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
                 // y of the columns c_wg + c0 .. from their raw scores
                 auto exponents = [&](const float(&raw)[kLoad], int c0, float2(&y)[kPart / 2]) {
 #pragma unroll
@@ -753,14 +781,6 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         } else {
                             const float4 fm = col4[(c_wg + c0) / 2 + p];
                             y[p] = fma2(v, mul2(ks2, make_float2(fm.x, fm.y)), make_float2(fm.z, fm.w));
-                        }
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int p = 0; p < kPart / 2; ++p) {
-                            const int2 lim = *reinterpret_cast<const int2 *>(col_lim + c_wg + c0 + 2 * p);
-                            if (!(valid && tok < lim.x)) y[p].x = -INFINITY;
-                            if (!(valid && tok < lim.y)) y[p].y = -INFINITY;
                         }
                     }
                 };
@@ -810,7 +830,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                             if (i < PT - 1) {
                                                 h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
                                                 h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                                v = sub2(v, h[e]);
+                                                v.x -= h[e].x; v.y -= h[e].y;
                                             }
                                         }
                                         u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
