@@ -11,19 +11,19 @@
 // with the query columns (new tokens x query heads of one kv head) as N.  The other operand has to be e4m3 too, so a
 // query element and a softmax weight are written as sums of e4m3 terms of four significant bits each, the i-th scaled by
 // 16^i: their products are exact and accumulate in float32, so nothing of the cache is converted anywhere and what is
-// lost is only what the last term rounds off (bf16 q: two terms, exact; bf16 weights: three terms, 2^-13 of a weight, or
-// two, 2^-9, where many columns share a tile; float32: six terms, 2^-25).
+// lost is only what the last term rounds off (bf16 q: two terms, exact; bf16 weights: three terms, 2^-12 of a weight, or
+// two, 2^-8, where many columns share a tile; float32: six terms, 2^-24).
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
-// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 3 below the
+// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 2 or 4 below the
 // maximum, so weights stay in e4m3's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
 // power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
 // segment.
 //
-// Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 54 us (39 us of it
-// in the tiles); 2048 new tokens over 18432 902 us (650 TFLOP/s), where the softmax warps' instruction issue bounds it (54 % of
-// the slots, tensor pipe 32 %); float32, six ragged sequences up to 4096 tokens 16.7 us.  128 columns over four warpgroups
-// were faster than over two or 96 over three (918, 992 and 951 us at one step), eight at a time faster than sixteen (946).
+// Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
+// it in the tiles); 2048 new tokens over 18432 896 us (650 TFLOP/s), bound by the softmax warps (54 % of the issue slots,
+// tensor pipe 32 %); float32, six ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster
+// than over two or 96 over three (879, 992 and 961 us at about the same step), sixteen columns at a time than eight (909).
 //
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.
@@ -39,7 +39,6 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr float kLagTo = 3.0f;                            // after a raise of Mu the largest weight is 2^3
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
@@ -55,6 +54,10 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int PAR
     static constexpr int kThreads = 128 * WGS + 64;
     // the largest weight: e4m3 ends at 448, and a second term that is scaled by 16 needs the first one's step to be 16
     static constexpr float kLagMax = CHAIN ? 8.75f : 8.0f;
+    // and after a raise of Mu: room to grow before the next one, against what the last term loses of the small weights (chained
+    // terms: 2^-10; output error at 2048 new tokens over 18432, bf16's own rounding included, 0.0022 at 3, 0.0019 at 4, 0.0016
+    // being the rounding's; 869 and 898 us)
+    static constexpr float kLagTo = CHAIN ? 4.0f : 2.0f;
     static constexpr int NS = CHAIN ? QC : (QC * QT + 15) / 16 * 16;          // columns of S, of O
     static constexpr int NO = CHAIN ? QC : (QC * PT + 15) / 16 * 16;
     static constexpr int kTmemUsed = 2 * NS + NO;
@@ -814,7 +817,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                         if constexpr (C::CHAIN) {
                             // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
-                            // make up for it: an error below 2^-10 beside a largest weight of 2^3 and more
+                            // make up for it: an error below 2^-10 beside a largest weight of 2^4 and more
 #pragma unroll
                             for (int i = 0; i < PT; ++i)
 #pragma unroll
@@ -872,7 +875,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 bool again = false;
                 for (;;) {
                     if (raise) {
-                        // Mu to 3 below the column maxima, and what has been summed rescaled
+                        // Mu to kLagTo below the column maxima, and what has been summed rescaled
                         if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
 #pragma unroll 1
                         for (int c0 = 0; c0 < QW; c0 += kPart) {
@@ -891,7 +894,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         bool unset = false;
                         if (row < QW) {
                             const int c = c_wg + row;
-                            const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - kLagTo;
+                            const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - C::kLagTo;
                             const bool first = col_set[c] == 0, seen = m > -INFINITY;
                             const float d = seen && (first || m > 0.f) ? m : 0.f;
                             mu_at(c) -= d;

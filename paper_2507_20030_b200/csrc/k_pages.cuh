@@ -304,8 +304,8 @@ struct StoreArgs {
 // It reads a run once into registers, takes the largest finite magnitude, settles the page's scale, re-rounds the page's
 // older rows if the scale grew, and writes the new codes: the data is read once and written once.  What it takes is a chain
 // of dependent loads (slots, rows) and one barrier, so every warp finds the runs by itself and registers are kept few, for
-// CTAs enough to cover it.  Measured: 32768 tokens x 8 heads, bf16, 40.5 us (5.0 TB/s; the ALU pipe is at 67 %), 2.8 us for 16
-// tokens.
+// CTAs enough to cover it.  Measured: 32768 tokens x 8 heads, bf16, 33.7 us (6.0 TB/s; with half the rows a thread 40.3 us, bound
+// by instructions), 2.6 us for 16 tokens.
 template <typename T, int PAGE>
 __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 128 ? 8 : PAGE * sizeof(T) <= 256 ? 4 : 2) k_page_store(const StoreArgs a) {
     constexpr int kRows = kStoreThreads<T, PAGE> / 16, kIter = (PAGE + kRows - 1) / kRows, kWords = (PAGE + 31) / 32;
