@@ -21,7 +21,7 @@
 // segment.
 //
 // Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
-// it in the tiles); 2048 new tokens over 18432 896 us (650 TFLOP/s), bound by the softmax warps (54 % of the issue slots,
+// it in the tiles); 2048 new tokens over 18432 896 us (650 TFLOP/s), bound by the softmax warps (58 % of the issue slots,
 // tensor pipe 32 %); float32, six ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster
 // than over two or 96 over three (879, 992 and 961 us at about the same step), sixteen columns at a time than eight (909).
 //
