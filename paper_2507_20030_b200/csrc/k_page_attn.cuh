@@ -11,8 +11,9 @@
 // with the query columns (new tokens x query heads of one kv head) as N.  The other operand has to be e4m3 too, so a
 // query element and a softmax weight are written as sums of e4m3 terms of four significant bits each, the i-th scaled by
 // 16^i: their products are exact and accumulate in float32, so nothing of the cache is converted anywhere and what is
-// lost is only what the last term rounds off (bf16 q: two terms, exact; bf16 weights: three terms, 2^-12 of a weight, or
-// two, 2^-8, where many columns share a tile; float32: six terms, 2^-24).
+// lost is only what the last term rounds off (bf16 q: two terms; weights: three terms for bf16, 2^-12 of a weight, six for
+// float32, 2^-24).  Where 128 columns share a tile, the weights are f16 and the V tile is converted to f16 (exact) before the
+// second product, which costs as much as two e4m3 terms and keeps small weights.
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
 // follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 2 or 4 below the
@@ -21,9 +22,9 @@
 // segment.
 //
 // Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
-// it in the tiles); 2048 new tokens over 18432 896 us (650 TFLOP/s), bound by the softmax warps (58 % of the issue slots,
-// tensor pipe 32 %); float32, six ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster
-// than over two or 96 over three (879, 992 and 961 us at about the same step), sixteen columns at a time than eight (909).
+// it in the tiles); 2048 new tokens over 18432 931 us (629 TFLOP/s), bound by the softmax warps; float32, six
+// ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster than over two or 96 over three (879,
+// 992 and 961 us with e4m3 weights), eight columns at a time than sixteen (931, 952).
 //
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.
@@ -43,36 +44,41 @@ constexpr float kMuNone = -3e38f;                         // a part that saw no 
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
 
-// Instances: QC query columns over WGS softmax warpgroups, QT / PT terms of q / of the weights, the terms side by side as
-// further columns of one product (CHAIN = false: few columns, one pass over the tile) or added up in the same accumulator
-// (CHAIN = true).
-template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool CHAIN_, int PART_, int STAGES_, int CTAS_> struct AttnCfg {
+// Instances: QC query columns over WGS softmax warpgroups.  Few columns (WIDE = false): QT / PT e4m3 terms of q / of the weights
+// side by side as further columns of one product, V as it lies.  Many (WIDE = true): QT terms of q added up in the same accumulator;
+// weights in f16, which holds them to 2^-11 down to 2^-20 of the largest and to 2^-31 of it below, and V converted to f16 (exact)
+// by the softmax warps, a tile at a time into one buffer (two more warps that convert it were slower, 1016 us for 931 at 2048 new
+// tokens over 18432: with one buffer their work lies between two products).  (Two e4m3 terms on one grid lost every weight below 2^-14 of the largest: beside a
+// loud token thousands of those are half of the output.)  KST / VST: tiles of K and of V on their way.
+template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool WIDE_, int PART_, int KST_, int VST_, int CTAS_> struct AttnCfg {
     using T = T_;
-    static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, PART = PART_, STAGES = STAGES_, CTAS = CTAS_;
-    static constexpr bool CHAIN = CHAIN_;
+    static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, PART = PART_, KST = KST_, VST = VST_, CTAS = CTAS_;
+    static constexpr bool WIDE = WIDE_;
     static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
     static constexpr int kThreads = 128 * WGS + 64;
-    // the largest weight: e4m3 ends at 448, and a second term that is scaled by 16 needs the first one's step to be 16
-    static constexpr float kLagMax = CHAIN ? 8.75f : 8.0f;
-    // and after a raise of Mu: room to grow before the next one, against what the last term loses of the small weights (chained
-    // terms: 2^-10; output error at 2048 new tokens over 18432, bf16's own rounding included, 0.0022 at 3, 0.0019 at 4, 0.0016
-    // being the rounding's; 869 and 898 us)
-    static constexpr float kLagTo = CHAIN ? 4.0f : 2.0f;
-    static constexpr int NS = CHAIN ? QC : (QC * QT + 15) / 16 * 16;          // columns of S, of O
-    static constexpr int NO = CHAIN ? QC : (QC * PT + 15) / 16 * 16;
+    // the largest weight: f16 ends at 2^16; e4m3 at 448, and a second term that is scaled by 16 needs the first one's step to be 16
+    static constexpr float kLagMax = WIDE ? 15.5f : 8.0f;
+    // and after a raise of Mu: room to grow before the next one, against the bits of the small weights (2048 new tokens over
+    // 18432: 985 us at 10, 931 at 6, 930 at 4)
+    static constexpr float kLagTo = WIDE ? 6.0f : 2.0f;
+    static constexpr int NS = WIDE ? QC : (QC * QT + 15) / 16 * 16;           // columns of S, of O
+    static constexpr int NO = WIDE ? QC : (QC * PT + 15) / 16 * 16;
     static constexpr int kTmemUsed = 2 * NS + NO;
     static constexpr uint32_t kTmemCols = kTmemUsed <= 32 ? 32 : kTmemUsed <= 64 ? 64 : kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
-    static constexpr uint32_t PW = NO <= 32 ? 32 : NO <= 64 ? 64 : 128;       // bytes of a token's weights (one term's, if CHAIN)
-    static constexpr uint32_t kPBytes = (CHAIN ? PT : 1) * kTile * PW;
-    static constexpr uint32_t kQBytes = (CHAIN ? QT * QC : NS) * 128;
-    static constexpr uint32_t kOffQ = STAGES * 2 * kTileBytes;
+    static constexpr uint32_t PW = NO <= 32 ? 32 : NO <= 64 ? 64 : 128;       // bytes of a token's e4m3 weights
+    static constexpr uint32_t kPBytes = WIDE ? 2 * kTile * QC : kTile * PW;
+    static constexpr uint32_t kHBytes = WIDE ? 2 * kTileBytes : 0;            // a V tile in f16
+    static constexpr uint32_t kQBytes = (WIDE ? QT * QC : NS) * 128;
+    static constexpr uint32_t kOffV = KST * kTileBytes;
+    static constexpr uint32_t kOffQ = kOffV + VST * kTileBytes;
     static constexpr uint32_t kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
-    static constexpr uint32_t kOffMisc = kOffP + 2 * kPBytes;
-    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + STAGES * 32) + 256 + 1024;
+    static constexpr uint32_t kOffH = kOffP + 2 * kPBytes;
+    static constexpr uint32_t kOffMisc = kOffH + kHBytes;
+    static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + KST * 32) + 256 + 1024;
     static constexpr uint32_t kSmemBlocks = 4 * (kMaxBlocks + 1);             // MODE 1 appends its prefix sums
-    static_assert(!CHAIN || PW >= NO, "a chained term fits its rows");
-    static_assert(!CHAIN || (PART % 8 == 0 && QW % PART == 0), "whole parts");
-    static_assert(WGS == 1 || CHAIN, "warpgroups share chained columns");
+    static_assert(!WIDE || (QC == 128 && WGS == 4 && PT == 1 && KST <= VST + 1), "the layouts of the wide form");
+    static_assert(!WIDE || (PART % 8 == 0 && QW % PART == 0), "whole parts");
+    static_assert(WIDE || (WGS == 1 && KST == VST), "a tile's K and V leave together");
 };
 
 struct AttnArgs {
@@ -227,6 +233,13 @@ __device__ __forceinline__ float lead4(float w) {
     return fabsf(w) >= 0.015625f ? h : 0.f;
 }
 
+// Two e4m3 codes (the lower 16 bits) as f16: exact, NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
+    uint32_t h;
+    asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(codes));
+    return h;
+}
+
 // One unit of work is the columns of one (sequence, kv head, block of new tokens); a segment is a run of its tiles.
 struct Segment {
     int b, h, tok0, n_tok;       // first query row (of q, out) and number of query tokens
@@ -346,13 +359,13 @@ __global__ void __launch_bounds__(C::kThreads, C::CTAS)
 k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a) {
     using namespace umma;
     using T = typename C::T;
-    constexpr int QC = C::QC, QW = C::QW, WGS = C::WGS, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, STAGES = C::STAGES;
+    constexpr int QC = C::QC, QW = C::QW, WGS = C::WGS, QT = C::QT, PT = C::PT, NS = C::NS, NO = C::NO, KST = C::KST, VST = C::VST;
     constexpr int kSoftmax = 128 * WGS, kWarpTma = 4 * WGS, kWarpMma = 4 * WGS + 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
-    auto k_tile = [&](int s) { return base + (uint32_t)s * 2 * kTileBytes; };
-    auto v_tile = [&](int s) { return base + (uint32_t)s * 2 * kTileBytes + kTileBytes; };
+    auto k_tile = [&](int s) { return base + (uint32_t)s * kTileBytes; };
+    auto v_tile = [&](int s) { return base + C::kOffV + (uint32_t)s * kTileBytes; };
     const uint32_t q_base = base + C::kOffQ;
     auto p_tile = [&](int p) { return base + C::kOffP + (uint32_t)p * C::kPBytes; };
     float *col = reinterpret_cast<float *>(gbase + C::kOffMisc);             // per pair of columns: factors of the raw scores, -Mu
@@ -360,26 +373,29 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
     int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
     float *red = reinterpret_cast<float *>(col_set + QC);                    // [4][QC]
-    float *stage_ks = red + 4 * QC;                                          // [STAGES][32]: 8 k_scale, 8 v_scale, the largest |v_scale|, at 24 the pages that are there
-    uint64_t *bars = reinterpret_cast<uint64_t *>(stage_ks + STAGES * 32);
+    float *stage_ks = red + 4 * QC;                                          // [KST][32]: 8 k_scale, 8 v_scale, the largest |v_scale|, at 24 the pages that are there
+    uint64_t *bars = reinterpret_cast<uint64_t *>(stage_ks + KST * 32);
     const uint32_t bar0 = smem_u32(bars);
+    constexpr int kBars = 2 * (KST + VST);
     auto kfull = [&](int s) { return bar0 + 8 * s; };
-    auto vfull = [&](int s) { return bar0 + 8 * (STAGES + s); };
-    auto empty = [&](int s) { return bar0 + 8 * (2 * STAGES + s); };
-    auto sfull = [&](int i) { return bar0 + 8 * (3 * STAGES + i); };
-    auto pfull = [&](int i) { return bar0 + 8 * (3 * STAGES + 2 + i); };
-    auto pdone = [&](int i) { return bar0 + 8 * (3 * STAGES + 4 + i); };
-    const uint32_t qfull = bar0 + 8 * (3 * STAGES + 6);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 3 * STAGES + 7);
+    auto kempty = [&](int s) { return bar0 + 8 * (KST + s); };                // (narrow: of the tile's K and V)
+    auto vfull = [&](int s) { return bar0 + 8 * (2 * KST + s); };
+    auto vempty = [&](int s) { return bar0 + 8 * (2 * KST + VST + s); };      // wide only
+    auto sfull = [&](int i) { return bar0 + 8 * (kBars + i); };
+    auto pfull = [&](int i) { return bar0 + 8 * (kBars + 2 + i); };
+    auto pdone = [&](int i) { return bar0 + 8 * (kBars + 4 + i); };
+    const uint32_t qfull = bar0 + 8 * (kBars + 6);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars + 7);
     volatile uint32_t *abort_flag = tmem_slot + 1;
-    static_assert(8 * (3 * STAGES + 8) <= 256, "barriers fit the room behind the stages");
+    static_assert(8 * (kBars + 8) <= 256, "barriers fit the room behind the stages");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int page = 1 << a.page_shift;
 
     // ---- what needs nothing of the call's inputs, while the stream's previous kernel drains
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(kfull(s), 1); mbar_init(vfull(s), 1); mbar_init(empty(s), 1); }
+        for (int s = 0; s < KST; ++s) { mbar_init(kfull(s), 1); mbar_init(kempty(s), 1); }
+        for (int s = 0; s < VST; ++s) { mbar_init(vfull(s), 1); mbar_init(vempty(s), 4 * WGS); }
         for (int i = 0; i < 2; ++i) mbar_init(sfull(i), 1);
         for (int i = 0; i < 2; ++i) { mbar_init(pfull(i), 4 * WGS); mbar_init(pdone(i), 1); }
         mbar_init(qfull, 4 * WGS);
@@ -504,7 +520,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const int tiles_batch = 32 >> lg_ppt;                                 // a lane looks after one page of the next 32
         Work<MODE> w = w0;
         Segment s;
-        int it = 0, issued = 0;
+        int it = 0, issued_k = 0, issued_v = 0;
         while (w.next(a, QC, s)) {
             const int32_t *row = a.table + (size_t)s.b * a.W;
             auto fetch = [&](int t_first, int &id, float &ks, float &vs) {
@@ -529,21 +545,23 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 fetch(tb + tiles_batch, id_next, ks_next, vs_next);
                 const int tn = min(tiles_batch, s.t1 - tb);
                 for (int i = 0; i < tn; ++i, ++it) {
-                    const int st = it % STAGES;
-                    wait(empty(st), ((uint32_t)(it / STAGES) & 1u) ^ 1u, kErrAttnTma);
+                    const int st = it % KST, sv = it % VST;
+                    wait(kempty(st), ((uint32_t)(it / KST) & 1u) ^ 1u, kErrAttnTma);
                     const bool mine = (lane >> lg_ppt) == i;
                     const int k = lane & (ppt - 1);
                     const uint32_t have = __ballot_sync(0xffffffffu, mine && id >= 0) >> (i << lg_ppt);
                     const uint32_t bytes = (uint32_t)__popc(have) * (uint32_t)(page * kHeadDim);
                     dead = __any_sync(0xffffffffu, dead);
                     if (dead) continue;
+                    const int y = (id * a.H + s.h) << a.page_shift;
+                    const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
                     if (mine && id >= 0) {
-                        const int y = (id * a.H + s.h) << a.page_shift;
-                        const uint32_t off = (uint32_t)(k << a.page_shift) * kHeadDim;
                         tma_load_2d(k_tile(st) + off, &map_k, kfull(st), 0, y);
-                        tma_load_2d(v_tile(st) + off, &map_v, vfull(st), 0, y);
+                        if (!C::WIDE) tma_load_2d(v_tile(sv) + off, &map_v, vfull(sv), 0, y);
                     }
-                    // the scales (their loads may still be on their way) before the barrier's own arrival
+                    // the scales (their loads may still be on their way) before the barrier's own arrival.  Their room is free: the
+                    // softmax warps are done with the tile that had it (wide: they gave its V's room, which the tile before this
+                    // one has taken, so KST is at most VST + 1)
                     float *sc = stage_ks + st * 32;
                     const float v_max = warp_max(mine ? fabsf(vs) : 0.f);
                     if (mine) {
@@ -557,55 +575,68 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     __syncwarp();
                     if (lane == 0) {
                         mbar_expect_tx(kfull(st), bytes);
-                        mbar_expect_tx(vfull(st), bytes);
+                        if (!C::WIDE) mbar_expect_tx(vfull(sv), bytes);
                     }
-                    issued = it + 1;
+                    issued_k = it + 1;
+                    if constexpr (C::WIDE) {
+                        wait(vempty(sv), ((uint32_t)(it / VST) & 1u) ^ 1u, kErrAttnTma);
+                        dead = __any_sync(0xffffffffu, dead);
+                        if (dead) continue;
+                        if (mine && id >= 0) tma_load_2d(v_tile(sv) + off, &map_v, vfull(sv), 0, y);
+                        __syncwarp();
+                        if (lane == 0) mbar_expect_tx(vfull(sv), bytes);
+                    }
+                    issued_v = it + 1;
                 }
                 id = id_next; ks = ks_next; vs = vs_next;
             }
         }
-        if (dead)                                          // leave no copy in flight behind
-            for (int i = max(0, issued - STAGES); i < issued; ++i) {
-                mbar_wait(kfull(i % STAGES), (uint32_t)(i / STAGES) & 1u);
-                mbar_wait(vfull(i % STAGES), (uint32_t)(i / STAGES) & 1u);
-            }
+        if (dead) {                                        // leave no copy in flight behind
+            for (int i = max(0, issued_k - KST); i < issued_k; ++i) mbar_wait(kfull(i % KST), (uint32_t)(i / KST) & 1u);
+            for (int i = max(0, issued_v - VST); i < issued_v; ++i) mbar_wait(vfull(i % VST), (uint32_t)(i / VST) & 1u);
+        }
     } else if (warp == kWarpMma) {
         // ------------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
-            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO);
+            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO);   // (format 0: e4m3, or f16)
             Work<MODE> w = w0;
             Segment s;
             int it = 0;                                    // tiles whose S has been issued
             uint32_t seg = 0;
             auto scores = [&]() {
-                const int st = it % STAGES;
-                wait(kfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnMma);
+                const int st = it % KST;
+                wait(kfull(st), (uint32_t)(it / KST) & 1u, kErrAttnMma);
                 if (!dead) {
                     tc_fence_after();
 #pragma unroll
-                    for (int term = 0; term < (C::CHAIN ? QT : 1); ++term)
+                    for (int term = 0; term < (C::WIDE ? QT : 1); ++term)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             mma_f8(tmem_s + (it & 1) * NS, desc_kmajor_sw128(k_tile(st) + k * 32),
                                    desc_kmajor_sw128(q_base + term * QC * 128 + k * 32), kIdescS, (term | k) ? 1u : 0u);
                     mma_commit(sfull(it & 1));
+                    if (C::WIDE) mma_commit(kempty(st));
                 }
                 ++it;
             };
             auto output = [&](int i, bool first) {
-                const int st = i % STAGES, pb = i & 1;
+                const int sv = i % VST, pb = i & 1;
                 wait(pfull(pb), (uint32_t)(i >> 1) & 1u, kErrAttnMma);
-                wait(vfull(st), (uint32_t)(i / STAGES) & 1u, kErrAttnMma);
+                if (!C::WIDE) wait(vfull(sv), (uint32_t)(i / VST) & 1u, kErrAttnMma);
                 if (!dead) {
                     tc_fence_after();
+                    if constexpr (C::WIDE) {
 #pragma unroll
-                    for (int term = 0; term < (C::CHAIN ? PT : 1); ++term)
+                        for (int k = 0; k < 8; ++k)        // 16 tokens each
+                            mma_bf16(tmem_o, desc_mnmajor_sw128(base + C::kOffH + k * 2048, kTileBytes),
+                                     desc_mnmajor_sw128(p_tile(pb) + k * 2048, kTileBytes), kIdescO, (!first || k) ? 1u : 0u);
+                    } else {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            mma_f8(tmem_o, desc_mnmajor_sw128(v_tile(st) + k * 4096, kTileBytes),
-                                   desc_mn_rows<C::PW>(p_tile(pb) + (term * kTile + k * 32) * C::PW), kIdescO,
-                                   (!first || term || k) ? 1u : 0u);
-                    mma_commit(empty(st));
+                            mma_f8(tmem_o, desc_mnmajor_sw128(v_tile(sv) + k * 4096, kTileBytes),
+                                   desc_mn_rows<C::PW>(p_tile(pb) + k * 32 * C::PW), kIdescO, (!first || k) ? 1u : 0u);
+                        mma_commit(kempty(i % KST));
+                    }
                     mma_commit(pdone(pb));
                 }
             };
@@ -625,10 +656,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         const int wg = warp >> 2, row = tid & 127, c_wg = wg * QW;            // this thread's token / channel, its first column
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kTerm = 1.0f / 16.0f;
-        auto mu_at = [&](int c) -> float & { return C::CHAIN ? col[c] : col[(c >> 1) * 4 + 2 + (c & 1)]; };   // -Mu of column c
+        auto mu_at = [&](int c) -> float & { return C::WIDE ? col[c] : col[(c >> 1) * 4 + 2 + (c & 1)]; };   // -Mu of column c
         const float2 *col_mu = reinterpret_cast<const float2 *>(col);
         const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
-        constexpr int kPart = C::CHAIN ? C::PART : QW, kLoad = C::CHAIN ? C::PART : NS;  // columns at a time, raw scores of them
+        constexpr int kPart = C::WIDE ? C::PART : QW, kLoad = C::WIDE ? C::PART : NS;  // columns at a time, raw scores of them
         Work<MODE> w = w0;
         Segment s;
         int it = 0;
@@ -646,7 +677,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             // one power of two for all columns where they are many (it stays out of the softmax's inner loop): an element is
             // then off by at most 2^-16 of the largest of them; one for each column otherwise
             float unit_top = 0.f;
-            if constexpr (C::CHAIN) {
+            if constexpr (C::WIDE) {
                 uint32_t m = 0;
 #pragma unroll
                 for (int j = 0; j < kEach; ++j)
@@ -664,7 +695,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const int c = warp + 4 * WGS * j;
                 float x[4] = {q_in[j].x, q_in[j].y, q_in[j].z, q_in[j].w};
                 uint32_t m = __float_as_uint(unit_top);
-                if constexpr (!C::CHAIN) {
+                if constexpr (!C::WIDE) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
                     m = __reduce_max_sync(0xffffffffu, m);
@@ -675,7 +706,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
                 if (lane == 0) {
-                    if (!C::CHAIN) col[(c >> 1) * 4 + (c & 1)] = unit_cs;
+                    if (!C::WIDE) col[(c >> 1) * 4 + (c & 1)] = unit_cs;
                     mu_at(c) = 0.f;
                     col_lim[c] = c < n_cols ? s.see0 + (int)(c * a.inv_g >> 16) : 0;
                     col_set[c] = c < n_cols ? 0 : 1;
@@ -688,7 +719,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         if (i < QT - 1) {
                             t[e] = lead4(x[e]);
                             x[e] -= t[e];
-                            if (!C::CHAIN) x[e] *= 16.0f;
+                            if (!C::WIDE) x[e] *= 16.0f;
                         } else {
                             t[e] = x[e];
                         }
@@ -698,7 +729,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + mn_chunk<128>(r, (uint32_t)lane >> 2) + (lane & 3) * 4) = codes;
                 }
             }
-            if constexpr (!C::CHAIN && NS > QC * QT)
+            if constexpr (!C::WIDE && NS > QC * QT)
                 for (int r = QC * QT + warp; r < NS; r += 4)
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + r * 128 + lane * 4) = 0u;
             fence_proxy_async();
@@ -709,13 +740,14 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
             for (int p = 0; p < QW / 2; ++p) l[p] = make_float2(0.f, 0.f);
             unsigned long long poison = 0;                 // columns (of the warpgroup) whose channel `row` met a NaN value
-            static_assert(!C::CHAIN || QW == 32, "one pair of chunks a warpgroup");
-            const uint32_t p_off = mn_chunk<C::PW>(row, (uint32_t)c_wg >> 4);
+            static_assert(!C::WIDE || QW == 32, "four chunks of eight columns a warpgroup");
+            // wide: where this row's first chunk of eight weights lies (64 columns a block of 128-byte rows); k further: bits 4, 5
+            const uint32_t p_off = (c_wg >> 6) * kTileBytes + mn_chunk<128>(row, (uint32_t)(c_wg & 63) >> 3);
             bool unset_any = true;                         // some column's Mu does not stand for a maximum yet
             float v_ref = 0.f, v_inv = 0.f;
 
             for (int t = s.t0; t < s.t1; ++t, ++it) {
-                const int st = it % STAGES, pb = it & 1;
+                const int st = it % KST, sv = it % VST, pb = it & 1;
                 bool done_max = false;                     // Mu has been set by this tile's maxima
                 // the scores of this tile are complete: so are its K copy, behind which the scales were written, and the
                 // output product of two tiles ago, issued before these scores, which read this tile's weight buffer
@@ -730,13 +762,13 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
                 const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
-                float kf = C::CHAIN ? ks * unit_cs : ks;
+                float kf = C::WIDE ? ks * unit_cs : ks;
                 if (masked) {
                     // a pass of its own over the scores, which leaves them multiplied by kf, or minus infinity: the loop below
                     // need not know of masks
 #pragma unroll 1
                     for (int c0 = 0; c0 < QW; c0 += 8) {
-                        constexpr int kTerms = C::CHAIN ? 1 : QT;
+                        constexpr int kTerms = C::WIDE ? 1 : QT;
                         float v[8 * kTerms];
 #pragma unroll
                         for (int i = 0; i < kTerms; ++i) tmem_ld8(ts + i * QC + c0, v + 8 * i);
@@ -771,7 +803,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                     for (int p = 0; p < kPart / 2; ++p) {
                         float2 v;
-                        if constexpr (C::CHAIN) {
+                        if constexpr (C::WIDE) {
                             v = make_float2(raw[2 * p], raw[2 * p + 1]);
                         } else {
                             v = make_float2(raw[(QT - 1) * QC + 2 * p], raw[(QT - 1) * QC + 2 * p + 1]);
@@ -779,7 +811,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             for (int i = QT - 2; i >= 0; --i)
                                 v = fma2(v, make_float2(kTerm, kTerm), make_float2(raw[i * QC + 2 * p], raw[i * QC + 2 * p + 1]));
                         }
-                        if constexpr (C::CHAIN) {
+                        if constexpr (C::WIDE) {
                             y[p] = fma2(v, ks2, col_mu[(c_wg + c0) / 2 + p]);
                         } else {
                             const float4 fm = col4[(c_wg + c0) / 2 + p];
@@ -788,7 +820,6 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                 };
                 uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
-                uint8_t *prow0 = prow + p_off, *prow1 = prow + (p_off ^ 16u);
                 // weights, their sum, their e4m3 terms; returns the largest exponent
                 auto weights = [&](auto repeat) {
                     float excess = -INFINITY;
@@ -815,34 +846,14 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             }
                             y[p] = mul2(y[p], r2);
                         }
-                        if constexpr (C::CHAIN) {
-                            // below 2^-6 the leading bits are rounded to e4m3's subnormal grid and the second term does not
-                            // make up for it: an error below 2^-10 beside a largest weight of 2^4 and more
+                        if constexpr (C::WIDE) {
 #pragma unroll
-                            for (int i = 0; i < PT; ++i)
+                            for (int j = 0; j < kPart; j += 8) {
+                                uint32_t u[4];
 #pragma unroll
-                                for (int j = 0; j < kPart; j += 8) {
-                                    uint32_t u[2];
-#pragma unroll
-                                    for (int k = 0; k < 2; ++k) {
-                                        float2 h[2];
-#pragma unroll
-                                        for (int e = 0; e < 2; ++e) {
-                                            float2 &v = y[j / 2 + 2 * k + e];
-                                            h[e] = v;
-                                            if (i < PT - 1) {
-                                                h[e].x = __uint_as_float(__float_as_uint(v.x) & 0xfff00000u);
-                                                h[e].y = __uint_as_float(__float_as_uint(v.y) & 0xfff00000u);
-                                                v.x -= h[e].x; v.y -= h[e].y;
-                                            }
-                                        }
-                                        u[k] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
-                                    }
-                                    // (16-byte chunks k and k + 1 of a row, k even, differ in address bit 4 alone)
-                                    const int c = c0 + j;
-                                    uint8_t *at = (c & 16) ? prow1 : prow0;
-                                    *reinterpret_cast<uint2 *>(at + i * kTile * C::PW + ((c & ~31) >> 4) * 16 + (c & 8)) = make_uint2(u[0], u[1]);
-                                }
+                                for (int k = 0; k < 4; ++k) u[k] = pack_f16(y[j / 2 + k].x, y[j / 2 + k].y);
+                                *reinterpret_cast<uint4 *>(prow + (p_off ^ (uint32_t)((c0 + j) >> 3 << 4))) = make_uint4(u[0], u[1], u[2], u[3]);
+                            }
                         } else {
                             const float2 sixteen = make_float2(16.f, 16.f);
                             uint32_t u[NO / 4];
@@ -910,7 +921,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     if (t > s.t0 && (raise || o_factor != 1.f)) {
                         if (!raise) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
                         tc_fence_after();
-                        constexpr int kCols = C::CHAIN ? QW : NO;
+                        constexpr int kCols = C::WIDE ? QW : NO;
 #pragma unroll 1
                         for (int c0 = 0; c0 < kCols; c0 += 16) {
                             float o[16];
@@ -932,43 +943,79 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     if (done_max || !softmax_any(excess > C::kLagMax, 2 + wg, 128)) break;
                     raise = again = true;
                 }
-                uint8_t *vtile = gbase + (uint32_t)st * 2 * kTileBytes + kTileBytes;
-                if (masked) wait(vfull(st), (uint32_t)(it / STAGES) & 1u, kErrAttnSoftmax);   // it is read and written below
-                if (masked && !valid && wg == 0) {         // 0 * NaN is not 0: values behind the end must not reach the product
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vtile + row * 128)[k] = make_uint4(0u, 0u, 0u, 0u);
-                }
-                if (MODE != 0 && s.n_tok > 1 && (t + 1) * kTile > s.see0) {
-                    // a NaN value of a token that some columns see and others do not: taken out of the product, and noted
-                    // for the columns that see it
+                uint8_t *vtile = gbase + C::kOffV + (uint32_t)sv * kTileBytes;
+                // some columns see a token of this tile that others do not
+                const bool ragged = MODE != 0 && s.n_tok > 1 && (t + 1) * kTile > s.see0;
+                const int n_live = min(kTile, s.live - t * kTile);
+                auto cell = [&](int r) { return vtile + mn_chunk<128>(r, (uint32_t)row >> 4) + (row & 15); };
+                auto note_nan = [&](int r) {               // the columns that see token r
+                    const int c = max(0, max(0, t * kTile + r + 1 - s.see0) * a.G - c_wg);   // the first of them
+                    if (c < 64) poison |= ~0ull << c;
+                };
+                if constexpr (C::WIDE) {
+                    // this thread's share of the V tile in f16: WGS threads a token.  The product of the tile before read the buffer
+                    wait(vfull(sv), (uint32_t)(it / VST) & 1u, kErrAttnSoftmax);
+                    if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
                     bool nan = false;
-                    if (valid && wg == 0) {
+                    uint8_t *to = gbase + C::kOffH + (wg >> 1) * kTileBytes;     // 64 channels a block
+                    if (!masked) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const uint4 v = reinterpret_cast<const uint4 *>(vtile + row * 128)[k];
-                            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) nan |= __vcmpeq4(u[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
+                        for (int j = 2 * wg; j < 2 * wg + 2; ++j) {              // 16 channels
+                            const uint4 v = *reinterpret_cast<const uint4 *>(vtile + mn_chunk<128>(row, j));
+                            const uint4 lo = make_uint4(e4m3x2_to_f16x2(v.x), e4m3x2_to_f16x2(v.x >> 16), e4m3x2_to_f16x2(v.y), e4m3x2_to_f16x2(v.y >> 16));
+                            const uint4 hi = make_uint4(e4m3x2_to_f16x2(v.z), e4m3x2_to_f16x2(v.z >> 16), e4m3x2_to_f16x2(v.w), e4m3x2_to_f16x2(v.w >> 16));
+                            *reinterpret_cast<uint4 *>(to + mn_chunk<128>(row, (2 * j) & 7)) = lo;
+                            *reinterpret_cast<uint4 *>(to + mn_chunk<128>(row, (2 * j + 1) & 7)) = hi;
+                        }
+                    } else {
+                        // 0 * NaN is not 0: values behind the end must not reach the product, nor a NaN value of a token that some
+                        // columns see and others do not: that one is noted for the columns that see it
+#pragma unroll 1
+                        for (int i = 0; i < 8; ++i) {                            // four channels
+                            const int j = 2 * wg + (i >> 2);
+                            const uint32_t u = *reinterpret_cast<const uint32_t *>(vtile + mn_chunk<128>(row, j) + (i & 3) * 4);
+                            const uint32_t is_nan = __vcmpeq4(u & 0x7f7f7f7fu, 0x7f7f7f7fu), drop = !valid ? 0xffffffffu : ragged ? is_nan : 0u;
+                            nan |= valid && is_nan != 0u;
+                            *reinterpret_cast<uint2 *>(to + mn_chunk<128>(row, (2 * j + (i >> 1 & 1)) & 7) + (i & 1) * 8) =
+                                make_uint2(e4m3x2_to_f16x2(u) & ~__byte_perm(drop, 0u, 0x1100), e4m3x2_to_f16x2(u >> 16) & ~__byte_perm(drop, 0u, 0x3322));
                         }
                     }
-                    if (softmax_any(nan, 1, kSoftmax)) {
-                        const int n = min(kTile, s.live - t * kTile);
-                        auto cell = [&](int r) { return vtile + mn_chunk<128>(r, (uint32_t)row >> 4) + (row & 15); };
-                        for (int r = 0; r < n; ++r)
-                            if ((*cell(r) & 0x7f) == 0x7f) {
-                                const int c = max(0, max(0, t * kTile + r + 1 - s.see0) * a.G - c_wg);   // first column that sees it
-                                if (c < 64) poison |= ~0ull << c;
+                    if (ragged && softmax_any(nan, 1, kSoftmax))
+                        for (int r = 0; r < n_live; ++r)
+                            if (((have >> (r >> a.page_shift)) & 1u) && (*cell(r) & 0x7f) == 0x7f) note_nan(r);
+                } else {
+                    if (masked) wait(vfull(sv), (uint32_t)(it / VST) & 1u, kErrAttnSoftmax);   // it is read and written below
+                    if (masked && !valid) {                // 0 * NaN is not 0
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(vtile + row * 128)[k] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    if (ragged) {
+                        bool nan = false;
+                        if (valid) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const uint4 v = reinterpret_cast<const uint4 *>(vtile + row * 128)[k];
+                                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) nan |= __vcmpeq4(u[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
                             }
-                        softmax_bar(1, kSoftmax);
-                        if (wg == 0)
-                            for (int r = 0; r < n; ++r)
-                                if ((*cell(r) & 0x7f) == 0x7f) *cell(r) = 0;
+                        }
+                        if (softmax_any(nan, 1, kSoftmax)) {
+                            for (int r = 0; r < n_live; ++r)
+                                if ((*cell(r) & 0x7f) == 0x7f) {
+                                    note_nan(r);
+                                    *cell(r) = 0;
+                                }
+                        }
                     }
                 }
                 fence_proxy_async();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(pfull(pb));
+                if (lane == 0) {
+                    mbar_arrive(pfull(pb));
+                    if (C::WIDE) mbar_arrive(vempty(sv));
+                }
             }
 
             // -- the segment's end: sums over the 128 token rows, then this thread's channel of every column
@@ -1022,7 +1069,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 if (whole) store1(out_row + col_lim[c], v);
                 else part_row[col_lim[c]] = v;
             };
-            if constexpr (C::CHAIN) {
+            if constexpr (C::WIDE) {
 #pragma unroll 1
                 for (int c0 = 0; c0 < QW; c0 += 16) {
                     float o[16];
