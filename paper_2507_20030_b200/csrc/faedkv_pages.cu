@@ -138,8 +138,8 @@ int make_map(faedkv_pages *pg, CUtensorMap *map, const void *codes) {
 }
 
 //                                  type           columns, warpgroups, terms of q and w, wide, columns at a time, tiles of K and V, CTAs per SM
-using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 3, false, 8, 3, 3, 2>;
-using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 6, false, 8, 2, 2, 2>;
+using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 4, false, 8, 3, 3, 2>;
+using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 8, false, 8, 2, 2, 2>;
 using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 128, 4, 2, 1, true, 8, 3, 2, 1>;
 constexpr int kDecodeCtas = DecodeBf16::CTAS;
 static_assert(kDecodeCtas == DecodeF32::CTAS && DecodeF32::QC == 8 && DecodeBf16::QC == 8, "one plan for both types");

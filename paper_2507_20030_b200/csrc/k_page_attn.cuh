@@ -8,16 +8,18 @@
 // into shared memory, and both products take them as their 128-row A operand,
 //     S[token, col]   = sum_d  K[token, d] * q[col, d]        (A = the K tile, K-major)
 //     O[d, col]      += sum_n  V[n, d]     * w[n, col]        (A = the V tile, MN-major)
-// with the query columns (new tokens x query heads of one kv head) as N.  The other operand has to be e4m3 too, so a
-// query element and a softmax weight are written as sums of e4m3 terms of four significant bits each, the i-th scaled by
-// 16^i: their products are exact and accumulate in float32, so nothing of the cache is converted anywhere and what is
-// lost is only what the last term rounds off (bf16 q: two terms; weights: three terms for bf16, 2^-12 of a weight, six for
-// float32, 2^-24).  Where 128 columns share a tile, the weights are f16 and the V tile is converted to f16 (exact) before the
-// second product, which costs as much as two e4m3 terms and keeps small weights.
+// with the query columns (new tokens x query heads of one kv head) as N.  The other operand has to be of eight bits too, so a
+// query element is written as a sum of e4m3 terms of four significant bits each, the i-th scaled by 16^i, and a softmax
+// weight as a sum of e5m2 terms of three, scaled by 8^i: their products are exact and accumulate in float32, so nothing of
+// the cache is converted anywhere and what is lost is only what the last term rounds off (bf16 q: two terms; weights: four
+// terms for bf16, 2^-12 of a weight and 2^-34 of the column's largest, eight for float32, 2^-24 and 2^-46).  e5m2 for the
+// weights because of its range: with e4m3 terms a weight had fewer bits the smaller it was, and below 2^-20 of the largest
+// none.  Where 128 columns share a tile, the weights are f16 and the V tile is converted to f16 (exact) before the second
+// product, which costs as much as two e4m3 terms and keeps small weights.
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
-// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 8 or so, and then to 2 or 4 below the
-// maximum, so weights stay in e4m3's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
+// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 15 or so, and then to 6 or 8 below the
+// maximum, so weights stay in their format's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
 // power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
 // segment.
 //
@@ -44,28 +46,28 @@ constexpr float kMuNone = -3e38f;                         // a part that saw no 
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
 
-// Instances: QC query columns over WGS softmax warpgroups.  Few columns (WIDE = false): QT / PT e4m3 terms of q / of the weights
-// side by side as further columns of one product, V as it lies.  Many (WIDE = true): QT terms of q added up in the same accumulator;
+// Instances: QC query columns over WGS softmax warpgroups.  Few columns (WIDE = false): QT e4m3 terms of q, PT e5m2 terms of the
+// weights side by side as further columns of one product, V as it lies.  Many (WIDE = true): QT terms of q added up in the same accumulator;
 // weights in f16, which holds them to 2^-11 down to 2^-20 of the largest and to 2^-31 of it below, and V converted to f16 (exact)
 // by the softmax warps, a tile at a time into one buffer (two more warps that convert it were slower, 1016 us for 931 at 2048 new
-// tokens over 18432: with one buffer their work lies between two products).  (Two e4m3 terms on one grid lost every weight below 2^-14 of the largest: beside a
-// loud token thousands of those are half of the output.)  KST / VST: tiles of K and of V on their way.
+// tokens over 18432: with one buffer their work lies between two products).  (Two e4m3 terms on one grid lost every weight below
+// 2^-14 of the largest: beside a loud token thousands of those are half of the output.)  KST / VST: tiles of K and of V on their way.
 template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool WIDE_, int PART_, int KST_, int VST_, int CTAS_> struct AttnCfg {
     using T = T_;
     static constexpr int QC = QC_, WGS = WGS_, QT = QT_, PT = PT_, PART = PART_, KST = KST_, VST = VST_, CTAS = CTAS_;
     static constexpr bool WIDE = WIDE_;
     static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
     static constexpr int kThreads = 128 * WGS + 64;
-    // the largest weight: f16 ends at 2^16; e4m3 at 448, and a second term that is scaled by 16 needs the first one's step to be 16
-    static constexpr float kLagMax = WIDE ? 15.5f : 8.0f;
+    // the largest weight: f16 ends at 2^16, e5m2 at 1.75 2^15, which the terms that follow must not be rounded beyond
+    static constexpr float kLagMax = WIDE ? 15.5f : 15.0f;
     // and after a raise of Mu: room to grow before the next one, against the bits of the small weights (2048 new tokens over
     // 18432: 985 us at 10, 931 at 6, 930 at 4)
-    static constexpr float kLagTo = WIDE ? 6.0f : 2.0f;
+    static constexpr float kLagTo = WIDE ? 6.0f : 8.0f;
     static constexpr int NS = WIDE ? QC : (QC * QT + 15) / 16 * 16;           // columns of S, of O
     static constexpr int NO = WIDE ? QC : (QC * PT + 15) / 16 * 16;
     static constexpr int kTmemUsed = 2 * NS + NO;
     static constexpr uint32_t kTmemCols = kTmemUsed <= 32 ? 32 : kTmemUsed <= 64 ? 64 : kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
-    static constexpr uint32_t PW = NO <= 32 ? 32 : NO <= 64 ? 64 : 128;       // bytes of a token's e4m3 weights
+    static constexpr uint32_t PW = NO <= 32 ? 32 : NO <= 64 ? 64 : 128;       // bytes of a token's e5m2 weights
     static constexpr uint32_t kPBytes = WIDE ? 2 * kTile * QC : kTile * PW;
     static constexpr uint32_t kHBytes = WIDE ? 2 * kTileBytes : 0;            // a V tile in f16
     static constexpr uint32_t kQBytes = (WIDE ? QT * QC : NS) * 128;
@@ -238,6 +240,21 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
     uint32_t h;
     asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(codes));
     return h;
+}
+
+// The leading three significant bits of w as an e5m2 value (0 below e5m2's normal range).
+__device__ __forceinline__ float lead3(float w) {
+    const float h = __uint_as_float(__float_as_uint(w) & 0xffe00000u);
+    return fabsf(w) >= 6.103515625e-05f ? h : 0.f;
+}
+// e5m2 codes, round to nearest even; the first in the lowest byte.
+__device__ __forceinline__ uint32_t to_e5m2x4(float a, float b, float c, float d) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "cvt.rn.satfinite.e5m2x2.f32 lo, %2, %1;\n\t"
+        "cvt.rn.satfinite.e5m2x2.f32 hi, %4, %3;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
 }
 
 // One unit of work is the columns of one (sequence, kv head, block of new tokens); a segment is a run of its tiles.
@@ -598,7 +615,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     } else if (warp == kWarpMma) {
         // ------------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
-            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO);   // (format 0: e4m3, or f16)
+            // formats: 0 is e4m3, or f16 in the wide form's second product; 1 e5m2 (the weights, operand B of the narrow form's)
+            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO) | (C::WIDE ? 0u : 1u << 10);
             Work<MODE> w = w0;
             Segment s;
             int it = 0;                                    // tiles whose S has been issued
@@ -655,7 +673,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         // ------------------------------------------------------------------------ softmax
         const int wg = warp >> 2, row = tid & 127, c_wg = wg * QW;            // this thread's token / channel, its first column
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        constexpr float kTerm = 1.0f / 16.0f;
+        constexpr float kTerm = 1.0f / 16.0f, kWeightTerm = 1.0f / 8.0f;
         auto mu_at = [&](int c) -> float & { return C::WIDE ? col[c] : col[(c >> 1) * 4 + 2 + (c & 1)]; };   // -Mu of column c
         const float2 *col_mu = reinterpret_cast<const float2 *>(col);
         const float4 *col4 = reinterpret_cast<const float4 *>(col);           // factors and -Mu of columns 2 p, 2 p + 1
@@ -820,7 +838,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     }
                 };
                 uint8_t *prow = gbase + C::kOffP + pb * C::kPBytes;
-                // weights, their sum, their e4m3 terms; returns the largest exponent
+                // weights, their sum, what the product takes of them; returns the largest exponent
                 auto weights = [&](auto repeat) {
                     float excess = -INFINITY;
                     float raw[2][kLoad];
@@ -855,7 +873,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 *reinterpret_cast<uint4 *>(prow + (p_off ^ (uint32_t)((c0 + j) >> 3 << 4))) = make_uint4(u[0], u[1], u[2], u[3]);
                             }
                         } else {
-                            const float2 sixteen = make_float2(16.f, 16.f);
+                            const float2 eight = make_float2(8.f, 8.f);
                             uint32_t u[NO / 4];
 #pragma unroll
                             for (int i = 0; i < NO / 4; ++i) u[i] = 0u;
@@ -869,11 +887,11 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                         float2 &v = y[j / 2 + e];
                                         h[e] = v;
                                         if (i < PT - 1) {
-                                            h[e] = make_float2(lead4(v.x), lead4(v.y));
-                                            v = mul2(sub2(v, h[e]), sixteen);
+                                            h[e] = make_float2(lead3(v.x), lead3(v.y));
+                                            v = mul2(sub2(v, h[e]), eight);
                                         }
                                     }
-                                    u[(i * QC + j) / 4] = to_e4m3x4(h[0].x, h[0].y, h[1].x, h[1].y);
+                                    u[(i * QC + j) / 4] = to_e5m2x4(h[0].x, h[0].y, h[1].x, h[1].y);
                                 }
 #pragma unroll
                             for (int k = 0; k < NO / 16; ++k)
@@ -939,7 +957,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         raise = false;
                     }
                     const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
-                    // a weight beyond 2^8 does not fit its terms: raise Mu, and the weights once more
+                    // a weight beyond 2^kLagMax does not fit its terms: raise Mu, and the weights once more
                     if (done_max || !softmax_any(excess > C::kLagMax, 2 + wg, 128)) break;
                     raise = again = true;
                 }
@@ -1086,7 +1104,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 for (int c = 0; c < QC; ++c) {
                     float v = o[(PT - 1) * QC + c];
 #pragma unroll
-                    for (int i = PT - 2; i >= 0; --i) v = fmaf(v, kTerm, o[i * QC + c]);
+                    for (int i = PT - 2; i >= 0; --i) v = fmaf(v, kWeightTerm, o[i * QC + c]);
                     put(c, v);
                 }
             }
