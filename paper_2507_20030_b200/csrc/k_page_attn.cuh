@@ -11,8 +11,9 @@
 // with the query columns (new tokens x query heads of one kv head) as N.  The other operand has to be of eight bits too, so a
 // query element is written as a sum of e4m3 terms of four significant bits each, the i-th scaled by 16^i, and a softmax
 // weight as a sum of e5m2 terms of three, scaled by 8^i: their products are exact and accumulate in float32, so nothing of
-// the cache is converted anywhere and what is lost is only what the last term rounds off (bf16 q: two terms; weights: four
-// terms for bf16, 2^-12 of a weight and 2^-34 of the column's largest, eight for float32, 2^-24 and 2^-46).  e5m2 for the
+// the cache is converted anywhere and what is lost is only what the last term rounds off (bf16 q: two terms, 2^-17 of its
+// row's largest element at most; weights: four terms for bf16, 2^-12 of a weight and 2^-34 of the column's largest, eight for
+// float32, 2^-24 and 2^-46).  e5m2 for the
 // weights because of its range: with e4m3 terms a weight had fewer bits the smaller it was, and below 2^-20 of the largest
 // none.  Where 128 columns share a tile, the weights are f16 and the V tile is converted to f16 (exact) before the second
 // product, which costs as much as two e4m3 terms and keeps small weights.
@@ -24,7 +25,7 @@
 // segment.
 //
 // Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
-// it in the tiles); 2048 new tokens over 18432 931 us (629 TFLOP/s), bound by the softmax warps; float32, six
+// it in the tiles); 2048 new tokens over 18432 969 us (603 TFLOP/s), bound by the softmax warps; float32, six
 // ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster than over two or 96 over three (879,
 // 992 and 961 us with e4m3 weights), eight columns at a time than sixteen (931, 952).
 //
@@ -78,7 +79,7 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool WIDE_, int PART
     static constexpr uint32_t kOffMisc = kOffH + kHBytes;
     static constexpr uint32_t kSmemBytes = kOffMisc + sizeof(float) * (9 * QC + KST * 32) + 256 + 1024;
     static constexpr uint32_t kSmemBlocks = 4 * (kMaxBlocks + 1);             // MODE 1 appends its prefix sums
-    static_assert(!WIDE || (QC == 128 && WGS == 4 && PT == 1 && KST <= VST + 1), "the layouts of the wide form");
+    static_assert(!WIDE || (QC == 128 && WGS == 4 && QT == 2 && PT == 1 && KST <= VST + 1), "the layouts of the wide form");
     static_assert(!WIDE || (PART % 8 == 0 && QW % PART == 0), "whole parts");
     static_assert(WIDE || (WGS == 1 && KST == VST), "a tile's K and V leave together");
 };
@@ -385,7 +386,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     auto v_tile = [&](int s) { return base + C::kOffV + (uint32_t)s * kTileBytes; };
     const uint32_t q_base = base + C::kOffQ;
     auto p_tile = [&](int p) { return base + C::kOffP + (uint32_t)p * C::kPBytes; };
-    float *col = reinterpret_cast<float *>(gbase + C::kOffMisc);             // per pair of columns: factors of the raw scores, -Mu
+    float *col = reinterpret_cast<float *>(gbase + C::kOffMisc);             // per pair of columns: factors of the raw scores, -Mu (wide: [QC] -Mu, [QC] factors)
     float *col_f = col + 2 * QC;                                             // [QC] 2^-raise
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
     int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
@@ -615,8 +616,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     } else if (warp == kWarpMma) {
         // ------------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
-            // formats: 0 is e4m3, or f16 in the wide form's second product; 1 e5m2 (the weights, operand B of the narrow form's)
-            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescO = make_idesc(0u, 1u, 1u, NO) | (C::WIDE ? 0u : 1u << 10);
+            // formats: 0 is e4m3, or f16 in the wide form's second product; 1 e5m2 (operand B: the wide form's second term of q, the
+            // narrow form's weights)
+            constexpr uint32_t kIdescS = make_idesc(0u, 0u, 0u, NS), kIdescS1 = kIdescS | 1u << 10, kIdescO = make_idesc(0u, 1u, 1u, NO) | (C::WIDE ? 0u : 1u << 10);
             Work<MODE> w = w0;
             Segment s;
             int it = 0;                                    // tiles whose S has been issued
@@ -631,7 +633,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             mma_f8(tmem_s + (it & 1) * NS, desc_kmajor_sw128(k_tile(st) + k * 32),
-                                   desc_kmajor_sw128(q_base + term * QC * 128 + k * 32), kIdescS, (term | k) ? 1u : 0u);
+                                   desc_kmajor_sw128(q_base + term * QC * 128 + k * 32), term ? kIdescS1 : kIdescS, (term | k) ? 1u : 0u);
                     mma_commit(sfull(it & 1));
                     if (C::WIDE) mma_commit(kempty(st));
                 }
@@ -692,59 +694,77 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const int c = warp + 4 * WGS * j, tok = c * a.inv_g >> 16;
                 q_in[j] = c < n_cols ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            // one power of two for all columns where they are many (it stays out of the softmax's inner loop): an element is
-            // then off by at most 2^-16 of the largest of them; one for each column otherwise
-            float unit_top = 0.f;
-            if constexpr (C::WIDE) {
-                uint32_t m = 0;
+            uint32_t top[kEach];                           // the columns' largest finite magnitudes
 #pragma unroll
-                for (int j = 0; j < kEach; ++j)
-                    m = max(max(m, max(finite_bits(q_in[j].x), finite_bits(q_in[j].y))), max(finite_bits(q_in[j].z), finite_bits(q_in[j].w)));
-                m = __reduce_max_sync(0xffffffffu, m);
-                if (lane == 0) red[warp] = __uint_as_float(m);
-                softmax_bar(1, kSoftmax);
-#pragma unroll
-                for (int i = 0; i < 4 * WGS; ++i) unit_top = fmaxf(unit_top, red[i]);
-                softmax_bar(1, kSoftmax);
-            }
+            for (int j = 0; j < kEach; ++j)
+                top[j] = __reduce_max_sync(0xffffffffu, max(max(finite_bits(q_in[j].x), finite_bits(q_in[j].y)), max(finite_bits(q_in[j].z), finite_bits(q_in[j].w))));
+            // Many columns, all within 2^3 of one another (but for zeros): one power of two for all, which stays out of the softmax's
+            // inner loop (2048 new tokens over 18432: 969 us; with a factor for each column always 1008).  Else each has its own
+            // (1000 us; in a pass over the scores as masks take, 942 and 1331)
+            bool common = false;
             float unit_cs = 0.f;
+            uint32_t unit_top = 0;
+            if constexpr (C::WIDE) {
+                uint32_t hi = 0, lo = 0x7fffffffu;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    hi = max(hi, top[j]);
+                    if (top[j] != 0u) lo = min(lo, top[j]);
+                }
+                if (lane == 0) *reinterpret_cast<uint2 *>(red + 2 * warp) = make_uint2(hi, lo);
+                softmax_bar(1, kSoftmax);
+#pragma unroll 4
+                for (int i = 0; i < 4 * WGS; ++i) {
+                    const uint2 r = *reinterpret_cast<const uint2 *>(red + 2 * i);
+                    hi = max(hi, r.x);
+                    lo = min(lo, r.y);
+                }
+                softmax_bar(1, kSoftmax);
+                common = hi == 0u || scale_for(__uint_as_float(hi)) <= 8.0f * scale_for(__uint_as_float(lo));
+                unit_top = hi;
+                unit_cs = 2.0f * scale_for(__uint_as_float(hi)) * a.scale_log2;
+            }
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const int c = warp + 4 * WGS * j;
                 float x[4] = {q_in[j].x, q_in[j].y, q_in[j].z, q_in[j].w};
-                uint32_t m = __float_as_uint(unit_top);
-                if constexpr (!C::WIDE) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) m = max(m, finite_bits(x[e]));
-                    m = __reduce_max_sync(0xffffffffu, m);
-                }
-                const float qs = 2.0f * scale_for(__uint_as_float(m));
-                unit_cs = qs * a.scale_log2;
+                const float qs = 2.0f * scale_for(__uint_as_float(common ? unit_top : top[j]));       // the largest element to 112 .. 224
                 const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] * inv : __uint_as_float(0x7fffffffu);
                 if (lane == 0) {
-                    if (!C::WIDE) col[(c >> 1) * 4 + (c & 1)] = unit_cs;
+                    col[C::WIDE ? QC + c : (c >> 1) * 4 + (c & 1)] = qs * a.scale_log2;
                     mu_at(c) = 0.f;
                     col_lim[c] = c < n_cols ? s.see0 + (int)(c * a.inv_g >> 16) : 0;
                     col_set[c] = c < n_cols ? 0 : 1;
                 }
-#pragma unroll
-                for (int i = 0; i < QT; ++i) {
-                    float t[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (i < QT - 1) {
-                            t[e] = lead4(x[e]);
-                            x[e] -= t[e];
-                            if (!C::WIDE) x[e] *= 16.0f;
-                        } else {
-                            t[e] = x[e];
-                        }
-                    }
-                    const uint32_t codes = to_e4m3x4(t[0], t[1], t[2], t[3]);
-                    const uint32_t r = (uint32_t)(i * QC + c);
+                auto put_codes = [&](int term, uint32_t codes) {
+                    const uint32_t r = (uint32_t)(term * QC + c);
                     *reinterpret_cast<uint32_t *>(gbase + C::kOffQ + mn_chunk<128>(r, (uint32_t)lane >> 2) + (lane & 3) * 4) = codes;
+                };
+                if constexpr (C::WIDE) {
+                    // both terms on one grid: what the first leaves of an element above 2^-6 has three significant bits (bf16's eight
+                    // less its four, and a sign), which e5m2 holds; of smaller ones e5m2's rounding is at most 2^-14
+                    float hi[4];
+                    const uint32_t codes = to_e4m3x4(x[0], x[1], x[2], x[3]);
+                    from_e4m3x4(codes, hi);
+                    put_codes(0, codes);
+                    put_codes(1, to_e5m2x4(x[0] - hi[0], x[1] - hi[1], x[2] - hi[2], x[3] - hi[3]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < QT; ++i) {
+                        float t[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (i < QT - 1) {
+                                t[e] = lead4(x[e]);
+                                x[e] = (x[e] - t[e]) * 16.0f;
+                            } else {
+                                t[e] = x[e];
+                            }
+                        }
+                        put_codes(i, to_e4m3x4(t[0], t[1], t[2], t[3]));
+                    }
                 }
             }
             if constexpr (!C::WIDE && NS > QC * QT)
@@ -782,8 +802,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
                 float kf = C::WIDE ? ks * unit_cs : ks;
                 if (masked) {
-                    // a pass of its own over the scores, which leaves them multiplied by kf, or minus infinity: the loop below
-                    // need not know of masks
+                    // a pass of its own over the scores, which leaves them multiplied by their factor, or minus infinity: the loop
+                    // below need not know of masks
 #pragma unroll 1
                     for (int c0 = 0; c0 < QW; c0 += 8) {
                         constexpr int kTerms = C::WIDE ? 1 : QT;
@@ -795,7 +815,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         for (int e = 0; e < 8; ++e) {
 #pragma unroll
                             for (int i = kTerms - 2; i >= 0; --i) v[8 * i + e] = fmaf(v[8 * (i + 1) + e], kTerm, v[8 * i + e]);
-                            v[e] = valid && tok < col_lim[c_wg + c0 + e] ? v[e] * kf : -INFINITY;
+                            const float f = C::WIDE ? ks * col[QC + c_wg + c0 + e] : ks;
+                            v[e] = valid && tok < col_lim[c_wg + c0 + e] ? v[e] * f : -INFINITY;
 #pragma unroll
                             for (int i = 1; i < kTerms; ++i) v[8 * i + e] = 0.f;
                         }
@@ -805,6 +826,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     tmem_st_wait();
                     kf = 1.f;
                 }
+                const bool own = C::WIDE && !masked && !common;            // each column's factor is still to come
+                if (own) kf = ks;
                 const float2 ks2 = make_float2(kf, kf);
                 // a column without a maximum: Mu is settled before the weights are taken; a larger v_scale than any before: Vref
                 bool raise = unset_any;
@@ -818,6 +841,12 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const float2 r2 = make_float2(vs * v_inv, vs * v_inv);
                 // y of the columns c_wg + c0 .. from their raw scores
                 auto exponents = [&](const float(&raw)[kLoad], int c0, float2(&y)[kPart / 2]) {
+                    if (C::WIDE && own) {
+#pragma unroll
+                        for (int p = 0; p < kPart / 2; ++p)
+                            y[p] = fma2(make_float2(raw[2 * p], raw[2 * p + 1]), mul2(ks2, col_mu[(QC + c_wg + c0) / 2 + p]), col_mu[(c_wg + c0) / 2 + p]);
+                        return;
+                    }
 #pragma unroll
                     for (int p = 0; p < kPart / 2; ++p) {
                         float2 v;

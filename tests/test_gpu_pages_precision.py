@@ -27,7 +27,7 @@ def fk():
 # row's largest.  `wide`: bf16 calls with more than eight query columns a sequence.
 WEIGHT = {"wide": 2.0 ** -11, "bf16": 2.0 ** -12, "f32": 2.0 ** -24}
 FLOOR = {"wide": 2.0 ** -31, "bf16": 2.0 ** -34, "f32": 2.0 ** -46}
-QUERY = {"wide": 2.0 ** -20, "bf16": 2.0 ** -20, "f32": 2.0 ** -30}
+QUERY = {"wide": 2.0 ** -17, "bf16": 2.0 ** -17, "f32": 2.0 ** -30}
 
 
 def check(kind, got, q, K, V, seen, scale=1.0 / math.sqrt(128), floor_v=None):
@@ -144,3 +144,27 @@ def test_decode_beside_a_loud_token(fk, dtype, loud, spread):
     kind = "bf16" if dtype == torch.bfloat16 else "f32"
     rows = slice(0, 160)
     check(kind, out[rows].reshape(-1, 128), q[rows].reshape(-1, 128), K[0], V[0], torch.full((160 * G,), n, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------------ loud queries
+
+@pytest.mark.parametrize("louder", [2.0 ** 4, 2.0 ** 8, 2.0 ** 12, 2.0 ** 18])
+@pytest.mark.parametrize("where", ["head", "token"])
+def test_a_loud_query_among_quiet_ones(fk, louder, where):
+    """One head, or one token, has a loud element (on a channel where the keys are zero): the rows beside it keep their bits."""
+    rng = np.random.default_rng(int(math.log2(louder)))
+    n, G, B, new = 600, 4, 3, 40
+    table, codes, scales, (K, V) = sequence(rng, n, 2, 32, 0.0, "ordinary")
+    codes[0].view(torch.uint8)[int(table[0]), :, 0] = 0
+    K[:, 0] = 0.0
+    q = queries(rng, B * new, 2 * G, 0.0, torch.bfloat16)
+    if where == "head":
+        q[:, 2, 0] = louder
+    else:
+        q[::7, :, 0] = louder
+    out = run(fk, torch.bfloat16, q, G, 32, table, codes, scales, n, B, new)
+    seen = (n - new + 1 + torch.arange(new, device="cuda")).repeat_interleave(G)
+    for b in range(B):
+        for h in range(2):
+            at = (slice(b * new, (b + 1) * new), slice(h * G, (h + 1) * G))
+            check("wide", out[at].reshape(-1, 128), q[at].reshape(-1, 128), K[h], V[h], seen)
