@@ -459,9 +459,10 @@ size_t faedkv_pages_attn_bytes(const faedkv_pages *pg, int batch, int n_tokens);
  * scale = 0 means 1/sqrt(head_dim).  A token that sees nothing (kv_len[b] = 0) gets a row of zeros.  Scales need not be
  * powers of two.  ws: faedkv_pages_attn_bytes(), overwritten; calls that overlap need one each.
  * Rounding: the cache's codes are used as they are; an element of q is held to 2^-17 (bf16) or 2^-30 (float32) of the largest
- * of its 128; scores, maxima and sums are float32; a softmax weight is held to 2^-24 of itself and 2^-46 of its row's largest
- * (float32), 2^-12 and 2^-34 (bf16), or 2^-11 and 2^-31 (bf16 calls with more than eight query columns, tokens x query heads
- * per kv head, a sequence); out is rounded once.  Results do not depend on the order in which blocks of the GPU run. */
+ * of its 128; scores, maxima and sums are float32; a softmax weight, times its page's v_scale, is held to 2^-24 of
+ * itself and 2^-46 of its row's largest (float32), 2^-12 and 2^-34 (bf16), or 2^-11 and 2^-31 (bf16 calls with more than eight
+ * query columns, tokens x query heads per kv head, a sequence), where the v_scales of a sequence's pages of one head lie within 2^20
+ * of one another; out is rounded once.  Results do not depend on the order in which blocks of the GPU run. */
 int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
                       const int32_t *kv_len, const int32_t *table, const void *k_pages, const void *v_pages,
                       const float *k_scale, const float *v_scale, float scale, void *out, void *ws, size_t ws_bytes,

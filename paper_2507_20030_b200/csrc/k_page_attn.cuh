@@ -19,10 +19,12 @@
 // product, which costs as much as two e4m3 terms and keeps small weights.
 //
 // Softmax runs in base 2: y = s * (k_scale * scale * log2 e) - Mu, p = 2^y, l += p, weights w = p * (v_scale / Vref).  Mu
-// follows the column maximum lazily: it is raised (and O, l rescaled) only when some y exceeds 15 or so, and then to 6 or 8 below the
-// maximum, so weights stay in their format's range and most tiles exchange one vote instead of a maximum per column.  Vref is the
-// power of two above the largest v_scale met so far; raising it rescales O alone.  O stays in TMEM over all tiles of a
-// segment.
+// follows the column's largest weight lazily: it is raised (and O, l rescaled) only when some weight exceeds 2^15 or so, and then
+// to 2^-6 or 2^-8 of the largest, so weights stay in their format's range and most tiles exchange one vote instead of a maximum per
+// column.  It follows the weights and not p, so a page of large values that hardly counts takes no bits from the others.  Vref is
+// the power of two above the first tile's largest v_scale; only a scale 2^20 beyond it moves it, which rescales O alone: p, and
+// with it l, stays within 2^20 of the weights, in float32's reach (pages of zeros have the smallest scale, and their tokens
+// count in l all the same).  O stays in TMEM over all tiles of a segment.
 //
 // Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
 // it in the tiles); 2048 new tokens over 18432 969 us (603 TFLOP/s), bound by the softmax warps; float32, six
@@ -43,6 +45,7 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
+constexpr float kScaleRange = 1048576.f;                  // of v_scale about Vref
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
@@ -60,7 +63,7 @@ template <typename T_, int QC_, int WGS_, int QT_, int PT_, bool WIDE_, int PART
     static constexpr int QW = QC / WGS;                                       // columns of a warpgroup
     static constexpr int kThreads = 128 * WGS + 64;
     // the largest weight: f16 ends at 2^16, e5m2 at 1.75 2^15, which the terms that follow must not be rounded beyond
-    static constexpr float kLagMax = WIDE ? 15.5f : 15.0f;
+    static constexpr float kMostWeight = WIDE ? 46336.f : 32768.f;
     // and after a raise of Mu: room to grow before the next one, against the bits of the small weights (2048 new tokens over
     // 18432: 985 us at 10, 931 at 6, 930 at 4)
     static constexpr float kLagTo = WIDE ? 6.0f : 8.0f;
@@ -829,10 +832,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const bool own = C::WIDE && !masked && !common;            // each column's factor is still to come
                 if (own) kf = ks;
                 const float2 ks2 = make_float2(kf, kf);
-                // a column without a maximum: Mu is settled before the weights are taken; a larger v_scale than any before: Vref
+                // a column without a maximum: Mu is settled before the weights are taken; a v_scale far beyond those before: Vref
                 bool raise = unset_any;
                 float o_factor = 1.f;
-                if (v_max > v_ref) {
+                if (v_max > v_ref * kScaleRange) {
                     const float up = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
                     if (v_ref > 0.f) o_factor = v_ref / up;
                     v_ref = up;
@@ -935,6 +938,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     if (raise) {
                         // Mu to kLagTo below the column maxima, and what has been summed rescaled
                         if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
+                        const float lift = __log2f(fmaxf(fabsf(r2.x), 1.f / kScaleRange));
 #pragma unroll 1
                         for (int c0 = 0; c0 < QW; c0 += kPart) {
                             float raw[kLoad];
@@ -944,7 +948,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             exponents(raw, c0, y);
 #pragma unroll
                             for (int p = 0; p < kPart / 2; ++p) {
-                                const float m0 = warp_max(y[p].x), m1 = warp_max(y[p].y);
+                                const float m0 = warp_max(y[p].x + lift), m1 = warp_max(y[p].y + lift);
                                 if (lane == 0) *reinterpret_cast<float2 *>(red + (warp & 3) * QC + c_wg + c0 + 2 * p) = make_float2(m0, m1);
                             }
                         }
@@ -956,8 +960,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             const bool first = col_set[c] == 0, seen = m > -INFINITY;
                             const float d = seen && (first || m > 0.f) ? m : 0.f;
                             mu_at(c) -= d;
-                            // 1: nothing has been summed yet; 0: what has been is beyond float32's reach
-                            col_f[c] = first ? 1.f : d > 64.f ? 0.f : ex2(-d);
+                            // 1: nothing has been summed yet; 0: what has been is beyond float32's reach, or was summed as infinity
+                            // (p of a tile that is taken again reaches 2^(d + kLagTo + 20))
+                            col_f[c] = first ? 1.f : d > 96.f ? 0.f : ex2(-d);
                             if (seen) col_set[c] = 1;
                             unset = first && !seen;
                         }
@@ -986,8 +991,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         raise = false;
                     }
                     const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
-                    // a weight beyond 2^kLagMax does not fit its terms: raise Mu, and the weights once more
-                    if (done_max || !softmax_any(excess > C::kLagMax, 2 + wg, 128)) break;
+                    // a weight beyond its format's range (or, beside a far smaller scale, p beyond l's): raise Mu, and the weights
+                    // once more
+                    if (done_max || !softmax_any(ex2(excess) * fmaxf(fabsf(r2.x), 1.f / kScaleRange) > C::kMostWeight, 2 + wg, 128)) break;
                     raise = again = true;
                 }
                 uint8_t *vtile = gbase + C::kOffV + (uint32_t)sv * kTileBytes;

@@ -168,3 +168,29 @@ def test_a_loud_query_among_quiet_ones(fk, louder, where):
         for h in range(2):
             at = (slice(b * new, (b + 1) * new), slice(h * G, (h + 1) * G))
             check("wide", out[at].reshape(-1, 128), q[at].reshape(-1, 128), K[h], V[h], seen)
+
+
+# ------------------------------------------------------------------------------------------------ pages of different scales
+
+@pytest.mark.parametrize("kind", ["wide", "bf16", "f32"])
+@pytest.mark.parametrize("at", [1, 40])
+def test_a_page_of_loud_values_that_hardly_counts(fk, kind, at):
+    """One page's values are 2^19 times the others' and its tokens' scores 42 nats down, so that it adds 2^-40 of the output:
+    the other pages, with a loud token of their own and equal scores, keep their weights' bits wherever the loud page stands."""
+    rng = np.random.default_rng(at)
+    n, page, G, loud = 4096, 64, 8, 9.8
+    B, new = (150, 16) if kind == "wide" else (600, None)
+    dtype = torch.float32 if kind == "f32" else torch.bfloat16
+    table, codes, scales, (K, V) = sequence(rng, n, 1, page, loud, "zero", spread=0.0)
+    rows = slice(at * page, (at + 1) * page)
+    codes[0][int(table[at]), 0, :, 1] = -448.0
+    K[0, rows, 1] = -28.0
+    scales[1][int(table[at])] *= 2.0 ** 19
+    V[0, rows] *= 2.0 ** 19
+    q = queries(rng, B * (new or 1), G, loud, dtype)
+    q[:, :, 1] = 17.0                                      # 17 * 28 / sqrt(128) = 42
+    out = run(fk, dtype, q, G, page, table, codes, scales, n, B, new)
+    m = new or 4
+    seen = (n - m + 1 + torch.arange(m, device="cuda")) if new else torch.full((m,), n, device="cuda")
+    # what the loud page adds is counted as an error of its own share, not as the scale of the others' floor
+    check(kind, out[:m].reshape(-1, 128), q[:m].reshape(-1, 128), K[0], V[0], seen.repeat_interleave(G), floor_v=V[0, :page].abs().max())
