@@ -335,7 +335,8 @@ __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 12
     float *scales = which == 0 ? a.scale[0] : a.scale[1];
     const int c8 = (tid & 15) * 8, row_t = tid >> 4;
     const size_t step = (size_t)kRows * a.ld;
-    for (int turn = 0; j < n_tile; ++turn) {
+    int turn = 0;                                         // runs done: two buffers of maxima, so one barrier a run keeps them apart.  A
+    while (j < n_tile) {                                  // token that is skipped passes no barrier and must not change the buffer
         const int slot = slots[j];
         const int r0 = slot & (PAGE - 1), cap = min(PAGE - r0, n_rest - j);
         // run length: up to the first token whose slot does not follow
@@ -387,6 +388,7 @@ __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 12
         if (lane == 0) max_s[turn & 1][warp] = amax;
         __syncthreads();
         amax = __reduce_max_sync(0xffffffffu, max_s[turn & 1][lane & (kWarps - 1)]);
+        ++turn;
         float s = scale_for(__uint_as_float(amax));
         uint8_t *dst = codes + ph * (size_t)(PAGE * kHeadDim) + row_t * kHeadDim + c8;
         if (r0 > 0) {
