@@ -284,7 +284,8 @@ int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n
     if (ws == nullptr) return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL workspace passed to faedkv_pages_tables");
     pages::k_page_plan<false><<<1, pages::kPlanThreads, 0, st>>>(a);
     if (int r = launch_check(pg, "k_page_plan")) return r;
-    CUDA_TRY(pg, launch_pdl(pages::k_page_slots, dim3((n_tokens + 255) / 256), dim3(256), 0, st, a));
+    if (n_tokens == 0) return FAEDKV_OK;                   // lengths and released pages only
+    CUDA_TRY(pg, launch_pdl(pages::k_page_slots, dim3((unsigned)(((long long)n_tokens + 255) / 256)), dim3(256), 0, st, a));
     return launch_check(pg, "k_page_slots");
 }
 
