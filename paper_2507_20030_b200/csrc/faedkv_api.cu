@@ -125,11 +125,13 @@ int fail(faedkv_ctx *ctx, int code, const char *fmt, ...) {
     return code;
 }
 
-#define CUDA_TRY(ctx, expr)                                                                   \
-    do {                                                                                      \
-        cudaError_t e_ = (expr);                                                              \
-        if (e_ != cudaSuccess)                                                                \
-            return fail(ctx, FAEDKV_ERR_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_)); \
+#define CUDA_TRY(ctx, expr)                                                                  \
+    do {                                                                                     \
+        cudaError_t e_ = (expr);                                                             \
+        if (e_ != cudaSuccess) {                                                             \
+            cudaGetLastError(); /* reported here: not by the next call's launch */           \
+            return fail(ctx, FAEDKV_ERR_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_));\
+        }                                                                                    \
     } while (0)
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -46,8 +46,10 @@ int fail(faedkv_pages *pg, int code, const char *fmt, ...) {
 #define CUDA_TRY(pg, expr)                                                                   \
     do {                                                                                     \
         cudaError_t e_ = (expr);                                                             \
-        if (e_ != cudaSuccess)                                                               \
-            return fail(pg, FAEDKV_ERR_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_)); \
+        if (e_ != cudaSuccess) {                                                             \
+            cudaGetLastError(); /* reported here: not by the next call's launch */           \
+            return fail(pg, FAEDKV_ERR_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_));\
+        }                                                                                    \
     } while (0)
 
 // Makes the handle's device current for the length of a call.
@@ -55,8 +57,9 @@ struct DeviceGuard {
     int before = -1;
     bool ok = false;
     explicit DeviceGuard(const faedkv_pages *pg) {
-        if (cudaGetDevice(&before) != cudaSuccess) { before = -1; return; }
+        if (cudaGetDevice(&before) != cudaSuccess) { before = -1; cudaGetLastError(); return; }
         ok = before == pg->device || cudaSetDevice(pg->device) == cudaSuccess;
+        if (!ok) cudaGetLastError();
         if (before == pg->device) before = -1;
     }
     ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
