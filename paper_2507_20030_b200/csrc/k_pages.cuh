@@ -408,16 +408,27 @@ __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 12
                 s = s_old;
             }
         }
-        // 1 / s: exact for the powers of two that this kernel writes; a scale of another origin is divided by
-        const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0u && __float_as_uint(s) - 1u < (254u << 23) - 1u;
-        const float inv = pow2 ? __uint_as_float((254u << 23) - __float_as_uint(s)) : __fdiv_rn(1.0f, s);
         dst += r0 * kHeadDim;
+        if ((__float_as_uint(s) & 0x7fffffu) == 0u && __float_as_uint(s) - 1u < (254u << 23) - 1u) {
+            const float inv = __uint_as_float((254u << 23) - __float_as_uint(s));    // 1 / s, exact for the powers of two that this kernel writes
 #pragma unroll
-        for (int k = 0; k < kIter; ++k) {
-            if (row_t + k * kRows < n) {
+            for (int k = 0; k < kIter; ++k) {
+                if (row_t + k * kRows < n) {
+                    float v[8];
+                    raw[k].get(v);
+                    *reinterpret_cast<uint2 *>(dst + k * kRows * kHeadDim) = to_e4m3x8(v, inv);
+                }
+            }
+        } else {                                          // a scale of another origin: divided by, the rows read again
+#pragma unroll 1
+            for (int k = 0; row_t + k * kRows < n; ++k) {
+                Raw8<T> again;
                 float v[8];
-                raw[k].get(v);
-                *reinterpret_cast<uint2 *>(dst + k * kRows * kHeadDim) = to_e4m3x8(v, inv);
+                again.load(src + k * step);
+                again.get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __fdiv_rn(v[e], s);
+                *reinterpret_cast<uint2 *>(dst + k * kRows * kHeadDim) = to_e4m3x8(v, 1.0f);
             }
         }
         if (tid == 0) scales[ph] = s;
