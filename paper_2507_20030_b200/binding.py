@@ -513,11 +513,15 @@ class Pages:
             if not ws.is_contiguous() or ws.get_device() != self._index or ws.numel() * ws.element_size() < nbytes:
                 raise ValueError(f"ws must be a contiguous tensor of at least {nbytes} bytes on {self.device}")
             return ws
+        return self._empty(nbytes, torch.uint8, stream)
+
+    def _empty(self, shape, dtype, stream):
+        """Memory of the call's stream: the allocator may hand out again what the current stream is still working on."""
         if stream is None:
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            return torch.empty(shape, dtype=dtype, device=self.device)
         s = torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
         with torch.cuda.stream(s):
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _on(self, stream):
         """The stream's handle; by default the current stream of the handle's device."""
@@ -577,13 +581,14 @@ class Pages:
                                                 self._on(stream)))
 
     def load(self, kv_len, table, k_pages, v_pages, k_scale, v_scale, L: int, K_out=None, V_out=None, stream=None):
-        """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end."""
+        """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end.  What is not given is allocated on the call's
+        stream."""
         batch = kv_len.shape[0]
         shape = (batch, self.n_kv_heads, L, self.head_dim)
         if K_out is None:
-            K_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+            K_out = self._empty(shape, self.torch_dtype, stream)
         if V_out is None:
-            V_out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+            V_out = self._empty(shape, self.torch_dtype, stream)
         need = self._need
         kv = need("kv_len", kv_len, torch.int32, (batch,))
         tb = need("table", table, torch.int32, (batch, self.max_pages))
