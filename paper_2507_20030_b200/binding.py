@@ -582,20 +582,30 @@ class Pages:
 
     def load(self, kv_len, table, k_pages, v_pages, k_scale, v_scale, L: int, K_out=None, V_out=None, stream=None):
         """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end.  What is not given is allocated on the call's
-        stream."""
-        batch = kv_len.shape[0]
+        stream.  Without k_pages and k_scale, or without v_pages and v_scale (None), only the other one is read back."""
+        batch, need = kv_len.shape[0], self._need
         shape = (batch, self.n_kv_heads, L, self.head_dim)
-        if K_out is None:
-            K_out = self._empty(shape, self.torch_dtype, stream)
-        if V_out is None:
-            V_out = self._empty(shape, self.torch_dtype, stream)
-        need = self._need
         kv = need("kv_len", kv_len, torch.int32, (batch,))
         tb = need("table", table, torch.int32, (batch, self.max_pages))
-        self._check(self._lib.faedkv_pages_load(
-            self._h, kv, tb, batch, L, *self._cache(k_pages, v_pages, k_scale, v_scale), need("K_out", K_out, self._dtype, shape),
-            need("V_out", V_out, self._dtype, shape), self._on(stream)))
-        return K_out, V_out
+        out, ptrs = [], []
+        for which, codes, scale, rows in (("k", k_pages, k_scale, K_out), ("v", v_pages, v_scale, V_out)):
+            if codes is None and scale is None and rows is None:
+                out.append(None)
+                ptrs.append((None, None, None))
+                continue
+            if codes is None or scale is None:
+                raise ValueError(f"{which}_pages and {which}_scale go together" + ("" if rows is None else f", and with {which.upper()}_out"))
+            c = need(which + "_pages", codes, torch.float8_e4m3fn, self._code_shape)
+            s = need(which + "_scale", scale, torch.float32, self._scale_shape)
+            if rows is None:
+                rows = self._empty(shape, self.torch_dtype, stream)
+            out.append(rows)
+            ptrs.append((c, s, need(which.upper() + "_out", rows, self._dtype, shape)))
+        (kc, ks, ko), (vc, vs, vo) = ptrs
+        if kc is None and vc is None:
+            raise ValueError("neither K nor V to read back")
+        self._check(self._lib.faedkv_pages_load(self._h, kv, tb, batch, L, kc, vc, ks, vs, ko, vo, self._on(stream)))
+        return tuple(out)
 
     def launch_count(self) -> int:
         return int(self._lib.faedkv_pages_launch_count(self._h))
