@@ -429,9 +429,13 @@ size_t faedkv_pages_bytes(const faedkv_pages *pg);
  *                       = t_len[b] and the slots of its tokens are -1.  It does not fit when its tokens exceed the table
  *                       row or n_tokens, or when the stack does not hold its pages and those of the requests before
  *                       it; in the last case every later request that needs a page waits too.
- * q_start[b] counts the tokens before request b (finished ones count none), slots[i] = page * page_size + row of token
- * i < n_tokens, -1 where it has none.  *n_free_out is the new height of the stack.  ws: faedkv_pages_tables_bytes(),
- * overwritten, 4-byte aligned (NULL where that is 0).  kv_len may be t_len itself, n_free_out may be n_free. */
+ * q_start[b] counts the tokens before request b (finished ones count none; those that do not fit count too), slots[i] =
+ * page * page_size + row of token i < n_tokens, -1 where it has none.  A request does not fit exactly where it has new tokens and
+ * kv_len[b] is still t_len[b].  faedkv_pages_store() skips its tokens.  faedkv_pages_attn() does not know of it: the rows of its
+ * tokens are then those of as many of its OLDER tokens (or left as they were, with status 0x105, where q_start passes n_tokens),
+ * and the caller drops them; every other request's rows are right.  *n_free_out is the new height of the stack.  ws:
+ * faedkv_pages_tables_bytes(), overwritten, 4-byte aligned (NULL where that is 0).  kv_len may be t_len itself, n_free_out may be
+ * n_free. */
 size_t faedkv_pages_tables_bytes(const faedkv_pages *pg, int batch, int n_tokens);
 int faedkv_pages_tables(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, int32_t *table,
                         int32_t *free_pages, const int32_t *n_free, int n_tokens, int32_t *q_start, int32_t *kv_len,
@@ -454,7 +458,8 @@ size_t faedkv_pages_attn_bytes(const faedkv_pages *pg, int batch, int n_tokens);
 /* Attention of the newest tokens over the cache:
  *   out[i] = softmax_n( scale * q[i] . K[n] ) V[n],   n < kv_len[b] - n_new + (i - q_start[b]) + 1
  * for the n_new = q_start[b + 1] - q_start[b] newest tokens of every sequence b: causal among themselves, and each sees
- * itself (store first).  q_start = NULL: one token per sequence, n_tokens = batch (a decode step).  q: token rows ld_q
+ * itself (store first).  q_start = NULL: row b is the one new token of sequence b, n_tokens = batch (a decode step of them all; where some
+ * wait, pass q_start, since faedkv_pages_tables packs the tokens).  q: token rows ld_q
  * elements apart (as ld_new), [n_q_heads][head_dim] each; out: contiguous [n_tokens][n_q_heads][head_dim]; both kv_dtype.
  * scale = 0 means 1/sqrt(head_dim).  A token that sees nothing (kv_len[b] = 0) gets a row of zeros.  Scales need not be
  * powers of two.  ws: faedkv_pages_attn_bytes(), overwritten; calls that overlap need one each.
