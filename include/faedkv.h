@@ -382,7 +382,7 @@ int faedkv_decode_attn_static(int n_dft, int n_kv_heads, int n_q_heads, int kv_d
  *   k_pages, v_pages  e4m3 codes [n_pages][n_kv_heads][page_size][head_dim]
  *   k_scale, v_scale  float32 [n_pages][n_kv_heads];  value = code * scale
  *   table             int32 [batch][max_pages]: the pages of each sequence in order; entries behind its last page are
- *                     not read
+ *                     not used
  *   kv_len            int32 [batch], cached tokens of each sequence
  * The pages, scales, tables and lengths are the caller's; the handle holds the configuration and one status word.
  * New tokens of a step lie one sequence after the other in token tensors [n_tokens][heads][head_dim]; sequence b owns

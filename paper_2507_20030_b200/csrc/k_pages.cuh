@@ -285,7 +285,7 @@ template <> struct Raw8<float> {
 };
 
 // Threads of a store CTA: few, since finding a run costs each warp about as much as 16 KB of its rows, but no more than 32
-// registers of rows a thread.
+// registers of rows a thread (64 for pages of 128 float32 rows).
 template <typename T, int PAGE> constexpr int kStoreThreads = PAGE * sizeof(T) <= 128 ? 128 : 256;
 
 struct StoreArgs {
