@@ -485,6 +485,13 @@ int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *ta
 int faedkv_pages_device_status(faedkv_pages *pg, void *stream);
 int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream);
 
+/* Test and diagnostics hooks of the paged attention, as faedkv_test_hooks() (host state of the handle; they apply to the calls that
+ * follow).  wait_limit_ns: time limit of each of its bounded waits (0 = about one second).  withhold_tile: 0 = off; t >= 1 = at the
+ * t-th tile of every CTA one warp keeps back the signal that the tile's weights are there, so that the CTA's waits run out: the
+ * kernel leaves a code in the status word (0x41 .. 0x43), waits for its own copies, frees its tensor memory and returns.  The
+ * output of such a call is invalid. */
+int faedkv_pages_test_hooks(faedkv_pages *pg, unsigned long long wait_limit_ns, int withhold_tile);
+
 /* Kernels enqueued through this handle so far. */
 unsigned long long faedkv_pages_launch_count(const faedkv_pages *pg);
 

@@ -21,6 +21,8 @@ struct faedkv_pages {
     unsigned int attr_set = 0;                 // attention instances already opted in to large shared memory
     void *encode = nullptr;                    // cuTensorMapEncodeTiled
     unsigned long long launches = 0;
+    unsigned long long wait_limit_ns = umma::kWaitLimitNs;   // faedkv_pages_test_hooks
+    int withhold_tile = 0;
     char err[512] = {0};
 };
 
@@ -360,7 +362,7 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
                             c.max_pages, c.n_pages, pg->page_shift, p.blocks,
                             65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
-                            static_cast<unsigned char *>(ws), pg->dev_status};
+                            static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
     if (c.kv_dtype == FAEDKV_F32)
         return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st)
                : p.shared         ? launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st)
@@ -413,6 +415,13 @@ int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream) {
     const DeviceGuard guard(pg);
     if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
     CUDA_TRY(pg, cudaMemsetAsync(pg->dev_status, 0, sizeof(unsigned int), static_cast<cudaStream_t>(stream)));
+    return FAEDKV_OK;
+}
+
+int faedkv_pages_test_hooks(faedkv_pages *pg, unsigned long long wait_limit_ns, int withhold_tile) {
+    if (pg == nullptr || withhold_tile < 0) return FAEDKV_ERR_INVALID_ARG;
+    pg->wait_limit_ns = wait_limit_ns == 0 ? umma::kWaitLimitNs : wait_limit_ns;
+    pg->withhold_tile = withhold_tile;
     return FAEDKV_OK;
 }
 

@@ -98,6 +98,8 @@ struct AttnArgs {
     float scale_log2;                                     // scale * log2(e)
     unsigned char *ws;
     unsigned int *status;
+    unsigned long long wait_limit;                        // ns, of a bounded wait
+    int withhold;                                         // test hook: the tile (from 1) whose weights are not announced; 0: none
 };
 
 // Workspace of MODE 0 and 1: header, records, two partial results per CTA (of the unit it goes on with, of the one it leaves).
@@ -528,7 +530,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     bool dead = false;                                    // a bounded wait gave up: no further waits, run out
     auto wait = [&](uint32_t bar, uint32_t parity, unsigned int code) {
         if (dead || mbar_try_wait(bar, parity)) return;
-        if (*abort_flag || !mbar_wait(bar, parity)) {
+        if (*abort_flag || !mbar_wait(bar, parity, a.wait_limit)) {
             if (!*abort_flag) atomicExch(a.status, code);
             *abort_flag = 1;
             dead = true;
@@ -613,8 +615,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
         }
         if (dead) {                                        // leave no copy in flight behind
-            for (int i = max(0, issued_k - KST); i < issued_k; ++i) mbar_wait(kfull(i % KST), (uint32_t)(i / KST) & 1u);
-            for (int i = max(0, issued_v - VST); i < issued_v; ++i) mbar_wait(vfull(i % VST), (uint32_t)(i / VST) & 1u);
+            for (int i = max(0, issued_k - KST); i < issued_k; ++i) mbar_wait(kfull(i % KST), (uint32_t)(i / KST) & 1u, a.wait_limit);
+            for (int i = max(0, issued_v - VST); i < issued_v; ++i) mbar_wait(vfull(i % VST), (uint32_t)(i / VST) & 1u, a.wait_limit);
         }
     } else if (warp == kWarpMma) {
         // ------------------------------------------------------------------------ MMA issuer
@@ -625,6 +627,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             Work<MODE> w = w0;
             Segment s;
             int it = 0;                                    // tiles whose S has been issued
+            int last_s = -1, last_o = -1;                  // the last products that were
             uint32_t seg = 0;
             auto scores = [&]() {
                 const int st = it % KST;
@@ -639,6 +642,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                    desc_kmajor_sw128(q_base + term * QC * 128 + k * 32), term ? kIdescS1 : kIdescS, (term | k) ? 1u : 0u);
                     mma_commit(sfull(it & 1));
                     if (C::WIDE) mma_commit(kempty(st));
+                    last_s = it;
                 }
                 ++it;
             };
@@ -661,6 +665,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         mma_commit(kempty(i % KST));
                     }
                     mma_commit(pdone(pb));
+                    last_o = i;
                 }
             };
             while (w.next(a, QC, s)) {
@@ -673,6 +678,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     output(i, t == s.t0);
                 }
             }
+            // no product may be on its way when the tensor memory is given back (it never is, unless the softmax warps gave up)
+            if (last_s >= 0) mbar_wait(sfull(last_s & 1), (uint32_t)(last_s >> 1) & 1u, a.wait_limit);
+            if (last_o >= 0) mbar_wait(pdone(last_o & 1), (uint32_t)(last_o >> 1) & 1u, a.wait_limit);
         }
     } else {
         // ------------------------------------------------------------------------ softmax
@@ -1066,7 +1074,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(pfull(pb));
+                    if (warp != 0 || it + 1 != a.withhold) mbar_arrive(pfull(pb));
                     if (C::WIDE) mbar_arrive(vempty(sv));
                 }
             }
