@@ -492,6 +492,9 @@ int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream);
  * output of such a call is invalid. */
 int faedkv_pages_test_hooks(faedkv_pages *pg, unsigned long long wait_limit_ns, int withhold_tile);
 
+/* faedkv_debug_word() for the kernels of the paged cache. */
+long long faedkv_pages_debug_word(faedkv_pages *pg, void *stream);
+
 /* Kernels enqueued through this handle so far. */
 unsigned long long faedkv_pages_launch_count(const faedkv_pages *pg);
 

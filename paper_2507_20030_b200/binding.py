@@ -36,7 +36,7 @@ EXPORTS = [
     "faedkv_reset_device_status", "faedkv_test_hooks", "faedkv_debug_build", "faedkv_debug_word",
     "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables_bytes", "faedkv_pages_tables",
     "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
-    "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks",
+    "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_debug_word",
 ]
 
 STATIC_SCRATCH_BYTES = 8 << 20
@@ -163,6 +163,8 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_reset_device_status.restype = _int
     lib.faedkv_pages_test_hooks.argtypes = [_vp, ctypes.c_ulonglong, _int]
     lib.faedkv_pages_test_hooks.restype = _int
+    lib.faedkv_pages_debug_word.argtypes = [_vp, _vp]
+    lib.faedkv_pages_debug_word.restype = _ll
     lib.faedkv_pages_launch_count.argtypes = [_vp]
     lib.faedkv_pages_launch_count.restype = ctypes.c_ulonglong
     _lib = lib
@@ -621,3 +623,6 @@ class Pages:
     def test_hooks(self, wait_limit_ns: int = 0, withhold_tile: int = 0):
         """faedkv_pages_test_hooks: wait limit of the attention's bounded waits and the withheld-signal test."""
         self._check(self._lib.faedkv_pages_test_hooks(self._h, int(wait_limit_ns), int(withhold_tile)))
+
+    def debug_word(self, stream=None) -> int:
+        return int(self._lib.faedkv_pages_debug_word(self._h, self._on(stream)))

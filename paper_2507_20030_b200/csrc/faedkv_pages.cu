@@ -425,6 +425,23 @@ int faedkv_pages_test_hooks(faedkv_pages *pg, unsigned long long wait_limit_ns, 
     return FAEDKV_OK;
 }
 
+long long faedkv_pages_debug_word(faedkv_pages *pg, void *stream) {
+    if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
+#ifdef FAEDKV_DEBUG
+    const DeviceGuard guard(pg);
+    if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
+    unsigned int w = 0, zero = 0;
+    CUDA_TRY(pg, cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
+    CUDA_TRY(pg, cudaMemcpyFromSymbol(&w, g_faedkv_debug_word, sizeof(w)));
+    CUDA_TRY(pg, cudaMemcpyToSymbol(g_faedkv_debug_word, &zero, sizeof(zero)));
+    if (w != 0) fail(pg, FAEDKV_ERR_INVALID_ARG, "bounds check failed: file tag %u, line %u", w >> 16, w & 0xffffu);
+    return (long long)w;
+#else
+    (void)stream;
+    return 0;
+#endif
+}
+
 unsigned long long faedkv_pages_launch_count(const faedkv_pages *pg) { return pg ? pg->launches : 0ULL; }
 
 }  // extern "C"

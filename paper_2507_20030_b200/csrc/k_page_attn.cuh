@@ -549,7 +549,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             auto fetch = [&](int t_first, int &id, float &ks, float &vs) {
                 const long long p = ((long long)t_first << lg_ppt) + lane;
                 id = -1; ks = 0.f; vs = 0.f;
-                if ((p << a.page_shift) < s.live && t_first + (lane >> lg_ppt) < s.t1) {
+                if ((p << a.page_shift) < s.live && t_first + (lane >> lg_ppt) < s.t1 && FAEDKV_IN_BOUNDS(kTagPageAttn, p >= 0 && p < a.W && s.b >= 0 && s.b < a.B && s.h < a.H)) {
                     id = row[p];
                     if (id < 0 || id >= a.n_pages) {
                         flag(a.status, kBadPage);
@@ -703,7 +703,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const int c = warp + 4 * WGS * j, tok = c * a.inv_g >> 16;
-                q_in[j] = c < n_cols ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
+                q_in[j] = c < n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 >= 0 && s.tok0 + tok < a.n_tokens) ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
             uint32_t top[kEach];                           // the columns' largest finite magnitudes
 #pragma unroll
@@ -1123,7 +1123,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             T *out_row = static_cast<T *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
             float *part_row = whole ? nullptr : slot + 2 * QC + row;
             auto put = [&](int c, float v) {
-                if (c >= n_cols) return;
+                if (c >= n_cols || !FAEDKV_IN_BOUNDS(kTagPageAttn, !whole || s.tok0 + (int)(c * a.inv_g >> 16) < a.n_tokens)) return;
                 const float f = col_f[c];
                 v = f == 0.f ? 0.f : v * f * v_ref;        // no token: zero
                 if (MODE != 0 && poison != 0 && ((poison >> (c - c_wg)) & 1ull)) v = __uint_as_float(0x7fffffffu);
@@ -1190,10 +1190,12 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
     const int cta0 = cta_of(first), cta1 = cta_of(first + tiles - 1);
     if (MODE == 0 ? cta0 == cta1 : cta0 + 1 != (int)blockIdx.x) return;       // one CTA had it all; another one's join
     const int n = cta1 - cta0 + 1;
+    if (!FAEDKV_IN_BOUNDS(kTagPageAttn, cta0 >= 0 && cta1 < ctas)) return;
     const float *slots = reinterpret_cast<const float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, ctas));
     auto slot = [&](int i) { return slots + (size_t)(2 * (cta0 + i) + (i == 0 ? 1 : 0)) * attn_slot_floats(qc); };
     auto store = [&](int c, float o) {
         const int tok = c / a.G;
+        if (!FAEDKV_IN_BOUNDS(kTagPageAttn, tok0 >= 0 && tok0 + tok < a.n_tokens && h >= 0 && h < a.H)) return;
         store1(static_cast<T *>(a.out) + (((size_t)(tok0 + tok) * a.H + h) * a.G + (c - tok * a.G)) * kHeadDim + d, o);
     };
     const int c_end = min((int)(blockIdx.y + 1) * each, n_cols);

@@ -72,10 +72,11 @@ __device__ __forceinline__ void place_token(const TablesArgs &a, int i, const in
             const int first = start[b], n = start[b + 1] - first;
             const int t = a.kv_len[b] - n, pos = t + (i - first);
             const int p = pos >> a.page_shift, old = (t + (1 << a.page_shift) - 1) >> a.page_shift;
-            int id;
-            if (p < old) {
+            int id = -1;
+            if (!FAEDKV_IN_BOUNDS(kTagPages, b < a.B && p >= 0 && p < a.W)) {
+            } else if (p < old) {
                 id = a.table[(size_t)b * a.W + p];
-            } else {
+            } else if (FAEDKV_IN_BOUNDS(kTagPages, page0 + p - old < base[a.B] && base[a.B] <= a.n_pages)) {
                 id = a.free_pages[base[a.B] - 1 - (page0 + p - old)];
                 if ((pos & ((1 << a.page_shift) - 1)) == 0) a.table[(size_t)b * a.W + p] = id;
             }
@@ -372,6 +373,7 @@ __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 12
                 else raw[k].zero();
             }
         }
+        if (!FAEDKV_IN_BOUNDS(kTagPages, pg >= 0 && pg < a.n_pages && n >= 1 && r0 + n <= PAGE && at + n <= n_rest)) continue;
         const size_t ph = (size_t)pg * a.H + h;
         const float s_old = r0 > 0 ? scales[ph] : 0.f;
 #pragma unroll
@@ -500,7 +502,7 @@ __global__ void __launch_bounds__(256) k_page_load(const LoadArgs a) {
     const size_t ph = (size_t)(id < 0 ? 0 : id) * a.H + h;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        if (a.out[t] == nullptr) continue;
+        if (a.out[t] == nullptr || !FAEDKV_IN_BOUNDS(kTagPages, n_in <= n_out && n0 + n_out <= a.L && ph < (size_t)a.n_pages * a.H)) continue;
         const float s = n_in > 0 ? a.scale[t][ph] : 0.f;
         const uint8_t *src = a.codes[t] + (ph << a.page_shift) * kHeadDim + el;
         T *dst = static_cast<T *>(a.out[t]) + (((size_t)b * a.H + h) * a.L + n0) * kHeadDim + el;
