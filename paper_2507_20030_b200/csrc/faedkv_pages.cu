@@ -163,7 +163,11 @@ AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
     const faedkv_pages_config &c = pg->cfg;
     AttnPlan p{};
     p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
-    // more query columns per sequence than 8: a block of 128 columns reads the cache once for all of them
+    // more than 8 query columns a sequence on average: blocks of 128 columns, which read the cache once for all of theirs.  The host
+    // does not know how the tokens lie: where every sequence has as many, blocks of 8 stay ahead to 16 columns or 24 (16 x 16384
+    // tokens, 8 kv heads: 115 us in 8s and 244 in 128s at 8 columns, 185 and 246 at 16, 266 and 247 at 24), but one long chunk
+    // among decoding requests would go over its cache once for every 8 of them (120 tokens over 65536 beside 63 requests of 1000, 11
+    // columns on average: 803 and 343 us; 320 tokens, 24 on average: 1973 and 650), so the rule leans to the side that loses less
     p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / pg->gq) + batch;

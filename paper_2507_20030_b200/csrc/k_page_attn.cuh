@@ -26,10 +26,11 @@
 // with it l, stays within 2^20 of the weights, in float32's reach (pages of zeros have the smallest scale, and their tokens
 // count in l all the same).  O stays in TMEM over all tiles of a segment.
 //
-// Measured: a decode step over 16 x 16384 tokens of 8 kv heads 90 us (6.0 TB/s of codes), over 131072 tokens 53.5 us (39 us of
-// it in the tiles); 2048 new tokens over 18432 969 us (603 TFLOP/s), bound by the softmax warps; float32, six
-// ragged sequences up to 4096 tokens 16.4 us.  128 columns over four warpgroups were faster than over two or 96 over three (879,
-// 992 and 961 us with e4m3 weights), eight columns at a time than sixteen (931, 952).
+// Measured: a decode step over 16 x 16384 tokens of 8 kv heads 89 us (6.0 TB/s of codes), over 131072 tokens 54 us (39 us of
+// it in the tiles); 2048 new tokens over 18432 962 us (608 TFLOP/s), bound by the softmax warps (an instruction issued in 53 %
+// of the cycles, tensor pipe 29 %); float32, six ragged sequences up to 4096 tokens 17.3 us.  128 columns over four warpgroups
+// were faster than over two or 96 over three (879, 992 and 961 us with e4m3 weights), eight columns at a time than sixteen
+// (931, 952 with f16 weights and one scale for q).
 //
 // A CTA: one to four softmax warpgroups (thread = token row of S, channel row of O; a warpgroup has its share of the
 // columns), a TMA warp, an MMA warp.

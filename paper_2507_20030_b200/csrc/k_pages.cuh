@@ -305,8 +305,8 @@ struct StoreArgs {
 // It reads a run once into registers, takes the largest finite magnitude, settles the page's scale, re-rounds the page's
 // older rows if the scale grew, and writes the new codes: the data is read once and written once.  What it takes is a chain
 // of dependent loads (slots, rows) and one barrier, so every warp finds the runs by itself and registers are kept few, for
-// CTAs enough to cover it.  Measured: 32768 tokens x 8 heads, bf16, 33.7 us (6.0 TB/s; with half the rows a thread 40.3 us, bound
-// by instructions), 2.6 us for 16 tokens.
+// CTAs enough to cover it.  Measured: 32768 tokens x 8 heads, bf16, 34.1 us (5.9 TB/s; with half the rows a thread 40.3 us, bound
+// by instructions), 2.5 us for 16 tokens.
 template <typename T, int PAGE>
 __global__ void __launch_bounds__(kStoreThreads<T, PAGE>, PAGE * sizeof(T) <= 128 ? 8 : PAGE * sizeof(T) <= 256 ? 4 : 2) k_page_store(const StoreArgs a) {
     constexpr int kRows = kStoreThreads<T, PAGE> / 16, kIter = (PAGE + kRows - 1) / kRows, kWords = (PAGE + 31) / 32;
@@ -477,7 +477,7 @@ template <> struct RowPart<float> {
 };
 
 // Grid (pages of the longest row, H, sequences); a CTA turns one page of one head, K and V, into rows, four rows a thread in
-// flight: 62.5 us for 4 x 16384 tokens x 8 heads, bf16 (6.2 TB/s).  Rounding: to the tensor type, once (code * scale is exact in float32 for a power of two, else rounded there too).
+// flight: 62.9 us for 4 x 16384 tokens x 8 heads, bf16 (6.2 TB/s).  Rounding: to the tensor type, once (code * scale is exact in float32 for a power of two, else rounded there too).
 template <typename T>
 __global__ void __launch_bounds__(256) k_page_load(const LoadArgs a) {
     using Part = RowPart<T>;
