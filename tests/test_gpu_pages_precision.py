@@ -194,3 +194,37 @@ def test_a_page_of_loud_values_that_hardly_counts(fk, kind, at):
     seen = (n - m + 1 + torch.arange(m, device="cuda")) if new else torch.full((m,), n, device="cuda")
     # what the loud page adds is counted as an error of its own share, not as the scale of the others' floor
     check(kind, out[:m].reshape(-1, 128), q[:m].reshape(-1, 128), K[0], V[0], seen.repeat_interleave(G), floor_v=V[0, :page].abs().max())
+
+
+# ------------------------------------------------------------------------------------------------ shapes
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pow2", [True, False])
+@pytest.mark.parametrize("page,H,G,lens,new", [
+    (16, 2, 4, [127, 128, 129, 1], None), (128, 1, 7, [2500, 3], None), (32, 3, 1, [5000], None), (64, 1, 8, [640, 12000], None),
+    (16, 1, 3, [700, 129, 64], [43, 1, 64]), (64, 2, 5, [5000], [40]), (128, 1, 8, [900, 260], [100, 250]), (32, 1, 2, [2100, 31], [3, 1]),
+])
+def test_every_element_within_its_own_rounding(fk, dtype, pow2, page, H, G, lens, new):
+    """Random pages of different scales, ragged lengths, both widths: the bound of every element is its own."""
+    rng = np.random.default_rng(sum(lens) + page + pow2)
+    B, W = len(lens), max(ref.pages_of(n, page) for n in lens)
+    n_pages = sum(ref.pages_of(n, page) for n in lens) + 1
+    table = ref.spread(lens, page, n_pages, W, rng)
+    kc, ks = ref.random_cache(rng, n_pages, H, page, lens, table, pow2)
+    vc, vs = ref.random_cache(rng, n_pages, H, page, lens, table, pow2)
+    n_new = new or [1] * B
+    start = np.concatenate([[0], np.cumsum(n_new)])
+    q = torch.from_numpy(rng.standard_normal((int(start[-1]), H * G, 128))).to(dtype).cuda()
+    pg = fk.Pages(n_kv_heads=H, n_q_heads=H * G, page_size=page, n_pages=n_pages, max_pages=W, max_batch=B,
+                  kv_dtype=fk.BF16 if dtype == torch.bfloat16 else fk.F32)
+    out = torch.full_like(q, 7.0)
+    pg.attn(q, ref.ints(lens), ref.ints(table), ref.cuda8(kc), ref.cuda8(vc), ref.cuda32(ks), ref.cuda32(vs), out,
+            q_start=None if new is None else ref.ints(start))
+    assert pg.device_status() == 0
+    kind = "f32" if dtype == torch.float32 else "wide" if new and int(start[-1]) * G > 8 * B else "bf16"
+    for b, (n, m) in enumerate(zip(lens, n_new)):
+        K, V = [torch.from_numpy(ref.rows_of(c, s, table[b], n, page)).cuda() for c, s in ((kc, ks), (vc, vs))]
+        seen = (n - m + 1 + torch.arange(m, device="cuda")).repeat_interleave(G)
+        for h in range(H):
+            at = (slice(int(start[b]), int(start[b + 1])), slice(h * G, (h + 1) * G))
+            check(kind, out[at].reshape(-1, 128), q[at].reshape(-1, 128), K[h], V[h], seen)
