@@ -14,8 +14,9 @@ masks keeping 1/8 of the bins):
 
 Beside the timed step the line carries: `prefill_fft` (the same prefill through prefill_mode = FFT, the
 paper's own O(N log N) route, for comparison with the tensor-core contraction that `value` measures) and
-`decode.configs` (decode us / layer / step at the configs[2] and configs[3] shapes, whose state comes
-from a real prefill).
+`decode_summary` (decode us / layer / step at the configs[2] and configs[3] shapes, whose state comes
+from a real prefill).  The sections behind it (`decode.configs`, `sweep`) go to stderr as a record of their own:
+with them the line is longer than what is kept of a program's output.
 
 Inputs are resident in HBM before the timed region; every layer's tensors are distinct and the layers
 are cycled (4 GiB of K/V, 2 GiB of coefficients), so nothing survives in the 126 MB L2 between uses.
@@ -49,6 +50,16 @@ UNIT = "tokens/s"
 WORKLOAD = dict(name="configs[1]: Llama-3-8B-shaped full cache, prefill 32768 tokens at 1/8 bin retention",
                 config=1, n_layers=32, n_kv_heads=8, n_q_heads=32, head_dim=128, batch=1, T=32768,
                 M=4096, mask="mixed")
+
+
+def split_details(line):
+    """The line without its long sections, and those."""
+    short = {k: v for k, v in line.items() if k != "sweep"}
+    details = {"sweep": line.get("sweep")}
+    if "decode" in short:
+        details["decode"] = {"configs": short["decode"].get("configs")}
+        short["decode"] = {k: v for k, v in short["decode"].items() if k != "configs"}
+    return short, details
 
 
 def workload_config(W, prefill_path, twiddle_terms):
@@ -942,6 +953,9 @@ def run_ours(args):
         summary["cfg0"] = {"prefill_us": round(config0["prefill_us"], 1), "append_us": round(config0["append_us_per_step"], 2),
                            "recon_us": round(config0["reconstruct_us"], 1)}
     line["decode_summary"] = summary
+    line, details = split_details(line)
+    print(json.dumps({"bench_details": details}), file=sys.stderr)
+    sys.stderr.flush()
     print(json.dumps(line))
     if world > 1:
         dist.destroy_process_group()
