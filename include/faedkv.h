@@ -480,8 +480,50 @@ int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *ta
                       const void *v_pages, const float *k_scale, const float *v_scale, void *K_out, void *V_out,
                       void *stream);
 
+/* ---- pages that several requests share ----
+ * A page may stand in the rows of several requests: answers to one prompt, beams of a search, requests behind one common text.  The
+ * block tables are the only record of it: a page is in use exactly while a row names it among its first
+ * ceil(kv_len / page_size) entries.  Only whole pages are shared, so faedkv_pages_store() never writes to one, as long as a
+ * request's length does not go back (other than to 0 through faedkv_pages_release()).  Where pages are shared, requests finish
+ * through faedkv_pages_release(); faedkv_pages_tables() would push a shared page once for each of them.  After it the same n_new may
+ * go to faedkv_pages_tables(), which finds nothing left to push for requests of length 0.
+ * These calls take batch * max_pages < 2^31. */
+
+/* New requests begin as copies of others.  For i < n_forks (n_forks <= batch) row dst[i] becomes the first
+ * n = min(len[i], kv_len[src[i]]) tokens of row src[i] (len = NULL: all of them): its n / page_size whole pages are shared; the
+ * n % page_size rows behind them, K and V, are copied with their scales to a page from the top of the stack; kv_len[dst[i]] = n.
+ * Forks are served in the order of the call.  One that needs a page and finds none gets nothing: kv_len[dst[i]] = 0.  Whatever
+ * row dst[i] held is forgotten, not given back.  src[i] < 0: nothing is done.  A row outside the batch, a dst that is also a src
+ * of the call, and a dst that an earlier fork names are refused (nothing is done, status 0x106).  Pages that are not dst's fresh one are
+ * only read; table entries behind a row's last page are left as they were.  *n_free_out is the new height of the stack; it may be
+ * n_free.  ws: faedkv_pages_fork_bytes() (0 for arguments that the call would refuse), overwritten, 4-byte aligned. */
+size_t faedkv_pages_fork_bytes(const faedkv_pages *pg, int batch, int n_forks);
+int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, const int32_t *len, int n_forks, int batch,
+                      int32_t *kv_len, int32_t *table, const int32_t *free_pages, const int32_t *n_free, int32_t *n_free_out,
+                      void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *ws, void *stream);
+
+/* Finished requests (n_new[b] < 0, as for faedkv_pages_tables()) give back their pages: those that no running request names are
+ * pushed on the stack, each once, in the order of the first finished row that names it and of the pages in that row.  kv_len[b] = 0
+ * for them, t_len[b] for the others; *n_free_out is the new height.  kv_len may be t_len, n_free_out may be n_free.
+ * ws: faedkv_pages_release_bytes(), overwritten, 4-byte aligned. */
+size_t faedkv_pages_release_bytes(const faedkv_pages *pg);
+int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, const int32_t *table,
+                         int32_t *free_pages, const int32_t *n_free, int32_t *kv_len, int32_t *n_free_out, void *ws, void *stream);
+
+/* Move the pages in use to the front of the pool, so that its end can be handed to something else (coefficient planes, a smaller
+ * pool).  With n pages in use, the k-th page in use from n on moves, codes and scales, to the k-th page below n that is not; the
+ * others stay.  new_id[p] (int32 [n_pages]) is the new number of page p, -1 where no row names it; table_out is the table with
+ * new numbers (entries that name no page of their row are copied; it may be table); the stack becomes the n_pages - n pages that are
+ * left, the lowest on top, *n_free its height.  A page that no row names is free afterwards: what is to be kept needs a row.  Pages from
+ * n on keep their bytes, so a call with table_out apart from table can be repeated.  ws: faedkv_pages_compact_bytes(), overwritten,
+ * 4-byte aligned. */
+size_t faedkv_pages_compact_bytes(const faedkv_pages *pg);
+int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, const int32_t *table, int32_t *table_out,
+                         int32_t *free_pages, int32_t *n_free, int32_t *new_id, void *k_pages, void *v_pages, float *k_scale,
+                         float *v_scale, void *ws, void *stream);
+
 /* Status word (host read; synchronises `stream`): 0, or the code of the first index that was not followed (0x101 a page,
- * 0x102 a slot, 0x103 a length, 0x104 the free stack, 0x105 a start) or of a bounded wait that gave up (0x4x). */
+ * 0x102 a slot, 0x103 a length, 0x104 the free stack, 0x105 a start, 0x106 a row) or of a bounded wait that gave up (0x4x). */
 int faedkv_pages_device_status(faedkv_pages *pg, void *stream);
 int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream);
 

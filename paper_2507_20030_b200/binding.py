@@ -35,7 +35,8 @@ EXPORTS = [
     "faedkv_device_status", "faedkv_launch_count", "faedkv_decode_attn_static",
     "faedkv_reset_device_status", "faedkv_test_hooks", "faedkv_debug_build", "faedkv_debug_word",
     "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables_bytes", "faedkv_pages_tables",
-    "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
+    "faedkv_pages_fork_bytes", "faedkv_pages_fork", "faedkv_pages_release_bytes", "faedkv_pages_release", "faedkv_pages_compact_bytes",
+    "faedkv_pages_compact", "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
     "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_debug_word",
 ]
 
@@ -157,6 +158,18 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_attn.restype = _int
     lib.faedkv_pages_load.argtypes = [_vp, _vp, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.faedkv_pages_load.restype = _int
+    lib.faedkv_pages_fork_bytes.argtypes = [_vp, _int, _int]
+    lib.faedkv_pages_fork_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_fork.argtypes = [_vp, _vp, _vp, _vp, _int, _int, *[_vp] * 11]
+    lib.faedkv_pages_fork.restype = _int
+    lib.faedkv_pages_release_bytes.argtypes = [_vp]
+    lib.faedkv_pages_release_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_release.argtypes = [_vp, _vp, _vp, _int, *[_vp] * 7]
+    lib.faedkv_pages_release.restype = _int
+    lib.faedkv_pages_compact_bytes.argtypes = [_vp]
+    lib.faedkv_pages_compact_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_compact.argtypes = [_vp, _vp, _int, *[_vp] * 11]
+    lib.faedkv_pages_compact.restype = _int
     lib.faedkv_pages_device_status.argtypes = [_vp, _vp]
     lib.faedkv_pages_device_status.restype = _int
     lib.faedkv_pages_reset_device_status.argtypes = [_vp, _vp]
@@ -610,6 +623,37 @@ class Pages:
             raise ValueError("neither K nor V to read back")
         self._check(self._lib.faedkv_pages_load(self._h, kv, tb, batch, L, kc, vc, ks, vs, ko, vo, self._on(stream)))
         return tuple(out)
+
+    # -- pages that several requests share
+    def fork(self, src, dst, kv_len, table, free_pages, n_free, n_free_out, k_pages, v_pages, k_scale, v_scale, length=None, ws=None,
+             stream=None):
+        """Rows dst begin as copies of the first `length` tokens (all of them without it) of rows src; kv_len and table in place."""
+        n, batch, i32, need = src.numel(), kv_len.shape[0], torch.int32, self._need
+        args = (need("src", src, i32, (n,)), need("dst", dst, i32, (n,)), None if length is None else need("length", length, i32, (n,)), n, batch,
+                need("kv_len", kv_len, i32, (batch,)), need("table", table, i32, (batch, self.max_pages)),
+                need("free_pages", free_pages, i32, self._pool_shape), need("n_free", n_free, i32, (1,)),
+                need("n_free_out", n_free_out, i32, (1,)), *self._cache(k_pages, v_pages, k_scale, v_scale))
+        w = self._workspace(ws, 4 * (n + batch), stream)   # faedkv_pages_fork_bytes()
+        self._check(self._lib.faedkv_pages_fork(self._h, *args, w.data_ptr(), self._on(stream)))
+
+    def release(self, t_len, n_new, table, free_pages, n_free, kv_len, n_free_out, ws=None, stream=None):
+        """Requests with n_new < 0 give back the pages that no other request names."""
+        batch, i32, need = t_len.shape[0], torch.int32, self._need
+        args = (need("t_len", t_len, i32, (batch,)), need("n_new", n_new, i32, (batch,)), batch,
+                need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, self._pool_shape),
+                need("n_free", n_free, i32, (1,)), need("kv_len", kv_len, i32, (batch,)), need("n_free_out", n_free_out, i32, (1,)))
+        w = self._workspace(ws, self._lib.faedkv_pages_release_bytes(self._h), stream)
+        self._check(self._lib.faedkv_pages_release(self._h, *args, w.data_ptr(), self._on(stream)))
+
+    def compact(self, kv_len, table, table_out, free_pages, n_free, new_id, k_pages, v_pages, k_scale, v_scale, ws=None, stream=None):
+        """The pages in use to the front of the pool; free_pages, n_free and new_id are written, table_out may be table."""
+        batch, i32, need = kv_len.shape[0], torch.int32, self._need
+        rows = (batch, self.max_pages)
+        args = (need("kv_len", kv_len, i32, (batch,)), batch, need("table", table, i32, rows), need("table_out", table_out, i32, rows),
+                need("free_pages", free_pages, i32, self._pool_shape), need("n_free", n_free, i32, (1,)),
+                need("new_id", new_id, i32, self._pool_shape), *self._cache(k_pages, v_pages, k_scale, v_scale))
+        w = self._workspace(ws, self._lib.faedkv_pages_compact_bytes(self._h), stream)
+        self._check(self._lib.faedkv_pages_compact(self._h, *args, w.data_ptr(), self._on(stream)))
 
     def launch_count(self) -> int:
         return int(self._lib.faedkv_pages_launch_count(self._h))

@@ -27,7 +27,7 @@ __device__ __forceinline__ bool debug_in_bounds(bool ok, unsigned int where) {
 #endif
 // file tags of FAEDKV_IN_BOUNDS
 constexpr unsigned int kTagAppend = 1, kTagAttnFft = 2, kTagAttnCol = 3, kTagRecon2 = 4, kTagPrefillUmma = 5,
-                       kTagDftSimt = 6, kTagWindow = 7, kTagFftEngine = 8, kTagReconFft = 9, kTagPrefillFft = 10, kTagPages = 11, kTagPageAttn = 12;
+                       kTagDftSimt = 6, kTagWindow = 7, kTagFftEngine = 8, kTagReconFft = 9, kTagPrefillFft = 10, kTagPages = 11, kTagPageAttn = 12, kTagPageShare = 13;
 
 // (k * n) mod P with k, n < 2^31: the product fits 64 bits, so the reduced
 // phase index is exact however long the sequence is.

@@ -1,0 +1,103 @@
+// Host side of pages that several requests share: fork, release, compact.  See include/faedkv.h for the contract of every call.
+#include "pages_host.cuh"
+#include "k_page_share.cuh"
+
+namespace {
+
+// Rows and entries of a call's block table: places in it are counted in 32 bits.
+int check_table(faedkv_pages *pg, int batch) {
+    if (int r = check_batch(pg, batch)) return r;
+    if ((long long)batch * pg->cfg.max_pages >= (1LL << 31))
+        return fail(pg, FAEDKV_ERR_SHAPE, "batch %d * max_pages %d is 2^31 or more", batch, pg->cfg.max_pages);
+    return FAEDKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t faedkv_pages_fork_bytes(const faedkv_pages *pg, int batch, int n_forks) {
+    if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_forks < 0 || n_forks > batch) return 0;
+    return sizeof(int32_t) * ((size_t)n_forks + batch);
+}
+
+int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, const int32_t *len, int n_forks, int batch,
+                      int32_t *kv_len, int32_t *table, const int32_t *free_pages, const int32_t *n_free, int32_t *n_free_out,
+                      void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *ws, void *stream) {
+    const CallRange nvtx_range("faedkv_pages_fork");
+    if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
+    if (int r = check_table(pg, batch)) return r;
+    if (n_forks < 0 || n_forks > batch) return fail(pg, FAEDKV_ERR_SHAPE, "n_forks = %d outside [0, batch=%d]", n_forks, batch);
+    if (((src == nullptr || dst == nullptr) && n_forks > 0) || kv_len == nullptr || table == nullptr || free_pages == nullptr ||
+        n_free == nullptr || n_free_out == nullptr || k_pages == nullptr || v_pages == nullptr || k_scale == nullptr ||
+        v_scale == nullptr || ws == nullptr)
+        return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_fork");
+    if (int r = check_align(pg, {k_pages, v_pages, k_scale, v_scale}, {src, dst, len, kv_len, table, free_pages, n_free, n_free_out, ws})) return r;
+    const DeviceGuard guard(pg);
+    if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const faedkv_pages_config &c = pg->cfg;
+    const pages::ForkArgs a{src, dst, len, free_pages, n_free, kv_len, table, n_free_out, static_cast<int32_t *>(ws),
+                            {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
+                            n_forks, batch, c.max_pages, c.n_kv_heads, c.n_pages, pg->page_shift, pg->dev_status};
+    pages::k_page_fork_plan<<<1, pages::kPlanThreads, 0, st>>>(a);
+    if (int r = launch_check(pg, "k_page_fork_plan")) return r;
+    if (n_forks == 0) return FAEDKV_OK;
+    CUDA_TRY(pg, launch_pdl(pages::k_page_fork_copy, dim3(n_forks, 2 * c.n_kv_heads), dim3(256), 0, st, a));
+    return launch_check(pg, "k_page_fork_copy");
+}
+
+size_t faedkv_pages_release_bytes(const faedkv_pages *pg) {
+    return pg ? sizeof(int32_t) * ((size_t)pg->cfg.n_pages + pages::kCluster) : 0;
+}
+
+int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *n_new, int batch, const int32_t *table,
+                         int32_t *free_pages, const int32_t *n_free, int32_t *kv_len, int32_t *n_free_out, void *ws, void *stream) {
+    const CallRange nvtx_range("faedkv_pages_release");
+    if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
+    if (int r = check_table(pg, batch)) return r;
+    if (t_len == nullptr || n_new == nullptr || table == nullptr || free_pages == nullptr || n_free == nullptr || kv_len == nullptr ||
+        n_free_out == nullptr || ws == nullptr)
+        return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_release");
+    if (int r = check_align(pg, {}, {t_len, n_new, table, free_pages, n_free, kv_len, n_free_out, ws})) return r;
+    const DeviceGuard guard(pg);
+    if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
+    const pages::ReleaseArgs a{t_len, n_new, table, n_free, free_pages, kv_len, n_free_out, static_cast<int32_t *>(ws), batch,
+                               pg->cfg.max_pages, pg->cfg.n_pages, pg->page_shift, pg->dev_status};
+    int parts = 1;                                         // warps of a row, where there are fewer rows than warps
+    while (parts < 32 && 2 * parts * batch <= pages::kCluster * pages::kPlanThreads / 32) parts *= 2;
+    pages::k_page_release<<<pages::kCluster, pages::kPlanThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, parts);
+    return launch_check(pg, "k_page_release");
+}
+
+size_t faedkv_pages_compact_bytes(const faedkv_pages *pg) {
+    return pg ? sizeof(int32_t) * (pages::kCompactHead + 2 * (size_t)(pg->cfg.n_pages / 2)) : 0;
+}
+
+int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, const int32_t *table, int32_t *table_out,
+                         int32_t *free_pages, int32_t *n_free, int32_t *new_id, void *k_pages, void *v_pages, float *k_scale,
+                         float *v_scale, void *ws, void *stream) {
+    const CallRange nvtx_range("faedkv_pages_compact");
+    if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
+    if (int r = check_table(pg, batch)) return r;
+    if (kv_len == nullptr || table == nullptr || table_out == nullptr || free_pages == nullptr || n_free == nullptr ||
+        new_id == nullptr || k_pages == nullptr || v_pages == nullptr || k_scale == nullptr || v_scale == nullptr || ws == nullptr)
+        return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_compact");
+    if (int r = check_align(pg, {k_pages, v_pages, k_scale, v_scale}, {kv_len, table, table_out, free_pages, n_free, new_id, ws})) return r;
+    const DeviceGuard guard(pg);
+    if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const faedkv_pages_config &c = pg->cfg;
+    const pages::CompactArgs a{kv_len, table, table_out, free_pages, n_free, new_id, static_cast<int32_t *>(ws),
+                               {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
+                               batch, c.max_pages, c.n_kv_heads, c.n_pages, pg->page_shift, pg->dev_status};
+    pages::k_page_compact_plan<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a);
+    if (int r = launch_check(pg, "k_page_compact_plan")) return r;
+    CUDA_TRY(pg, launch_pdl(pages::k_page_move, dim3(pg->n_sm * 8), dim3(256), 0, st, a));
+    return launch_check(pg, "k_page_move");
+}
+
+}  // extern "C"
+
+// The checked build's word of this file's kernels (each translation unit has one).
+long long pages_share_debug_word(faedkv_pages *pg) { return debug_word_here(pg); }

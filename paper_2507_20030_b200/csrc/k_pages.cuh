@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const TablesArgs a) 
 
 // The slots of many tokens.  The search for a token's request is a chain of loads: in shared memory while it fits.
 constexpr int kSlotsBatch = 4096;
-__global__ void __launch_bounds__(256) k_page_slots(const TablesArgs a) {
+static __global__ void __launch_bounds__(256) k_page_slots(const TablesArgs a) {
     __shared__ int32_t start_s[kSlotsBatch + 1];
     pdl_wait();
     const bool fits = a.B <= kSlotsBatch;
