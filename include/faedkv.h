@@ -473,6 +473,21 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
                       const float *k_scale, const float *v_scale, float scale, void *out, void *ws, size_t ws_bytes,
                       void *stream);
 
+/* Differential attention of the newest tokens over the cache, for models whose heads subtract two softmax maps: a query row and a cached
+ * key are two halves of 64 channels, [q1 | q2] and [K1 | K2], and
+ *   out[i, g] = norm( softmax_n( scale * q1 . K1[n] ) V[n]  -  lam[g] * softmax_n( scale * q2 . K2[n] ) V[n] ),
+ * over the tokens that faedkv_pages_attn() would see.  lam: float32 [n_q_heads], the learned weight of the second map (a model computes it
+ * once from its vectors).  With gain (float32 [128], 16-byte aligned) norm(o) = o * gain / sqrt(mean(o^2) + eps) over the 128 channels;
+ * a constant factor of the model's goes into gain.  gain = NULL: norm(o) = o.  scale = 0 means 1/sqrt(64).  The handle has 1 to 4
+ * query heads per kv head (a head counts twice).  Everything else, the rounding of each map with it, as faedkv_pages_attn(); what
+ * cancels between the maps is lost of the difference.  A token that sees nothing gets zeros.
+ * ws: faedkv_pages_attn_diff_bytes() (0 for arguments that the call would refuse), 16-byte aligned, overwritten. */
+size_t faedkv_pages_attn_diff_bytes(const faedkv_pages *pg, int batch, int n_tokens);
+int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
+                           const int32_t *kv_len, const int32_t *table, const void *k_pages, const void *v_pages,
+                           const float *k_scale, const float *v_scale, float scale, const float *lam, const float *gain, float eps,
+                           void *out, void *ws, size_t ws_bytes, void *stream);
+
 /* The cached tokens as rows: K_out, V_out [batch][n_kv_heads][L][head_dim] (kv_dtype), zero from row kv_len[b] on, in the
  * layout that faedkv_compress_prefill() and faedkv_prefill_windowed() take.  A sequence longer than L is cut.  Either of
  * (k_pages, k_scale, K_out) or (v_pages, v_scale, V_out) may be all NULL. */

@@ -36,7 +36,8 @@ EXPORTS = [
     "faedkv_reset_device_status", "faedkv_test_hooks", "faedkv_debug_build", "faedkv_debug_word",
     "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables_bytes", "faedkv_pages_tables",
     "faedkv_pages_fork_bytes", "faedkv_pages_fork", "faedkv_pages_release_bytes", "faedkv_pages_release", "faedkv_pages_compact_bytes",
-    "faedkv_pages_compact", "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_load", "faedkv_pages_device_status",
+    "faedkv_pages_compact", "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_attn_diff_bytes", "faedkv_pages_attn_diff",
+    "faedkv_pages_load", "faedkv_pages_device_status",
     "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_debug_word",
 ]
 
@@ -156,6 +157,11 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_attn.argtypes = [_vp, _vp, _ll, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
                                       ctypes.c_size_t, _vp]
     lib.faedkv_pages_attn.restype = _int
+    lib.faedkv_pages_attn_diff_bytes.argtypes = [_vp, _int, _int]
+    lib.faedkv_pages_attn_diff_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_attn_diff.argtypes = [_vp, _vp, _ll, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
+                                           ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
+    lib.faedkv_pages_attn_diff.restype = _int
     lib.faedkv_pages_load.argtypes = [_vp, _vp, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.faedkv_pages_load.restype = _int
     lib.faedkv_pages_fork_bytes.argtypes = [_vp, _int, _int]
@@ -574,15 +580,23 @@ class Pages:
         self._check(self._lib.faedkv_pages_store(self._h, k, v, ld, s, n, *self._cache(k_pages, v_pages, k_scale, v_scale),
                                                  self._on(stream)))
 
-    def attn_bytes(self, batch: int, n_tokens: int) -> int:
-        """Workspace of attn(): a function of the handle's configuration and the two counts alone, so it is asked for once."""
-        key = (batch, n_tokens)
-        n = self._attn_bytes.get(key)
-        if n is None:
+    def _bytes(self, call, batch, n):
+        """A workspace's size, a function of the handle's configuration and two counts alone, so it is asked for once."""
+        key = (call, batch, n)
+        size = self._attn_bytes.get(key)
+        if size is None:
             if len(self._attn_bytes) > 4096:
                 self._attn_bytes.clear()
-            n = self._attn_bytes[key] = self._lib.faedkv_pages_attn_bytes(self._h, batch, n_tokens)
-        return n
+            size = self._attn_bytes[key] = getattr(self._lib, call)(self._h, batch, n)
+        return size
+
+    def attn_bytes(self, batch: int, n_tokens: int) -> int:
+        """Workspace of attn()."""
+        return self._bytes("faedkv_pages_attn_bytes", batch, n_tokens)
+
+    def attn_diff_bytes(self, batch: int, n_tokens: int) -> int:
+        """Workspace of attn_diff()."""
+        return self._bytes("faedkv_pages_attn_diff_bytes", batch, n_tokens)
 
     def attn(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, out, q_start=None, scale: float = 0.0, ws=None, stream=None):
         batch, i32, need = kv_len.shape[0], torch.int32, self._need
@@ -596,6 +610,24 @@ class Pages:
         w = self._workspace(ws, nbytes, stream)
         self._check(self._lib.faedkv_pages_attn(self._h, qp, ld, st, n, batch, kv, tb, *cache, scale, o, w.data_ptr(), nbytes,
                                                 self._on(stream)))
+
+    def attn_diff(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, lam, out, q_start=None, gain=None, eps: float = 0.0,
+                  scale: float = 0.0, ws=None, stream=None):
+        """Differential attention: softmax over the first 64 channels minus lam times softmax over the last 64, normalised where a gain
+        is given."""
+        batch, i32, f32, need = kv_len.shape[0], torch.int32, torch.float32, self._need
+        qp, n, ld = self._rows("q", q, self.n_q_heads)
+        o = need("out", out, self._dtype, (n, self.n_q_heads, self.head_dim))
+        st = None if q_start is None else need("q_start", q_start, i32, (batch + 1,))
+        kv = need("kv_len", kv_len, i32, (batch,))
+        tb = need("table", table, i32, (batch, self.max_pages))
+        lm = need("lam", lam, f32, (self.n_q_heads,))
+        gn = None if gain is None else need("gain", gain, f32, (self.head_dim,))
+        cache = self._cache(k_pages, v_pages, k_scale, v_scale)
+        nbytes = self.attn_diff_bytes(batch, n)
+        w = self._workspace(ws, nbytes, stream)
+        self._check(self._lib.faedkv_pages_attn_diff(self._h, qp, ld, st, n, batch, kv, tb, *cache, scale, lm, gn, eps, o, w.data_ptr(),
+                                                     nbytes, self._on(stream)))
 
     def load(self, kv_len, table, k_pages, v_pages, k_scale, v_scale, L: int, K_out=None, V_out=None, stream=None):
         """K, V rows [batch, n_kv_heads, L, head_dim], zero behind each sequence's end.  What is not given is allocated on the call's

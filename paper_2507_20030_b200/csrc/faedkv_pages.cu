@@ -1,7 +1,7 @@
 // Host side of the paged 8-bit cache: argument checks and launches.  See include/faedkv.h for the contract of every call.
 #include "pages_host.cuh"
 #include "k_pages.cuh"
-#include "k_page_attn.cuh"
+#include "pages_attn_host.cuh"
 
 namespace {
 
@@ -13,72 +13,6 @@ void launch_store(const pages::StoreArgs &a, int page, dim3 grid, cudaStream_t s
         case 64: pages::k_page_store<T, 64><<<grid, pages::kStoreThreads<T, 64>, 0, st>>>(a); break;
         default: pages::k_page_store<T, 128><<<grid, pages::kStoreThreads<T, 128>, 0, st>>>(a); break;
     }
-}
-
-//                                  type           columns, warpgroups, terms of q and w, wide, columns at a time, tiles of K and V, CTAs per SM
-using DecodeBf16 = pages::AttnCfg<__nv_bfloat16, 8, 1, 2, 4, false, 8, 3, 3, 2>;
-using DecodeF32 = pages::AttnCfg<float, 8, 1, 6, 8, false, 8, 2, 2, 2>;
-using ChunkBf16 = pages::AttnCfg<__nv_bfloat16, 128, 4, 2, 1, true, 8, 3, 2, 1>;
-constexpr int kDecodeCtas = DecodeBf16::CTAS;
-static_assert(kDecodeCtas == DecodeF32::CTAS && DecodeF32::QC == 8 && DecodeBf16::QC == 8, "one plan for both types");
-
-// How a call is cut up.
-struct AttnPlan {
-    bool wide;               // 128 columns a unit instead of 8
-    int qc, blocks;          // columns of a unit; blocks of new tokens, at most
-    bool shared;             // blocks few enough for their tiles to be shared out evenly (MODE 1); else a CTA each (MODE 2)
-    long long max_tiles;     // of a table row
-    int ctas0, ctas1;        // MODE 0 and 1
-    size_t bytes0, bytes1;   // workspace of MODE 0, of the others
-};
-
-AttnPlan plan_attn(const faedkv_pages *pg, int batch, int n_tokens) {
-    const faedkv_pages_config &c = pg->cfg;
-    AttnPlan p{};
-    p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
-    // more than 8 query columns a sequence on average: blocks of 128 columns, which read the cache once for all of theirs.  The host
-    // does not know how the tokens lie: where every sequence has as many, blocks of 8 stay ahead to 16 columns or 24 (16 x 16384
-    // tokens, 8 kv heads: 115 us in 8s and 244 in 128s at 8 columns, 185 and 246 at 16, 266 and 247 at 24), but one long chunk
-    // among decoding requests would go over its cache once for every 8 of them (120 tokens over 65536 beside 63 requests of 1000, 11
-    // columns on average: 803 and 343 us; 320 tokens, 24 on average: 1973 and 650), so the rule leans to the side that loses less
-    p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * pg->gq > 8LL * batch;
-    p.qc = p.wide ? ChunkBf16::QC : 8;
-    p.blocks = n_tokens / (p.qc / pg->gq) + batch;
-    p.shared = p.blocks <= pages::kMaxBlocks && p.blocks * (p.max_tiles + pages::kUnitCost) < (1LL << 31);   // (32-bit positions)
-    auto ctas = [&](long long units, int per_sm) {
-        const long long most = (long long)pg->n_sm * per_sm, tiles = p.max_tiles * units;
-        return (int)(tiles < most ? tiles : most);
-    };
-    auto slots = [&](int n_ctas, int qc) { return (size_t)n_ctas * 2 * pages::attn_slot_floats(qc) * sizeof(float); };
-    const long long units0 = (long long)batch * c.n_kv_heads, units1 = (long long)p.blocks * c.n_kv_heads;
-    p.ctas0 = ctas(units0, kDecodeCtas);
-    p.ctas1 = ctas(units1, p.wide ? ChunkBf16::CTAS : kDecodeCtas);
-    p.bytes0 = pages::attn_meta_bytes(0, (size_t)units0, 0) + slots(p.ctas0, 8);
-    p.bytes1 = p.shared ? pages::attn_meta_bytes(1, 0, (size_t)p.ctas1) + slots(p.ctas1, p.qc) : 16;
-    return p;
-}
-
-template <typename C, int MODE>
-int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int attr_bit,
-                cudaStream_t st) {
-    auto kernel = pages::k_page_attn<C, MODE>;
-    constexpr uint32_t smem = C::kSmemBytes + (MODE == 1 ? C::kSmemBlocks : 0);
-    if (!(pg->attr_set & (1u << attr_bit))) {
-        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        pg->attr_set |= 1u << attr_bit;
-    }
-    const dim3 grid = MODE == 0 ? dim3(p.ctas0) : MODE == 1 ? dim3(p.ctas1) : dim3(p.blocks, a.H);
-    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
-    if (int r = launch_check(pg, "k_page_attn")) return r;
-    if (MODE == 2 || p.max_tiles == 1) return FAEDKV_OK;                     // no unit is ever in parts
-    if constexpr (MODE != 2) {
-        const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 16;
-        const dim3 jgrid((unsigned)(MODE == 0 ? a.B * a.H : p.ctas1), (cols + each - 1) / each);
-        CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<typename C::T, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC,
-                                each, MODE == 0 ? p.ctas0 : p.ctas1));
-        return launch_check(pg, "k_page_attn_join");
-    }
-    return FAEDKV_OK;
 }
 
 }  // namespace
@@ -203,7 +137,7 @@ int faedkv_pages_store(faedkv_pages *pg, const void *k_new, const void *v_new, l
 size_t faedkv_pages_attn_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
     if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_tokens < 0) return 0;
     if ((long long)n_tokens + batch > (1LL << 30)) return 0;
-    const AttnPlan p = plan_attn(pg, batch, n_tokens);
+    const AttnPlan p = plan_attn(pg, pg->gq, batch, n_tokens);
     return n_tokens == batch && p.bytes0 > p.bytes1 ? p.bytes0 : p.bytes1;
 }
 
@@ -235,19 +169,12 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     CUtensorMap mk, mv;
     if (int r = make_map(pg, &mk, k_pages)) return r;
     if (int r = make_map(pg, &mv, v_pages)) return r;
-    const AttnPlan p = plan_attn(pg, batch, n_tokens);
+    const AttnPlan p = plan_attn(pg, pg->gq, batch, n_tokens);
     const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
                             c.max_pages, c.n_pages, pg->page_shift, p.blocks,
                             65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
-    if (c.kv_dtype == FAEDKV_F32)
-        return q_start == nullptr ? launch_attn<DecodeF32, 0>(pg, mk, mv, a, p, 0, st)
-               : p.shared         ? launch_attn<DecodeF32, 1>(pg, mk, mv, a, p, 1, st)
-                                  : launch_attn<DecodeF32, 2>(pg, mk, mv, a, p, 2, st);
-    if (q_start == nullptr) return launch_attn<DecodeBf16, 0>(pg, mk, mv, a, p, 3, st);
-    if (p.wide)
-        return p.shared ? launch_attn<ChunkBf16, 1>(pg, mk, mv, a, p, 4, st) : launch_attn<ChunkBf16, 2>(pg, mk, mv, a, p, 5, st);
-    return p.shared ? launch_attn<DecodeBf16, 1>(pg, mk, mv, a, p, 6, st) : launch_attn<DecodeBf16, 2>(pg, mk, mv, a, p, 7, st);
+    return dispatch_attn<0>(pg, mk, mv, a, p, 0, st);
 }
 
 int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *table, int batch, int L, const void *k_pages,
@@ -309,7 +236,7 @@ long long faedkv_pages_debug_word(faedkv_pages *pg, void *stream) {
     if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
     CUDA_TRY(pg, cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
     long long first = 0;
-    for (long long (*word)(faedkv_pages *) : {debug_word_here, pages_share_debug_word}) {
+    for (long long (*word)(faedkv_pages *) : {debug_word_here, pages_share_debug_word, pages_diff_debug_word}) {
         const long long w = word(pg);
         if (w < 0) return w;
         if (first == 0) first = w;

@@ -1,0 +1,68 @@
+// Host side of differential attention over the paged 8-bit cache.  See include/faedkv.h for the contract of the call.
+#include "pages_attn_host.cuh"
+#include "k_page_diff.cuh"
+
+namespace {
+
+size_t maps_at(const faedkv_pages *pg, int batch, int n_tokens) {   // where the maps' results lie in the workspace
+    const AttnPlan p = plan_attn(pg, 2 * pg->gq, batch, n_tokens);
+    return ((n_tokens == batch && p.bytes0 > p.bytes1 ? p.bytes0 : p.bytes1) + 15) / 16 * 16;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t faedkv_pages_attn_diff_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
+    if (pg == nullptr || pg->gq > 4 || batch < 1 || batch > pg->cfg.max_batch || n_tokens < 0) return 0;
+    if ((long long)n_tokens + batch > (1LL << 30)) return 0;
+    return maps_at(pg, batch, n_tokens) + sizeof(float) * 2 * kHeadDim * (size_t)n_tokens * pg->cfg.n_q_heads;
+}
+
+int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
+                           const int32_t *kv_len, const int32_t *table, const void *k_pages, const void *v_pages,
+                           const float *k_scale, const float *v_scale, float scale, const float *lam, const float *gain, float eps,
+                           void *out, void *ws, size_t ws_bytes, void *stream) {
+    const CallRange nvtx_range("faedkv_pages_attn_diff");
+    if (pg == nullptr) return FAEDKV_ERR_INVALID_ARG;
+    if (int r = check_batch(pg, batch)) return r;
+    const faedkv_pages_config &c = pg->cfg;
+    if (pg->gq > 4) return fail(pg, FAEDKV_ERR_UNSUPPORTED, "differential attention takes 1 to 4 query heads per kv head, not %d", pg->gq);
+    if (n_tokens < 0 || (long long)n_tokens + batch > (1LL << 30))
+        return fail(pg, FAEDKV_ERR_SHAPE, "n_tokens = %d outside [0, 2^30 - batch]", n_tokens);
+    if (q_start == nullptr && n_tokens != batch)
+        return fail(pg, FAEDKV_ERR_SHAPE, "without q_start there is one token per sequence: n_tokens = %d, batch = %d", n_tokens, batch);
+    if (!(scale >= 0.0f) || std::isinf(scale)) return fail(pg, FAEDKV_ERR_INVALID_ARG, "scale must be >= 0 and finite");
+    if (!(eps >= 0.0f) || std::isinf(eps)) return fail(pg, FAEDKV_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+    if (n_tokens == 0) return FAEDKV_OK;
+    if (q == nullptr || kv_len == nullptr || table == nullptr || k_pages == nullptr || v_pages == nullptr || k_scale == nullptr ||
+        v_scale == nullptr || lam == nullptr || out == nullptr || ws == nullptr)
+        return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_attn_diff");
+    if (int r = check_align(pg, {q, k_pages, v_pages, k_scale, v_scale, gain, out, ws}, {q_start, kv_len, table, lam})) return r;
+    if (int r = check_ld(pg, "ld_q", ld_q, c.n_q_heads)) return r;
+    const size_t need = faedkv_pages_attn_diff_bytes(pg, batch, n_tokens);
+    if (ws_bytes < need) return fail(pg, FAEDKV_ERR_SHAPE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
+    if (scale == 0.0f) scale = 0.125f;
+    const DeviceGuard guard(pg);
+    if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    CUtensorMap mk, mv;
+    if (int r = make_map(pg, &mk, k_pages)) return r;
+    if (int r = make_map(pg, &mv, v_pages)) return r;
+    const int gq = 2 * pg->gq;
+    const AttnPlan p = plan_attn(pg, gq, batch, n_tokens);
+    float *maps = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + maps_at(pg, batch, n_tokens));
+    const pages::AttnArgs a{q, maps, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, gq, c.max_pages,
+                            c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)gq + 1u, scale * 1.44269504088896341f,
+                            static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
+    if (int r = dispatch_attn<1>(pg, mk, mv, a, p, 8, st)) return r;
+    const pages::DiffArgs d{maps, lam, gain, out, q_start, n_tokens, batch, c.n_q_heads, eps};
+    const dim3 grid((unsigned)(((long long)n_tokens * c.n_q_heads + 7) / 8));
+    if (c.kv_dtype == FAEDKV_BF16) CUDA_TRY(pg, launch_pdl(pages::k_page_diff<__nv_bfloat16>, grid, dim3(256), 0, st, d));
+    else CUDA_TRY(pg, launch_pdl(pages::k_page_diff<float>, grid, dim3(256), 0, st, d));
+    return launch_check(pg, "k_page_diff");
+}
+
+}  // extern "C"
+
+long long pages_diff_debug_word(faedkv_pages *pg) { return debug_word_here(pg); }

@@ -378,7 +378,13 @@ template <> struct Work<2> {
     }
 };
 
-template <typename C, int MODE>
+// FORM 0: softmax attention.  FORM 1, differential attention: a head's query row and the cached keys are two halves of 64 channels, and
+// each half has a softmax of its own over the same values; a column is (head, half), G counts both, and its query is zero in the other half,
+// so one product over 128 channels gives either score.  The results of the columns are float32 and meet in k_page_diff.
+template <typename C, int FORM> struct AttnOut { using T = typename C::T; };
+template <typename C> struct AttnOut<C, 1> { using T = float; };
+
+template <typename C, int MODE, int FORM>
 __global__ void __launch_bounds__(C::kThreads, C::CTAS)
 k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a) {
     using namespace umma;
@@ -699,12 +705,14 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             const int n_cols = s.n_tok * a.G;
             // -- the query columns as e4m3 terms, each column with a power of two of its own
             constexpr int kEach = QC / (4 * WGS);          // columns of a warp: their loads first, then the work
-            const T *q_row = static_cast<const T *>(a.q) + (size_t)s.tok0 * a.ld_q + (size_t)s.h * a.G * kHeadDim + lane * 4;
+            constexpr int kMaps = FORM == 1 ? 2 : 1;       // columns of a query row
+            const T *q_row = static_cast<const T *>(a.q) + (size_t)s.tok0 * a.ld_q + (size_t)s.h * (a.G / kMaps) * kHeadDim + lane * 4;
             float4 q_in[kEach];
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const int c = warp + 4 * WGS * j, tok = c * a.inv_g >> 16;
-                q_in[j] = c < n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 >= 0 && s.tok0 + tok < a.n_tokens) ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
+                q_in[j] = c < n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 >= 0 && s.tok0 + tok < a.n_tokens) ? load4(q_row + (size_t)tok * a.ld_q + (c - tok * a.G) / kMaps * kHeadDim) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (FORM == 1 && ((c - tok * a.G) & 1) != lane >> 4) q_in[j] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
             uint32_t top[kEach];                           // the columns' largest finite magnitudes
 #pragma unroll
@@ -1121,7 +1129,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
             }
             softmax_bar(1, kSoftmax);
-            T *out_row = static_cast<T *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
+            using Out = typename AttnOut<C, FORM>::T;
+            Out *out_row = static_cast<Out *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
             float *part_row = whole ? nullptr : slot + 2 * QC + row;
             auto put = [&](int c, float v) {
                 if (c >= n_cols || !FAEDKV_IN_BOUNDS(kTagPageAttn, !whole || s.tok0 + (int)(c * a.inv_g >> 16) < a.n_tokens)) return;

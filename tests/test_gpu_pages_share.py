@@ -370,27 +370,25 @@ def test_the_c_calls_refuse_what_they_cannot_do(fk):
     i = ref.ints([0] * 64).data_ptr()
     c = [x.data_ptr() for x in cache.args()]
     lib, n0 = fk.load(), pg.launch_count()
-    calls = {
-        lib.faedkv_pages_fork: [pg._h, i, i, i, 4, 4, i, i, i, i, i, *c, i, None],
-        lib.faedkv_pages_release: [pg._h, i, i, 4, i, i, i, i, i, i, None],
-        lib.faedkv_pages_compact: [pg._h, i, 4, i, i, i, i, i, *c, i, None],
-    }
-    for call, good in calls.items():
-        at = {lib.faedkv_pages_fork: (5, 3), lib.faedkv_pages_release: (3, None), lib.faedkv_pages_compact: (2, None)}[call]
+    fork, release, compact = lib.faedkv_pages_fork, lib.faedkv_pages_release, lib.faedkv_pages_compact
+    # arguments, where the batch stands, which others are no tensors, which may be NULL
+    calls = [(fork, [pg._h, i, i, i, 4, 4, i, i, i, i, i, *c, i, None], 5, (4,), 3), (release, [pg._h, i, i, 4, i, i, i, i, i, i, None], 3, (), None),
+             (compact, [pg._h, i, 4, i, i, i, i, i, *c, i, None], 2, (), None)]
+    for call, good, at, counts, optional in calls:
         for k, x in enumerate(good[1:-1], 1):
-            if k == 4 and call is lib.faedkv_pages_fork or k == at[0]:
+            if k == at or k in counts:
                 continue
-            if k != at[1]:
+            if k != optional:
                 assert call(*good[:k], None, *good[k + 1:]) == -1, (call.__name__, k)
-            assert call(*good[:k], x + 2, *good[k + 1:]) == -2, (call.__name__, k)
+            assert call(*good[:k], x + 2, *good[k + 1:]) == -5, (call.__name__, k)
             assert b"aligned" in lib.faedkv_pages_last_error(pg._h)
         for batch in (0, -1, 5):
-            assert call(*good[:at[0]], batch, *good[at[0] + 1:]) == -3, (call.__name__, batch)
-        assert call(big._h, *good[1:at[0]], 32, *good[at[0] + 1:]) == -3
+            assert call(*good[:at], batch, *good[at + 1:]) == -3, (call.__name__, batch)
+        assert call(big._h, *good[1:at], 32, *good[at + 1:]) == -3
         assert b"2^31" in lib.faedkv_pages_last_error(big._h)
-    good = calls[lib.faedkv_pages_fork]
+    good = calls[0][1]
     for n in (-1, 5):
-        assert lib.faedkv_pages_fork(*good[:4], n, *good[5:]) == -3
+        assert fork(*good[:4], n, *good[5:]) == -3
         assert lib.faedkv_pages_fork_bytes(pg._h, 4, n) == 0
     assert lib.faedkv_pages_fork_bytes(pg._h, 4, 4) == 32 and lib.faedkv_pages_fork_bytes(pg._h, 5, 4) == 0
     assert pg.launch_count() == n0 and big.launch_count() == 0 and pg.device_status() == 0
