@@ -473,6 +473,20 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
                       const float *k_scale, const float *v_scale, float scale, void *out, void *ws, size_t ws_bytes,
                       void *stream);
 
+/* faedkv_pages_attn() of one new token of every row (a decode step), where groups of rows share their first pages: rows group_start[g] ..
+ * group_start[g + 1] - 1 (int32 [n_groups + 1], ascending, 1 <= n_groups <= batch) hold their first shared_len[g] tokens in the same
+ * pages, as faedkv_pages_fork() leaves them; of those, whole pages count.  They are read once for a block of the group's query heads, through
+ * the table row of the first row of the block that has them all; what a row holds behind them is read for itself.  A row that holds less
+ * than its group shares is attended alone, as is the only row of a group and one that stands in no group or in one whose bounds
+ * are not rows of the batch (status 0x105).  q, out, scale and results as faedkv_pages_attn(), rounding as there (bf16: a softmax weight
+ * is held to 2^-11 of itself and 2^-31 of its row's largest); the tables are not searched for other shared pages.  ws: faedkv_pages_attn_shared_bytes() (0 for arguments that the call
+ * would refuse), 16-byte aligned, overwritten. */
+size_t faedkv_pages_attn_shared_bytes(const faedkv_pages *pg, int batch, int n_groups);
+int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *group_start, const int32_t *shared_len,
+                             int n_groups, int batch, const int32_t *kv_len, const int32_t *table, const void *k_pages,
+                             const void *v_pages, const float *k_scale, const float *v_scale, float scale, void *out, void *ws,
+                             size_t ws_bytes, void *stream);
+
 /* Differential attention of the newest tokens over the cache, for models whose heads subtract two softmax maps: a query row and a cached
  * key are two halves of 64 channels, [q1 | q2] and [K1 | K2], and
  *   out[i, g] = norm( softmax_n( scale * q1 . K1[n] ) V[n]  -  lam[g] * softmax_n( scale * q2 . K2[n] ) V[n] ),

@@ -37,6 +37,7 @@ EXPORTS = [
     "faedkv_pages_create", "faedkv_pages_destroy", "faedkv_pages_last_error", "faedkv_pages_bytes", "faedkv_pages_tables_bytes", "faedkv_pages_tables",
     "faedkv_pages_fork_bytes", "faedkv_pages_fork", "faedkv_pages_release_bytes", "faedkv_pages_release", "faedkv_pages_compact_bytes",
     "faedkv_pages_compact", "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_attn_diff_bytes", "faedkv_pages_attn_diff",
+    "faedkv_pages_attn_shared_bytes", "faedkv_pages_attn_shared",
     "faedkv_pages_load", "faedkv_pages_device_status",
     "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_debug_word",
 ]
@@ -157,6 +158,11 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_attn.argtypes = [_vp, _vp, _ll, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
                                       ctypes.c_size_t, _vp]
     lib.faedkv_pages_attn.restype = _int
+    lib.faedkv_pages_attn_shared_bytes.argtypes = [_vp, _int, _int]
+    lib.faedkv_pages_attn_shared_bytes.restype = ctypes.c_size_t
+    lib.faedkv_pages_attn_shared.argtypes = [_vp, _vp, _ll, _vp, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
+                                             ctypes.c_size_t, _vp]
+    lib.faedkv_pages_attn_shared.restype = _int
     lib.faedkv_pages_attn_diff_bytes.argtypes = [_vp, _int, _int]
     lib.faedkv_pages_attn_diff_bytes.restype = ctypes.c_size_t
     lib.faedkv_pages_attn_diff.argtypes = [_vp, _vp, _ll, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
@@ -594,6 +600,10 @@ class Pages:
         """Workspace of attn()."""
         return self._bytes("faedkv_pages_attn_bytes", batch, n_tokens)
 
+    def attn_shared_bytes(self, batch: int, n_groups: int) -> int:
+        """Workspace of attn_shared()."""
+        return self._bytes("faedkv_pages_attn_shared_bytes", batch, n_groups)
+
     def attn_diff_bytes(self, batch: int, n_tokens: int) -> int:
         """Workspace of attn_diff()."""
         return self._bytes("faedkv_pages_attn_diff_bytes", batch, n_tokens)
@@ -610,6 +620,23 @@ class Pages:
         w = self._workspace(ws, nbytes, stream)
         self._check(self._lib.faedkv_pages_attn(self._h, qp, ld, st, n, batch, kv, tb, *cache, scale, o, w.data_ptr(), nbytes,
                                                 self._on(stream)))
+
+    def attn_shared(self, q, kv_len, table, group_start, shared_len, k_pages, v_pages, k_scale, v_scale, out, scale: float = 0.0, ws=None,
+                    stream=None):
+        """attn() of one new token of every row, where the rows of a group hold their first shared_len[g] tokens in the same pages."""
+        batch, groups, i32, need = kv_len.shape[0], shared_len.shape[0], torch.int32, self._need
+        qp, n, ld = self._rows("q", q, self.n_q_heads)
+        if n != batch:
+            raise ValueError(f"q must have one token for each of {batch} rows, got {n}")
+        o = need("out", out, self._dtype, (n, self.n_q_heads, self.head_dim))
+        kv = need("kv_len", kv_len, i32, (batch,))
+        tb = need("table", table, i32, (batch, self.max_pages))
+        gs, sl = need("group_start", group_start, i32, (groups + 1,)), need("shared_len", shared_len, i32, (groups,))
+        cache = self._cache(k_pages, v_pages, k_scale, v_scale)
+        nbytes = self.attn_shared_bytes(batch, groups)
+        w = self._workspace(ws, nbytes, stream)
+        self._check(self._lib.faedkv_pages_attn_shared(self._h, qp, ld, gs, sl, groups, batch, kv, tb, *cache, scale, o, w.data_ptr(), nbytes,
+                                                       self._on(stream)))
 
     def attn_diff(self, q, kv_len, table, k_pages, v_pages, k_scale, v_scale, lam, out, q_start=None, gain=None, eps: float = 0.0,
                   scale: float = 0.0, ws=None, stream=None):

@@ -236,7 +236,7 @@ long long faedkv_pages_debug_word(faedkv_pages *pg, void *stream) {
     if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
     CUDA_TRY(pg, cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
     long long first = 0;
-    for (long long (*word)(faedkv_pages *) : {debug_word_here, pages_share_debug_word, pages_diff_debug_word}) {
+    for (long long (*word)(faedkv_pages *) : {debug_word_here, pages_share_debug_word, pages_diff_debug_word, pages_shared_debug_word}) {
         const long long w = word(pg);
         if (w < 0) return w;
         if (first == 0) first = w;

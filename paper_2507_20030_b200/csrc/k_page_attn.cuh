@@ -101,6 +101,8 @@ struct AttnArgs {
     unsigned int *status;
     unsigned long long wait_limit;                        // ns, of a bounded wait
     int withhold;                                         // test hook: the tile (from 1) whose weights are not announced; 0: none
+    const int32_t *group_start, *shared_len;              // MODE 3 and 4: groups of rows, and the tokens that the rows of each share
+    int n_groups;
 };
 
 // Workspace of MODE 0 and 1: header, records, two partial results per CTA (of the unit it goes on with, of the one it leaves).
@@ -110,6 +112,22 @@ __host__ __device__ constexpr size_t attn_meta_bytes(int mode, size_t units, siz
     return 16 + (mode == 0 ? sizeof(UnitMeta) * units : (sizeof(CtaMeta) * ctas + 15) / 16 * 16);
 }
 __host__ __device__ constexpr size_t attn_slot_floats(int qc) { return (size_t)qc * (kHeadDim + 2); }
+// Workspace of MODE 3 and 4: header, prefix sums of the blocks' sizes, results of whole units by query row (cols of them: rows x heads), first
+// those of the shared blocks, then those of the rows' own; MODE 3 two partial results per CTA behind them.
+__host__ __device__ constexpr size_t shared_before_bytes(int blocks) { return 16 + ((size_t)blocks + 4) / 4 * 16; }
+__host__ __device__ constexpr size_t shared_meta_bytes(int blocks, size_t cols) {
+    return shared_before_bytes(blocks) + 2 * cols * (sizeof(float2) + sizeof(float) * kHeadDim);
+}
+struct SharedParts {
+    float2 *stat;                                         // Mu and the sum
+    float *o;
+    __device__ __forceinline__ SharedParts(unsigned char *ws, int blocks, int B, int heads, int own) {
+        const size_t cols = (size_t)B * heads;
+        float2 *s = reinterpret_cast<float2 *>(ws + shared_before_bytes(blocks));
+        stat = s + own * cols;
+        o = reinterpret_cast<float *>(s + 2 * cols) + own * cols * kHeadDim;
+    }
+};
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -269,6 +287,7 @@ struct Segment {
     int b, h, tok0, n_tok;       // first query row (of q, out) and number of query tokens
     int see0;                    // tokens that the first query token sees (its column limit); the i-th sees see0 + i
     int live;                    // tokens that the last one sees, >= 0
+    int page0, own;              // place in the table row of the unit's first page, from where the tokens above are counted; Block's own
     int t0, t1, tiles;           // tiles of the segment, of the unit
     long long first;             // position of the unit's first tile among all
 };
@@ -286,7 +305,7 @@ __device__ __forceinline__ int tiles_of(long long live) { return live <= 0 ? 1 :
 
 // Which new tokens block v of a call with blocks of tq holds: block v - (q_start[b] / tq + b) of sequence b, since sequences
 // begin at distinct numbers of that form.  Not every v is a block.
-struct Block { int b, tok0, n_tok, see0, live; };
+struct Block { int b, tok0, n_tok, see0, live, page0, own; };   // own: 1 a row's own block of MODE 3 and 4
 __device__ __forceinline__ bool find_block(const AttnArgs &a, int tq, int v, bool report, Block &k) {
     int lo = 0, hi = a.B - 1;
     while (lo < hi) {
@@ -305,7 +324,74 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int tq, int v, boo
     k.n_tok = min(tq, n - j * tq);
     k.see0 = (int)clamp_len(a, lo, report) - n + j * tq + 1;
     k.live = max(0, k.see0 + k.n_tok - 1);
+    k.page0 = k.own = 0;
     return true;
+}
+
+// MODE 3 and 4, a decode step of rows that share pages: first blocks of a group's rows over the tokens that it shares, then for each row
+// a block of its own over those behind.  The blocks of rows are numbered as above; row b's own is shared_blocks() + b.
+// The whole pages that row b shares with its group, in tokens: none for the only row of a group, for one that is shorter than what its
+// group shares, and for one that stands in no group.  g, first: the group, its first row.
+__device__ __forceinline__ int shared_of(const AttnArgs &a, int b, int live, bool report, int &g, int &first) {
+    int lo = 0, hi = a.n_groups - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.group_start[mid] <= b) lo = mid; else hi = mid - 1;
+    }
+    g = lo;
+    first = a.group_start[lo];
+    const int end = a.group_start[lo + 1];
+    if (first < 0 || end > a.B || b < first || b >= end) {
+        if (report) flag(a.status, kBadStart);
+        return 0;
+    }
+    const int n = a.shared_len[lo] >> a.page_shift << a.page_shift;
+    if (n < 0 || n > a.W << a.page_shift) {
+        if (report) flag(a.status, kBadLength);
+        return 0;
+    }
+    return end - first > 1 && live >= n ? n : 0;
+}
+__host__ __device__ __forceinline__ int shared_blocks(int B, int n_groups, int tq) { return B / tq + n_groups; }
+__device__ __forceinline__ bool find_shared(const AttnArgs &a, int tq, int v, bool report, Block &k) {
+    const int n_shared = shared_blocks(a.B, a.n_groups, tq);
+    int g, first;
+    if (v >= n_shared) {
+        const int b = v - n_shared, live = (int)clamp_len(a, b, report), n = shared_of(a, b, live, report, g, first);
+        k.b = k.tok0 = b;
+        k.n_tok = k.own = 1;
+        k.page0 = n >> a.page_shift;
+        k.see0 = k.live = live - n;
+        return live > n;
+    }
+    int lo = 0, hi = a.n_groups - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.group_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
+    }
+    first = a.group_start[lo];
+    const int n = a.group_start[lo + 1] - first;
+    if (first < 0 || n < 0 || first > a.B - n) return false;   // (reported with its rows)
+    const int j = v - (first / tq + lo);
+    if (j < 0 || (long long)j * tq >= n) return false;
+    k.tok0 = first + j * tq;
+    k.n_tok = min(tq, n - j * tq);
+    // read through the first row that has them all; a row that has not, or none, is left to its own block
+    for (int b = k.tok0; b < k.tok0 + k.n_tok; ++b) {
+        const int share = shared_of(a, b, (int)clamp_len(a, b, false), false, g, first);
+        if (share > 0) {
+            k.b = b;
+            k.see0 = k.live = share;
+            k.page0 = k.own = 0;
+            return true;
+        }
+    }
+    return false;
+}
+template <int MODE>
+__device__ __forceinline__ bool find_unit(const AttnArgs &a, int tq, int v, bool report, Block &k) {
+    if constexpr (MODE >= 3) return find_shared(a, tq, v, report, k);
+    else return find_block(a, tq, v, report, k);
 }
 
 // MODE 0, a decode step: the tiles of all (sequence, head) units in a row are cut into equal shares, one per CTA; a share
@@ -320,7 +406,7 @@ template <> struct Work<0> {
     long long pos, end;
     __device__ __forceinline__ bool next(const AttnArgs &a, int, Segment &s) {
         if (pos >= end) return false;
-        s.b = b; s.h = h; s.tok0 = b; s.n_tok = 1;
+        s.b = b; s.h = h; s.tok0 = b; s.n_tok = 1; s.page0 = s.own = 0;
         s.live = (int)clamp_len(a, b, false);
         s.see0 = s.live;
         const int tiles = tiles_of(s.live);
@@ -335,7 +421,7 @@ template <> struct Work<0> {
     }
 };
 
-template <> struct Work<1> {
+template <int MODE> struct WorkShares {
     int v, h, per_head;
     long long pos, end;
     const int32_t *before;                                // [blocks + 1]: positions of one head's blocks before block v
@@ -353,8 +439,8 @@ template <> struct Work<1> {
             if (++v == a.blocks) { v = 0; ++h; }
             if (s.t1 <= s.t0) continue;                   // the share ended before the unit's first tile
             Block k;
-            if (!find_block(a, qc / a.G, block, false, k)) return false;
-            s.b = k.b; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live;
+            if (!find_unit<MODE>(a, qc / a.G, block, false, k)) return false;
+            s.b = k.b; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live; s.page0 = k.page0; s.own = k.own;
             s.tiles = size - kUnitCost;
             s.first = u0 + kUnitCost;
             return true;
@@ -362,21 +448,25 @@ template <> struct Work<1> {
         return false;
     }
 };
+template <> struct Work<1> : WorkShares<1> {};
+template <> struct Work<3> : WorkShares<3> {};
 
-template <> struct Work<2> {
+template <int MODE> struct WorkOne {
     bool done;
     __device__ __forceinline__ bool next(const AttnArgs &a, int qc, Segment &s) {
         if (done) return false;
         done = true;
         Block k;
         // the blocks that see most first
-        if (!find_block(a, qc / a.G, (int)(gridDim.x - 1 - blockIdx.x), threadIdx.x == 0, k)) return false;
-        s.b = k.b; s.h = blockIdx.y; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live;
+        if (!find_unit<MODE>(a, qc / a.G, (int)(gridDim.x - 1 - blockIdx.x), threadIdx.x == 0, k)) return false;
+        s.b = k.b; s.h = blockIdx.y; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live; s.page0 = k.page0; s.own = k.own;
         s.tiles = tiles_of(s.live);
         s.t0 = 0; s.t1 = s.tiles; s.first = 0;
         return true;
     }
 };
+template <> struct Work<2> : WorkOne<2> {};
+template <> struct Work<4> : WorkOne<4> {};
 
 // FORM 0: softmax attention.  FORM 1, differential attention: a head's query row and the cached keys are two halves of 64 channels, and
 // each half has a softmax of its own over the same values; a column is (head, half), G counts both, and its query is zero in the other half,
@@ -484,11 +574,11 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         tc_fence_before();
         __syncthreads();
         w0 = place;
-    } else if constexpr (MODE == 1) {
+    } else if constexpr (MODE == 1 || MODE == 3) {
         int32_t *before = reinterpret_cast<int32_t *>(gbase + C::kOffMisc + (C::kSmemBytes - 1024 - C::kOffMisc));
         for (int v = tid; v < a.blocks; v += C::kThreads) {
             Block k;
-            before[v + 1] = find_block(a, QC / a.G, v, blockIdx.x == 0, k) ? kUnitCost + tiles_of(k.live) : 0;
+            before[v + 1] = find_unit<MODE>(a, QC / a.G, v, blockIdx.x == 0, k) ? kUnitCost + tiles_of(k.live) : 0;
         }
         if (tid == 0) before[0] = 0;
         __syncthreads();
@@ -512,7 +602,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         w0.end = min(total, w0.pos + share);
         w0.per_head = per_head;
         if (tid == 0 && blockIdx.x == 0) *reinterpret_cast<long long *>(a.ws) = share;
-        if (tid == 0) reinterpret_cast<CtaMeta *>(a.ws + 16)[blockIdx.x].tiles = 0;
+        if (MODE == 1 && tid == 0) reinterpret_cast<CtaMeta *>(a.ws + 16)[blockIdx.x].tiles = 0;
+        if (MODE == 3 && blockIdx.x == 0)                  // the join finds the units' parts by these
+            for (int v = tid; v <= a.blocks; v += C::kThreads) reinterpret_cast<int32_t *>(a.ws + 16)[v] = before[v];
         if (w0.pos < w0.end) {
             w0.h = (int)(w0.pos / per_head);
             const int in = (int)(w0.pos - (long long)w0.h * per_head);
@@ -554,9 +646,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         while (w.next(a, QC, s)) {
             const int32_t *row = a.table + (size_t)s.b * a.W;
             auto fetch = [&](int t_first, int &id, float &ks, float &vs) {
-                const long long p = ((long long)t_first << lg_ppt) + lane;
+                const long long p_live = ((long long)t_first << lg_ppt) + lane, p = MODE >= 3 ? s.page0 + p_live : p_live;
                 id = -1; ks = 0.f; vs = 0.f;
-                if ((p << a.page_shift) < s.live && t_first + (lane >> lg_ppt) < s.t1 && FAEDKV_IN_BOUNDS(kTagPageAttn, p >= 0 && p < a.W && s.b >= 0 && s.b < a.B && s.h < a.H)) {
+                if ((p_live << a.page_shift) < s.live && t_first + (lane >> lg_ppt) < s.t1 && FAEDKV_IN_BOUNDS(kTagPageAttn, p >= 0 && p < a.W && s.b >= 0 && s.b < a.B && s.h < a.H)) {
                     id = row[p];
                     if (id < 0 || id >= a.n_pages) {
                         flag(a.status, kBadPage);
@@ -755,7 +847,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 if (lane == 0) {
                     col[C::WIDE ? QC + c : (c >> 1) * 4 + (c & 1)] = qs * a.scale_log2;
                     mu_at(c) = 0.f;
-                    col_lim[c] = c < n_cols ? s.see0 + (int)(c * a.inv_g >> 16) : 0;
+                    col_lim[c] = c >= n_cols ? 0 : MODE >= 3 ? s.see0 : s.see0 + (int)(c * a.inv_g >> 16);
                     col_set[c] = c < n_cols ? 0 : 1;
                 }
                 auto put_codes = [&](int term, uint32_t codes) {
@@ -1015,7 +1107,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
                 uint8_t *vtile = gbase + C::kOffV + (uint32_t)sv * kTileBytes;
                 // some columns see a token of this tile that others do not
-                const bool ragged = MODE != 0 && s.n_tok > 1 && (t + 1) * kTile > s.see0;
+                const bool ragged = (MODE == 1 || MODE == 2) && s.n_tok > 1 && (t + 1) * kTile > s.see0;
                 const int n_live = min(kTile, s.live - t * kTile);
                 auto cell = [&](int r) { return vtile + mn_chunk<128>(r, (uint32_t)row >> 4) + (row & 15); };
                 auto note_nan = [&](int r) {               // the columns that see token r
@@ -1102,10 +1194,20 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             if (s.t1 > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
             tc_fence_after();
             softmax_bar(1, kSoftmax);
-            const bool whole = MODE == 2 || (s.t0 == 0 && s.t1 == s.tiles);
+            const bool whole = MODE == 2 || MODE == 4 || (s.t0 == 0 && s.t1 == s.tiles);
             float *slot = nullptr;
+            // MODE 3 and 4: a whole unit's columns beside the rows that they belong to, for the join
+            const SharedParts parts(a.ws, a.blocks, a.B, a.H * a.G, s.own);
+            if (MODE >= 3 && whole) {
+                for (int c = tid; c < n_cols; c += kSoftmax) {
+                    const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
+                    const int k = c * a.inv_g >> 16;
+                    if (!FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 + k < a.B && s.h < a.H)) continue;
+                    parts.stat[((size_t)(s.tok0 + k) * a.H + s.h) * a.G + (c - k * a.G)] = make_float2(sum == 0.f ? kMuNone : -mu_at(c), sum);
+                }
+            }
             if (!whole) {
-                const size_t head = attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
+                const size_t head = MODE == 3 ? shared_meta_bytes(a.blocks, (size_t)a.B * a.H * a.G) : attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
                 slot = reinterpret_cast<float *>(a.ws + head) + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(QC);
                 for (int c = tid; c < n_cols; c += kSoftmax) {
                     const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
@@ -1129,8 +1231,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 col_f[c] = sum == 0.f ? 0.f : __frcp_rn(sum);
             }
             softmax_bar(1, kSoftmax);
-            using Out = typename AttnOut<C, FORM>::T;
-            Out *out_row = static_cast<Out *>(a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
+            using Out = std::conditional_t<MODE >= 3, float, typename AttnOut<C, FORM>::T>;
+            Out *out_row = static_cast<Out *>(MODE >= 3 ? parts.o : a.out) + ((size_t)s.tok0 * a.H + s.h) * a.G * kHeadDim + row;
             float *part_row = whole ? nullptr : slot + 2 * QC + row;
             auto put = [&](int c, float v) {
                 if (c >= n_cols || !FAEDKV_IN_BOUNDS(kTagPageAttn, !whole || s.tok0 + (int)(c * a.inv_g >> 16) < a.n_tokens)) return;

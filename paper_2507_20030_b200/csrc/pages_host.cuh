@@ -150,3 +150,4 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
 // The same of the other files.
 long long pages_share_debug_word(faedkv_pages *pg);
 long long pages_diff_debug_word(faedkv_pages *pg);
+long long pages_shared_debug_word(faedkv_pages *pg);
