@@ -4,9 +4,14 @@
 
 namespace {
 
-size_t maps_at(const faedkv_pages *pg, int batch, int n_tokens) {   // where the maps' results lie in the workspace
+// Blocks of many columns take the form with rows; the rule on where they begin is plan_attn()'s.
+AttnPlan plan_diff(const faedkv_pages *pg, int batch, int n_tokens) {
     const AttnPlan p = plan_attn(pg, 2 * pg->gq, batch, n_tokens);
-    return ((n_tokens == batch && p.bytes0 > p.bytes1 ? p.bytes0 : p.bytes1) + 15) / 16 * 16;
+    return p.wide ? plan_rows(pg, 2 * pg->gq, batch, n_tokens) : p;
+}
+size_t maps_at(const faedkv_pages *pg, int batch, int n_tokens) {   // where the maps' results lie in the workspace
+    const AttnPlan p = plan_diff(pg, batch, n_tokens), q = plan_attn(pg, 2 * pg->gq, batch, n_tokens);
+    return ((n_tokens == batch && q.bytes0 > p.bytes1 ? q.bytes0 : p.bytes1) + 15) / 16 * 16;
 }
 
 }  // namespace
@@ -50,12 +55,12 @@ int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, cons
     if (int r = make_map(pg, &mk, k_pages)) return r;
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const int gq = 2 * pg->gq;
-    const AttnPlan p = plan_attn(pg, gq, batch, n_tokens);
+    const AttnPlan p = q_start == nullptr ? plan_attn(pg, gq, batch, n_tokens) : plan_diff(pg, batch, n_tokens);
     float *maps = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + maps_at(pg, batch, n_tokens));
     const pages::AttnArgs a{q, maps, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, gq, c.max_pages,
                             c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
-    if (int r = dispatch_attn<1>(pg, mk, mv, a, p, 8, st)) return r;
+    if (int r = p.wide && q_start != nullptr ? dispatch_rows<1>(pg, mk, mv, a, p, 12, st) : dispatch_attn<1>(pg, mk, mv, a, p, 8, st)) return r;
     const pages::DiffArgs d{maps, lam, gain, out, q_start, n_tokens, batch, c.n_q_heads, eps};
     const dim3 grid((unsigned)(((long long)n_tokens * c.n_q_heads + 7) / 8));
     if (c.kv_dtype == FAEDKV_BF16) CUDA_TRY(pg, launch_pdl(pages::k_page_diff<__nv_bfloat16>, grid, dim3(256), 0, st, d));

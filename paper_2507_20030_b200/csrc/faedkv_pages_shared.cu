@@ -10,37 +10,47 @@ struct SharedPlan {
     size_t bytes;
 };
 
-template <typename C>
+// bf16: query columns as rows, 256 of them; float32: 8 columns.
 SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
     const faedkv_pages_config &c = pg->cfg;
+    const bool rows = c.kv_dtype == FAEDKV_BF16;
+    const int qc = rows ? pages::kRowsQC : DecodeF32::QC;
     SharedPlan p{};
-    p.tq = C::QC / pg->gq;
+    p.tq = qc / pg->gq;
     p.blocks = pages::shared_blocks(batch, n_groups, p.tq) + batch;
     const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
-    p.spread = p.blocks <= pages::kMaxBlocks && p.blocks * (max_tiles + pages::kUnitCost) < (1LL << 31);
-    const long long most = (long long)pg->n_sm * C::CTAS, tiles = max_tiles * p.blocks * c.n_kv_heads;
+    p.spread = p.blocks <= pages::kMaxBlocks && p.blocks * (2 * max_tiles + pages::kUnitCost) < (1LL << 31);
+    const long long most = (long long)pg->n_sm * (rows ? 1 : DecodeF32::CTAS), tiles = max_tiles * p.blocks * c.n_kv_heads;
     p.ctas = (int)(tiles < most ? tiles : most);
     p.bytes = pages::shared_meta_bytes(p.blocks, (size_t)batch * c.n_q_heads) +
-              (p.spread ? (size_t)p.ctas * 2 * pages::attn_slot_floats(C::QC) * sizeof(float) : 0);
+              (p.spread ? (size_t)p.ctas * 2 * pages::attn_slot_floats(qc) * sizeof(float) : 0);
     return p;
 }
 
-template <typename C>
-int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, pages::AttnArgs a, int bit, cudaStream_t st) {
-    const SharedPlan p = plan_shared<C>(pg, a.B, a.n_groups);
-    a.blocks = p.blocks;
-    auto kernel = p.spread ? pages::k_page_attn<C, 3, 0> : pages::k_page_attn<C, 4, 0>;
-    const uint32_t smem = C::kSmemBytes + (p.spread ? C::kSmemBlocks : 0);
-    if (!p.spread) ++bit;
-    if (!(pg->attr_set & (1u << bit))) {
-        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        pg->attr_set |= 1u << bit;
-    }
-    CUDA_TRY(pg, launch_pdl(kernel, p.spread ? dim3(p.ctas) : dim3(p.blocks, a.H), dim3(C::kThreads), smem, st, mk, mv, a));
-    if (int r = launch_check(pg, "k_page_attn")) return r;
-    auto join = p.spread ? pages::k_page_join_shared<typename C::T, 3> : pages::k_page_join_shared<typename C::T, 4>;
-    CUDA_TRY(pg, launch_pdl(join, dim3((unsigned)(a.B * a.H)), dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC, p.ctas));
+template <typename T, int MODE>
+int launch_join(faedkv_pages *pg, const pages::AttnArgs &a, int qc, int ctas, cudaStream_t st) {
+    CUDA_TRY(pg, launch_pdl(pages::k_page_join_shared<T, MODE>, dim3((unsigned)(a.B * a.H)), dim3(kHeadDim, pages::kJoinGroups), 0, st, a, qc,
+                            qc == pages::kRowsQC, ctas));
     return launch_check(pg, "k_page_join_shared");
+}
+
+template <int MODE>
+int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const SharedPlan &p, cudaStream_t st) {
+    const dim3 grid = MODE == 3 ? dim3(p.ctas) : dim3(p.blocks, a.H);
+    if (pg->cfg.kv_dtype == FAEDKV_BF16) {
+        if (int r = launch_rows<MODE, 0>(pg, mk, mv, a, grid, 16 + MODE, st)) return r;
+        return launch_join<__nv_bfloat16, MODE>(pg, a, pages::kRowsQC, p.ctas, st);
+    }
+    using C = DecodeF32;
+    auto kernel = pages::k_page_attn<C, MODE, 0>;
+    constexpr uint32_t smem = C::kSmemBytes + (MODE == 3 ? C::kSmemBlocks : 0);
+    if (!(pg->attr_set & (1u << (18 + MODE)))) {
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        pg->attr_set |= 1u << (18 + MODE);
+    }
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
+    if (int r = launch_check(pg, "k_page_attn")) return r;
+    return launch_join<float, MODE>(pg, a, C::QC, p.ctas, st);
 }
 
 }  // namespace
@@ -49,7 +59,7 @@ extern "C" {
 
 size_t faedkv_pages_attn_shared_bytes(const faedkv_pages *pg, int batch, int n_groups) {
     if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_groups < 1 || n_groups > batch) return 0;
-    return pg->cfg.kv_dtype == FAEDKV_F32 ? plan_shared<DecodeF32>(pg, batch, n_groups).bytes : plan_shared<DecodeBf16>(pg, batch, n_groups).bytes;
+    return plan_shared(pg, batch, n_groups).bytes;
 }
 
 int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *group_start, const int32_t *shared_len,
@@ -75,12 +85,13 @@ int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, co
     CUtensorMap mk, mv;
     if (int r = make_map(pg, &mk, k_pages)) return r;
     if (int r = make_map(pg, &mv, v_pages)) return r;
+    const SharedPlan p = plan_shared(pg, batch, n_groups);
     const pages::AttnArgs a{q, out, nullptr, kv_len, table, k_scale, v_scale, ld_q, batch, batch, c.n_kv_heads, pg->gq, c.max_pages,
-                            c.n_pages, pg->page_shift, 0, 65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
+                            c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile, group_start, shared_len,
                             n_groups};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return c.kv_dtype == FAEDKV_F32 ? launch_shared<DecodeF32>(pg, mk, mv, a, 16, st) : launch_shared<DecodeBf16>(pg, mk, mv, a, 18, st);
+    return p.spread ? launch_shared<3>(pg, mk, mv, a, p, st) : launch_shared<4>(pg, mk, mv, a, p, st);
 }
 
 }  // extern "C"

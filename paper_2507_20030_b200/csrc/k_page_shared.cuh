@@ -1,10 +1,10 @@
 // One new token of every row, where groups of rows share their first pages: the join.
 //
-// k_page_attn (MODE 3, 4) attends the rows of a group together over the tokens that they share, as columns of one product that reads each
+// k_page_rows or k_page_attn (MODE 3, 4) attends the rows of a group together over the tokens that they share, as columns of one product that reads each
 // shared page once, and each row alone over the tokens behind.  The two results of a query row, each in parts where it was split over
 // CTAs, meet here as parts of any softmax do: out = sum_i l_i 2^(m_i - m) o_i / sum_i l_i 2^(m_i - m), m the largest m_i.
 #pragma once
-#include "k_page_attn.cuh"
+#include "k_page_rows.cuh"
 
 namespace faedkv {
 namespace pages {
@@ -19,7 +19,7 @@ struct UnitParts {
 
 // Grid: a CTA for each (row, kv head); 128 channels x kJoinGroups of its columns.
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_join_shared(const AttnArgs a, const int qc, const int ctas) {
+__global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_join_shared(const AttnArgs a, const int qc, const bool rows, const int ctas) {
     pdl_wait();
     const int d = threadIdx.x, b = blockIdx.x / a.H, h = blockIdx.x - b * a.H, tq = qc / a.G;
     const int live = (int)clamp_len(a, b, false), n_shared = shared_blocks(a.B, a.n_groups, tq);
@@ -37,18 +37,20 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_join_shared(cons
             UnitParts &u = parts[own];
             u.n = 0;
             if (own ? live <= share : share == 0) continue;
-            const SharedParts rows(a.ws, a.blocks, a.B, a.H * a.G, own);
+            const SharedParts whole(a.ws, a.blocks, a.B, a.H * a.G, own);
             u.n = 1;
-            u.mu = reinterpret_cast<const float *>(rows.stat + i_row);
+            u.mu = reinterpret_cast<const float *>(whole.stat + i_row);
             u.sum = u.mu + 1;
-            u.o = rows.o + i_row * kHeadDim + d;
+            u.o = whole.o + i_row * kHeadDim + d;
             u.step = u.skip = 0;
             if constexpr (MODE == 3) {
                 const int j = own ? 0 : (b - first) / tq, v = own ? n_shared + b : first / tq + g + j;
-                const int tiles = before[v + 1] - before[v] - kUnitCost;
-                const long long pos = (long long)h * before[a.blocks] + before[v] + kUnitCost;
-                const int cta0 = (int)(pos / per_cta), cta1 = (int)((pos + tiles - 1) / per_cta);
-                if (!FAEDKV_IN_BOUNDS(kTagPageAttn, tiles > 0 && cta0 >= 0 && cta1 < ctas)) { u.n = 0; continue; }
+                // positions of the unit's tiles, of one tile
+                const int cost = rows ? kRowsCost : kUnitCost, n = before[v + 1] - before[v] - cost;
+                const int each = rows && !own ? rows_weight(min(tq, a.group_start[g + 1] - first - j * tq) * a.G) : 1;
+                const long long pos = (long long)h * before[a.blocks] + before[v] + cost;
+                const int cta0 = (int)(pos / per_cta), cta1 = (int)((pos + n - each) / per_cta);
+                if (!FAEDKV_IN_BOUNDS(kTagPageAttn, n > 0 && cta0 >= 0 && cta1 < ctas)) { u.n = 0; continue; }
                 if (cta0 != cta1) {
                     const int col = own ? c : (b - first - j * tq) * a.G + c;
                     const float *slot = slots + cta0 * step + step / 2;      // a part that begins a unit: the CTA's second

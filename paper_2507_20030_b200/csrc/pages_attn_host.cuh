@@ -2,6 +2,7 @@
 #pragma once
 #include "pages_host.cuh"
 #include "k_page_attn.cuh"
+#include "k_page_rows.cuh"
 
 namespace {
 
@@ -73,6 +74,43 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
     return FAEDKV_OK;
 }
 
+// The form with query columns as rows, for new tokens of bf16 calls: plan and launch.
+[[maybe_unused]] AttnPlan plan_rows(const faedkv_pages *pg, int gq, int batch, int n_tokens) {
+    AttnPlan p{};
+    p.max_tiles = ((long long)pg->cfg.max_pages * pg->cfg.page_size + pages::kTile - 1) / pages::kTile;
+    p.wide = true;
+    p.qc = pages::kRowsQC;
+    p.blocks = n_tokens / (p.qc / gq) + batch;
+    p.shared = p.blocks <= pages::kMaxBlocks && p.blocks * (2 * p.max_tiles + pages::kRowsCost) < (1LL << 31);
+    const long long tiles = p.max_tiles * p.blocks * pg->cfg.n_kv_heads;
+    p.ctas1 = (int)(tiles < pg->n_sm ? tiles : pg->n_sm);
+    p.bytes1 = p.shared ? pages::attn_meta_bytes(1, 0, (size_t)p.ctas1) + (size_t)p.ctas1 * 2 * pages::attn_slot_floats(p.qc) * sizeof(float) : 16;
+    return p;
+}
+
+template <int MODE, int FORM>
+int launch_rows(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, dim3 grid, int attr_bit, cudaStream_t st) {
+    auto kernel = pages::k_page_rows<MODE, FORM>;
+    if (!(pg->attr_set & (1u << attr_bit))) {
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pages::kRowsSmem));
+        pg->attr_set |= 1u << attr_bit;
+    }
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(pages::kRowsThreads), pages::kRowsSmem, st, mk, mv, a));
+    return launch_check(pg, "k_page_rows");
+}
+
+template <int FORM>
+int dispatch_rows(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int bit, cudaStream_t st) {
+    if (!p.shared) return launch_rows<2, FORM>(pg, mk, mv, a, dim3(p.blocks, a.H), bit, st);
+    if (int r = launch_rows<1, FORM>(pg, mk, mv, a, dim3(p.ctas1), bit + 1, st)) return r;
+    if (p.max_tiles == 1) return FAEDKV_OK;                                  // no unit is ever in parts
+    using Out = std::conditional_t<FORM == 1, float, __nv_bfloat16>;
+    const int cols = p.qc / a.G * a.G, each = 16;
+    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<Out, 1>, dim3((unsigned)p.ctas1, (cols + each - 1) / each), dim3(kHeadDim, pages::kJoinGroups), 0,
+                            st, a, p.qc, each, p.ctas1));
+    return launch_check(pg, "k_page_attn_join");
+}
+
 // The instance for a call: by type, new tokens, and how many blocks they make.  bit: the first of eight in attr_set.
 template <int FORM>
 int dispatch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int bit, cudaStream_t st) {
@@ -81,8 +119,9 @@ int dispatch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv
                : p.shared           ? launch_attn<DecodeF32, 1, FORM>(pg, mk, mv, a, p, bit + 1, st)
                                     : launch_attn<DecodeF32, 2, FORM>(pg, mk, mv, a, p, bit + 2, st);
     if (a.q_start == nullptr) return launch_attn<DecodeBf16, 0, FORM>(pg, mk, mv, a, p, bit + 3, st);
-    if (p.wide)
-        return p.shared ? launch_attn<ChunkBf16, 1, FORM>(pg, mk, mv, a, p, bit + 4, st) : launch_attn<ChunkBf16, 2, FORM>(pg, mk, mv, a, p, bit + 5, st);
+    if constexpr (FORM == 0)
+        if (p.wide)
+            return p.shared ? launch_attn<ChunkBf16, 1, FORM>(pg, mk, mv, a, p, bit + 4, st) : launch_attn<ChunkBf16, 2, FORM>(pg, mk, mv, a, p, bit + 5, st);
     return p.shared ? launch_attn<DecodeBf16, 1, FORM>(pg, mk, mv, a, p, bit + 6, st) : launch_attn<DecodeBf16, 2, FORM>(pg, mk, mv, a, p, bit + 7, st);
 }
 
