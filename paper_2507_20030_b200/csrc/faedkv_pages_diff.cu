@@ -60,11 +60,25 @@ int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, cons
     const pages::AttnArgs a{q, maps, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, gq, c.max_pages,
                             c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
-    if (int r = p.wide && q_start != nullptr ? dispatch_rows<1>(pg, mk, mv, a, p, 12, st) : dispatch_attn<1>(pg, mk, mv, a, p, 8, st)) return r;
     const pages::DiffArgs d{maps, lam, gain, out, q_start, n_tokens, batch, c.n_q_heads, eps};
+    if (p.wide && q_start != nullptr) {                    // whole units are finished where they are attended
+        if (!p.shared) return launch_rows<2, 1>(pg, mk, mv, a, d, dim3(p.blocks, a.H), 12, st);
+        if (int r = launch_rows<1, 1>(pg, mk, mv, a, d, dim3(p.ctas1), 13, st)) return r;
+        if (p.max_tiles == 1) return FAEDKV_OK;            // no unit is ever in parts
+        const dim3 grid((unsigned)p.ctas1, (p.qc / 2 + 7) / 8);
+        CUDA_TRY(pg, launch_pdl(pages::k_page_diff_join<__nv_bfloat16, 1>, grid, dim3(256), 0, st, a, d, p.qc, p.ctas1));
+        return launch_check(pg, "k_page_diff_join");
+    }
+    if (int r = dispatch_attn<1>(pg, mk, mv, a, p, 8, st)) return r;
+    const bool f32 = c.kv_dtype == FAEDKV_F32;
     const dim3 grid((unsigned)(((long long)n_tokens * c.n_q_heads + 7) / 8));
-    if (c.kv_dtype == FAEDKV_BF16) CUDA_TRY(pg, launch_pdl(pages::k_page_diff<__nv_bfloat16>, grid, dim3(256), 0, st, d));
-    else CUDA_TRY(pg, launch_pdl(pages::k_page_diff<float>, grid, dim3(256), 0, st, d));
+    if (q_start == nullptr) {
+        if (f32) CUDA_TRY(pg, launch_pdl(pages::k_page_diff_join<float, 0>, grid, dim3(256), 0, st, a, d, p.qc, p.ctas0));
+        else CUDA_TRY(pg, launch_pdl(pages::k_page_diff_join<__nv_bfloat16, 0>, grid, dim3(256), 0, st, a, d, p.qc, p.ctas0));
+        return launch_check(pg, "k_page_diff_join");
+    }
+    if (f32) CUDA_TRY(pg, launch_pdl(pages::k_page_diff<float>, grid, dim3(256), 0, st, d));
+    else CUDA_TRY(pg, launch_pdl(pages::k_page_diff<__nv_bfloat16>, grid, dim3(256), 0, st, d));
     return launch_check(pg, "k_page_diff");
 }
 

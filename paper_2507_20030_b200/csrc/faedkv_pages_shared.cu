@@ -29,7 +29,7 @@ SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
 
 template <typename T, int MODE>
 int launch_join(faedkv_pages *pg, const pages::AttnArgs &a, int qc, int ctas, cudaStream_t st) {
-    CUDA_TRY(pg, launch_pdl(pages::k_page_join_shared<T, MODE>, dim3((unsigned)(a.B * a.H)), dim3(kHeadDim, pages::kJoinGroups), 0, st, a, qc,
+    CUDA_TRY(pg, launch_pdl(pages::k_page_join_shared<T, MODE>, dim3((unsigned)(((long long)a.B * a.H * a.G + 7) / 8)), dim3(256), 0, st, a, qc,
                             qc == pages::kRowsQC, ctas));
     return launch_check(pg, "k_page_join_shared");
 }
@@ -38,7 +38,7 @@ template <int MODE>
 int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const SharedPlan &p, cudaStream_t st) {
     const dim3 grid = MODE == 3 ? dim3(p.ctas) : dim3(p.blocks, a.H);
     if (pg->cfg.kv_dtype == FAEDKV_BF16) {
-        if (int r = launch_rows<MODE, 0>(pg, mk, mv, a, grid, 16 + MODE, st)) return r;
+        if (int r = launch_rows<MODE, 0>(pg, mk, mv, a, pages::DiffArgs{}, grid, 16 + MODE, st)) return r;
         return launch_join<__nv_bfloat16, MODE>(pg, a, pages::kRowsQC, p.ctas, st);
     }
     using C = DecodeF32;

@@ -5,20 +5,10 @@
 // norm(o) = o * gain / sqrt(mean(o^2) + eps) over the head's 128 channels, or o itself without a gain.  k_page_attn computes the a_m as
 // columns of one pass over the cache: the codes of K and V are read once for both maps of all heads.
 #pragma once
-#include "common.cuh"
-#include "k_pages.cuh"
+#include "k_page_rows.cuh"
 
 namespace faedkv {
 namespace pages {
-
-struct DiffArgs {
-    const float *maps;                                    // [n_tokens][n_q_heads][2][128]
-    const float *lam, *gain;                              // [n_q_heads]; [128] or NULL
-    void *out;
-    const int32_t *q_start;                               // may be NULL: every row is a token
-    int n_tokens, B, HQ;
-    float eps;
-};
 
 // o of one head, four channels a lane, normalised and stored.
 template <typename T>
@@ -28,14 +18,65 @@ __device__ __forceinline__ void diff_finish(float4 a1, float4 a2, float lam, con
         float ss = fmaf(o.x, o.x, o.y * o.y) + fmaf(o.z, o.z, o.w * o.w);
 #pragma unroll
         for (int s = 16; s; s >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
-        const float m = ss * (1.0f / kHeadDim) + eps, r = m > 0.f ? rsqrtf(m) : m;   // a row of zeros stays one without eps; NaN stays NaN
+        const float r = diff_norm(ss, eps);
         const float4 w = load4(gain + 4 * lane);
         o = make_float4(o.x * (r * w.x), o.y * (r * w.y), o.z * (r * w.z), o.w * (r * w.w));
     }
     store4(out + 4 * lane, o);
 }
 
-// A warp for each (token, head).
+// Split units and, of a decode step, all others.  A warp for each head.  MODE 0: grid (tokens x heads / 8); MODE 1 (the form with rows, which finishes its
+// whole units itself): grid (CTAs, heads of a unit / 8), the second CTA of a shared unit looks after it.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(256) k_page_diff_join(const AttnArgs a, const DiffArgs diff, const int qc, const int ctas) {
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float *slots = reinterpret_cast<const float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, ctas));
+    const size_t step = 2 * attn_slot_floats(qc);
+    const int heads = a.G / 2;                             // of a kv head
+    const long long share = *reinterpret_cast<const long long *>(a.ws);
+    int tok, h, g, c;
+    long long first;
+    int tiles;
+    if constexpr (MODE == 0) {
+        const long long i = (long long)blockIdx.x * 8 + warp;
+        if (i >= (long long)a.n_tokens * diff.HQ) return;
+        tok = (int)(i / diff.HQ);
+        const int head = (int)(i - (long long)tok * diff.HQ);
+        h = head / heads;
+        g = head - h * heads;
+        c = 2 * g;
+        const UnitMeta m = reinterpret_cast<const UnitMeta *>(a.ws + 16)[(size_t)tok * a.H + h];
+        first = m.first; tiles = m.tiles;
+    } else {
+        const CtaMeta m = reinterpret_cast<const CtaMeta *>(a.ws + 16)[blockIdx.x];
+        first = m.first; tiles = m.tiles;
+        c = 2 * ((int)blockIdx.y * 8 + warp);
+        if (tiles == 0 || c >= m.n_cols) return;           // this CTA began with a unit of its own
+        const int k = c / a.G;
+        tok = m.tok0 + k;
+        h = m.h;
+        g = (c - k * a.G) >> 1;
+    }
+    const int cta0 = cta_of(first, share), cta1 = cta_of(first + tiles - 1, share);
+    if (MODE == 1 && cta0 + 1 != (int)blockIdx.x) return;  // another one's
+    if (!FAEDKV_IN_BOUNDS(kTagPageAttn, cta0 >= 0 && cta1 < ctas && tok >= 0 && tok < a.n_tokens && h >= 0 && h < a.H)) return;
+    const size_t row = ((size_t)tok * a.H + h) * heads + g;
+    float4 a1, a2;
+    if (cta0 == cta1) {                                    // one CTA had it all
+        const float *x = diff.maps + row * 2 * kHeadDim + 4 * lane;
+        a1 = load4(x);
+        a2 = load4(x + kHeadDim);
+    } else {
+        float4 maps[2];
+        gather_parts<2>([&](int i, int k) { return SlotColumn(slots + (cta0 + i) * step + (i == 0 ? step / 2 : 0), qc, c + k); }, cta1 - cta0 + 1, lane, maps);
+        a1 = maps[0];
+        a2 = maps[1];
+    }
+    diff_finish(a1, a2, diff.lam[row % diff.HQ], diff.gain, diff.eps, lane, static_cast<T *>(diff.out) + row * kHeadDim);
+}
+
+// Heads whose maps are complete, a warp for each (token, head).
 template <typename T>
 __global__ void __launch_bounds__(256) k_page_diff(const DiffArgs a) {
     pdl_wait();

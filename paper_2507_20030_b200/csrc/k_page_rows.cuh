@@ -25,7 +25,8 @@ namespace pages {
 constexpr int kRowsQC = 256, kRowsK = 3, kRowsV = 2, kRowsH = 2, kRowsRing = 8, kRowsSegs = 4;
 constexpr int kRowsConvert = 128, kRowsThreads = 256 + kRowsConvert + 128;  // 128 registers a thread at launch (the last warp only hands some on)
 constexpr int kRowsRegsSoftmax = 160, kRowsRegsConvert = 96, kRowsRegsIssue = 80;
-static_assert(2 * kRowsRegsSoftmax + kRowsRegsConvert + kRowsRegsIssue <= 4 * 124, "a launch with 128 registers a thread has these to share out");
+constexpr int kRowsRegsLaunch = 124;
+static_assert(2 * kRowsRegsSoftmax + kRowsRegsConvert + kRowsRegsIssue <= 4 * kRowsRegsLaunch, "a launch has these to share out");
 constexpr int kRowsCost = 6;                              // what a unit's start and end take, in tiles of one row tile
 constexpr uint32_t kRowsOffV = kRowsK * kTileBytes, kRowsOffH = kRowsOffV + kRowsV * kTileBytes;
 constexpr uint32_t kRowsOffQ = kRowsOffH + kRowsH * 2 * kTileBytes, kRowsOffMisc = kRowsOffQ + 4 * kTileBytes;
@@ -130,12 +131,86 @@ template <int MODE> struct RowsWork {
     }
 };
 
+// ---- parts of split units
+
+// Which CTA has a position, where each has `share` of them.  (A 32-bit division where that will do.)
+__device__ __forceinline__ int cta_of(long long pos, long long share) {
+    return pos < (1LL << 31) && share < (1LL << 31) ? (int)((uint32_t)pos / (uint32_t)share) : (int)(pos / share);
+}
+// A column's partial result: Mu, the sum, 128 channels divided by it.
+struct PartColumn { const float *mu, *sum, *o; };
+__device__ __forceinline__ PartColumn SlotColumn(const float *slot, int qc, int c) { return {slot + c, slot + qc + c, slot + 2 * qc + (size_t)c * kHeadDim}; }
+
+// N columns' results from their n parts, four channels a lane: sum_i l_i 2^(m_i - m) o_i / sum_i l_i 2^(m_i - m).  32 parts at a time: a lane has the
+// statistics of one, all have every one's output; eight parts' outputs are on their way together.
+template <int N, typename Part>
+__device__ __forceinline__ void gather_parts(Part part, int n, int lane, float4 (&o)[N]) {
+    float mu[N], sum[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) { mu[k] = kMuNone; sum[k] = 0.f; o[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int here = min(32, n - i0);
+        float w[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float m = kMuNone, l = 0.f;
+            if (lane < here) {
+                const PartColumn p = part(i0 + lane, k);
+                m = *p.mu;
+                l = *p.sum;
+            }
+            const float top = fmaxf(mu[k], warp_max(m)), back = ex2(mu[k] - top);
+            w[k] = l * ex2(m - top);
+            float all = w[k];
+#pragma unroll
+            for (int s = 16; s; s >>= 1) all += __shfl_xor_sync(0xffffffffu, all, s);
+            sum[k] = sum[k] * back + all;
+            o[k] = make_float4(o[k].x * back, o[k].y * back, o[k].z * back, o[k].w * back);
+            mu[k] = top;
+        }
+        for (int i = 0; i < here; i += 8) {
+            float4 x[N][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k][j] = i + j < here ? load4(part(i0 + i + j, k).o + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float f = __shfl_sync(0xffffffffu, w[k], (i + j) & 31);
+                    if (i + j < here) o[k] = make_float4(fmaf(x[k][j].x, f, o[k].x), fmaf(x[k][j].y, f, o[k].y), fmaf(x[k][j].z, f, o[k].z), fmaf(x[k][j].w, f, o[k].w));
+                }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float inv = sum[k] == 0.f ? 0.f : __frcp_rn(sum[k]);
+        o[k] = sum[k] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv);
+    }
+}
+
+// What FORM 1 does with the maps of a head (k_page_diff.cuh).
+struct DiffArgs {
+    const float *maps;                                    // [n_tokens][n_q_heads][2][128]
+    const float *lam, *gain;                              // [n_q_heads]; [128] or NULL
+    void *out;
+    const int32_t *q_start;                               // may be NULL: every row is a token
+    int n_tokens, B, HQ;
+    float eps;
+};
+// 1 / sqrt(mean(o^2) + eps) from the sum of squares: a row of zeros stays one without eps, NaN stays NaN.
+__device__ __forceinline__ float diff_norm(float squares, float eps) {
+    const float m = squares * (1.0f / kHeadDim) + eps;
+    return m > 0.f ? rsqrtf(m) : m;
+}
+
 template <int MODE, int FORM>
 __global__ void __launch_bounds__(kRowsThreads, 1)
-k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a) {
+k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttnArgs a, const DiffArgs diff) {
     using namespace umma;
     using T = __nv_bfloat16;
-    using Out = std::conditional_t<MODE >= 3 || FORM == 1, float, T>;
+    static_assert((MODE >= 3) == (FORM == 0), "rows of new tokens are differential attention's, rows that share pages softmax attention's");
     constexpr int kSoftmax = 256, kWarpTma = 12, kWarpScores = 13, kWarpOutput = 14;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -547,12 +622,15 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 // what the first term leaves of an element above 2^-6 has three significant bits (bf16's eight less its four, and a sign), which
                 // e5m2 holds; of smaller ones e5m2's rounding is at most 2^-14
                 uint8_t *at = gbase + q_off(c >> 7);
+                uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0, n0 = x0, n1 = x0;
+                if (there) { n0 = from[0]; n1 = from[1]; }
 #pragma unroll 1
-                for (int k = 0; k < 8; ++k) {              // 16 channels
+                for (int k = 0; k < 8; ++k) {              // 16 channels, the next ones on their way
                     uint32_t c1[4] = {0u, 0u, 0u, 0u}, c2[4] = {0u, 0u, 0u, 0u};
                     if (there && (FORM != 1 || k >> 2 == half)) {
-                        const int k0 = FORM == 1 ? k & 3 : k;
-                        const uint4 x0 = from[2 * k0], x1 = from[2 * k0 + 1];
+                        const int next = FORM == 1 ? (k & 3) + 1 : k + 1;
+                        x0 = n0; x1 = n1;
+                        if (2 * next < kLoads) { n0 = from[2 * next]; n1 = from[2 * next + 1]; }
                         const uint32_t u[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {      // 4 channels
@@ -591,8 +669,19 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sread(g));
                 };
+                // The two warps of a scheduler take turns with the exponentials: side by side they would both wait for the unit, and then both for the
+                // tensor cores.  Item q of the second warpgroup follows item q of the first
+                const int other = 2 * tiles_of_group(s, g ^ 1);
+                auto turn_begin = [&]() {
+                    if (g == 1 || (q > 0 && q - 1 < other)) softmax_bar(4 + 2 * (warp & 3) + g, 64);
+                };
+                auto turn_end = [&]() {
+                    if (g == 0 ? q < other : q + 1 < other) asm volatile("barrier.cta.arrive %0, %1;" ::"r"(5 + 2 * (warp & 3) - g), "r"(64) : "memory");
+                };
                 if (!warp_on) {
                     scores_read();
+                    turn_begin();
+                    turn_end();
                 } else {
                     float raw[2][32];
                     tmem_ld<32>(ts, raw[0]);
@@ -674,6 +763,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                         return sum;
                     };
+                    turn_begin();
                     for (bool again = false;; again = true) {
                         const float sum = plain ? weights(std::false_type{}) : weights(std::true_type{});
                         // beyond what f16 holds, or no reference yet: Mu is raised, and the weights once more
@@ -696,6 +786,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         l = make_float2(l.x * f, l.y * f);
                         if (q > 0 && __any_sync(0xffffffffu, f != 1.f)) rescale(f);
                     }
+                    turn_end();
                     l = add2(l, l_half);
                     tmem_st_wait();
                 }
@@ -728,7 +819,10 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             const bool whole = MODE == 2 || MODE == 4 || (s.t0 == 0 && s.t1 == s.tiles);
             const bool on = c < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 + tok < a.n_tokens && s.h < a.H);
             const SharedParts parts(a.ws, a.blocks, a.B, a.H * a.G, s.own);
-            const size_t out_row = ((size_t)(s.tok0 + tok) * a.H + s.h) * a.G + (c - tok * a.G);
+            auto row_of = [&](int col) {                   // of [n_tokens][H][G]
+                const int k = col * a.inv_g >> 16;
+                return ((size_t)(s.tok0 + k) * a.H + s.h) * a.G + (col - k * a.G);
+            };
             float *slot = nullptr;
             if (!whole) {
                 const size_t head = MODE == 3 ? shared_meta_bytes(a.blocks, (size_t)a.B * a.H * a.G) : attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
@@ -737,49 +831,121 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             if (on && (two || g == 0)) {
                 const float m = sum == 0.f ? kMuNone : mu;
                 if (!whole) { slot[c] = m; slot[kRowsQC + c] = sum; }
-                else if (MODE >= 3) parts.stat[out_row] = make_float2(m, sum);
+                else if (MODE >= 3) parts.stat[row_of(c)] = make_float2(m, sum);
             }
             // (MODE 1: where the join finds the unit's parts: as many positions as lie between its first tile's and its last one's)
             if (MODE == 1 && s.t0 > 0 && tid == 0) reinterpret_cast<CtaMeta *>(a.ws + 16)[blockIdx.x] = CtaMeta{s.first, (s.tiles - 1) * s.weight + 1, s.tok0, s.n_cols, s.h};
             const int *first = nan_first + (seg & 3u) * 128;
+            // 16 channels of this row
+            auto result = [&](int d, float(&o)[16]) {
+                tmem_ld<16>((two ? to : tmem_o(0) + lane_addr) + d, o);
+                tmem_ld_done<16>(o);
+                if (!two && s.t1 - s.t0 > 1) {
+                    float o1[16];
+                    tmem_ld<16>(tmem_o(1) + lane_addr + d, o1);
+                    tmem_ld_done<16>(o1);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = (f[0] == 0.f ? 0.f : o[e] * f[0]) + (f[1] == 0.f ? 0.f : o1[e] * f[1]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = f[0] == 0.f ? 0.f : o[e] * f[0];             // no token: zero
+                }
+                if (MODE == 1 || MODE == 2) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const int4 at = *reinterpret_cast<const int4 *>(first + d + e);
+                        if (lim > at.x) o[e] = __uint_as_float(0x7fffffffu);
+                        if (lim > at.y) o[e + 1] = __uint_as_float(0x7fffffffu);
+                        if (lim > at.z) o[e + 2] = __uint_as_float(0x7fffffffu);
+                        if (lim > at.w) o[e + 3] = __uint_as_float(0x7fffffffu);
+                    }
+                }
+            };
             const int d0 = two ? 0 : g * 64, d1 = two ? kHeadDim : d0 + 64;
-            Out *to_row = (MODE >= 3 ? reinterpret_cast<Out *>(parts.o) : static_cast<Out *>(a.out)) + out_row * kHeadDim;
-            float *to_part = whole ? nullptr : slot + 2 * kRowsQC + (size_t)c * kHeadDim;
-            if ((c & ~31) < s.n_cols)
+            if (FORM == 1 && whole) {
+                // the two maps of a head are rows of neighbouring threads: their difference, its norm (over two warpgroups' channels, where they have
+                // half each), and the head's output
+                const bool second = lane & 1;
+                const float lam = on ? diff.lam[s.h * (a.G >> 1) + ((c - tok * a.G) >> 1)] : 0.f;
+                auto difference = [&](int d, float(&o)[16]) {
+                    result(d, o);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = __shfl_xor_sync(0xffffffffu, o[e], 1);
+                        o[e] = second ? fmaf(-lam, o[e], x) : fmaf(-lam, x, o[e]);
+                    }
+                };
+                float squares = 0.f;
+                if (diff.gain != nullptr) {
+                    if (warp_on)
+#pragma unroll 1
+                        for (int d = d0; d < d1; d += 16) {
+                            float o[16];
+                            difference(d, o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) squares = fmaf(o[e], o[e], squares);
+                        }
+                    if (!two) {
+                        softmax_bar(1, kSoftmax);          // (row_cs has been read)
+                        row_cs[g * 128 + row] = squares;
+                        softmax_bar(1, kSoftmax);
+                        squares = row_cs[row] + row_cs[128 + row];
+                    }
+                }
+                const float r = diff_norm(squares, diff.eps);
+                T *out = static_cast<T *>(diff.out) + (row_of(c) >> 1) * kHeadDim;
+                if (warp_on)
+#pragma unroll 1
+                    for (int d = d0; d < d1; d += 16) {
+                        float o[16];
+                        difference(d, o);
+                        if (!on) continue;
+                        if (diff.gain != nullptr) {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 w = load4(diff.gain + d + e);
+                                o[e] *= r * w.x; o[e + 1] *= r * w.y; o[e + 2] *= r * w.z; o[e + 3] *= r * w.w;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; e += 4)     // half of them each
+                            store4(out + d + (second ? 8 : 0) + e, second ? make_float4(o[8 + e], o[9 + e], o[10 + e], o[11 + e]) : make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]));
+                    }
+            } else if (two) {
+                // 64 channels at a time through this warpgroup's rows of q, so that what is written together lies together
+                uint8_t *stage = gbase + q_off(g);
+                float *dst = whole ? parts.o : slot + 2 * kRowsQC;
+#pragma unroll 1
+                for (int part = 0; part < 2; ++part) {
+                    if (warp_on)
+#pragma unroll 1
+                        for (int d = 0; d < 64; d += 16) {
+                            float o[16];
+                            result(64 * part + d, o);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                *reinterpret_cast<float4 *>(stage + row * 256 + (((d >> 2) + e) ^ (row & 15)) * 16) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                    softmax_bar(12 + g, 128);
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = i * 8 + (row >> 4), k = row & 15, col = g * 128 + r;
+                        if (col < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, whole || slot != nullptr))
+                            *reinterpret_cast<float4 *>(dst + (whole ? row_of(col) : (size_t)col) * kHeadDim + 64 * part + 4 * k) = *reinterpret_cast<const float4 *>(stage + r * 256 + (k ^ (r & 15)) * 16);
+                    }
+                    softmax_bar(12 + g, 128);
+                }
+            } else if (warp_on) {
+                float *dst = (whole ? parts.o + row_of(c) * kHeadDim : slot + 2 * kRowsQC + (size_t)c * kHeadDim);
 #pragma unroll 1
                 for (int d = d0; d < d1; d += 16) {
                     float o[16];
-                    tmem_ld<16>((two ? to : tmem_o(0) + lane_addr) + d, o);
-                    tmem_ld_done<16>(o);
-                    if (!two && s.t1 - s.t0 > 1) {
-                        float o1[16];
-                        tmem_ld<16>(tmem_o(1) + lane_addr + d, o1);
-                        tmem_ld_done<16>(o1);
+                    result(d, o);
+                    if (on)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = (f[0] == 0.f ? 0.f : o[e] * f[0]) + (f[1] == 0.f ? 0.f : o1[e] * f[1]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = f[0] == 0.f ? 0.f : o[e] * f[0];         // no token: zero
-                    }
-                    if (MODE == 1 || MODE == 2) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const int4 at = *reinterpret_cast<const int4 *>(first + d + e);
-                            if (lim > at.x) o[e] = __uint_as_float(0x7fffffffu);
-                            if (lim > at.y) o[e + 1] = __uint_as_float(0x7fffffffu);
-                            if (lim > at.z) o[e + 2] = __uint_as_float(0x7fffffffu);
-                            if (lim > at.w) o[e + 3] = __uint_as_float(0x7fffffffu);
-                        }
-                    }
-                    if (on) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const float4 x = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                            if (whole) store4(to_row + d + e, x);
-                            else store4(to_part + d + e, x);
-                        }
-                    }
+                        for (int e = 0; e < 16; e += 4) store4(dst + d + e, make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]));
                 }
+            }
             tc_fence_before();
             softmax_bar(1, kSoftmax);                      // q, exch and O are free for the next segment
         }

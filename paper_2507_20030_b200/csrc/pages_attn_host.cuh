@@ -63,8 +63,9 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
     const dim3 grid = MODE == 0 ? dim3(p.ctas0) : MODE == 1 ? dim3(p.ctas1) : dim3(p.blocks, a.H);
     CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
     if (int r = launch_check(pg, "k_page_attn")) return r;
-    if (MODE == 2 || p.max_tiles == 1) return FAEDKV_OK;                     // no unit is ever in parts
-    if constexpr (MODE != 2) {
+    if (MODE == 2 || p.max_tiles == 1 ) return FAEDKV_OK;                     // no unit is ever in parts
+    if constexpr (MODE == 0 && FORM == 1) return FAEDKV_OK;                   // the caller puts the parts together
+    else if constexpr (MODE != 2) {
         const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 16;
         const dim3 jgrid((unsigned)(MODE == 0 ? a.B * a.H : p.ctas1), (cols + each - 1) / each);
         CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<Out, MODE>, jgrid, dim3(kHeadDim, pages::kJoinGroups), 0, st, a, (int)C::QC,
@@ -89,26 +90,18 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
 }
 
 template <int MODE, int FORM>
-int launch_rows(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, dim3 grid, int attr_bit, cudaStream_t st) {
+int launch_rows(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const pages::DiffArgs &diff, dim3 grid,
+                int attr_bit, cudaStream_t st) {
     auto kernel = pages::k_page_rows<MODE, FORM>;
     if (!(pg->attr_set & (1u << attr_bit))) {
+        cudaFuncAttributes f;                              // the kernel shares its registers out anew: it would wait for ones that the launch has not
+        CUDA_TRY(pg, cudaFuncGetAttributes(&f, kernel));
+        if (f.numRegs < pages::kRowsRegsLaunch) return fail(pg, FAEDKV_ERR_CUDA, "k_page_rows was built with %d registers", f.numRegs);
         CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pages::kRowsSmem));
         pg->attr_set |= 1u << attr_bit;
     }
-    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(pages::kRowsThreads), pages::kRowsSmem, st, mk, mv, a));
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(pages::kRowsThreads), pages::kRowsSmem, st, mk, mv, a, diff));
     return launch_check(pg, "k_page_rows");
-}
-
-template <int FORM>
-int dispatch_rows(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const AttnPlan &p, int bit, cudaStream_t st) {
-    if (!p.shared) return launch_rows<2, FORM>(pg, mk, mv, a, dim3(p.blocks, a.H), bit, st);
-    if (int r = launch_rows<1, FORM>(pg, mk, mv, a, dim3(p.ctas1), bit + 1, st)) return r;
-    if (p.max_tiles == 1) return FAEDKV_OK;                                  // no unit is ever in parts
-    using Out = std::conditional_t<FORM == 1, float, __nv_bfloat16>;
-    const int cols = p.qc / a.G * a.G, each = 16;
-    CUDA_TRY(pg, launch_pdl(pages::k_page_attn_join<Out, 1>, dim3((unsigned)p.ctas1, (cols + each - 1) / each), dim3(kHeadDim, pages::kJoinGroups), 0,
-                            st, a, p.qc, each, p.ctas1));
-    return launch_check(pg, "k_page_attn_join");
 }
 
 // The instance for a call: by type, new tokens, and how many blocks they make.  bit: the first of eight in attr_set.
