@@ -5,52 +5,77 @@
 namespace {
 
 struct SharedPlan {
-    int tq, blocks, ctas;    // rows of a shared block; blocks of rows, at most; CTAs
+    struct Launch {
+        int which, qc, n_shared, blocks, ctas;
+        bool rows;           // query columns as rows, 256 of them; else 8 columns
+        size_t head, slots;  // bytes of the header, of the partial results
+    } launch[2];
+    int n;                   // launches: one for all blocks, or one for the groups' and one for the rows' own
     bool spread;             // blocks few enough for their tiles to be shared out evenly (MODE 3); else a CTA each (MODE 4)
-    size_t bytes;
+    size_t whole, bytes;
 };
 
-// bf16: query columns as rows, 256 of them; float32: 8 columns.
 SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
     const faedkv_pages_config &c = pg->cfg;
-    const bool rows = c.kv_dtype == FAEDKV_BF16;
-    const int qc = rows ? pages::kRowsQC : DecodeF32::QC;
     SharedPlan p{};
-    p.tq = qc / pg->gq;
-    p.blocks = pages::shared_blocks(batch, n_groups, p.tq) + batch;
+    // groups of more than 32 query columns on average: the form with rows for what they share, eight columns for what each has behind it.  (Of that,
+    // a row has a few columns only, and a unit's start and end in the form with rows take as long as five tiles.)
+    p.n = c.kv_dtype == FAEDKV_BF16 && (long long)batch * pg->gq > 32LL * n_groups ? 2 : 1;
     const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
-    p.spread = p.blocks <= pages::kMaxBlocks && p.blocks * (2 * max_tiles + pages::kUnitCost) < (1LL << 31);
-    const long long most = (long long)pg->n_sm * (rows ? 1 : DecodeF32::CTAS), tiles = max_tiles * p.blocks * c.n_kv_heads;
-    p.ctas = (int)(tiles < most ? tiles : most);
-    p.bytes = pages::shared_meta_bytes(p.blocks, (size_t)batch * c.n_q_heads) +
-              (p.spread ? (size_t)p.ctas * 2 * pages::attn_slot_floats(qc) * sizeof(float) : 0);
+    p.spread = true;
+    for (int i = 0; i < p.n; ++i) {
+        SharedPlan::Launch &u = p.launch[i];
+        u.which = p.n == 1 ? 3 : 1 + i;
+        u.rows = p.n == 2 && i == 0;
+        u.qc = u.rows ? pages::kRowsQC : 8;
+        u.n_shared = u.which & 1 ? pages::shared_blocks(batch, n_groups, u.qc / pg->gq) : 0;
+        u.blocks = u.n_shared + (u.which & 2 ? batch : 0);
+        u.head = pages::shared_before_bytes(u.blocks);
+        p.spread = p.spread && u.blocks <= pages::kMaxBlocks && u.blocks * (2 * max_tiles + pages::kUnitCost) < (1LL << 31);
+        const long long most = (long long)pg->n_sm * (u.rows ? 1 : kDecodeCtas), tiles = max_tiles * u.blocks * c.n_kv_heads;
+        u.ctas = (int)(tiles < most ? tiles : most);
+        u.slots = (size_t)u.ctas * 2 * pages::attn_slot_floats(u.qc) * sizeof(float);
+    }
+    p.whole = pages::shared_whole_bytes((size_t)batch * c.n_q_heads);
+    p.bytes = p.whole;
+    for (int i = 0; i < p.n; ++i) p.bytes += p.launch[i].head + (p.spread ? p.launch[i].slots : 0);
     return p;
 }
 
-template <typename T, int MODE>
-int launch_join(faedkv_pages *pg, const pages::AttnArgs &a, int qc, int ctas, cudaStream_t st) {
-    CUDA_TRY(pg, launch_pdl(pages::k_page_join_shared<T, MODE>, dim3((unsigned)(((long long)a.B * a.H * a.G + 7) / 8)), dim3(256), 0, st, a, qc,
-                            qc == pages::kRowsQC, ctas));
-    return launch_check(pg, "k_page_join_shared");
+template <typename C, int MODE>
+int launch_few(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, dim3 grid, int attr_bit, cudaStream_t st) {
+    auto kernel = pages::k_page_attn<C, MODE, 0>;
+    constexpr uint32_t smem = C::kSmemBytes + (MODE == 3 ? C::kSmemBlocks : 0);
+    if (!(pg->attr_set & (1u << attr_bit))) {
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        pg->attr_set |= 1u << attr_bit;
+    }
+    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
+    return launch_check(pg, "k_page_attn");
 }
 
 template <int MODE>
-int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, const pages::AttnArgs &a, const SharedPlan &p, cudaStream_t st) {
-    const dim3 grid = MODE == 3 ? dim3(p.ctas) : dim3(p.blocks, a.H);
-    if (pg->cfg.kv_dtype == FAEDKV_BF16) {
-        if (int r = launch_rows<MODE, 0>(pg, mk, mv, a, pages::DiffArgs{}, grid, 16 + MODE, st)) return r;
-        return launch_join<__nv_bfloat16, MODE>(pg, a, pages::kRowsQC, p.ctas, st);
+int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, pages::AttnArgs a, const SharedPlan &p, cudaStream_t st) {
+    unsigned char *at = a.ws + p.whole;
+    a.whole = reinterpret_cast<float *>(a.ws);
+    const bool f32 = pg->cfg.kv_dtype == FAEDKV_F32;
+    pages::SharedLaunch done[2];
+    for (int i = 0; i < p.n; ++i) {
+        const SharedPlan::Launch &u = p.launch[i];
+        a.which = u.which;
+        a.blocks = u.blocks;
+        a.ws = at;
+        a.slots = reinterpret_cast<float *>(at + u.head);
+        at += u.head + (p.spread ? u.slots : 0);
+        const dim3 grid = MODE == 3 ? dim3(u.ctas) : dim3(u.blocks, a.H);
+        if (int r = u.rows ? launch_rows<MODE, 0>(pg, mk, mv, a, pages::DiffArgs{}, grid, 13 + MODE, st)
+                    : f32  ? launch_few<DecodeF32, MODE>(pg, mk, mv, a, grid, 15 + MODE, st)
+                           : launch_few<DecodeBf16, MODE>(pg, mk, mv, a, grid, 17 + MODE, st)) return r;
+        done[i] = {a.ws, a.slots, u.qc, u.rows ? pages::kRowsCost : pages::kUnitCost, u.rows, u.ctas, u.n_shared, u.blocks};
     }
-    using C = DecodeF32;
-    auto kernel = pages::k_page_attn<C, MODE, 0>;
-    constexpr uint32_t smem = C::kSmemBytes + (MODE == 3 ? C::kSmemBlocks : 0);
-    if (!(pg->attr_set & (1u << (18 + MODE)))) {
-        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        pg->attr_set |= 1u << (18 + MODE);
-    }
-    CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
-    if (int r = launch_check(pg, "k_page_attn")) return r;
-    return launch_join<float, MODE>(pg, a, C::QC, p.ctas, st);
+    auto join = f32 ? pages::k_page_join_shared<float, MODE> : pages::k_page_join_shared<__nv_bfloat16, MODE>;
+    CUDA_TRY(pg, launch_pdl(join, dim3((unsigned)(((long long)a.B * a.H * a.G + 7) / 8)), dim3(256), 0, st, a, done[0], done[p.n - 1]));
+    return launch_check(pg, "k_page_join_shared");
 }
 
 }  // namespace
@@ -87,9 +112,9 @@ int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, co
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const SharedPlan p = plan_shared(pg, batch, n_groups);
     const pages::AttnArgs a{q, out, nullptr, kv_len, table, k_scale, v_scale, ld_q, batch, batch, c.n_kv_heads, pg->gq, c.max_pages,
-                            c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
+                            c.n_pages, pg->page_shift, 0, 65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile, group_start, shared_len,
-                            n_groups};
+                            n_groups, 0, nullptr, nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return p.spread ? launch_shared<3>(pg, mk, mv, a, p, st) : launch_shared<4>(pg, mk, mv, a, p, st);
 }

@@ -101,8 +101,11 @@ struct AttnArgs {
     unsigned int *status;
     unsigned long long wait_limit;                        // ns, of a bounded wait
     int withhold;                                         // test hook: the tile (from 1) whose weights are not announced; 0: none
-    const int32_t *group_start, *shared_len;              // MODE 3 and 4: groups of rows, and the tokens that the rows of each share
-    int n_groups;
+    // MODE 3 and 4: groups of rows, and the tokens that the rows of each share; which blocks the launch has (1 those of groups, 2 the rows' own);
+    // results of whole units by query row, partial ones by CTA
+    const int32_t *group_start, *shared_len;
+    int n_groups, which;
+    float *whole, *slots;
 };
 
 // Workspace of MODE 0 and 1: header, records, two partial results per CTA (of the unit it goes on with, of the one it leaves).
@@ -112,20 +115,17 @@ __host__ __device__ constexpr size_t attn_meta_bytes(int mode, size_t units, siz
     return 16 + (mode == 0 ? sizeof(UnitMeta) * units : (sizeof(CtaMeta) * ctas + 15) / 16 * 16);
 }
 __host__ __device__ constexpr size_t attn_slot_floats(int qc) { return (size_t)qc * (kHeadDim + 2); }
-// Workspace of MODE 3 and 4: header, prefix sums of the blocks' sizes, results of whole units by query row (cols of them: rows x heads), first
-// those of the shared blocks, then those of the rows' own; MODE 3 two partial results per CTA behind them.
+// Workspace of MODE 3 and 4: for each launch a header with the prefix sums of its blocks' sizes, and (MODE 3) two partial results per CTA; for the call
+// the results of whole units by query row (cols of them: rows x heads), first those of the groups' blocks, then those of the rows' own.
 __host__ __device__ constexpr size_t shared_before_bytes(int blocks) { return 16 + ((size_t)blocks + 4) / 4 * 16; }
-__host__ __device__ constexpr size_t shared_meta_bytes(int blocks, size_t cols) {
-    return shared_before_bytes(blocks) + 2 * cols * (sizeof(float2) + sizeof(float) * kHeadDim);
-}
+__host__ __device__ constexpr size_t shared_whole_bytes(size_t cols) { return 2 * cols * (sizeof(float2) + sizeof(float) * kHeadDim); }
 struct SharedParts {
     float2 *stat;                                         // Mu and the sum
     float *o;
-    __device__ __forceinline__ SharedParts(unsigned char *ws, int blocks, int B, int heads, int own) {
-        const size_t cols = (size_t)B * heads;
-        float2 *s = reinterpret_cast<float2 *>(ws + shared_before_bytes(blocks));
+    __device__ __forceinline__ SharedParts(float *whole, size_t cols, int own) {
+        float2 *s = reinterpret_cast<float2 *>(whole);
         stat = s + own * cols;
-        o = reinterpret_cast<float *>(s + 2 * cols) + own * cols * kHeadDim;
+        o = whole + 4 * cols + own * cols * kHeadDim;
     }
 };
 
@@ -329,7 +329,7 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int tq, int v, boo
 }
 
 // MODE 3 and 4, a decode step of rows that share pages: first blocks of a group's rows over the tokens that it shares, then for each row
-// a block of its own over those behind.  The blocks of rows are numbered as above; row b's own is shared_blocks() + b.
+// a block of its own over those behind, or only the ones or the others.  The blocks of rows are numbered as above; row b's own is the b-th behind them.
 // The whole pages that row b shares with its group, in tokens: none for the only row of a group, for one that is shorter than what its
 // group shares, and for one that stands in no group.  g, first: the group, its first row.
 __device__ __forceinline__ int shared_of(const AttnArgs &a, int b, int live, bool report, int &g, int &first) {
@@ -354,7 +354,7 @@ __device__ __forceinline__ int shared_of(const AttnArgs &a, int b, int live, boo
 }
 __host__ __device__ __forceinline__ int shared_blocks(int B, int n_groups, int tq) { return B / tq + n_groups; }
 __device__ __forceinline__ bool find_shared(const AttnArgs &a, int tq, int v, bool report, Block &k) {
-    const int n_shared = shared_blocks(a.B, a.n_groups, tq);
+    const int n_shared = a.which & 1 ? shared_blocks(a.B, a.n_groups, tq) : 0;
     int g, first;
     if (v >= n_shared) {
         const int b = v - n_shared, live = (int)clamp_len(a, b, report), n = shared_of(a, b, live, report, g, first);
@@ -1197,7 +1197,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             const bool whole = MODE == 2 || MODE == 4 || (s.t0 == 0 && s.t1 == s.tiles);
             float *slot = nullptr;
             // MODE 3 and 4: a whole unit's columns beside the rows that they belong to, for the join
-            const SharedParts parts(a.ws, a.blocks, a.B, a.H * a.G, s.own);
+            const SharedParts parts(a.whole, (size_t)a.B * a.H * a.G, s.own);
             if (MODE >= 3 && whole) {
                 for (int c = tid; c < n_cols; c += kSoftmax) {
                     const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
@@ -1207,8 +1207,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
             }
             if (!whole) {
-                const size_t head = MODE == 3 ? shared_meta_bytes(a.blocks, (size_t)a.B * a.H * a.G) : attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
-                slot = reinterpret_cast<float *>(a.ws + head) + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(QC);
+                float *slots = MODE == 3 ? a.slots : reinterpret_cast<float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x));
+                slot = slots + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(QC);
                 for (int c = tid; c < n_cols; c += kSoftmax) {
                     const float sum = red[c] + red[QC + c] + red[2 * QC + c] + red[3 * QC + c];
                     slot[c] = sum == 0.f ? kMuNone : -mu_at(c);

@@ -818,15 +818,15 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
             const bool whole = MODE == 2 || MODE == 4 || (s.t0 == 0 && s.t1 == s.tiles);
             const bool on = c < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 + tok < a.n_tokens && s.h < a.H);
-            const SharedParts parts(a.ws, a.blocks, a.B, a.H * a.G, s.own);
+            const SharedParts parts(a.whole, (size_t)a.B * a.H * a.G, s.own);
             auto row_of = [&](int col) {                   // of [n_tokens][H][G]
                 const int k = col * a.inv_g >> 16;
                 return ((size_t)(s.tok0 + k) * a.H + s.h) * a.G + (col - k * a.G);
             };
             float *slot = nullptr;
             if (!whole) {
-                const size_t head = MODE == 3 ? shared_meta_bytes(a.blocks, (size_t)a.B * a.H * a.G) : attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x);
-                slot = reinterpret_cast<float *>(a.ws + head) + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(kRowsQC);
+                float *slots = MODE == 3 ? a.slots : reinterpret_cast<float *>(a.ws + attn_meta_bytes(MODE, (size_t)a.B * a.H, gridDim.x));
+                slot = slots + ((size_t)blockIdx.x * 2 + (s.t0 > 0 ? 0 : 1)) * attn_slot_floats(kRowsQC);
             }
             if (on && (two || g == 0)) {
                 const float m = sum == 0.f ? kMuNone : mu;
