@@ -525,7 +525,7 @@ int faedkv_pages_load(faedkv_pages *pg, const int32_t *kv_len, const int32_t *ta
  * row dst[i] held is forgotten, not given back.  src[i] < 0: nothing is done.  A row outside the batch, a dst that is also a src
  * of the call, and a dst that an earlier fork names are refused (nothing is done, status 0x106).  Pages that are not dst's fresh one are
  * only read; table entries behind a row's last page are left as they were.  *n_free_out is the new height of the stack; it may be
- * n_free.  ws: faedkv_pages_fork_bytes() (0 for arguments that the call would refuse), overwritten, 4-byte aligned. */
+ * n_free.  ws: faedkv_pages_fork_bytes(), overwritten, 4-byte aligned (NULL where that is 0). */
 size_t faedkv_pages_fork_bytes(const faedkv_pages *pg, int batch, int n_forks);
 int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, const int32_t *len, int n_forks, int batch,
                       int32_t *kv_len, int32_t *table, const int32_t *free_pages, const int32_t *n_free, int32_t *n_free_out,

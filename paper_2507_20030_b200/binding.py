@@ -692,8 +692,9 @@ class Pages:
                 need("kv_len", kv_len, i32, (batch,)), need("table", table, i32, (batch, self.max_pages)),
                 need("free_pages", free_pages, i32, self._pool_shape), need("n_free", n_free, i32, (1,)),
                 need("n_free_out", n_free_out, i32, (1,)), *self._cache(k_pages, v_pages, k_scale, v_scale))
-        w = self._workspace(ws, 4 * (n + batch), stream)   # faedkv_pages_fork_bytes()
-        self._check(self._lib.faedkv_pages_fork(self._h, *args, w.data_ptr(), self._on(stream)))
+        nbytes = self._bytes("faedkv_pages_fork_bytes", batch, n)
+        w = self._workspace(ws, nbytes, stream) if nbytes else None
+        self._check(self._lib.faedkv_pages_fork(self._h, *args, None if w is None else w.data_ptr(), self._on(stream)))
 
     def release(self, t_len, n_new, table, free_pages, n_free, kv_len, n_free_out, ws=None, stream=None):
         """Requests with n_new < 0 give back the pages that no other request names."""

@@ -12,13 +12,17 @@ int check_table(faedkv_pages *pg, int batch) {
     return FAEDKV_OK;
 }
 
+// Up to this many forks and rows the CTAs that copy find out for themselves what comes before them.  (16 rows forked into 256: 10 us with a plan in
+// one CTA before the copies.)
+bool forks_alone(int batch, int n_forks) { return n_forks <= pages::kForkSmall && batch <= pages::kForkRows; }
+
 }  // namespace
 
 extern "C" {
 
 size_t faedkv_pages_fork_bytes(const faedkv_pages *pg, int batch, int n_forks) {
     if (pg == nullptr || batch < 1 || batch > pg->cfg.max_batch || n_forks < 0 || n_forks > batch) return 0;
-    return sizeof(int32_t) * ((size_t)n_forks + batch);
+    return forks_alone(batch, n_forks) ? 0 : sizeof(int32_t) * ((size_t)n_forks + batch);
 }
 
 int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, const int32_t *len, int n_forks, int batch,
@@ -30,7 +34,7 @@ int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, 
     if (n_forks < 0 || n_forks > batch) return fail(pg, FAEDKV_ERR_SHAPE, "n_forks = %d outside [0, batch=%d]", n_forks, batch);
     if (((src == nullptr || dst == nullptr) && n_forks > 0) || kv_len == nullptr || table == nullptr || free_pages == nullptr ||
         n_free == nullptr || n_free_out == nullptr || k_pages == nullptr || v_pages == nullptr || k_scale == nullptr ||
-        v_scale == nullptr || ws == nullptr)
+        v_scale == nullptr || (ws == nullptr && !forks_alone(batch, n_forks)))
         return fail(pg, FAEDKV_ERR_INVALID_ARG, "NULL tensor passed to faedkv_pages_fork");
     if (int r = check_align(pg, {k_pages, v_pages, k_scale, v_scale}, {src, dst, len, kv_len, table, free_pages, n_free, n_free_out, ws})) return r;
     const DeviceGuard guard(pg);
@@ -40,10 +44,21 @@ int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, 
     const pages::ForkArgs a{src, dst, len, free_pages, n_free, kv_len, table, n_free_out, static_cast<int32_t *>(ws),
                             {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
                             n_forks, batch, c.max_pages, c.n_kv_heads, c.n_pages, pg->page_shift, pg->dev_status};
+    if (forks_alone(batch, n_forks)) {
+        const bool in_place = n_free_out == n_free;        // its height may be written once all have read it
+        if (n_forks > 0) {
+            int parts = 4 * pg->n_sm / n_forks;            // of a fork's copy: four CTAs a SM in all
+            parts = parts < 1 ? 1 : parts > 2 * c.n_kv_heads ? 2 * c.n_kv_heads : parts;
+            pages::k_page_fork<true><<<dim3(n_forks, parts), 256, 0, st>>>(a, !in_place);
+            if (int r = launch_check(pg, "k_page_fork")) return r;
+            if (!in_place) return FAEDKV_OK;
+        }
+        CUDA_TRY(pg, launch_pdl(pages::k_page_fork<false>, dim3(1), dim3(256), 0, st, a, true));
+        return launch_check(pg, "k_page_fork");
+    }
     pages::k_page_fork_plan<<<1, pages::kPlanThreads, 0, st>>>(a);
     if (int r = launch_check(pg, "k_page_fork_plan")) return r;
-    if (n_forks == 0) return FAEDKV_OK;
-    CUDA_TRY(pg, launch_pdl(pages::k_page_fork_copy, dim3(n_forks, 2 * c.n_kv_heads), dim3(256), 0, st, a));
+    CUDA_TRY(pg, launch_pdl(pages::k_page_fork_copy, dim3(n_forks), dim3(256), 0, st, a));
     return launch_check(pg, "k_page_fork_copy");
 }
 
@@ -64,9 +79,20 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     if (!guard.ok) return fail(pg, FAEDKV_ERR_CUDA, "cannot select device %d", pg->device);
     const pages::ReleaseArgs a{t_len, n_new, table, n_free, free_pages, kv_len, n_free_out, static_cast<int32_t *>(ws), batch,
                                pg->cfg.max_pages, pg->cfg.n_pages, pg->page_shift, pg->dev_status};
-    int parts = 1;                                         // warps of a row, where there are fewer rows than warps
-    while (parts < 32 && 2 * parts * batch <= pages::kCluster * pages::kPlanThreads / 32) parts *= 2;
-    pages::k_page_release<<<pages::kCluster, pages::kPlanThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, parts);
+    // parts of a row, a warp each: more than one where there are fewer rows than warps, or where that makes them short enough for registers
+    const int warps = pages::kCluster * pages::kPlanThreads / 32;
+    int parts = 1;
+    while (parts < 32 && 2 * parts * batch <= warps) parts *= 2;
+    int fits = parts;
+    while (fits < 32 && pg->cfg.max_pages > 256 * fits) fits *= 2;
+    const bool in_registers = pg->cfg.max_pages <= 256 * fits && fits * batch <= 4 * warps;
+    if (in_registers) parts = fits;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int each = !in_registers ? 0 : batch * parts <= warps ? 1 : batch * parts <= 2 * warps ? 2 : 4;
+    if (each == 1) pages::k_page_release_short<1><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
+    else if (each == 2) pages::k_page_release_short<2><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
+    else if (each == 4) pages::k_page_release_short<4><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
+    else pages::k_page_release<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
     return launch_check(pg, "k_page_release");
 }
 
@@ -91,7 +117,8 @@ int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, con
     const pages::CompactArgs a{kv_len, table, table_out, free_pages, n_free, new_id, static_cast<int32_t *>(ws),
                                {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
                                batch, c.max_pages, c.n_kv_heads, c.n_pages, pg->page_shift, pg->dev_status};
-    pages::k_page_compact_plan<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a);
+    if (c.n_pages <= pages::kCompactShort && (long long)batch * c.max_pages <= 16 * pages::kCompactShort) pages::k_page_compact_short<<<1, pages::kPlanThreads, 0, st>>>(a);
+    else pages::k_page_compact_plan<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a);
     if (int r = launch_check(pg, "k_page_compact_plan")) return r;
     CUDA_TRY(pg, launch_pdl(pages::k_page_move, dim3(pg->n_sm * 8), dim3(256), 0, st, a));
     return launch_check(pg, "k_page_move");

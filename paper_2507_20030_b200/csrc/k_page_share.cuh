@@ -47,48 +47,161 @@ struct ForkArgs {
     unsigned int *status;
 };
 
-// One CTA: which forks are done, their fresh pages, lengths.  A row that is both taken from and written, and all but the first
+// Tokens that fork i takes: none where it is refused (valid becomes false).
+__device__ __forceinline__ int fork_length(const ForkArgs &a, int i, int s, bool report) {
+    const long long cap = (long long)a.W << a.page_shift;
+    const int t = a.kv_len[s];
+    int n = t < 0 ? 0 : (int)min((long long)t, cap);
+    if (report && (t < 0 || t > cap)) flag(a.status, kBadLength);
+    if (a.len != nullptr) {
+        const int most = a.len[i];
+        if (report && most < 0) flag(a.status, kBadLength);
+        n = min(n, max(most, 0));
+    }
+    return n;
+}
+__device__ __forceinline__ bool fork_rows(const ForkArgs &a, int i, int &s, int &d) {
+    s = a.src[i];
+    d = a.dst[i];
+    return s >= 0 && s < a.B && d >= 0 && d < a.B;
+}
+
+// What is done for one fork, by `threads` of them in turn: the first entries of the table row, and the open page's rows (K and V of all heads).
+__device__ __forceinline__ void fork_copy(const ForkArgs &a, int s, int d, int n, int fresh, int tid, int threads) {
+    const int whole = n >> a.page_shift, rest = n & ((1 << a.page_shift) - 1);
+    const int32_t *from = a.table + (size_t)s * a.W;
+    int32_t *to = a.table + (size_t)d * a.W;
+    const int open = rest == 0 ? 0 : from[whole];
+    for (int p = tid; p < whole; p += threads) to[p] = from[p];
+    if (rest == 0 || !FAEDKV_IN_BOUNDS(kTagPageShare, whole < a.W && fresh >= 0 && fresh < a.n_pages)) return;
+    if (tid == 0) to[whole] = fresh;
+    if (open < 0 || open >= a.n_pages) {
+        if (tid == 0) flag(a.status, kBadPage);
+        return;
+    }
+    const size_t unit = (size_t)8 << a.page_shift;        // 16-byte pieces of a page of one head
+    const int each = rest * 8, all = 2 * a.H * each;       // < 2^23
+    const uint32_t inv = 0xffffffffu / (uint32_t)each + 1; // (u * inv >> 32 = u / each: u * each is less than 2^32 ...)
+    auto place = [&](int u, size_t &piece) {               // which tensor, and where in the page
+        int th = (int)__umulhi((uint32_t)u, inv);
+        if (th * each > u) --th;                           // (... but for the last rows of thousands of heads)
+        piece = (size_t)(th >> 1) * unit + (u - th * each);
+        return th & 1;
+    };
+    const size_t x0 = (size_t)open * a.H * unit, y0 = (size_t)fresh * a.H * unit;
+    for (int u0 = tid; u0 < all; u0 += 8 * threads) {
+        uint4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            size_t piece;
+            if (u0 + k * threads < all) v[k] = reinterpret_cast<const uint4 *>(place(u0 + k * threads, piece) ? a.codes[1] : a.codes[0])[x0 + piece];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            size_t piece;
+            if (u0 + k * threads < all) reinterpret_cast<uint4 *>(place(u0 + k * threads, piece) ? a.codes[1] : a.codes[0])[y0 + piece] = v[k];
+        }
+    }
+    for (int th = tid; th < 2 * a.H; th += threads) {
+        float *scale = th & 1 ? a.scale[1] : a.scale[0];
+        scale[(size_t)fresh * a.H + (th >> 1)] = scale[(size_t)open * a.H + (th >> 1)];
+    }
+}
+
+// Few forks among few rows: every CTA finds out for itself which forks before its own take a page; one launch, and no workspace.  Grid (forks, parts of
+// a fork's copy).  COPY = false, one CTA: the height of the stack alone, where it is written over the one that all have to read.
+constexpr int kForkSmall = 1024, kForkRows = 4096;
+template <bool COPY>
+static __global__ void __launch_bounds__(256) k_page_fork(const ForkArgs a, const bool height_too) {
+    __shared__ int32_t mark[kForkRows];                    // of a row: the first fork into it, -1 if one takes from it
+    __shared__ int counts[8];
+    if (!COPY) pdl_wait();
+    const int tid = threadIdx.x, me = COPY ? (int)blockIdx.x : a.n, page = 1 << a.page_shift;
+    const bool report = COPY && blockIdx.x == 0 && blockIdx.y == 0;
+    const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && report);
+    int src[kForkSmall / 256], dst[kForkSmall / 256];
+    bool valid[kForkSmall / 256];
+    for (int b = tid; b < a.B; b += 256) mark[b] = 0x7fffffff;
+#pragma unroll
+    for (int k = 0; k < kForkSmall / 256; ++k) {
+        const int i = tid + 256 * k;
+        valid[k] = i < a.n && fork_rows(a, i, src[k], dst[k]);
+        if (report && i < a.n && !valid[k] && src[k] >= 0) flag(a.status, kBadRow);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kForkSmall / 256; ++k)
+        if (valid[k]) {
+            atomicMin(mark + dst[k], tid + 256 * k);
+            atomicMin(mark + src[k], -1);
+        }
+    __syncthreads();
+    // pages that the forks before this CTA's take, and all
+    int before = 0, all = 0;
+#pragma unroll
+    for (int k = 0; k < kForkSmall / 256; ++k) {
+        const int i = tid + 256 * k;
+        if (!valid[k]) continue;
+        if (mark[dst[k]] != i) {
+            if (report) flag(a.status, kBadRow);
+            continue;
+        }
+        const bool need = (fork_length(a, i, src[k], report) & (page - 1)) != 0;
+        before += need && i < me;
+        all += need;
+    }
+    const int both = __reduce_add_sync(0xffffffffu, before << 16 | all);
+    if ((tid & 31) == 0) counts[tid >> 5] = both;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += counts[w];
+    if (height_too && tid == 0 && (!COPY || report)) *a.n_free_out = height - min(sum & 0xffff, height);
+    if (!COPY) return;
+    int s, d;
+    if (!fork_rows(a, me, s, d) || mark[d] != me) return;
+    const int n = fork_length(a, me, s, false), nth = (sum >> 16) + 1;
+    const bool need = (n & (page - 1)) != 0;
+    int fresh = -1;
+    bool ok = !need || nth <= height;
+    if (ok && need) {
+        fresh = a.free_pages[height - nth];
+        if (fresh < 0 || fresh >= a.n_pages) {
+            if (tid == 0) flag(a.status, kBadPage);
+            ok = false;
+        }
+    }
+    if (blockIdx.y == 0 && tid == 0) a.kv_len[d] = ok ? n : 0;
+    if (ok) fork_copy(a, s, d, n, fresh, blockIdx.y * 256 + tid, gridDim.y * 256);
+}
+
+// Many: one CTA finds which forks are done, their fresh pages, lengths.  A row that is both taken from and written, and all but the first
 // fork into a row, are refused: a mark for each row finds them (the smallest fork that writes it, -1 if one takes from it).
-__global__ void __launch_bounds__(kPlanThreads) k_page_fork_plan(const ForkArgs a) {
+static __global__ void __launch_bounds__(kPlanThreads) k_page_fork_plan(const ForkArgs a) {
     __shared__ long long warp_sums[32];
     const int tid = threadIdx.x, page = 1 << a.page_shift;
-    const long long cap = (long long)a.W << a.page_shift;
     const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0);
     int32_t *mark = a.ws + a.n;
-    auto rows = [&](int i, int &s, int &d) {
-        s = a.src[i];
-        d = a.dst[i];
-        return s >= 0 && s < a.B && d >= 0 && d < a.B;
-    };
     int s, d;
     for (int i = tid; i < a.n; i += kPlanThreads)
-        if (rows(i, s, d)) mark[s] = mark[d] = 0x7fffffff;
+        if (fork_rows(a, i, s, d)) mark[s] = mark[d] = 0x7fffffff;
         else if (s >= 0) flag(a.status, kBadRow);
     __syncthreads();
     for (int i = tid; i < a.n; i += kPlanThreads)
-        if (rows(i, s, d)) {
+        if (fork_rows(a, i, s, d)) {
             atomicMin(mark + d, i);
             atomicMin(mark + s, -1);
         }
     __syncthreads();
-    int taken = 0;
     long long before = 0;
     for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
         const int i = i0 + tid;
-        bool valid = i < a.n && rows(i, s, d);
+        bool valid = i < a.n && fork_rows(a, i, s, d);
         if (valid && __ldcg(mark + d) != i) {
             flag(a.status, kBadRow);
             valid = false;
         }
-        int n = 0;
-        if (valid) {
-            n = length_of(a.kv_len, s, cap, a.status);
-            if (a.len != nullptr) {
-                const int most = a.len[i];
-                if (most < 0) flag(a.status, kBadLength);
-                n = min(n, max(most, 0));
-            }
-        }
+        const int n = valid ? fork_length(a, i, s, true) : 0;
         const bool need = (n & (page - 1)) != 0;
         long long total;
         const long long upto = before + block_scan(need ? 1 : 0, warp_sums, &total);
@@ -105,41 +218,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_fork_plan(const ForkArgs 
         if (i < a.n) a.ws[i] = ok ? fresh : -2;
         if (valid) a.kv_len[d] = ok ? n : 0;
     }
-    taken = (int)min(before, (long long)height);
-    if (tid == 0) *a.n_free_out = height - taken;
+    if (tid == 0) *a.n_free_out = height - (int)min(before, (long long)height);
 }
-
-// Grid (forks, 2 H): one (tensor, head) of the open page, and a share of the table row.
-__global__ void __launch_bounds__(256) k_page_fork_copy(const ForkArgs a) {
+static __global__ void __launch_bounds__(256) k_page_fork_copy(const ForkArgs a) {
     pdl_wait();
-    const int i = blockIdx.x, tid = threadIdx.x, fresh = a.ws[i];
-    if (fresh == -2) return;
-    const int s = a.src[i], d = a.dst[i], n = a.kv_len[d], whole = n >> a.page_shift, rest = n & ((1 << a.page_shift) - 1);
-    const int32_t *from = a.table + (size_t)s * a.W;
-    int32_t *to = a.table + (size_t)d * a.W;
-    for (int p = blockIdx.y * 256 + tid; p < whole; p += gridDim.y * 256) to[p] = from[p];
-    if (rest == 0 || !FAEDKV_IN_BOUNDS(kTagPageShare, whole < a.W && fresh >= 0 && fresh < a.n_pages)) return;
-    if (blockIdx.y == 0 && tid == 0) to[whole] = fresh;
-    const int open = from[whole];
-    if (open < 0 || open >= a.n_pages) {
-        if (tid == 0) flag(a.status, kBadPage);
-        return;
-    }
-    const int which = blockIdx.y & 1, h = blockIdx.y >> 1;
-    uint8_t *codes = which == 0 ? a.codes[0] : a.codes[1];
-    float *scale = which == 0 ? a.scale[0] : a.scale[1];
-    const size_t row = (size_t)kHeadDim << a.page_shift, ph = (size_t)open * a.H + h, ph_new = (size_t)fresh * a.H + h;
-    const uint4 *x = reinterpret_cast<const uint4 *>(codes + ph * row);
-    uint4 *y = reinterpret_cast<uint4 *>(codes + ph_new * row);
-    uint4 v[4];                                           // a page of a head is 128 rows of 8 at most
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (tid + 256 * k < rest * 8) v[k] = x[tid + 256 * k];
-    const float sc = scale[ph];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (tid + 256 * k < rest * 8) y[tid + 256 * k] = v[k];
-    if (tid == 0) scale[ph_new] = sc;
+    const int i = blockIdx.x, fresh = a.ws[i];
+    if (fresh != -2) fork_copy(a, a.src[i], a.dst[i], a.kv_len[a.dst[i]], fresh, threadIdx.x, 256);
 }
 
 // ---- release ------------------------------------------------------------------------------------------
@@ -151,10 +235,107 @@ struct ReleaseArgs {
     unsigned int *status;
 };
 
+// One cluster.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
+//
+// Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store.
+template <int K>
+static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release_short(const ReleaseArgs a, const int parts) {
+    __shared__ int32_t count[32 * K + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
+    const long long cap = (long long)a.W << a.page_shift;
+    const int page = 1 << a.page_shift;
+    const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && rank == 0);
+    int32_t *totals = a.ws + a.n_pages;
+    int id[K][8], e[K], row[K];
+    bool gone[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int item = (rank * 32 + warp) * K + k;
+        row[k] = item / parts < a.B ? item / parts : -1;
+        const int b = max(row[k], 0), part = item - item / parts * parts;
+        gone[k] = row[k] >= 0 && a.n_new[b] < 0;
+        const int held = row[k] < 0 ? 0 : (int)(((long long)length_of(a.t_len, b, cap, a.status) + page - 1) >> a.page_shift);
+        const int run = (held + parts - 1) / parts, end = min(held, (part + 1) * run);
+        e[k] = b * a.W + part * run + lane;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) id[k][j] = part * run + 32 * j + lane < end ? a.table[e[k] + 32 * j] : -2;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (id[k][j] < -2 || id[k][j] == -1 || id[k][j] >= a.n_pages) {
+                flag(a.status, kBadPage);
+                id[k][j] = -2;
+            }
+            if (gone[k] && id[k][j] >= 0) a.ws[id[k][j]] = 0x7fffffff;
+        }
+    cluster_sync();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (row[k] >= 0 && lane == 0) a.kv_len[row[k]] = gone[k] ? 0 : a.t_len[row[k]];   // (kv_len may be t_len: the same warps have read it)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (id[k][j] >= 0) atomicMin(a.ws + id[k][j], gone[k] ? e[k] + 32 * j : -1);
+    }
+    cluster_sync();
+    uint32_t mine[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        int first[8];
+        mine[k] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) first[j] = gone[k] && id[k][j] >= 0 ? __ldcg(a.ws + id[k][j]) : -1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mine[k] |= (uint32_t)(first[j] == e[k] + 32 * j) << j;
+        const int n = __reduce_add_sync(0xffffffffu, __popc(mine[k]));
+        if (lane == 0) count[warp * K + k] = n;
+    }
+    __syncthreads();
+    if (warp == 0) {                                       // exclusive sums, the CTA's behind the last
+        int n[K], sum = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) { n[k] = count[lane * K + k]; sum += n[k]; }
+        int upto = sum;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, s);
+            if (lane >= s) upto += o;
+        }
+        int at = upto - sum;
+#pragma unroll
+        for (int k = 0; k < K; ++k) { count[lane * K + k] = at; at += n[k]; }
+        if (lane == 31) { count[32 * K] = upto; totals[rank] = upto; }
+    }
+    cluster_sync();
+    long long at0 = height, all = height;
+    for (int r = 0; r < kCluster; ++r) {
+        const int n = __ldcg(totals + r);
+        if (r < rank) at0 += n;
+        all += n;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        long long at = at0 + count[warp * K + k];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool push = (mine[k] >> j) & 1u;
+            const uint32_t m = __ballot_sync(0xffffffffu, push);
+            const long long to = at + __popc(m & ((1u << lane) - 1u));
+            if (push) {
+                if (to < a.n_pages) a.free_pages[to] = id[k][j];
+                else flag(a.status, kBadFreeList);
+            }
+            at += __popc(m);
+        }
+    }
+    if (tid == 0 && rank == 0) *a.n_free_out = (int)min(all, (long long)a.n_pages);   // (n_free_out may be n_free: all have read it)
+}
+
 constexpr int kReleaseItems = 65536 / kCluster;           // items of a CTA: one warp's part of a row
 
-// One cluster.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release(const ReleaseArgs a, const int parts) {
+// Any number of rows and pages: the runs are read again in every phase.
+static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release(const ReleaseArgs a, const int parts) {
     __shared__ long long warp_sums[32];
     __shared__ int32_t count[kReleaseItems];
     constexpr int kWarps = kPlanThreads / 32;
@@ -172,29 +353,51 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads)
         const int held = (int)(((long long)length_of(a.t_len, b, cap, a.status) + page - 1) >> a.page_shift);
         const int run = (held + parts - 1) / parts, end = min(held, (part + 1) * run);
         const int32_t *row = a.table + (size_t)b * a.W;
-        for (int p0 = part * run; p0 < end; p0 += 32) {
-            const int p = p0 + lane;
-            int id = p < end ? row[p] : -1;
-            if (p < end && (id < 0 || id >= a.n_pages)) {
-                flag(a.status, kBadPage);
-                id = -1;
-            }
-            f(b * a.W + p, id);
+        for (int p0 = part * run; p0 < end; p0 += 256) {   // eight entries a lane in flight
+            int id[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) id[k] = p0 + 32 * k + lane < end ? row[p0 + 32 * k + lane] : -1;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (p0 + 32 * k + lane < end && (id[k] < 0 || id[k] >= a.n_pages)) {
+                    flag(a.status, kBadPage);
+                    id[k] = -1;
+                }
+            f(b * a.W + p0 + lane, id);
         }
+    };
+    // the entries that are the first to name their page, and no running request names it: a bit each
+    auto pushed = [&](int e, const int(&id)[8]) {
+        int first[8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) first[k] = id[k] >= 0 ? __ldcg(a.ws + id[k]) : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m |= (uint32_t)(id[k] >= 0 && first[k] == e + 32 * k) << k;
+        return m;
     };
     for (int i = item0 + warp; i < item1; i += kWarps)
         if (a.n_new[i / parts] < 0)
-            entries(i, [&](int, int id) { if (id >= 0) a.ws[id] = 0x7fffffff; });
+            entries(i, [&](int, const int(&id)[8]) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (id[k] >= 0) a.ws[id[k]] = 0x7fffffff;
+            });
     cluster_sync();
     for (int i = item0 + warp; i < item1; i += kWarps) {
         const bool gone = a.n_new[i / parts] < 0;
-        entries(i, [&](int e, int id) { if (id >= 0) atomicMin(a.ws + id, gone ? e : -1); });
+        entries(i, [&](int e, const int(&id)[8]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (id[k] >= 0) atomicMin(a.ws + id[k], gone ? e + 32 * k : -1);
+        });
     }
     cluster_sync();
     for (int i = item0 + warp; i < item1; i += kWarps) {
         int n = 0;
         if (a.n_new[i / parts] < 0)
-            entries(i, [&](int e, int id) { n += __popc(__ballot_sync(0xffffffffu, id >= 0 && __ldcg(a.ws + id) == e)); });
+            entries(i, [&](int e, const int(&id)[8]) { n += __popc(pushed(e, id)); });
+        n = __reduce_add_sync(0xffffffffu, n);
         if (lane == 0) count[i - item0] = n;
     }
     __syncthreads();
@@ -218,15 +421,19 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads)
         const int b = i / parts;
         if (a.n_new[b] >= 0) continue;
         long long at = at0 + count[i - item0];
-        entries(i, [&](int e, int id) {
-            const bool push = id >= 0 && __ldcg(a.ws + id) == e;
-            const uint32_t m = __ballot_sync(0xffffffffu, push);
-            const long long to = at + __popc(m & ((1u << lane) - 1u));
-            if (push) {
-                if (to < a.n_pages) a.free_pages[to] = id;
-                else flag(a.status, kBadFreeList);
+        entries(i, [&](int e, const int(&id)[8]) {
+            const uint32_t mine = pushed(e, id);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool push = (mine >> k) & 1u;
+                const uint32_t m = __ballot_sync(0xffffffffu, push);
+                const long long to = at + __popc(m & ((1u << lane) - 1u));
+                if (push) {
+                    if (to < a.n_pages) a.free_pages[to] = id[k];
+                    else flag(a.status, kBadFreeList);
+                }
+                at += __popc(m);
             }
-            at += __popc(m);
         });
     }
     cluster_sync();                                       // kv_len may be t_len, n_free_out may be n_free
@@ -248,7 +455,7 @@ constexpr int kCompactHead = 32;                          // counts: live pages 
 
 // One cluster: which pages are in use, and where each goes.  With n of them, the pages in use from n on go to the pages below n
 // that are not, both in ascending order: the fewest moves, and no page is read and written.
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_compact_plan(const CompactArgs a) {
+static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_compact_plan(const CompactArgs a) {
     __shared__ long long warp_sums[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
     const long long cap = (long long)a.W << a.page_shift;
@@ -260,10 +467,16 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads)
     for (int i = rank * (kPlanThreads / 32) + warp; i < a.B * parts; i += warps) {
         const int b = i / parts, part = i - b * parts;
         const int held = (int)(((long long)length_of(a.kv_len, b, cap, a.status) + page - 1) >> a.page_shift);
-        for (int p = part * 32 + lane; p < held; p += parts * 32) {
-            const int id = a.table[(size_t)b * a.W + p];
-            if (id < 0 || id >= a.n_pages) flag(a.status, kBadPage);
-            else a.new_id[id] = 0;
+        for (int p0 = part * 256 + lane; p0 < held; p0 += parts * 256) {   // eight entries a lane in flight
+            int id[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) id[k] = p0 + 32 * k < held ? a.table[(size_t)b * a.W + p0 + 32 * k] : -1;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (p0 + 32 * k >= held) continue;
+                if (id[k] < 0 || id[k] >= a.n_pages) flag(a.status, kBadPage);
+                else a.new_id[id[k]] = 0;
+            }
         }
     }
     cluster_sync();
@@ -319,9 +532,74 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads)
     for (int k = me; k < n_moves; k += all) a.new_id[__ldcg(moves + k)] = __ldcg(holes + k);
 }
 
+// The same by one CTA with a bit for each page in shared memory, for pools of up to kCompactShort pages: a page's rank among those in use gives its place
+// in either list.
+constexpr int kCompactShort = 65536;
+static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_short(const CompactArgs a) {
+    __shared__ uint32_t used[kCompactShort / 32];
+    __shared__ int32_t before[kCompactShort / 32];        // pages in use before a word's
+    __shared__ long long warp_sums[32];
+    constexpr int kWords = kCompactShort / 32 / kPlanThreads;                // of a thread
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, page = 1 << a.page_shift;
+    const long long cap = (long long)a.W << a.page_shift;
+    int32_t *holes = a.ws + kCompactHead, *moves = holes + a.n_pages / 2;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) used[tid + i * kPlanThreads] = 0u;
+    __syncthreads();
+    const int parts = max(1, 32 / a.B);                    // warps of a row
+    for (int i = warp; i < a.B * parts; i += 32) {
+        const int b = i / parts, part = i - b * parts;
+        const int held = (int)(((long long)length_of(a.kv_len, b, cap, a.status) + page - 1) >> a.page_shift);
+        for (int p0 = part * 256 + lane; p0 < held; p0 += parts * 256) {     // eight entries a lane in flight
+            int id[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) id[k] = p0 + 32 * k < held ? a.table[(size_t)b * a.W + p0 + 32 * k] : -1;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (p0 + 32 * k >= held) continue;
+                if (id[k] < 0 || id[k] >= a.n_pages) flag(a.status, kBadPage);
+                else atomicOr(used + (id[k] >> 5), 1u << (id[k] & 31));
+            }
+        }
+    }
+    __syncthreads();
+    uint32_t word[kWords];
+    int live = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        word[i] = used[tid * kWords + i];
+        live += __popc(word[i]);
+    }
+    long long total;
+    int rank = (int)block_scan(live, warp_sums, &total) - live;
+    const int n = (int)total;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        before[tid * kWords + i] = rank;
+        rank += __popc(word[i]);
+    }
+    __syncthreads();
+    auto rank_of = [&](int p) { return before[p >> 5] + __popc(used[p >> 5] & ((1u << (p & 31)) - 1u)); };
+    const int n_low = n < a.n_pages ? rank_of(n) : n;      // in use below n
+    for (int p = tid; p < a.n_pages; p += kPlanThreads) {
+        const bool in_use = (used[p >> 5] >> (p & 31)) & 1u;
+        const int r = rank_of(p);
+        if (p < n && !in_use) holes[p - r] = p;
+        if (p >= n && in_use) moves[r - n_low] = p;
+        if (p < n || !in_use) a.new_id[p] = in_use ? p : -1;
+    }
+    for (int i = tid; i < a.n_pages - n; i += kPlanThreads) a.free_pages[i] = a.n_pages - 1 - i;
+    if (tid == 0) {
+        *a.n_free = a.n_pages - n;
+        a.ws[kCompactHead - 1] = n - n_low;
+    }
+    __syncthreads();
+    for (int k = tid; k < n - n_low; k += kPlanThreads) a.new_id[__ldcg(moves + k)] = __ldcg(holes + k);
+}
+
 // The pages that move, 16 KB of a tensor at a time, and the tables.
 constexpr int kMoveUnits = 1024;                          // of 16 bytes
-__global__ void __launch_bounds__(256) k_page_move(const CompactArgs a) {
+static __global__ void __launch_bounds__(256) k_page_move(const CompactArgs a) {
     pdl_wait();
     const int tid = threadIdx.x, page = 1 << a.page_shift;
     const long long cap = (long long)a.W << a.page_shift, n_entries = (long long)a.B * a.W;

@@ -164,7 +164,9 @@ def test_fork_flags_bad_pages_lengths_and_stack(fk):
 
 
 @pytest.mark.parametrize("page,W,B,n_pages", [(16, 4, 1, 9), (16, 30, 7, 200), (64, 9, 300, 1500), (16, 700, 5, 3000), (32, 3, 3000, 6000),
-                                              (16, 2, 20000, 30000), (16, 6000, 40, 9000)])
+                                              (16, 2, 20000, 30000), (16, 6000, 40, 9000),
+                                              (16, 200, 400, 9000), (32, 256, 256, 20000), (16, 257, 256, 20000), (64, 2, 512, 700), (64, 2, 513, 700),
+                                              (16, 257, 512, 20000), (16, 3, 1024, 2000), (16, 513, 256, 20000)])
 def test_release(fk, page, W, B, n_pages):
     rng = np.random.default_rng(B + W)
     table, kv, perm = _rows(rng, B, W, page, n_pages, range(B))
@@ -205,7 +207,8 @@ def test_release_flags_what_is_out_of_range(fk):
 
 
 @pytest.mark.parametrize("H,page,W,B,n_pages", [(1, 16, 3, 1, 5), (2, 16, 9, 6, 100), (5, 32, 20, 9, 333), (8, 64, 12, 30, 700), (3, 128, 5, 4, 31),
-                                                (1, 16, 40, 300, 20000), (2, 16, 1, 3, 1)])
+                                                (1, 16, 40, 300, 20000), (2, 16, 1, 3, 1),
+                                                (1, 16, 50, 1500, 66000), (1, 16, 300, 4000, 65536)])
 def test_compact(fk, H, page, W, B, n_pages):
     rng = np.random.default_rng(n_pages + W)
     for trial in range(3):
@@ -371,14 +374,14 @@ def test_the_c_calls_refuse_what_they_cannot_do(fk):
     c = [x.data_ptr() for x in cache.args()]
     lib, n0 = fk.load(), pg.launch_count()
     fork, release, compact = lib.faedkv_pages_fork, lib.faedkv_pages_release, lib.faedkv_pages_compact
-    # arguments, where the batch stands, which others are no tensors, which may be NULL
-    calls = [(fork, [pg._h, i, i, i, 4, 4, i, i, i, i, i, *c, i, None], 5, (4,), 3), (release, [pg._h, i, i, 4, i, i, i, i, i, i, None], 3, (), None),
-             (compact, [pg._h, i, 4, i, i, i, i, i, *c, i, None], 2, (), None)]
+    # arguments, where the batch stands, which others are no tensors, which may be NULL (fork: the lengths, and a workspace that few forks do not need)
+    calls = [(fork, [pg._h, i, i, i, 4, 4, i, i, i, i, i, *c, i, None], 5, (4,), (3, 15)), (release, [pg._h, i, i, 4, i, i, i, i, i, i, None], 3, (), ()),
+             (compact, [pg._h, i, 4, i, i, i, i, i, *c, i, None], 2, (), ())]
     for call, good, at, counts, optional in calls:
         for k, x in enumerate(good[1:-1], 1):
             if k == at or k in counts:
                 continue
-            if k != optional:
+            if k not in optional:
                 assert call(*good[:k], None, *good[k + 1:]) == -1, (call.__name__, k)
             assert call(*good[:k], x + 2, *good[k + 1:]) == -5, (call.__name__, k)
             assert b"aligned" in lib.faedkv_pages_last_error(pg._h)
@@ -390,7 +393,9 @@ def test_the_c_calls_refuse_what_they_cannot_do(fk):
     for n in (-1, 5):
         assert fork(*good[:4], n, *good[5:]) == -3
         assert lib.faedkv_pages_fork_bytes(pg._h, 4, n) == 0
-    assert lib.faedkv_pages_fork_bytes(pg._h, 4, 4) == 32 and lib.faedkv_pages_fork_bytes(pg._h, 5, 4) == 0
+    many = make(fk, n_pages=6, W=3, B=5000)
+    assert lib.faedkv_pages_fork_bytes(pg._h, 4, 4) == 0 and lib.faedkv_pages_fork_bytes(many._h, 5000, 4) == 4 * 5004
+    assert fork(many._h, *good[1:5], 5000, *good[6:15], None, None) == -1 and many.launch_count() == 0
     assert pg.launch_count() == n0 and big.launch_count() == 0 and pg.device_status() == 0
     out = ref.ints([0])
     pg.fork(ref.ints([]), ref.ints([]), ref.ints([0] * 4), ref.ints(np.zeros((4, 3))), ref.ints([0] * 6), ref.ints([5]), out, *cache.args())

@@ -75,7 +75,7 @@ def test_binding_refuses_wrong_tensors_of_the_page_calls(fk):
     refused_one_by_one(pg.release, release, [*ints, "n_new", "n_free_out"], wrong)
     compact = dict(base, table_out=i32(2, 4), new_id=i32(3), ws=ws, **cache)
     refused_one_by_one(pg.compact, compact, [*ints[1:], "table_out", "new_id", *cache], wrong)
-    for call, args in ((pg.fork, fork), (pg.release, release), (pg.compact, compact)):
+    for call, args in ((pg.fork, fork), (pg.release, release), (pg.compact, compact)):      # (the recorder asks for 64 bytes)
         with pytest.raises(ValueError, match="ws"):
             call(**{**args, "ws": torch.zeros(8, dtype=torch.uint8)})
     assert {name for name, _ in pg._lib.calls} == {"faedkv_pages_fork", "faedkv_pages_release", "faedkv_pages_compact"}
