@@ -12,6 +12,17 @@ int check_table(faedkv_pages *pg, int batch) {
     return FAEDKV_OK;
 }
 
+// A launch of one cluster; larger ones than the portable eight CTAs have to be asked for, once for each kernel.
+template <typename... Args>
+int launch_cluster(faedkv_pages *pg, const char *what, void (*kernel)(Args...), int attr_bit, cudaStream_t st, Args... args) {
+    if (!(pg->attr_set & (1u << attr_bit))) {
+        CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        pg->attr_set |= 1u << attr_bit;
+    }
+    kernel<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(args...);
+    return launch_check(pg, what);
+}
+
 // Up to this many forks and rows the CTAs that copy find out for themselves what comes before them.  (16 rows forked into 256: 10 us with a plan in
 // one CTA before the copies.)
 bool forks_alone(int batch, int n_forks) { return n_forks <= pages::kForkSmall && batch <= pages::kForkRows; }
@@ -85,15 +96,14 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     while (parts < 32 && 2 * parts * batch <= warps) parts *= 2;
     int fits = parts;
     while (fits < 32 && pg->cfg.max_pages > 256 * fits) fits *= 2;
-    const bool in_registers = pg->cfg.max_pages <= 256 * fits && fits * batch <= 4 * warps;
+    const bool in_registers = pg->cfg.max_pages <= 256 * fits && fits * batch <= 4 * warps && pg->cfg.n_pages <= pages::kReleaseShort;
     if (in_registers) parts = fits;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int each = !in_registers ? 0 : batch * parts <= warps ? 1 : batch * parts <= 2 * warps ? 2 : 4;
-    if (each == 1) pages::k_page_release_short<1><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
-    else if (each == 2) pages::k_page_release_short<2><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
-    else if (each == 4) pages::k_page_release_short<4><<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
-    else pages::k_page_release<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a, parts);
-    return launch_check(pg, "k_page_release");
+    return each == 1   ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<1>, 22, st, a, parts)
+           : each == 2 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<2>, 23, st, a, parts)
+           : each == 4 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<4>, 24, st, a, parts)
+                       : launch_cluster(pg, "k_page_release", pages::k_page_release, 25, st, a, parts);
 }
 
 size_t faedkv_pages_compact_bytes(const faedkv_pages *pg) {
@@ -117,9 +127,12 @@ int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, con
     const pages::CompactArgs a{kv_len, table, table_out, free_pages, n_free, new_id, static_cast<int32_t *>(ws),
                                {static_cast<uint8_t *>(k_pages), static_cast<uint8_t *>(v_pages)}, {k_scale, v_scale},
                                batch, c.max_pages, c.n_kv_heads, c.n_pages, pg->page_shift, pg->dev_status};
-    if (c.n_pages <= pages::kCompactShort && (long long)batch * c.max_pages <= 16 * pages::kCompactShort) pages::k_page_compact_short<<<1, pages::kPlanThreads, 0, st>>>(a);
-    else pages::k_page_compact_plan<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(a);
-    if (int r = launch_check(pg, "k_page_compact_plan")) return r;
+    if (c.n_pages <= pages::kCompactShort && (long long)batch * c.max_pages <= 16 * pages::kCompactShort) {
+        pages::k_page_compact_short<<<1, pages::kPlanThreads, 0, st>>>(a);
+        if (int r = launch_check(pg, "k_page_compact_short")) return r;
+    } else if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan, 26, st, a)) {
+        return r;
+    }
     CUDA_TRY(pg, launch_pdl(pages::k_page_move, dim3(pg->n_sm * 8), dim3(256), 0, st, a));
     return launch_check(pg, "k_page_move");
 }

@@ -12,7 +12,7 @@ namespace faedkv {
 namespace pages {
 
 constexpr unsigned int kBadRow = 0x106;                   // a row of the block table that there is not, or that may not be written
-constexpr int kCluster = 8;                               // CTAs that meet in one launch: as many as every part can be asked for
+constexpr int kCluster = 16;                              // CTAs that meet in one launch: the most there are (512 requests: 22 us with 8)
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -237,15 +237,27 @@ struct ReleaseArgs {
 
 // One cluster.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
 //
-// Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store.
+// Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store, and the pages that running
+// requests name are bits in shared memory, each CTA's own first, then all of them (as atomics to global memory, the entries of 512 requests took 20 us of
+// 25).
+constexpr int kReleaseShort = 65536;                      // pages
+__device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {        // what p is in another CTA of the cluster
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
 template <int K>
 static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release_short(const ReleaseArgs a, const int parts) {
     __shared__ int32_t count[32 * K + 1];
+    __shared__ uint32_t own[kReleaseShort / 32], live[kReleaseShort / 32];
+    const int words = (a.n_pages + 31) / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
     const long long cap = (long long)a.W << a.page_shift;
     const int page = 1 << a.page_shift;
     const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && rank == 0);
     int32_t *totals = a.ws + a.n_pages;
+    for (int w = tid; w < words; w += kPlanThreads) own[w] = 0u;
     int id[K][8], e[K], row[K];
     bool gone[K];
 #pragma unroll
@@ -260,6 +272,7 @@ static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanT
 #pragma unroll
         for (int j = 0; j < 8; ++j) id[k][j] = part * run + 32 * j + lane < end ? a.table[e[k] + 32 * j] : -2;
     }
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -268,24 +281,32 @@ static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanT
                 flag(a.status, kBadPage);
                 id[k][j] = -2;
             }
-            if (gone[k] && id[k][j] >= 0) a.ws[id[k][j]] = 0x7fffffff;
+            if (id[k][j] < 0) continue;
+            if (gone[k]) a.ws[id[k][j]] = 0x7fffffff;
+            else atomicOr(own + (id[k][j] >> 5), 1u << (id[k][j] & 31));
         }
     cluster_sync();
+    for (int w = tid; w < words; w += kPlanThreads) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < kCluster; ++r) m |= load_of_cta(own + w, r);
+        live[w] = m;
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (row[k] >= 0 && lane == 0) a.kv_len[row[k]] = gone[k] ? 0 : a.t_len[row[k]];   // (kv_len may be t_len: the same warps have read it)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (id[k][j] >= 0) atomicMin(a.ws + id[k][j], gone[k] ? e[k] + 32 * j : -1);
+            if (gone[k] && id[k][j] >= 0) atomicMin(a.ws + id[k][j], e[k] + 32 * j);
     }
-    cluster_sync();
+    cluster_sync();                                        // (and no CTA ends while another reads its bits)
     uint32_t mine[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         int first[8];
         mine[k] = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) first[j] = gone[k] && id[k][j] >= 0 ? __ldcg(a.ws + id[k][j]) : -1;
+        for (int j = 0; j < 8; ++j) first[j] = gone[k] && id[k][j] >= 0 && !((live[id[k][j] >> 5] >> (id[k][j] & 31)) & 1u) ? __ldcg(a.ws + id[k][j]) : -1;
 #pragma unroll
         for (int j = 0; j < 8; ++j) mine[k] |= (uint32_t)(first[j] == e[k] + 32 * j) << j;
         const int n = __reduce_add_sync(0xffffffffu, __popc(mine[k]));
@@ -451,7 +472,7 @@ struct CompactArgs {
     int B, W, H, n_pages, page_shift;
     unsigned int *status;
 };
-constexpr int kCompactHead = 32;                          // counts: live pages of each CTA's range, then holes, then pages that move; at 31 all of those
+constexpr int kCompactHead = 64;                          // counts: live pages of each CTA's range, then holes, then pages that move; the last: all of those
 
 // One cluster: which pages are in use, and where each goes.  With n of them, the pages in use from n on go to the pages below n
 // that are not, both in ascending order: the fewest moves, and no page is read and written.

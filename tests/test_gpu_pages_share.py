@@ -166,7 +166,7 @@ def test_fork_flags_bad_pages_lengths_and_stack(fk):
 @pytest.mark.parametrize("page,W,B,n_pages", [(16, 4, 1, 9), (16, 30, 7, 200), (64, 9, 300, 1500), (16, 700, 5, 3000), (32, 3, 3000, 6000),
                                               (16, 2, 20000, 30000), (16, 6000, 40, 9000),
                                               (16, 200, 400, 9000), (32, 256, 256, 20000), (16, 257, 256, 20000), (64, 2, 512, 700), (64, 2, 513, 700),
-                                              (16, 257, 512, 20000), (16, 3, 1024, 2000), (16, 513, 256, 20000)])
+                                              (16, 257, 512, 20000), (16, 3, 1024, 2000), (16, 513, 256, 20000), (16, 9, 30, 65536), (16, 9, 30, 65537)])
 def test_release(fk, page, W, B, n_pages):
     rng = np.random.default_rng(B + W)
     table, kv, perm = _rows(rng, B, W, page, n_pages, range(B))
