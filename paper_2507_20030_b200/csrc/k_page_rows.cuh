@@ -35,6 +35,17 @@ constexpr uint32_t kRowsSmem = kRowsOffMisc + 4 * kRowsFloats + 384 + 64 * kRows
 static_assert(kRowsSmem <= 232448, "shared memory of a CTA");
 static_assert(kRowsRing >= kRowsK + 3, "scales outlive their tile's K");
 
+// Two f16 as e4m3 or e5m2 codes (the lower 16 bits), nearest even.
+__device__ __forceinline__ uint32_t f16x2_to_e4m3x2(uint32_t h) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 c;\n\tcvt.rn.satfinite.e4m3x2.f16x2 c, %1;\n\tcvt.u32.u16 %0, c;\n\t}" : "=r"(r) : "r"(h));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2_to_e5m2x2(uint32_t h) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 c;\n\tcvt.rn.satfinite.e5m2x2.f16x2 c, %1;\n\tcvt.u32.u16 %0, c;\n\t}" : "=r"(r) : "r"(h));
+    return r;
+}
 // The MMA warp goes through its code with all lanes and issues by one, so that descriptors stay in uniform registers: an instruction issued by a
 // lane in a branch of its own takes some 95 cycles, more than its product.
 __device__ __forceinline__ uint32_t elect_one() {
@@ -592,58 +603,89 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         int count = 0, it = 0;                            // this warpgroup's tiles, and all, of the segments before
         for (uint32_t seg = 0; next_segment(seg, s); ++seg) {
             const bool two = s.weight == 2;
-            // -- the rows of q as two terms, each row with a power of two of its own: a row a thread (one row tile: the first warpgroup's)
             const int c = (two ? g * 128 : 0) + row, tok = c * a.inv_g >> 16;              // this thread's row, and its token
             const bool warp_on = (c & ~31) < s.n_cols;
-            if (warp_on && (two || g == 0)) {
-                constexpr int kMaps = FORM == 1 ? 2 : 1, kLoads = 16 / kMaps;            // rows of a query row; a map is half of it
-                const int head = c - tok * a.G, half = FORM == 1 ? head & 1 : 0;
-                const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (size_t)(s.tok0 + tok) * a.ld_q + ((size_t)s.h * (a.G / kMaps) + head / kMaps) * kHeadDim + half * 64);
-                const bool there = c < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 >= 0 && s.tok0 + tok < a.n_tokens);
-                uint32_t top = 0;                          // the largest finite magnitude
-                if (there) {
-                    __nv_bfloat162 m = __floats2bfloat162_rn(0.f, 0.f);
+            // -- the rows of q as two terms, each row with a power of two of its own.  Half a warp has a row of q (and, differential, the rows of its two
+            // maps), 16 bytes a lane, the next one on its way.  (A row a thread took 17 000 cycles, a line for each lane of a load; eight rows at a time
+            // 21 000: instructions that are run once come from afar.)
+            {
+                constexpr int kMaps = FORM == 1 ? 2 : 1;
+                const int l16 = lane & 15, map = FORM == 1 ? l16 >> 3 : 0;
+                const int first = (two ? g * (128 / kMaps) + (warp & 3) * 2 : warp * 2) + (lane >> 4), step = two ? 8 : 16;
+                const int end = min(two ? (g + 1) * 128 : 128, (s.n_cols + 31) / 32 * 32) / kMaps;   // rows up to whole warps' are zero
+                auto load = [&](int r) {
+                    const int col = r * kMaps, k = col * a.inv_g >> 16;
+                    const bool there = r < end && col < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, s.tok0 >= 0 && s.tok0 + k < a.n_tokens);
+                    const T *from = static_cast<const T *>(a.q) + (size_t)(s.tok0 + k) * a.ld_q + ((size_t)s.h * (a.G / kMaps) + (col - k * a.G) / kMaps) * kHeadDim + l16 * 8;
+                    return there ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
+                };
+                constexpr int kTogether = FORM == 1 ? 1 : 2;               // rows of a half warp at a time (two make the other form slower)
+                uint4 next[kTogether];
 #pragma unroll
-                    for (int i = 0; i < kLoads; ++i) {     // (NaN is passed over)
-                        const uint4 x = from[i];
-                        const __nv_bfloat162 *u = reinterpret_cast<const __nv_bfloat162 *>(&x);
-                        m = __hmax2(m, __hmax2(__hmax2(__habs2(u[0]), __habs2(u[1])), __hmax2(__habs2(u[2]), __habs2(u[3]))));
-                    }
-                    top = max(__float_as_uint(__low2float(m)), __float_as_uint(__high2float(m)));
-                    if (top >= 0x7f800000u) {              // an infinity among them: again, without
-                        top = 0;
+                for (int j = 0; j < kTogether; ++j) next[j] = load(first + j * step);
 #pragma unroll 1
-                        for (int i = 0; i < 8 * kLoads; ++i) top = max(top, finite_bits(__bfloat162float(reinterpret_cast<const T *>(from)[i])));
+                for (int r0 = first; r0 - (lane >> 4) < end; r0 += kTogether * step) {
+                    uint32_t u[kTogether][4], top[kTogether];
+                    bool odd = false;
+#pragma unroll
+                    for (int j = 0; j < kTogether; ++j) {
+                        u[j][0] = next[j].x; u[j][1] = next[j].y; u[j][2] = next[j].z; u[j][3] = next[j].w;
+                        next[j] = load(r0 + (kTogether + j) * step);
+                        // the largest magnitude of the row (of the map), as bf16 bits; where an infinity or NaN is among them, of the others
+                        top[j] = __vmaxu2(__vmaxu2(u[j][0] & 0x7fff7fffu, u[j][1] & 0x7fff7fffu), __vmaxu2(u[j][2] & 0x7fff7fffu, u[j][3] & 0x7fff7fffu));
+                        odd |= max(top[j] & 0xffffu, top[j] >> 16) >= 0x7f80u;
                     }
-                }
-                const float qs = 2.0f * scale_for(__uint_as_float(top));                 // the largest element to 112 .. 224
-                const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
-                row_cs[c] = qs * a.scale_log2;
-                // what the first term leaves of an element above 2^-6 has three significant bits (bf16's eight less its four, and a sign), which
-                // e5m2 holds; of smaller ones e5m2's rounding is at most 2^-14
-                uint8_t *at = gbase + q_off(c >> 7);
-                uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0, n0 = x0, n1 = x0;
-                if (there) { n0 = from[0]; n1 = from[1]; }
+                    odd = __any_sync(0xffffffffu, odd);
+                    if (odd) {
+#pragma unroll
+                        for (int j = 0; j < kTogether; ++j) {
+                            top[j] = 0;
 #pragma unroll 1
-                for (int k = 0; k < 8; ++k) {              // 16 channels, the next ones on their way
-                    uint32_t c1[4] = {0u, 0u, 0u, 0u}, c2[4] = {0u, 0u, 0u, 0u};
-                    if (there && (FORM != 1 || k >> 2 == half)) {
-                        const int next = FORM == 1 ? (k & 3) + 1 : k + 1;
-                        x0 = n0; x1 = n1;
-                        if (2 * next < kLoads) { n0 = from[2 * next]; n1 = from[2 * next + 1]; }
-                        const uint32_t u[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {      // 4 channels
-                            float f[4] = {__uint_as_float(u[2 * i] << 16), __uint_as_float(u[2 * i] & 0xffff0000u), __uint_as_float(u[2 * i + 1] << 16), __uint_as_float(u[2 * i + 1] & 0xffff0000u)}, hi[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) f[e] = fabsf(f[e]) < INFINITY ? f[e] * inv : __uint_as_float(0x7fffffffu);
-                            c1[i] = to_e4m3x4(f[0], f[1], f[2], f[3]);
-                            from_e4m3x4(c1[i], hi);
-                            c2[i] = to_e5m2x4(f[0] - hi[0], f[1] - hi[1], f[2] - hi[2], f[3] - hi[3]);
+                            for (int e = 0; e < 8; ++e) {
+                                const uint32_t m = (e < 2 ? u[j][0] : e < 4 ? u[j][1] : e < 6 ? u[j][2] : u[j][3]) >> (16 * (e & 1)) & 0x7fffu;
+                                if (m < 0x7f80u) top[j] = max(top[j], m);
+                            }
                         }
                     }
-                    *reinterpret_cast<uint4 *>(at + mn_chunk<128>(row, k)) = make_uint4(c1[0], c1[1], c1[2], c1[3]);
-                    *reinterpret_cast<uint4 *>(at + kTileBytes + mn_chunk<128>(row, k)) = make_uint4(c2[0], c2[1], c2[2], c2[3]);
+#pragma unroll
+                    for (int o = 1; o < 16 / kMaps; o <<= 1)
+#pragma unroll
+                        for (int j = 0; j < kTogether; ++j) top[j] = __vmaxu2(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+#pragma unroll
+                    for (int j = 0; j < kTogether; ++j) {
+                        const int r = r0 + j * step;
+                        const float qs = 2.0f * scale_for(__uint_as_float(max(top[j] & 0xffffu, top[j] >> 16) << 16));    // the largest element to 112 .. 224
+                        const float inv = __uint_as_float((254u << 23) - __float_as_uint(qs));
+                        // what the first term leaves of an element above 2^-6 has three significant bits (bf16's eight less its four, and a sign),
+                        // which e5m2 holds; of smaller ones e5m2's rounding is at most 2^-14
+                        uint32_t c1[4], c2[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float lo = __uint_as_float(u[j][e] << 16) * inv, hi = __uint_as_float(u[j][e] & 0xffff0000u) * inv;
+                            if (odd) {                     // infinities and NaN make their row's scores NaN
+                                if (!(fabsf(lo) < INFINITY)) lo = __uint_as_float(0x7fffffffu);
+                                if (!(fabsf(hi) < INFINITY)) hi = __uint_as_float(0x7fffffffu);
+                            }
+                            const uint32_t h = pack_f16(lo, hi);                                 // exact (or, of elements far below the row's largest, to 2^-25)
+                            c1[e] = f16x2_to_e4m3x2(h);
+                            const uint32_t back = e4m3x2_to_f16x2(c1[e]);
+                            const __half2 left = __hsub2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&back));
+                            c2[e] = f16x2_to_e5m2x2(*reinterpret_cast<const uint32_t *>(&left));
+                        }
+                        if (r < end) {
+                            const int col = r * kMaps + map;
+                            uint8_t *at = gbase + q_off(col >> 7) + (l16 & 1) * 8;
+                            const uint32_t here = mn_chunk<128>((uint32_t)(col & 127), (uint32_t)l16 >> 1);
+                            *reinterpret_cast<uint2 *>(at + here) = make_uint2(c1[0] | c1[1] << 16, c1[2] | c1[3] << 16);
+                            *reinterpret_cast<uint2 *>(at + kTileBytes + here) = make_uint2(c2[0] | c2[1] << 16, c2[2] | c2[3] << 16);
+                            if (FORM == 1) {               // the map's other half
+                                const uint32_t zero = mn_chunk<128>((uint32_t)(col & 127), (uint32_t)(l16 ^ 8) >> 1);
+                                *reinterpret_cast<uint2 *>(at + zero) = make_uint2(0u, 0u);
+                                *reinterpret_cast<uint2 *>(at + kTileBytes + zero) = make_uint2(0u, 0u);
+                            }
+                            if ((l16 & (16 / kMaps - 1)) == 0) row_cs[col] = qs * a.scale_log2;
+                        }
+                    }
                 }
             }
             fence_proxy_async();
@@ -763,9 +805,10 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         }
                         return sum;
                     };
-                    turn_begin();
                     for (bool again = false;; again = true) {
+                        if (!again) turn_begin();
                         const float sum = plain ? weights(std::false_type{}) : weights(std::true_type{});
+                        if (!again) turn_end();
                         // beyond what f16 holds, or no reference yet: Mu is raised, and the weights once more
                         const bool need = !set || !(sum <= kMostSum);
                         if (again || !__any_sync(0xffffffffu, need)) break;
@@ -786,7 +829,6 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         l = make_float2(l.x * f, l.y * f);
                         if (q > 0 && __any_sync(0xffffffffu, f != 1.f)) rescale(f);
                     }
-                    turn_end();
                     l = add2(l, l_half);
                     tmem_st_wait();
                 }
@@ -930,8 +972,8 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll 4
                     for (int i = 0; i < 16; ++i) {
                         const int r = i * 8 + (row >> 4), k = row & 15, col = g * 128 + r;
-                        if (col < s.n_cols && FAEDKV_IN_BOUNDS(kTagPageAttn, whole || slot != nullptr))
-                            *reinterpret_cast<float4 *>(dst + (whole ? row_of(col) : (size_t)col) * kHeadDim + 64 * part + 4 * k) = *reinterpret_cast<const float4 *>(stage + r * 256 + (k ^ (r & 15)) * 16);
+                        const float4 x = *reinterpret_cast<const float4 *>(stage + r * 256 + (k ^ (r & 15)) * 16);
+                        if (col < s.n_cols) *reinterpret_cast<float4 *>(dst + (whole ? row_of(col) : (size_t)col) * kHeadDim + 64 * part + 4 * k) = x;
                     }
                     softmax_bar(12 + g, 128);
                 }
