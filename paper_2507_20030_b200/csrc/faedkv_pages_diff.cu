@@ -4,10 +4,14 @@
 
 namespace {
 
-// Blocks of many columns take the form with rows; the rule on where they begin is plan_attn()'s.
+// Blocks of many columns take the form with rows: more than eight a sequence on average, as in plan_attn(), unless all of them in eights over the longest
+// sequence that the tables hold would take less than the 20 us that the other form needs at least (3.1 ns a tile of eight columns).
 AttnPlan plan_diff(const faedkv_pages *pg, int batch, int n_tokens) {
-    const AttnPlan p = plan_attn(pg, 2 * pg->gq, batch, n_tokens);
-    return p.wide ? plan_rows(pg, 2 * pg->gq, batch, n_tokens) : p;
+    const int gq = 2 * pg->gq;
+    const AttnPlan p = plan_attn(pg, gq, batch, n_tokens);
+    if (!p.wide) return p;
+    const double tiles = ((double)n_tokens * gq / 8 + batch) * (double)p.max_tiles * pg->cfg.n_kv_heads;
+    return tiles * 3.1 > 20000.0 ? plan_rows(pg, gq, batch, n_tokens) : plan_attn(pg, gq, batch, n_tokens, false);
 }
 size_t maps_at(const faedkv_pages *pg, int batch, int n_tokens) {   // where the maps' results lie in the workspace
     const AttnPlan p = plan_diff(pg, batch, n_tokens), q = plan_attn(pg, 2 * pg->gq, batch, n_tokens);

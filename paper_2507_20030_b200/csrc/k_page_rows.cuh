@@ -27,7 +27,7 @@ constexpr int kRowsConvert = 128, kRowsThreads = 256 + kRowsConvert + 128;  // 1
 constexpr int kRowsRegsSoftmax = 160, kRowsRegsConvert = 96, kRowsRegsIssue = 80;
 constexpr int kRowsRegsLaunch = 124;
 static_assert(2 * kRowsRegsSoftmax + kRowsRegsConvert + kRowsRegsIssue <= 4 * kRowsRegsLaunch, "a launch has these to share out");
-constexpr int kRowsCost = 6;                              // what a unit's start and end take, in tiles of one row tile
+constexpr int kRowsCost = 13;                             // what a unit's start and end take, in tiles of one row tile (1024 new tokens over 9216: 229 us at 6, 197 at 10, 194 at 13, 199 at 20)
 constexpr uint32_t kRowsOffV = kRowsK * kTileBytes, kRowsOffH = kRowsOffV + kRowsV * kTileBytes;
 constexpr uint32_t kRowsOffQ = kRowsOffH + kRowsH * 2 * kTileBytes, kRowsOffMisc = kRowsOffQ + 4 * kTileBytes;
 constexpr uint32_t kRowsFloats = kRowsQC + 2 * 128 * 4 + kRowsRing * 40 + 4 * 128;

@@ -23,8 +23,8 @@ struct AttnPlan {
     size_t bytes0, bytes1;   // workspace of MODE 0, of the others
 };
 
-// gq: query columns of a token and kv head.
-[[maybe_unused]] AttnPlan plan_attn(const faedkv_pages *pg, int gq, int batch, int n_tokens) {
+// gq: query columns of a token and kv head.  wide: whether blocks of many columns may be taken.
+[[maybe_unused]] AttnPlan plan_attn(const faedkv_pages *pg, int gq, int batch, int n_tokens, bool wide = true) {
     const faedkv_pages_config &c = pg->cfg;
     AttnPlan p{};
     p.max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
@@ -33,7 +33,7 @@ struct AttnPlan {
     // tokens, 8 kv heads: 115 us in 8s and 244 in 128s at 8 columns, 185 and 246 at 16, 266 and 247 at 24), but one long chunk
     // among decoding requests would go over its cache once for every 8 of them (120 tokens over 65536 beside 63 requests of 1000, 11
     // columns on average: 803 and 343 us; 320 tokens, 24 on average: 1973 and 650), so the rule leans to the side that loses less
-    p.wide = c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * gq > 8LL * batch;
+    p.wide = wide && c.kv_dtype == FAEDKV_BF16 && (long long)n_tokens * gq > 8LL * batch;
     p.qc = p.wide ? ChunkBf16::QC : 8;
     p.blocks = n_tokens / (p.qc / gq) + batch;
     p.shared = p.blocks <= pages::kMaxBlocks && p.blocks * (p.max_tiles + pages::kUnitCost) < (1LL << 31);   // (32-bit positions)

@@ -41,10 +41,10 @@ def expect(got, kind, q, K, V, seen, scale, lam, gain, eps, what):
         close(got[:, g], o, e, what)
 
 
-def case(fk, dtype, page, H, G, lens, new=None, pad=0, gain=True, eps=1e-5, scale=None, lam=None, qmul=1.0, pow2=True, strided=False, stream=None, seed=0):
+def case(fk, dtype, page, H, G, lens, new=None, pad=0, gain=True, eps=1e-5, scale=None, lam=None, qmul=1.0, pow2=True, strided=False, seed=0, width=1):
     rng = np.random.default_rng(sum(lens) + page + H * 31 + G + seed)
     B = len(lens)
-    W = max(1, max(ref.pages_of(n, page) for n in lens)) + 1
+    W = max(1, max(ref.pages_of(n, page) for n in lens)) + width
     n_pages = sum(ref.pages_of(n, page) for n in lens) + 2
     table = ref.spread(lens, page, n_pages, W, rng)
     (kc, ks), (vc, vs) = [ref.random_cache(rng, n_pages, H, page, lens, table, pow2) for _ in range(2)]
@@ -61,7 +61,7 @@ def case(fk, dtype, page, H, G, lens, new=None, pad=0, gain=True, eps=1e-5, scal
     args = (q, ref.ints(lens), ref.ints(table), ref.cuda8(kc), ref.cuda8(vc), ref.cuda32(ks), ref.cuda32(vs), lam, out)
     kw = dict(q_start=None if new is None else ref.ints(start), gain=gain, eps=eps, scale=scale or 0.0)
     pg.attn_diff(*args, **kw)
-    kind = "f32" if dtype == torch.float32 else "wide" if new is not None and n * 2 * G > 8 * B else "bf16"
+    kind = "f32" if dtype == torch.float32 else "wide" if new is not None and n * 2 * G > 8 * B else "bf16"    # (the wider of the two forms' bounds)
     for b in range(B):
         K, V = [torch.from_numpy(ref.rows_of(c, s, table[b], lens[b], page)).cuda() for c, s in ((kc, ks), (vc, vs))]
         m = counts[b]
@@ -98,6 +98,20 @@ def test_decode(fk, dtype, page, H, G, lens, gain):
 def test_new_tokens(fk, dtype, page, H, G, lens, new, pad):
     case(fk, dtype, page, H, G, lens, new, pad)
     case(fk, dtype, page, H, G, lens, new, pad, gain=False, strided=True)
+    for gain in (True, False) if dtype == torch.bfloat16 else ():            # wide tables: the form with query columns as rows, where there are many
+        case(fk, dtype, page, H, G, lens, new, pad, gain=gain, strided=gain, width=60000)
+
+
+@pytest.mark.parametrize("page,H,G,lens,new", [
+    (64, 1, 4, [5000], [40]),               # few blocks, the cached tokens split over CTAs: two row tiles
+    (16, 2, 2, [3000, 700], [20, 3]),       # one row tile, split
+    (128, 3, 4, [1900, 260], [100, 250]),
+    (32, 1, 1, [2100], [700]),
+    (64, 8, 1, [129, 4000], [129, 33]),
+])
+def test_new_tokens_over_split_caches(fk, page, H, G, lens, new):
+    case(fk, torch.bfloat16, page, H, G, lens, new, width=20000)
+    case(fk, torch.bfloat16, page, H, G, lens, new, gain=False, width=20000, qmul=4.0)
 
 
 def test_more_blocks_than_are_shared_out(fk):
@@ -106,7 +120,7 @@ def test_more_blocks_than_are_shared_out(fk):
     for dtype in (torch.bfloat16, torch.float32):
         case(fk, dtype, 16, 1, 1, lens)
         case(fk, dtype, 16, 1, 2, lens, [min(n, 1 + i % 3) for i, n in enumerate(lens)], 2)
-    case(fk, torch.bfloat16, 16, 1, 1, [n + 9 for n in lens], [10] * 1100)
+    case(fk, torch.bfloat16, 16, 1, 1, [n + 9 for n in lens], [10] * 1100, width=3000)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -115,6 +129,7 @@ def test_scale_lambda_and_eps(fk, dtype):
     case(fk, dtype, 16, 2, 2, [300, 70], lam=[0.0, 1.0, -0.5, 3.0])
     case(fk, dtype, 64, 1, 4, [1500], qmul=8.0)
     case(fk, dtype, 64, 1, 2, [700], [300], qmul=6.0, strided=True)
+    case(fk, dtype, 64, 1, 2, [700], [300], qmul=6.0, width=9000)
     case(fk, dtype, 16, 1, 2, [0, 33], eps=0.0)                            # a row of zeros stays one
     case(fk, dtype, 16, 1, 2, [33, 3], eps=10.0)
 
@@ -139,8 +154,9 @@ def test_nan_reaches_the_rows_that_see_it(fk, which):
     (kc, ks), (vc, vs) = [ref.random_cache(rng, 4, H, page, [n], table) for _ in range(2)]
     at = n - 4                                                 # seen by the last four tokens
     (kc, vc)[which][table[0, at // page], 0, at % page, 70] = 127
-    for new in (None, [m]):
-        pg = fk.Pages(n_kv_heads=H, n_q_heads=G, page_size=page, n_pages=4, max_pages=3, max_batch=1)
+    for new, width in ((None, 3), ([m], 3), ([m], 200000)):
+        table = np.concatenate([table[:, :3], np.full((1, width - 3), 0x7fffffff)], axis=1)
+        pg = fk.Pages(n_kv_heads=H, n_q_heads=G, page_size=page, n_pages=4, max_pages=width, max_batch=1)
         rows = m if new else 1
         q = torch.from_numpy(rng.standard_normal((rows, G, 128))).bfloat16().cuda()
         out = torch.full((rows, G, 128), 7.0, dtype=torch.bfloat16, device="cuda")

@@ -39,10 +39,13 @@ def layout(rng, page, groups):
     return np.asarray(table), lens, n_pages, W
 
 
-def case(fk, dtype, page, H, G, groups, shared=None, starts=None, status=0, scale=None, qmul=1.0, pow2=True, strided=False, edit=None, check_rows=None):
+def case(fk, dtype, page, H, G, groups, shared=None, starts=None, status=0, scale=None, qmul=1.0, pow2=True, strided=False, edit=None, check_rows=None, width=0):
     rng = np.random.default_rng(sum(s for s, _ in groups) + page + 31 * H + G)
     table, lens, n_pages, W = layout(rng, page, groups)
     B = len(lens)
+    if width:                                                # wide tables: bf16 groups of many query columns take the form with rows
+        table = np.concatenate([table, np.full((B, width), 0x7fffffff)], axis=1)
+        W += width
     (kc, ks), (vc, vs) = [ref.random_cache(rng, n_pages, H, page, lens, table, pow2) for _ in range(2)]
     if edit is not None:
         edit(table, kc, vc)
@@ -85,6 +88,20 @@ BOTH = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 ])
 def test_groups(fk, dtype, page, H, G, groups):
     case(fk, dtype, page, H, G, groups, pow2=page != 32, strided=page == 64)
+    if dtype == torch.bfloat16:
+        case(fk, dtype, page, H, G, groups, pow2=page != 32, width=100000, qmul=3.0 if page == 128 else 1.0)
+
+
+@pytest.mark.parametrize("page,H,G,groups", [
+    (16, 1, 8, [(2048, [2050] * 33)]),                                     # two row tiles and some, split over CTAs
+    (64, 2, 4, [(4096, [4100 + 9 * i for i in range(64)]), (640, [700] * 12)]),
+    (32, 5, 2, [(1600, [1601 + i for i in range(64)])]),                   # one row tile of 128
+    (16, 2, 7, [(160, [0, 150, 161, 160, 17, 300] + [170] * 31)]),         # rows shorter than their group among many
+    (128, 1, 5, [(8192, [8200] * 13), (0, [5] * 13)]),
+])
+def test_groups_of_many_columns(fk, page, H, G, groups):
+    case(fk, torch.bfloat16, page, H, G, groups, width=50000)
+    case(fk, torch.bfloat16, page, H, G, groups, width=50000, qmul=5.0, strided=True, pow2=False)
 
 
 @BOTH
@@ -126,6 +143,9 @@ def test_more_blocks_than_are_shared_out(fk, dtype):
     assert sum(len(r) for _, r in groups) > 1024
     rows = sum(len(r) for _, r in groups)
     case(fk, dtype, 16, 2, 2, groups, check_rows=sorted({*range(0, rows, 5), *range(rows - 40, rows)}))
+    if dtype == torch.bfloat16:
+        groups = [(96, [100 + i % 30 for i in range(700)]), (32, [33] * 400 + [50] * 20)]
+        case(fk, dtype, 16, 1, 2, groups, check_rows=range(0, 1120, 9), width=5000)
 
 
 @BOTH
