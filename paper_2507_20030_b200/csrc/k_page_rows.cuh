@@ -345,11 +345,11 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         if (!there_x) wait(x.bar, x.parity, kErrAttnMma);
         if (!there_y) wait(y.bar, y.parity, kErrAttnMma);
     };
-    // The next segment, from the ring (the other warps): finding it is a chain of loads that the TMA warp has gone through ahead of them.
+    // The next segment, from the ring (the other warps): finding it is a chain of loads that the TMA warp has gone through ahead of them.  Warps that gave up
+    // go through the segments as the others do, since those meet them at barriers; the TMA warp marks the end in any case.
     auto next_segment = [&](uint32_t seg, RowsSegment &s) {
         const int at = seg % kRowsSegs;
-        wait(gfull(at), (seg / kRowsSegs) & 1u, kErrAttnSoftmax);
-        if (dead) return false;
+        if (!__all_sync(0xffffffffu, mbar_wait(gfull(at), (seg / kRowsSegs) & 1u, 8 * a.wait_limit))) return false;
         const int *r = seg_ring + 16 * at;
         s.b = 0; s.page0 = 0;
         s.h = r[0]; s.tok0 = r[1]; s.n_tok = r[2]; s.see0 = r[3]; s.live = r[4]; s.own = r[5]; s.t0 = r[6]; s.t1 = r[7]; s.tiles = r[8];
@@ -376,7 +376,8 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         RowsWork<MODE> w = w0;
         RowsSegment s;
         int it = 0, issued_k = 0, issued_v = 0;
-        for (uint32_t seg = 0;; ++seg) {
+        uint32_t seg = 0;
+        for (;; ++seg) {
             const bool more = w.next(a, s);
             const int at = seg % kRowsSegs;
             wait(gempty(at), ((seg / kRowsSegs) & 1u) ^ 1u, kErrAttnTma);
@@ -465,7 +466,13 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 id = id_next; ks = ks_next; vs = vs_next;
             }
         }
-        if (dead) {                                        // leave no copy in flight behind
+        if (dead && lane == 0) {                           // the end, for those who did not give up
+            if (mbar_wait(gempty(seg % kRowsSegs), ((seg / kRowsSegs) & 1u) ^ 1u, 4 * a.wait_limit)) {
+                seg_ring[16 * (seg % kRowsSegs) + 9] = 0;
+                mbar_arrive(gfull(seg % kRowsSegs));
+            }
+        }
+        {                                                  // leave no copy in flight behind, whoever gave up
             for (int i = max(0, issued_k - kRowsK); i < issued_k; ++i) mbar_wait(kfull(i % kRowsK), (uint32_t)(i / kRowsK) & 1u, a.wait_limit);
             for (int i = max(0, issued_v - kRowsV); i < issued_v; ++i) mbar_wait(vfull(i % kRowsV), (uint32_t)(i / kRowsV) & 1u, a.wait_limit);
         }
@@ -530,6 +537,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRowsRegsConvert));
         // ------------------------------------------------------------------------ V tiles to f16, a token a thread
         RowsSegment s;
+        const int row = tid - kSoftmax;
         int it = 0;
         uint32_t h_uses = 0;
         for (uint32_t seg = 0; next_segment(seg, s); ++seg) {
@@ -542,45 +550,45 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const bool all = whole_tile(s, t, have), ragged = (MODE == 1 || MODE == 2) && s.n_tok > 1 && (t + 1) * kTile > s.see0;
                 const uint8_t *from = gbase + kRowsOffV + (uint32_t)sv * kTileBytes;
                 uint8_t *to = gbase + kRowsOffH + (uint32_t)hb * 2 * kTileBytes;
-                {
-                    const int row = tid - 256;
-                    uint4 v[8];
+                uint4 v[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint4 *>(from + mn_chunk<128>(row, j));
-                    wait(hempty(hb), ((h_uses >> hb ^ (uint32_t)round) & 1u) ^ 1u, kErrAttnSoftmax);
-                    // (the segment four before has been written out: its place is free)
-                    if ((MODE == 1 || MODE == 2) && i == 0) {
-                        first[row] = 0x7fffffff;
-                        softmax_bar(3, kRowsConvert);
-                    }
-                    if (!all) {
-                        // 0 * NaN is not 0: values behind the end must not reach the product, nor a NaN value of a token that some rows see and
-                        // others do not: it is noted by its channel, for the rows that see it
-                        const int tok = t * kTile + row;
-                        const bool valid = tok < s.live && ((have >> (row >> a.page_shift)) & 1u);
+                for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint4 *>(from + mn_chunk<128>(row, j));
+                wait(hempty(hb), ((h_uses >> hb ^ (uint32_t)round) & 1u) ^ 1u, kErrAttnSoftmax);
+                // the third buffer is also the second row tile's q, and the room its results go out through: those of the segment before are done with
+                // it once this segment's q is there
+                if (hb == 2 && round == 0) wait(qfull, seg & 1u, kErrAttnSoftmax);
+                // (the segment four before has been written out: its place is free)
+                if ((MODE == 1 || MODE == 2) && i == 0) {
+                    first[row] = 0x7fffffff;
+                    softmax_bar(3, kRowsConvert);
+                }
+                if (!all) {
+                    // 0 * NaN is not 0: values behind the end must not reach the product, nor a NaN value of a token that some rows see and
+                    // others do not: it is noted by its channel, for the rows that see it
+                    const int tok = t * kTile + row;
+                    const bool valid = tok < s.live && ((have >> (row >> a.page_shift)) & 1u);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if (!valid) v[j] = make_uint4(0u, 0u, 0u, 0u);
-                            uint32_t *u = reinterpret_cast<uint32_t *>(&v[j]);
+                    for (int j = 0; j < 8; ++j) {
+                        if (!valid) v[j] = make_uint4(0u, 0u, 0u, 0u);
+                        uint32_t *u = reinterpret_cast<uint32_t *>(&v[j]);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const uint32_t is_nan = ragged ? ((u[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : 0u;   // the top bit of each NaN code
-                                if (is_nan != 0u) {
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t is_nan = ragged ? ((u[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : 0u;   // the top bit of each NaN code
+                            if (is_nan != 0u) {
 #pragma unroll 1
-                                    for (int e = 0; e < 4; ++e)
-                                        if ((is_nan >> (8 * e + 7)) & 1u) atomicMin(first + 16 * j + 4 * k + e, tok);
-                                    u[k] &= ~((is_nan >> 7) * 255u);
-                                }
+                                for (int e = 0; e < 4; ++e)
+                                    if ((is_nan >> (8 * e + 7)) & 1u) atomicMin(first + 16 * j + 4 * k + e, tok);
+                                u[k] &= ~((is_nan >> 7) * 255u);
                             }
                         }
                     }
+                }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {                            // 16 channels
-                        const uint4 lo = make_uint4(e4m3x2_to_f16x2(v[j].x), e4m3x2_to_f16x2(v[j].x >> 16), e4m3x2_to_f16x2(v[j].y), e4m3x2_to_f16x2(v[j].y >> 16));
-                        const uint4 hi = make_uint4(e4m3x2_to_f16x2(v[j].z), e4m3x2_to_f16x2(v[j].z >> 16), e4m3x2_to_f16x2(v[j].w), e4m3x2_to_f16x2(v[j].w >> 16));
-                        *reinterpret_cast<uint4 *>(to + (j >> 2) * kTileBytes + mn_chunk<128>(row, (2 * j) & 7)) = lo;
-                        *reinterpret_cast<uint4 *>(to + (j >> 2) * kTileBytes + mn_chunk<128>(row, (2 * j + 1) & 7)) = hi;
-                    }
+                for (int j = 0; j < 8; ++j) {                            // 16 channels
+                    const uint4 lo = make_uint4(e4m3x2_to_f16x2(v[j].x), e4m3x2_to_f16x2(v[j].x >> 16), e4m3x2_to_f16x2(v[j].y), e4m3x2_to_f16x2(v[j].y >> 16));
+                    const uint4 hi = make_uint4(e4m3x2_to_f16x2(v[j].z), e4m3x2_to_f16x2(v[j].z >> 16), e4m3x2_to_f16x2(v[j].w), e4m3x2_to_f16x2(v[j].w >> 16));
+                    *reinterpret_cast<uint4 *>(to + (j >> 2) * kTileBytes + mn_chunk<128>(row, (2 * j) & 7)) = lo;
+                    *reinterpret_cast<uint4 *>(to + (j >> 2) * kTileBytes + mn_chunk<128>(row, (2 * j + 1) & 7)) = hi;
                 }
                 fence_proxy_async();
                 __syncwarp();

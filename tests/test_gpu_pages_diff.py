@@ -114,6 +114,22 @@ def test_new_tokens_over_split_caches(fk, page, H, G, lens, new):
     case(fk, torch.bfloat16, page, H, G, lens, new, gain=False, width=20000, qmul=4.0)
 
 
+@pytest.mark.parametrize("page,H,G,lens,new", [
+    (64, 2, 4, [30000, 30000], [40, 40]),    # a block of 64 columns behind one of 256, on one CTA
+    (16, 2, 4, [4000, 2600, 5000], [36, 70, 33]),
+    (32, 1, 2, [9000], [130]),
+])
+@pytest.mark.parametrize("gain", [True, False])
+def test_blocks_of_one_row_tile_behind_blocks_of_two(fk, page, H, G, lens, new, gain):
+    """A CTA goes from a block with two row tiles on to one with a single one, whose values have more room: again and again, the same bits."""
+    pg, args, kw, out = case(fk, torch.bfloat16, page, H, G, lens, new, 2, gain=gain, width=60000)
+    first = out.clone()
+    for _ in range(10):
+        out.fill_(7.0)
+        pg.attn_diff(*args, **kw)
+        assert torch.equal(out, first)
+
+
 def test_more_blocks_than_are_shared_out(fk):
     rng = np.random.default_rng(2)
     lens = rng.integers(1, 20, 1100).tolist()

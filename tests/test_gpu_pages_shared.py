@@ -194,6 +194,19 @@ def test_a_call_gives_the_same_bits_again(fk):
         assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("groups", [
+    [(20480, [20500 + i for i in range(64)]), (30720, [30800] * 20)],        # a block of 80 columns behind one of 256, on one CTA
+    [(20480, [20500 + i for i in range(70)])],
+])
+def test_many_columns_give_the_same_bits_again(fk, groups):
+    pg, args, out = case(fk, torch.bfloat16, 64, 2, 4, groups, width=50000)
+    first = out.clone()
+    for _ in range(10):
+        out.zero_()
+        pg.attn_shared(*args)
+        assert torch.equal(out, first)
+
+
 def test_captured_and_on_another_stream(fk):
     pg, args, out = case(fk, torch.bfloat16, 64, 2, 4, [(640, [700, 641, 999]), (0, [5, 130])])
     want, q0 = out.clone(), args[0].clone()
