@@ -59,6 +59,9 @@ def test_null_handles_are_refused(fk):
     assert lib.faedkv_pages_fork(z, z, z, z, 0, 1, z, z, z, z, z, z, z, z, z, z, z) == -1
     assert lib.faedkv_pages_release(z, z, z, 1, z, z, z, z, z, z, z) == -1
     assert lib.faedkv_pages_compact(z, z, 1, z, z, z, z, z, z, z, z, z, z, z) == -1
+    assert lib.faedkv_pages_attn_shared(z, z, 256, z, z, 1, 1, z, z, z, z, z, z, 0.0, z, z, 0, z) == -1
+    assert lib.faedkv_pages_attn_diff(z, z, 256, z, 1, 1, z, z, z, z, z, z, 0.0, z, z, 0.0, z, z, 0, z) == -1
+    assert lib.faedkv_pages_attn_shared_bytes(z, 1, 1) == 0 and lib.faedkv_pages_attn_diff_bytes(z, 1, 1) == 0
     assert lib.faedkv_pages_fork_bytes(z, 1, 1) == 0 and lib.faedkv_pages_release_bytes(z) == 0 and lib.faedkv_pages_compact_bytes(z) == 0
 
 
@@ -83,6 +86,31 @@ def test_binding_refuses_wrong_tensors_of_the_page_calls(fk):
     assert args == (None, fork["src"].data_ptr(), fork["dst"].data_ptr(), fork["length"].data_ptr(), 2, 2, fork["kv_len"].data_ptr(),
                     fork["table"].data_ptr(), fork["free_pages"].data_ptr(), fork["n_free"].data_ptr(), fork["n_free_out"].data_ptr(),
                     codes.data_ptr(), codes.data_ptr(), scale.data_ptr(), scale.data_ptr(), ws.data_ptr(), 77)
+
+
+def test_binding_refuses_wrong_tensors_of_the_attention_calls(fk):
+    pg = bare(fk)
+    codes, scale = torch.zeros(3, 2, 16, 128, dtype=torch.float8_e4m3fn), torch.zeros(3, 2)
+    cache = dict(k_pages=codes, v_pages=codes.clone(), k_scale=scale, v_scale=scale.clone())
+    ws = torch.zeros(64, dtype=torch.uint8)
+    rows = torch.zeros(2, 4, 128, dtype=torch.bfloat16)
+    base = dict(q=rows, kv_len=i32(2), table=i32(2, 4), out=rows.clone(), ws=ws, **cache)
+    shared = dict(base, group_start=i32(2), shared_len=i32(1))
+    refused_one_by_one(pg.attn_shared, shared, ["q", "table", "group_start", "out", *cache], wrong)
+    diff = dict(base, lam=torch.zeros(4), gain=torch.ones(128), q_start=i32(3))
+    refused_one_by_one(pg.attn_diff, diff, ["q", "table", "q_start", "lam", "gain", "out", *cache], wrong)
+    with pytest.raises(ValueError, match="one token for each of 2 rows"):
+        pg.attn_shared(**{**shared, "q": torch.zeros(3, 4, 128, dtype=torch.bfloat16), "out": torch.zeros(3, 4, 128, dtype=torch.bfloat16)})
+    for call, args in ((pg.attn_shared, shared), (pg.attn_diff, diff)):
+        with pytest.raises(ValueError, match="ws"):
+            call(**{**args, "ws": torch.zeros(8, dtype=torch.uint8)})
+    calls = {name: args for name, args in pg._lib.calls}
+    c = [cache[k].data_ptr() for k in ("k_pages", "v_pages", "k_scale", "v_scale")]
+    ptr = {k: t.data_ptr() for k, t in {**shared, **diff}.items()}
+    assert calls["faedkv_pages_attn_shared"] == (None, ptr["q"], 512, ptr["group_start"], ptr["shared_len"], 1, 2, ptr["kv_len"], ptr["table"], *c, 0.0,
+                                                 ptr["out"], ptr["ws"], 64, 77)
+    assert calls["faedkv_pages_attn_diff"] == (None, ptr["q"], 512, ptr["q_start"], 2, 2, ptr["kv_len"], ptr["table"], *c, 0.0, ptr["lam"],
+                                               ptr["gain"], 0.0, ptr["out"], ptr["ws"], 64, 77)
 
 
 def test_reference_fork_release_compact_by_hand():
