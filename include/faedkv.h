@@ -479,8 +479,8 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
  * the table row of the first row of the block that has them all; what a row holds behind them is read for itself.  A row that holds less
  * than its group shares is attended alone, as is the only row of a group and one that stands in no group or in one whose bounds
  * are not rows of the batch (status 0x105).  q, out, scale and results as faedkv_pages_attn(), rounding as there (bf16: a softmax weight
- * is held to 2^-11 of itself and 2^-31 of its row's largest); the tables are not searched for other shared pages.  ws: faedkv_pages_attn_shared_bytes() (0 for arguments that the call
- * would refuse), 16-byte aligned, overwritten. */
+ * is held to 2^-11 of itself and 2^-31 of its row's largest); the tables are not searched for other shared pages.
+ * ws: faedkv_pages_attn_shared_bytes() (0 for arguments that the call would refuse), 16-byte aligned, overwritten. */
 size_t faedkv_pages_attn_shared_bytes(const faedkv_pages *pg, int batch, int n_groups);
 int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *group_start, const int32_t *shared_len,
                              int n_groups, int batch, const int32_t *kv_len, const int32_t *table, const void *k_pages,

@@ -87,6 +87,8 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float
 // (Letting the predecessor release its dependents early, by griddepcontrol.launch_dependents at its start,
 // was measured slower here: the waiting CTAs hold shared memory and registers the predecessor still needs.)
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the next kernel's CTAs begin where this one's have ended, for a next kernel that has work of its own before its pdl_wait().
+__device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Streaming (evict-first) 16-byte global accesses for planes that are touched
 // once per call and are far larger than L2.

@@ -23,8 +23,7 @@ int launch_cluster(faedkv_pages *pg, const char *what, void (*kernel)(Args...), 
     return launch_check(pg, what);
 }
 
-// Up to this many forks and rows the CTAs that copy find out for themselves what comes before them.  (16 rows forked into 256: 10 us with a plan in
-// one CTA before the copies.)
+// Up to this many forks and rows the CTAs that copy find out for themselves what comes before them: the marks fit shared memory.
 bool forks_alone(int batch, int n_forks) { return n_forks <= pages::kForkSmall && batch <= pages::kForkRows; }
 
 }  // namespace

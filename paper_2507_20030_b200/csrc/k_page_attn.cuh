@@ -523,7 +523,9 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         fence_barrier_init();
     }
     if (warp == kWarpMma) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
-    pdl_wait();                                            // (releasing the join from here on was slower: 17.5 us, not 16.5, at six ragged sequences)
+    // (releasing the join from here on was slower: 17.5 us, not 16.5, at six ragged sequences)
+    // The launch of the rows' own tokens needs nothing of the one of the groups' before it, which has waited for all that came earlier.
+    if (MODE < 3 || a.which != 2) pdl_wait();
 
     // ---- this CTA's work
     Work<MODE> w0;
@@ -1274,6 +1276,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         tc_fence_after();
         tmem_dealloc(tmem, C::kTmemCols);
     }
+    if (MODE >= 3 && a.which == 2) pdl_wait();             // the join waits for this launch, and by it for the other
 }
 
 // Joins the partial results of a unit: rescaled to the largest Mu, summed in order, divided.  They lie in the slots of the

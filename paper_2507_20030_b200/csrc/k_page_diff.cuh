@@ -2,8 +2,10 @@
 //
 //     out[i, g] = norm(a1 - lam[g] * a2),   a_m = softmax(scale * q_m . K_m) V,   q = [q_1 | q_2], K = [K_1 | K_2], 64 channels each
 //
-// norm(o) = o * gain / sqrt(mean(o^2) + eps) over the head's 128 channels, or o itself without a gain.  k_page_attn computes the a_m as
-// columns of one pass over the cache: the codes of K and V are read once for both maps of all heads.
+// norm(o) = o * gain / sqrt(mean(o^2) + eps) over the head's 128 channels, or o itself without a gain.  k_page_attn and k_page_rows compute the a_m as
+// columns (rows) of one pass over the cache: the codes of K and V are read once for both maps of all heads, and a map's query is zero in the other's
+// channels, so that one product over 128 channels gives either score; half of its multiplications are with zero, which costs a decode step nothing (16 x
+// 16384 tokens, 8 kv heads: 89 us, the bytes alone 82) and a prompt a quarter of its products.
 #pragma once
 #include "k_page_rows.cuh"
 

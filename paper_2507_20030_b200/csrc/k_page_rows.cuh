@@ -16,6 +16,11 @@
 // two row tiles over the same tokens (K, V and the conversion shared); one of up to 128 rows gives every other tile of tokens to each
 // warpgroup, and the two results meet as parts of a softmax do.  Four warps convert V; a TMA warp; one warp issues the first product and one
 // the second, since what an issuer waits for between products would leave the tensor cores idle.
+//
+// What bounds it is the two softmax warps of a scheduler: a half tile of both takes them some 2500 cycles, of which the exponentials are 1024 and the
+// tensor cores' products as many; the rest is what a warp waits for between its steps (loads from tensor memory, its turn, stores), and registers leave
+// no room for a third.  1024 + 1 + 333 new tokens over 9216 + 4001 + 333, 8 kv x 16 differential heads: 190 us, 0.35 of the tensor cores' measured rate
+// (303 in k_page_attn's form with 128 columns).
 #pragma once
 #include "k_page_attn.cuh"
 
@@ -27,7 +32,7 @@ constexpr int kRowsConvert = 128, kRowsThreads = 256 + kRowsConvert + 128;  // 1
 constexpr int kRowsRegsSoftmax = 160, kRowsRegsConvert = 96, kRowsRegsIssue = 80;
 constexpr int kRowsRegsLaunch = 124;
 static_assert(2 * kRowsRegsSoftmax + kRowsRegsConvert + kRowsRegsIssue <= 4 * kRowsRegsLaunch, "a launch has these to share out");
-constexpr int kRowsCost = 13;                             // what a unit's start and end take, in tiles of one row tile (1024 new tokens over 9216: 229 us at 6, 197 at 10, 194 at 13, 199 at 20)
+constexpr int kRowsCost = 13;                             // what a unit's start and end take, in tiles of one row tile (1024 new tokens over 9216: 228 us at 6, 193 at 10, 190 at 13, 192 at 16, 196 at 20)
 constexpr uint32_t kRowsOffV = kRowsK * kTileBytes, kRowsOffH = kRowsOffV + kRowsV * kTileBytes;
 constexpr uint32_t kRowsOffQ = kRowsOffH + kRowsH * 2 * kTileBytes, kRowsOffMisc = kRowsOffQ + 4 * kTileBytes;
 constexpr uint32_t kRowsFloats = kRowsQC + 2 * 128 * 4 + kRowsRing * 40 + 4 * 128;
@@ -46,7 +51,7 @@ __device__ __forceinline__ uint32_t f16x2_to_e5m2x2(uint32_t h) {
     asm("{\n\t.reg .b16 c;\n\tcvt.rn.satfinite.e5m2x2.f16x2 c, %1;\n\tcvt.u32.u16 %0, c;\n\t}" : "=r"(r) : "r"(h));
     return r;
 }
-// The MMA warp goes through its code with all lanes and issues by one, so that descriptors stay in uniform registers: an instruction issued by a
+// An MMA warp goes through its code with all lanes and issues by one, so that descriptors stay in uniform registers: an instruction issued by a
 // lane in a branch of its own takes some 95 cycles, more than its product.
 __device__ __forceinline__ uint32_t elect_one() {
     uint32_t r;
@@ -274,6 +279,9 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
     if (warp == kWarpScores) tmem_alloc(smem_u32(tmem_slot), 512);
     pdl_wait();
+    // the rows' own tokens: their CTAs begin where these have ended (64 rows behind 32768 tokens 92.5 us without, 88.8 so; a join released like this, which
+    // can only wait, costs 2 us)
+    if (MODE >= 3) pdl_release();
 
     // ---- this CTA's work
     RowsWork<MODE> w0;
@@ -720,7 +728,8 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     if (lane == 0) mbar_arrive(sread(g));
                 };
                 // The two warps of a scheduler take turns with the exponentials: side by side they would both wait for the unit, and then both for the
-                // tensor cores.  Item q of the second warpgroup follows item q of the first
+                // tensor cores.  Item q of the second warpgroup follows item q of the first.  A turn ends with the third quarter of them, since a warp
+                // alone does not fill the unit (1024 new tokens over 9216: 193.5 us after a quarter or half, 189.5 so, 193 at their end)
                 const int other = 2 * tiles_of_group(s, g ^ 1);
                 auto turn_begin = [&]() {
                     if (g == 1 || (q > 0 && q - 1 < other)) softmax_bar(4 + 2 * (warp & 3) + g, 64);
@@ -788,7 +797,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         for (int p = 0; p < 8; ++p)
                             y[k][p] = fma2(make_float2(raw[k >> 1][(k & 1) * 16 + 2 * p], raw[k >> 1][(k & 1) * 16 + 2 * p + 1]), make_float2(kf[k], kf[k]), make_float2(add[k], add[k]));
                     // the weights, into their place; returns their sum
-                    auto weights = [&](auto general) {
+                    auto weights = [&](auto general, bool again) {
                         float sum = 0.f;
                         l_half = make_float2(0.f, 0.f);
 #pragma unroll
@@ -808,6 +817,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                                 }
                                 l_half = fma2(part, make_float2(inv_r, inv_r), l_half);
                                 sum += part.x + part.y;
+                                if (k == 2 && !again) turn_end();
                             }
                             tmem_st16u(tp + 16 * i, packed);
                         }
@@ -815,8 +825,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     };
                     for (bool again = false;; again = true) {
                         if (!again) turn_begin();
-                        const float sum = plain ? weights(std::false_type{}) : weights(std::true_type{});
-                        if (!again) turn_end();
+                        const float sum = plain ? weights(std::false_type{}, again) : weights(std::true_type{}, again);
                         // beyond what f16 holds, or no reference yet: Mu is raised, and the weights once more
                         const bool need = !set || !(sum <= kMostSum);
                         if (again || !__any_sync(0xffffffffu, need)) break;

@@ -12,7 +12,7 @@ namespace faedkv {
 namespace pages {
 
 constexpr unsigned int kBadRow = 0x106;                   // a row of the block table that there is not, or that may not be written
-constexpr int kCluster = 16;                              // CTAs that meet in one launch: the most there are (512 requests: 22 us with 8)
+constexpr int kCluster = 16;                              // CTAs that meet in one launch: the most there are
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -108,8 +108,8 @@ __device__ __forceinline__ void fork_copy(const ForkArgs &a, int s, int d, int n
     }
 }
 
-// Few forks among few rows: every CTA finds out for itself which forks before its own take a page; one launch, and no workspace.  Grid (forks, parts of
-// a fork's copy).  COPY = false, one CTA: the height of the stack alone, where it is written over the one that all have to read.
+// Few forks among few rows: every CTA finds out for itself which forks before its own take a page; one launch, and no workspace (8 forks: 15.7 us a call
+// with a plan in one CTA before the copies, 10.7 so; 16 rows into 256: 10 and 9 us on the device, of which the bytes are 2).  Grid (forks, parts of a fork's copy).  COPY = false, one CTA: the height of the stack alone, where it is written over the one that all have to read.
 constexpr int kForkSmall = 1024, kForkRows = 4096;
 template <bool COPY>
 static __global__ void __launch_bounds__(256) k_page_fork(const ForkArgs a, const bool height_too) {
@@ -238,8 +238,9 @@ struct ReleaseArgs {
 // One cluster.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
 //
 // Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store, and the pages that running
-// requests name are bits in shared memory, each CTA's own first, then all of them (as atomics to global memory, the entries of 512 requests took 20 us of
-// 25).
+// requests name are bits in shared memory, each CTA's own first, then all of them.  What bounds it is the chain: lengths, entries, three meetings of the
+// cluster, the stack.  (512 requests of up to 256 pages: 34 us with each row read in every phase and eight CTAs; 25 with the entries in registers and the
+// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  Seven of eight rows: 9.5 and 6.5 us.)
 constexpr int kReleaseShort = 65536;                      // pages
 __device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {        // what p is in another CTA of the cluster
     uint32_t at, v;
@@ -618,7 +619,8 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_short(cons
     for (int k = tid; k < n - n_low; k += kPlanThreads) a.new_id[__ldcg(moves + k)] = __ldcg(holes + k);
 }
 
-// The pages that move, 16 KB of a tensor at a time, and the tables.
+// The pages that move, 16 KB of a tensor at a time, and the tables.  Bound by memory: 2048 of 8192 pages (8 heads of 64 tokens, 268 MB read and as many
+// written) 97 us with the plan before it, 82 at the rate of a plain copy.
 constexpr int kMoveUnits = 1024;                          // of 16 bytes
 static __global__ void __launch_bounds__(256) k_page_move(const CompactArgs a) {
     pdl_wait();

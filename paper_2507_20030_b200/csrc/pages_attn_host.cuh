@@ -63,7 +63,7 @@ int launch_attn(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv, 
     const dim3 grid = MODE == 0 ? dim3(p.ctas0) : MODE == 1 ? dim3(p.ctas1) : dim3(p.blocks, a.H);
     CUDA_TRY(pg, launch_pdl(kernel, grid, dim3(C::kThreads), smem, st, mk, mv, a));
     if (int r = launch_check(pg, "k_page_attn")) return r;
-    if (MODE == 2 || p.max_tiles == 1 ) return FAEDKV_OK;                     // no unit is ever in parts
+    if (MODE == 2 || p.max_tiles == 1) return FAEDKV_OK;                     // no unit is ever in parts
     if constexpr (MODE == 0 && FORM == 1) return FAEDKV_OK;                   // the caller puts the parts together
     else if constexpr (MODE != 2) {
         const int cols = MODE == 0 ? a.G : C::QC / a.G * a.G, each = MODE == 0 ? 1 : 16;
