@@ -14,12 +14,22 @@ int check_table(faedkv_pages *pg, int batch) {
 
 // A launch of one cluster; larger ones than the portable eight CTAs have to be asked for, once for each kernel.
 template <typename... Args>
-int launch_cluster(faedkv_pages *pg, const char *what, void (*kernel)(Args...), int attr_bit, cudaStream_t st, Args... args) {
+int launch_cluster(faedkv_pages *pg, const char *what, void (*kernel)(Args...), int attr_bit, int ctas, cudaStream_t st, Args... args) {
     if (!(pg->attr_set & (1u << attr_bit))) {
         CUDA_TRY(pg, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         pg->attr_set |= 1u << attr_bit;
     }
-    kernel<<<pages::kCluster, pages::kPlanThreads, 0, st>>>(args...);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(pages::kPlanThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CUDA_TRY(pg, cudaLaunchKernelEx(&cfg, kernel, args...));
     return launch_check(pg, what);
 }
 
@@ -90,19 +100,21 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     const pages::ReleaseArgs a{t_len, n_new, table, n_free, free_pages, kv_len, n_free_out, static_cast<int32_t *>(ws), batch,
                                pg->cfg.max_pages, pg->cfg.n_pages, pg->page_shift, pg->dev_status};
     // parts of a row, a warp each: more than one where there are fewer rows than warps, or where that makes them short enough for registers
-    const int warps = pages::kCluster * pages::kPlanThreads / 32;
-    int parts = 1;
-    while (parts < 32 && 2 * parts * batch <= warps) parts *= 2;
-    int fits = parts;
-    while (fits < 32 && pg->cfg.max_pages > 256 * fits) fits *= 2;
-    const bool in_registers = pg->cfg.max_pages <= 256 * fits && fits * batch <= 4 * warps && pg->cfg.n_pages <= pages::kReleaseShort;
-    if (in_registers) parts = fits;
+    const int warps = pages::kPlanThreads / 32, most = pages::kCluster * warps;
+    int parts = 1, ctas = pages::kCluster;
+    while (parts < 32 && pg->cfg.max_pages > 256 * parts) parts *= 2;
+    const bool in_registers = pg->cfg.max_pages <= 256 * parts && parts * batch <= 4 * most && pg->cfg.n_pages <= pages::kReleaseShort;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int each = !in_registers ? 0 : batch * parts <= warps ? 1 : batch * parts <= 2 * warps ? 2 : 4;
-    return each == 1   ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<1>, 22, st, a, parts)
-           : each == 2 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<2>, 23, st, a, parts)
-           : each == 4 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<4>, 24, st, a, parts)
-                       : launch_cluster(pg, "k_page_release", pages::k_page_release, 25, st, a, parts);
+    if (in_registers)                                      // as few CTAs as have the warps: a larger cluster takes longer to begin and to meet (32 rows 8.6 us with 16, 6.5 with one)
+        while (ctas > 1 && parts * batch <= ctas / 2 * warps) ctas /= 2;
+    else
+        parts = 1;
+    while (parts < 32 && 2 * parts * batch <= ctas * warps) parts *= 2;
+    const int each = !in_registers ? 0 : batch * parts <= most ? 1 : batch * parts <= 2 * most ? 2 : 4;
+    return each == 1   ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<1>, 22, ctas, st, a, parts)
+           : each == 2 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<2>, 23, ctas, st, a, parts)
+           : each == 4 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<4>, 24, ctas, st, a, parts)
+                       : launch_cluster(pg, "k_page_release", pages::k_page_release, 25, ctas, st, a, parts);
 }
 
 size_t faedkv_pages_compact_bytes(const faedkv_pages *pg) {
@@ -129,7 +141,7 @@ int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, con
     if (c.n_pages <= pages::kCompactShort && (long long)batch * c.max_pages <= 16 * pages::kCompactShort) {
         pages::k_page_compact_short<<<1, pages::kPlanThreads, 0, st>>>(a);
         if (int r = launch_check(pg, "k_page_compact_short")) return r;
-    } else if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan, 26, st, a)) {
+    } else if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan, 26, pages::kCluster, st, a)) {
         return r;
     }
     CUDA_TRY(pg, launch_pdl(pages::k_page_move, dim3(pg->n_sm * 8), dim3(256), 0, st, a));

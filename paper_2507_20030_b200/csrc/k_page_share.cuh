@@ -235,12 +235,13 @@ struct ReleaseArgs {
     unsigned int *status;
 };
 
-// One cluster.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
+// One cluster, the grid.  A row is cut into `parts` runs of pages, one a warp's: one where there are rows enough for the warps.
 //
 // Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store, and the pages that running
 // requests name are bits in shared memory, each CTA's own first, then all of them.  What bounds it is the chain: lengths, entries, three meetings of the
 // cluster, the stack.  (512 requests of up to 256 pages: 34 us with each row read in every phase and eight CTAs; 25 with the entries in registers and the
-// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  Seven of eight rows: 9.5 and 6.5 us.)
+// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  Eight rows: 7.9 us with sixteen CTAs, 5.8
+// with one.)
 constexpr int kReleaseShort = 65536;                      // pages
 __device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {        // what p is in another CTA of the cluster
     uint32_t at, v;
@@ -249,11 +250,11 @@ __device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {   
     return v;
 }
 template <int K>
-static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release_short(const ReleaseArgs a, const int parts) {
+static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(const ReleaseArgs a, const int parts) {
     __shared__ int32_t count[32 * K + 1];
     __shared__ uint32_t own[kReleaseShort / 32], live[kReleaseShort / 32];
     const int words = (a.n_pages + 31) / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank(), ctas = (int)gridDim.x;
     const long long cap = (long long)a.W << a.page_shift;
     const int page = 1 << a.page_shift;
     const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && rank == 0);
@@ -290,7 +291,7 @@ static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanT
     for (int w = tid; w < words; w += kPlanThreads) {
         uint32_t m = 0;
 #pragma unroll
-        for (int r = 0; r < kCluster; ++r) m |= load_of_cta(own + w, r);
+        for (int r = 0; r < kCluster; ++r) m |= r < ctas ? load_of_cta(own + w, r) : 0u;
         live[w] = m;
     }
 #pragma unroll
@@ -331,7 +332,7 @@ static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanT
     }
     cluster_sync();
     long long at0 = height, all = height;
-    for (int r = 0; r < kCluster; ++r) {
+    for (int r = 0; r < ctas; ++r) {
         const int n = __ldcg(totals + r);
         if (r < rank) at0 += n;
         all += n;
@@ -357,7 +358,7 @@ static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanT
 constexpr int kReleaseItems = 65536 / kCluster;           // items of a CTA: one warp's part of a row
 
 // Any number of rows and pages: the runs are read again in every phase.
-static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_release(const ReleaseArgs a, const int parts) {
+static __global__ void __launch_bounds__(kPlanThreads) k_page_release(const ReleaseArgs a, const int parts) {
     __shared__ long long warp_sums[32];
     __shared__ int32_t count[kReleaseItems];
     constexpr int kWarps = kPlanThreads / 32;
@@ -477,7 +478,7 @@ constexpr int kCompactHead = 64;                          // counts: live pages 
 
 // One cluster: which pages are in use, and where each goes.  With n of them, the pages in use from n on go to the pages below n
 // that are not, both in ascending order: the fewest moves, and no page is read and written.
-static __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kPlanThreads) k_page_compact_plan(const CompactArgs a) {
+static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_plan(const CompactArgs a) {
     __shared__ long long warp_sums[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
     const long long cap = (long long)a.W << a.page_shift;
