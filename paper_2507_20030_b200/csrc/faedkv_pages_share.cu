@@ -105,7 +105,7 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     while (parts < 32 && pg->cfg.max_pages > 256 * parts) parts *= 2;
     const bool in_registers = pg->cfg.max_pages <= 256 * parts && parts * batch <= 4 * most && pg->cfg.n_pages <= pages::kReleaseShort;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (in_registers)                                      // as few CTAs as have the warps: a larger cluster takes longer to begin and to meet (32 rows 8.6 us with 16, 6.5 with one)
+    if (in_registers)                                      // as few CTAs as have the warps: a larger cluster takes longer to begin and to meet
         while (ctas > 1 && parts * batch <= ctas / 2 * warps) ctas /= 2;
     else
         parts = 1;

@@ -240,7 +240,7 @@ struct ReleaseArgs {
 // Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store, and the pages that running
 // requests name are bits in shared memory, each CTA's own first, then all of them.  What bounds it is the chain: lengths, entries, three meetings of the
 // cluster, the stack.  (512 requests of up to 256 pages: 34 us with each row read in every phase and eight CTAs; 25 with the entries in registers and the
-// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  Eight rows: 7.9 us with sixteen CTAs, 5.8
+// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  32 rows: 8.6 us with sixteen CTAs, 5.4
 // with one.)
 constexpr int kReleaseShort = 65536;                      // pages
 __device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {        // what p is in another CTA of the cluster
@@ -290,8 +290,8 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
     cluster_sync();
     for (int w = tid; w < words; w += kPlanThreads) {
         uint32_t m = 0;
-#pragma unroll
-        for (int r = 0; r < kCluster; ++r) m |= r < ctas ? load_of_cta(own + w, r) : 0u;
+#pragma unroll 4
+        for (int r = 0; r < ctas; ++r) m |= load_of_cta(own + w, r);
         live[w] = m;
     }
 #pragma unroll
