@@ -234,6 +234,26 @@ def test_captured_and_on_another_stream(fk):
         assert torch.equal(out, want)
 
 
+def test_two_calls_at_once(fk):
+    """Two streams with a workspace each, launches of both forms side by side: again and again, the same bits."""
+    pairs = []
+    for groups in ([(2048, [2050 + 7 * i for i in range(70)]), (640, [700] * 9)], [(4096, [4200] * 33)]):
+        pg, args, out = case(fk, torch.bfloat16, 16, 2, 4, groups, width=50000)
+        n = len(args[1])
+        ws = torch.empty(pg.attn_shared_bytes(n, len(groups)), dtype=torch.uint8, device="cuda")
+        pairs.append((pg, args, out, out.clone(), ws, torch.cuda.Stream()))
+    for _ in range(5):
+        torch.cuda.synchronize()
+        for pg, args, out, want, ws, st in pairs:
+            with torch.cuda.stream(st):
+                for _ in range(3):
+                    out.zero_()
+                    pg.attn_shared(*args, ws=ws)
+        torch.cuda.synchronize()
+        for pg, args, out, want, ws, st in pairs:
+            assert torch.equal(out, want) and pg.device_status() == 0
+
+
 def test_lengths_that_grow_under_a_captured_step(fk):
     """The lengths are read on the device: a graph of one step serves rows as they grow past their shared tokens."""
     rng = np.random.default_rng(9)
