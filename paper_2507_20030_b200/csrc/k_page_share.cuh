@@ -254,7 +254,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
     __shared__ int32_t count[32 * K + 1];
     __shared__ uint32_t own[kReleaseShort / 32], live[kReleaseShort / 32];
     const int words = (a.n_pages + 31) / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank(), ctas = (int)gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank(), ctas = K > 1 ? kCluster : (int)gridDim.x;
     const long long cap = (long long)a.W << a.page_shift;
     const int page = 1 << a.page_shift;
     const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && rank == 0);
@@ -290,7 +290,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
     cluster_sync();
     for (int w = tid; w < words; w += kPlanThreads) {
         uint32_t m = 0;
-#pragma unroll 4
+#pragma unroll(K > 1 ? kCluster : 4)
         for (int r = 0; r < ctas; ++r) m |= load_of_cta(own + w, r);
         live[w] = m;
     }
@@ -332,6 +332,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
     }
     cluster_sync();
     long long at0 = height, all = height;
+#pragma unroll(K > 1 ? kCluster : 1)
     for (int r = 0; r < ctas; ++r) {
         const int n = __ldcg(totals + r);
         if (r < rank) at0 += n;
