@@ -586,14 +586,14 @@ class Pages:
         self._check(self._lib.faedkv_pages_store(self._h, k, v, ld, s, n, *self._cache(k_pages, v_pages, k_scale, v_scale),
                                                  self._on(stream)))
 
-    def _bytes(self, call, batch, n):
-        """A workspace's size, a function of the handle's configuration and two counts alone, so it is asked for once."""
-        key = (call, batch, n)
+    def _bytes(self, call, *counts):
+        """A workspace's size, a function of the handle's configuration and the counts alone, so it is asked for once."""
+        key = (call, counts)
         size = self._attn_bytes.get(key)
         if size is None:
             if len(self._attn_bytes) > 4096:
                 self._attn_bytes.clear()
-            size = self._attn_bytes[key] = getattr(self._lib, call)(self._h, batch, n)
+            size = self._attn_bytes[key] = getattr(self._lib, call)(self._h, *counts)
         return size
 
     def attn_bytes(self, batch: int, n_tokens: int) -> int:
@@ -702,7 +702,7 @@ class Pages:
         args = (need("t_len", t_len, i32, (batch,)), need("n_new", n_new, i32, (batch,)), batch,
                 need("table", table, i32, (batch, self.max_pages)), need("free_pages", free_pages, i32, self._pool_shape),
                 need("n_free", n_free, i32, (1,)), need("kv_len", kv_len, i32, (batch,)), need("n_free_out", n_free_out, i32, (1,)))
-        w = self._workspace(ws, self._lib.faedkv_pages_release_bytes(self._h), stream)
+        w = self._workspace(ws, self._bytes("faedkv_pages_release_bytes"), stream)
         self._check(self._lib.faedkv_pages_release(self._h, *args, w.data_ptr(), self._on(stream)))
 
     def compact(self, kv_len, table, table_out, free_pages, n_free, new_id, k_pages, v_pages, k_scale, v_scale, ws=None, stream=None):
@@ -712,7 +712,7 @@ class Pages:
         args = (need("kv_len", kv_len, i32, (batch,)), batch, need("table", table, i32, rows), need("table_out", table_out, i32, rows),
                 need("free_pages", free_pages, i32, self._pool_shape), need("n_free", n_free, i32, (1,)),
                 need("new_id", new_id, i32, self._pool_shape), *self._cache(k_pages, v_pages, k_scale, v_scale))
-        w = self._workspace(ws, self._lib.faedkv_pages_compact_bytes(self._h), stream)
+        w = self._workspace(ws, self._bytes("faedkv_pages_compact_bytes"), stream)
         self._check(self._lib.faedkv_pages_compact(self._h, *args, w.data_ptr(), self._on(stream)))
 
     def launch_count(self) -> int:
