@@ -20,13 +20,14 @@ SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
     SharedPlan p{};
     // One launch, eight columns a block, or two: the form with rows for what groups share, eight columns for what each row has behind it.  In eights a
     // tile of a group costs 0.39 ns a column (3.1 ns a block: 148 SMs side by side), in the form with rows 10.7 ns up to 128 columns and 22 ns at 256, and
-    // 14 us once.  (8 kv heads x 4 query heads, us in eights and with rows: one group of 16 rows over 8192 tokens 31 and 36, over 32768 67 and 52; of 64
-    // rows over 2048 47 and 45, over 32768 219 and 86; four groups of 8 rows over 8192 49 and 52, of 16 82 and 62.)  The host knows the tables' width, not
-    // the lengths: where they are far apart the second launch is taken too early, which costs those 14 us at most.
+    // 10 us once.  (8 kv heads x 4 query heads, 60 tokens behind, us in eights and with rows: one group of 16 rows over 8192 tokens 31 and 35, over 16384 43
+    // and 39; of 32 rows over 2048 28 and 33, over 4096 35.5 and 34.4; of 64 rows over 1024 36 and 40, over 2048 44 and 42, over 32768 218 and 81; four groups
+    // of 8 rows over 8192 48 and 52, of 16 79 and 60.)  The host knows the tables' width, not the lengths: where they are far apart the second launch is
+    // taken too early, which costs those 10 us at most.
     const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
     const double cols = (double)batch * pg->gq / n_groups, group_tiles = (double)max_tiles * c.n_kv_heads * n_groups;
     const double saved = group_tiles * (0.39 * cols - (cols <= 128 ? 10.7 : 0.086 * cols));
-    p.n = c.kv_dtype == FAEDKV_BF16 && saved > 14000.0 ? 2 : 1;
+    p.n = c.kv_dtype == FAEDKV_BF16 && saved > 10000.0 ? 2 : 1;
     p.spread = true;
     for (int i = 0; i < p.n; ++i) {
         SharedPlan::Launch &u = p.launch[i];
