@@ -195,7 +195,7 @@ def test_a_call_gives_the_same_bits_again(fk):
 
 
 @pytest.mark.parametrize("groups", [
-    [(20480, [20500 + i for i in range(64)]), (30720, [30800] * 20)],        # a block of 80 columns behind one of 256, on one CTA
+    [(20480, [20500 + i for i in range(64)]), (30848, [30900] * 20)],        # a block of 80 columns behind one of 256, on one CTA
     [(20480, [20500 + i for i in range(70)])],
 ])
 def test_many_columns_give_the_same_bits_again(fk, groups):
