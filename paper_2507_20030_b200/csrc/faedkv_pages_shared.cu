@@ -37,7 +37,7 @@ SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
         u.n_shared = u.which & 1 ? pages::shared_blocks(batch, n_groups, u.qc / pg->gq) : 0;
         u.blocks = u.n_shared + (u.which & 2 ? batch : 0);
         u.head = pages::shared_before_bytes(u.blocks);
-        p.spread = p.spread && u.blocks <= pages::kMaxBlocks && u.blocks * (2 * max_tiles + pages::kUnitCost) < (1LL << 31);
+        p.spread = p.spread && u.blocks <= pages::kMaxBlocks && u.blocks * (2 * max_tiles + pages::kRowsCost) < (1LL << 31);
         const long long most = (long long)pg->n_sm * (u.rows ? 1 : kDecodeCtas), tiles = max_tiles * u.blocks * c.n_kv_heads;
         u.ctas = (int)(tiles < most ? tiles : most);
         u.slots = (size_t)u.ctas * 2 * pages::attn_slot_floats(u.qc) * sizeof(float);
@@ -77,7 +77,7 @@ int launch_shared(faedkv_pages *pg, const CUtensorMap &mk, const CUtensorMap &mv
         if (int r = u.rows ? launch_rows<MODE, 0>(pg, mk, mv, a, pages::DiffArgs{}, grid, 13 + MODE, st)
                     : f32  ? launch_few<DecodeF32, MODE>(pg, mk, mv, a, grid, 15 + MODE, st)
                            : launch_few<DecodeBf16, MODE>(pg, mk, mv, a, grid, 17 + MODE, st)) return r;
-        done[i] = {a.ws, a.slots, u.qc, u.rows ? pages::kRowsCost : pages::kUnitCost, u.rows, u.ctas, u.n_shared, u.blocks};
+        done[i] = {a.ws, a.slots, u.qc, u.rows ? pages::kRowsCost : pages::kSharedCost, u.rows, u.ctas, u.n_shared, u.blocks};
     }
     auto join = f32 ? pages::k_page_join_shared<float, MODE> : pages::k_page_join_shared<__nv_bfloat16, MODE>;
     CUDA_TRY(pg, launch_pdl(join, dim3((unsigned)(((long long)a.B * a.H * a.G + 7) / 8)), dim3(256), 0, st, a, done[0], done[p.n - 1]));

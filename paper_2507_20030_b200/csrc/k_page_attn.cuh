@@ -399,6 +399,10 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int tq, int v, bool
 // as prefix sums in shared memory; a unit counts for kUnitCost positions more than it has tiles, which is what its queries,
 // its first maxima and its output take.  MODE 2, more blocks than MODE 1 takes: a CTA per unit.
 constexpr int kUnitCost = 8;
+// In a decode step over shared pages (MODE 3) fewer, since no unit has more than eight columns or a mask of its own: eight rows behind 2048 tokens 17.4 us
+// at 8, 16.5 at 6, 16.3 at 4, 16.0 at 2, behind 8192 22.9, 22.7, 21.9 and 25.2, five float32 rows of seven heads behind 4000 23.1, 23.1, 22.6 and 24.1.
+constexpr int kSharedCost = 4;
+__host__ __device__ constexpr int unit_cost(int mode) { return mode == 3 ? kSharedCost : kUnitCost; }
 template <int MODE> struct Work;
 
 template <> struct Work<0> {
@@ -431,8 +435,8 @@ template <int MODE> struct WorkShares {
                 if (++v == a.blocks) { v = 0; ++h; }
             const long long u0 = (long long)h * per_head + before[v];
             const int size = before[v + 1] - before[v], to = (int)min((long long)size, end - u0);
-            s.t0 = max(0, (int)(pos - u0) - kUnitCost);
-            s.t1 = max(0, to - kUnitCost);
+            s.t0 = max(0, (int)(pos - u0) - unit_cost(MODE));
+            s.t1 = max(0, to - unit_cost(MODE));
             s.h = h;
             const int block = v;
             pos = u0 + to;
@@ -441,8 +445,8 @@ template <int MODE> struct WorkShares {
             Block k;
             if (!find_unit<MODE>(a, qc / a.G, block, false, k)) return false;
             s.b = k.b; s.tok0 = k.tok0; s.n_tok = k.n_tok; s.see0 = k.see0; s.live = k.live; s.page0 = k.page0; s.own = k.own;
-            s.tiles = size - kUnitCost;
-            s.first = u0 + kUnitCost;
+            s.tiles = size - unit_cost(MODE);
+            s.first = u0 + unit_cost(MODE);
             return true;
         }
         return false;
@@ -580,7 +584,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         int32_t *before = reinterpret_cast<int32_t *>(gbase + C::kOffMisc + (C::kSmemBytes - 1024 - C::kOffMisc));
         for (int v = tid; v < a.blocks; v += C::kThreads) {
             Block k;
-            before[v + 1] = find_unit<MODE>(a, QC / a.G, v, blockIdx.x == 0, k) ? kUnitCost + tiles_of(k.live) : 0;
+            before[v + 1] = find_unit<MODE>(a, QC / a.G, v, blockIdx.x == 0, k) ? unit_cost(MODE) + tiles_of(k.live) : 0;
         }
         if (tid == 0) before[0] = 0;
         __syncthreads();

@@ -5,7 +5,7 @@
 // CTAs, meet here as parts of any softmax do: out = sum_i l_i 2^(m_i - m) o_i / sum_i l_i 2^(m_i - m), m the largest m_i.
 //
 // Measured, 8 kv x 32 query heads: 64 rows behind 32768 common tokens and 512 of their own 88 us (read by each row for itself they are 64 times the bytes;
-// the shared pages, the tails and the products each take 20 us at full rate), 8 rows behind 2048 17 us, mostly start, join and its launch.
+// the shared pages, the tails and the products each take 20 us at full rate), 8 rows behind 2048 16.5 us, mostly start, join and its launch.
 #pragma once
 #include "k_page_rows.cuh"
 
