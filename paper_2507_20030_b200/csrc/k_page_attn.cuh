@@ -310,7 +310,7 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int tq, int v, boo
     int lo = 0, hi = a.B - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (a.q_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
+        if (a.q_start[mid] / tq <= v - mid) lo = mid; else hi = mid - 1;   // (any int32 may stand there: no sum with it)
     }
     const int first = a.q_start[lo], n = a.q_start[lo + 1] - first;
     if (first < 0 || n < 0 || first > a.n_tokens - n) {
@@ -367,7 +367,7 @@ __device__ __forceinline__ bool find_shared(const AttnArgs &a, int tq, int v, bo
     int lo = 0, hi = a.n_groups - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (a.group_start[mid] / tq + mid <= v) lo = mid; else hi = mid - 1;
+        if (a.group_start[mid] / tq <= v - mid) lo = mid; else hi = mid - 1;   // (any int32 may stand there: no sum with it)
     }
     first = a.group_start[lo];
     const int n = a.group_start[lo + 1] - first;

@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(256) k_page_join_shared(const AttnArgs a, cons
             const int tq = u.qc / a.G, j = own ? 0 : (b - first) / tq, v = own ? u.n_shared + b : first / tq + g + j;
             // positions of the unit's tiles, of one tile
             const int size = before[v + 1] - before[v] - u.cost;
+            if (size <= 0) { n[own] = 0; continue; }       // (no such block)
             const int each = u.rows && !own ? rows_weight(min(tq, a.group_start[g + 1] - first - j * tq) * a.G) : 1;
             const long long pos = (long long)h * before[u.blocks] + before[v] + u.cost;
             const int from = cta_of(pos, per_cta), to = cta_of(pos + size - each, per_cta);

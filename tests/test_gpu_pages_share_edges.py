@@ -1,0 +1,39 @@
+"""Shared pages and differential attention at the edges of what their calls accept: starts that are any int32, steps without
+forks, every wrong table entry."""
+import numpy as np
+import pytest
+import torch
+
+import pages_ref as ref
+from test_gpu_pages_shared import case as shared_case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fk():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    from paper_2507_20030_b200 import binding, build
+    build.build()
+    binding.load()
+    return binding
+
+
+BOTH = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+MOST, LEAST = 2 ** 31 - 1, -2 ** 31
+
+
+@BOTH
+@pytest.mark.parametrize("G", [2, 5, 8])
+@pytest.mark.parametrize("starts", [
+    [0, 4, MOST, 5, 8],                                     # the search for a block passes the largest int32
+    [0, 4, MOST, MOST, MOST],
+    [0, 4, LEAST, LEAST, LEAST],
+    [LEAST, 0, 4, MOST, MOST],
+    [MOST, LEAST, MOST, 0, 4],
+])
+def test_groups_beside_starts_that_are_no_rows(fk, dtype, G, starts):
+    """Whatever stands beside them: rows of no group, and of one whose bounds are not rows, are attended alone."""
+    g = [(64, [70, 80, 64, 90]), (128, [130, 140, 150, 129])]
+    shared_case(fk, dtype, 16, 2, G, g, starts=starts, shared=[64, 64, 64, 64], status=0x105)
