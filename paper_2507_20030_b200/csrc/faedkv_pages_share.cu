@@ -78,6 +78,7 @@ int faedkv_pages_fork(faedkv_pages *pg, const int32_t *src, const int32_t *dst, 
     }
     pages::k_page_fork_plan<<<1, pages::kPlanThreads, 0, st>>>(a);
     if (int r = launch_check(pg, "k_page_fork_plan")) return r;
+    if (n_forks == 0) return FAEDKV_OK;                    // the height of the stack only
     CUDA_TRY(pg, launch_pdl(pages::k_page_fork_copy, dim3(n_forks), dim3(256), 0, st, a));
     return launch_check(pg, "k_page_fork_copy");
 }

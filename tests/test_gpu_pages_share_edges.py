@@ -37,3 +37,18 @@ def test_groups_beside_starts_that_are_no_rows(fk, dtype, G, starts):
     """Whatever stands beside them: rows of no group, and of one whose bounds are not rows, are attended alone."""
     g = [(64, [70, 80, 64, 90]), (128, [130, 140, 150, 129])]
     shared_case(fk, dtype, 16, 2, G, g, starts=starts, shared=[64, 64, 64, 64], status=0x105)
+
+
+@pytest.mark.parametrize("B", [4, 4096, 4097, 5000])
+def test_a_step_without_forks(fk, B):
+    """On either side of the batch from which forks are planned ahead of the copies: the height goes through, nothing else changes."""
+    pg = fk.Pages(n_kv_heads=1, n_q_heads=1, page_size=16, n_pages=40, max_pages=3, max_batch=B)
+    cache = pg.alloc()
+    none, free = torch.empty(0, dtype=torch.int32, device="cuda"), ref.ints(np.arange(40)[::-1].copy())
+    kv, table = ref.ints(np.arange(B) % 48), ref.ints(np.arange(3 * B).reshape(B, 3) % 40)
+    kv0, table0 = kv.clone(), table.clone()
+    nf, out = ref.ints([17]), ref.ints([-1])
+    pg.fork(none, none, kv, table, free, nf, out, *cache)
+    pg.fork(none, none, kv, table, free, nf, nf, *cache, length=none)
+    assert out.tolist() == [17] and nf.tolist() == [17] and pg.device_status() == 0
+    assert torch.equal(kv, kv0) and torch.equal(table, table0)
