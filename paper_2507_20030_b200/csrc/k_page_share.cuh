@@ -272,14 +272,14 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
         const int run = (held + parts - 1) / parts, end = min(held, (part + 1) * run);
         e[k] = b * a.W + part * run + lane;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) id[k][j] = part * run + 32 * j + lane < end ? a.table[e[k] + 32 * j] : -2;
+        for (int j = 0; j < 8; ++j) id[k][j] = part * run + 32 * j + lane < end ? max(a.table[e[k] + 32 * j], -1) : -2;   // -2: no entry
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (id[k][j] < -2 || id[k][j] == -1 || id[k][j] >= a.n_pages) {
+            if (id[k][j] == -1 || id[k][j] >= a.n_pages) {
                 flag(a.status, kBadPage);
                 id[k][j] = -2;
             }

@@ -52,3 +52,20 @@ def test_a_step_without_forks(fk, B):
     pg.fork(none, none, kv, table, free, nf, nf, *cache, length=none)
     assert out.tolist() == [17] and nf.tolist() == [17] and pg.device_status() == 0
     assert torch.equal(kv, kv0) and torch.equal(table, table0)
+
+
+@pytest.mark.parametrize("W,B", [(3, 2), (300, 40), (3, 600), (9000, 9)])        # the runs' registers, one and more of a warp; read again
+@pytest.mark.parametrize("bad", [-1, -2, -3, LEAST, MOST, 50])
+def test_release_flags_every_entry_that_is_no_page(fk, W, B, bad):
+    pg = fk.Pages(n_kv_heads=1, n_q_heads=1, page_size=16, n_pages=50, max_pages=W, max_batch=B)
+    for row in (0, B - 1):
+        for n_new, want in ((-1, [7, 3, 6]), (1, [7])):
+            table = np.full((B, W), bad)
+            table[row, :3] = [3, bad, 6]                       # the other rows are empty
+            kv, nn = np.zeros(B, dtype=np.int64), np.zeros(B, dtype=np.int64)
+            kv[row], nn[row] = 40, n_new
+            free, nf, out = ref.ints([7] + [-9] * 49), ref.ints([1]), ref.ints(np.zeros(B))
+            pg.release(ref.ints(kv), ref.ints(nn), ref.ints(table), free, nf, out, nf)
+            assert free.tolist()[:nf.item()] == want and set(free.tolist()[nf.item():]) == {-9}
+            assert out[row].item() == (0 if n_new < 0 else 40) and pg.device_status() == 0x101
+            pg.reset_device_status()
