@@ -17,9 +17,20 @@ template <typename T>
 __device__ __forceinline__ void diff_finish(float4 a1, float4 a2, float lam, const float *gain, float eps, int lane, T *out) {
     float4 o = make_float4(fmaf(-lam, a2.x, a1.x), fmaf(-lam, a2.y, a1.y), fmaf(-lam, a2.z, a1.z), fmaf(-lam, a2.w, a1.w));
     if (gain != nullptr) {
-        float ss = fmaf(o.x, o.x, o.y * o.y) + fmaf(o.z, o.z, o.w * o.w);
+        auto squares = [&]() {
+            float ss = fmaf(o.x, o.x, o.y * o.y) + fmaf(o.z, o.z, o.w * o.w);
 #pragma unroll
-        for (int s = 16; s; s >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+            for (int s = 16; s; s >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+            return ss;
+        };
+        float ss = squares();
+        const float m = ss * (1.0f / kHeadDim) + eps;
+        if (!diff_in_range(m)) {                           // (the same in all lanes)
+            const float unit = diff_unit(m);
+            o = make_float4(o.x * unit, o.y * unit, o.z * unit, o.w * unit);
+            ss = squares();
+            eps = eps * unit * unit;
+        }
         const float r = diff_norm(ss, eps);
         const float4 w = load4(gain + 4 * lane);
         o = make_float4(o.x * (r * w.x), o.y * (r * w.y), o.z * (r * w.z), o.w * (r * w.w));

@@ -215,6 +215,10 @@ struct DiffArgs {
     int n_tokens, B, HQ;
     float eps;
 };
+// What a row is multiplied by before it is squared once more, where its mean square m is beyond 2^-100 .. 2^120: there squares leave float32's range, o and
+// the result do not.  (2^-70 and 2^75 put every float32 where 128 squares add up; eps goes with the square of it.)
+__device__ __forceinline__ bool diff_in_range(float m) { return m >= 0x1p-100f && m <= 0x1p120f; }
+__device__ __forceinline__ float diff_unit(float m) { return m > 1.f ? 0x1p-70f : 0x1p75f; }
 // 1 / sqrt(mean(o^2) + eps) from the sum of squares: a row of zeros stays one without eps, NaN stays NaN.
 __device__ __forceinline__ float diff_norm(float squares, float eps) {
     const float m = squares * (1.0f / kHeadDim) + eps;
@@ -934,15 +938,16 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         o[e] = second ? fmaf(-lam, o[e], x) : fmaf(-lam, x, o[e]);
                     }
                 };
-                float squares = 0.f;
-                if (diff.gain != nullptr) {
+                float squares = 0.f, unit = 1.f;
+                for (bool again = false; diff.gain != nullptr; again = true) {
+                    squares = 0.f;
                     if (warp_on)
 #pragma unroll 1
                         for (int d = d0; d < d1; d += 16) {
                             float o[16];
                             difference(d, o);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) squares = fmaf(o[e], o[e], squares);
+                            for (int e = 0; e < 16; ++e) squares = fmaf(o[e] * unit, o[e] * unit, squares);
                         }
                     if (!two) {
                         softmax_bar(1, kSoftmax);          // (row_cs has been read)
@@ -950,8 +955,14 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         softmax_bar(1, kSoftmax);
                         squares = row_cs[row] + row_cs[128 + row];
                     }
+                    if (again) break;
+                    // once more, in another unit, where some row's squares are out of range (both threads of a row find the same)
+                    const float m = squares * (1.0f / kHeadDim) + diff.eps;
+                    const bool odd = on && !diff_in_range(m);
+                    if (!(two ? (bool)__any_sync(0xffffffffu, odd) : softmax_any(odd, 1, kSoftmax))) break;
+                    if (odd) unit = diff_unit(m);
                 }
-                const float r = diff_norm(squares, diff.eps);
+                const float r = diff_norm(squares, diff.eps * unit * unit);
                 T *out = static_cast<T *>(diff.out) + (row_of(c) >> 1) * kHeadDim;
                 if (warp_on)
 #pragma unroll 1
@@ -963,6 +974,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll
                             for (int e = 0; e < 16; e += 4) {
                                 const float4 w = load4(diff.gain + d + e);
+                                o[e] *= unit; o[e + 1] *= unit; o[e + 2] *= unit; o[e + 3] *= unit;
                                 o[e] *= r * w.x; o[e + 1] *= r * w.y; o[e + 2] *= r * w.z; o[e + 3] *= r * w.w;
                             }
                         }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import pages_ref as ref
+from test_gpu_pages_diff import expect
 from test_gpu_pages_shared import case as shared_case
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +70,46 @@ def test_release_flags_every_entry_that_is_no_page(fk, W, B, bad):
             assert free.tolist()[:nf.item()] == want and set(free.tolist()[nf.item():]) == {-9}
             assert out[row].item() == (0 if n_new < 0 else 40) and pg.device_status() == 0x101
             pg.reset_device_status()
+
+
+def diff_call(fk, dtype, page, H, G, lens, new, edit, gain, eps, width=1, scale=None, seed=0):
+    """attn_diff over a random cache that edit(rng, table, kc, ks, vc, vs) has changed, against 64 bits row by row."""
+    rng = np.random.default_rng(sum(lens) + page + H + 7 * G + seed)
+    B, counts = len(lens), new or [1] * len(lens)
+    W = max(ref.pages_of(n, page) for n in lens) + width
+    n_pages = sum(ref.pages_of(n, page) for n in lens) + 2
+    table = ref.spread(lens, page, n_pages, W, rng)
+    (kc, ks), (vc, vs) = [ref.random_cache(rng, n_pages, H, page, lens, table) for _ in range(2)]
+    edit(rng, table, kc, ks, vc, vs)
+    pg = fk.Pages(n_kv_heads=H, n_q_heads=H * G, page_size=page, n_pages=n_pages, max_pages=W, max_batch=B,
+                  kv_dtype=fk.BF16 if dtype == torch.bfloat16 else fk.F32)
+    q = torch.from_numpy(rng.standard_normal((sum(counts), H * G, 128))).to(dtype).cuda()
+    lam = torch.from_numpy(rng.uniform(0.2, 0.8, H * G)).float().cuda()
+    gain = torch.from_numpy(rng.uniform(0.5, 1.5, 128)).float().cuda() if gain else None
+    out = torch.full_like(q, 7.0)
+    start = np.concatenate([[0], np.cumsum(counts)])
+    pg.attn_diff(q, ref.ints(lens), ref.ints(table), ref.cuda8(kc), ref.cuda8(vc), ref.cuda32(ks), ref.cuda32(vs), lam, out,
+                 q_start=None if new is None else ref.ints(start), gain=gain, eps=eps)
+    kind = "f32" if dtype == torch.float32 else "wide" if new is not None else "bf16"
+    for b in range(B):
+        K, V = [torch.from_numpy(ref.rows_of(c, s, table[b], lens[b], page)).cuda() for c, s in ((kc, ks), (vc, vs))]
+        rows = slice(start[b], start[b + 1])
+        seen = lens[b] - counts[b] + 1 + torch.arange(counts[b], device="cuda")
+        for h in range(H):
+            hs = slice(h * G, (h + 1) * G)
+            expect(out[rows, hs], kind, q[rows, hs], K[h], V[h], seen, 0.125, lam[hs], gain, eps, (b, h))
+    assert pg.device_status() == 0
+
+
+@BOTH
+@pytest.mark.parametrize("exponent", [-100, -75, -50, 0, 50, 70, 100])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_the_norm_of_heads_whose_squares_are_beyond_float32(fk, dtype, exponent, eps):
+    """Values of 2^exponent: their squares are no float32, the head over its root mean square is of order one (or, where eps is more, a float32 still)."""
+    def edit(rng, table, kc, ks, vc, vs):
+        vs *= 2.0 ** exponent
+    diff_call(fk, dtype, 16, 2, 2, [300, 17, 129], None, edit, True, eps)                      # decode
+    diff_call(fk, dtype, 16, 1, 2, [40, 9], [7, 9], edit, True, eps)                           # new tokens, eight columns
+    if dtype == torch.bfloat16:
+        diff_call(fk, dtype, 64, 2, 2, [700, 300], [100, 20], edit, True, eps, width=60000)    # columns as rows, two row tiles and one
+        diff_call(fk, dtype, 64, 1, 4, [5000], [10], edit, True, eps, width=20000)             # split, one row tile
