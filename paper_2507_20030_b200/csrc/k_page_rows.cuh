@@ -9,7 +9,11 @@
 //
 // Softmax in base 2: y = s * (k_scale * q_scale * scale * log2 e) - Mu, p = 2^y, l += p, w = p * (v_scale / Vref).  Mu follows the row's largest weight
 // lazily: when the weights of half a tile sum up to more than 2^15.5 it is raised by a whole number that puts the largest at 2^6 .. 2^7, what was summed (l and O) is
-// multiplied by a power of two, and they are taken once more.  No maximum is formed otherwise.  Weights therefore keep 2^-11 of themselves and 2^-31 of the row's largest.  Vref as in k_page_attn.
+// multiplied by a power of two, and they are taken once more.  No maximum is formed otherwise.  Weights w therefore keep 2^-11 of themselves and 2^-31 of the
+// row's largest.  Vref is the power of two above the first tile's largest v_scale.  It stays, so that a page of other values changes nothing for those
+// that follow: y has the logarithm of v_scale / Vref in it, from 2^-80 to 2^60, and p is 2^y times the inverse, which float32 holds with a sum of a
+// billion tokens (with Vref raised for pages beyond 2^20 and lower ones held to 2^-20, ordinary pages behind one 2^26 times as loud lost their weights'
+// bits, behind one 2^31 times all of them).  Only a v_scale beyond 2^60 of it moves Vref, and O with it.
 //
 // Two softmax warpgroups work on half tiles, 64 tokens.  Each has room for one half's scores and for two halves' weights in tensor memory: once it has the
 // scores in registers the next ones are computed, and no product waits for another one's end.  A unit of more than 128 rows is
@@ -32,6 +36,7 @@ constexpr int kRowsConvert = 128, kRowsThreads = 256 + kRowsConvert + 128;  // 1
 constexpr int kRowsRegsSoftmax = 160, kRowsRegsConvert = 96, kRowsRegsIssue = 80;
 constexpr int kRowsRegsLaunch = 124;
 static_assert(2 * kRowsRegsSoftmax + kRowsRegsConvert + kRowsRegsIssue <= 4 * kRowsRegsLaunch, "a launch has these to share out");
+constexpr float kRowsScaleUp = 0x1p60f, kRowsScaleDown = -80.f;   // of v_scale about Vref; the logarithm
 constexpr int kRowsCost = 13;                             // what a unit's start and end take, in tiles of one row tile (1024 new tokens over 9216: 228 us at 6, 193 at 10, 190 at 13, 192 at 16, 196 at 20)
 constexpr uint32_t kRowsOffV = kRowsK * kTileBytes, kRowsOffH = kRowsOffV + kRowsV * kTileBytes;
 constexpr uint32_t kRowsOffQ = kRowsOffH + kRowsH * 2 * kTileBytes, kRowsOffMisc = kRowsOffQ + 4 * kTileBytes;
@@ -153,6 +158,8 @@ template <int MODE> struct RowsWork {
 __device__ __forceinline__ int cta_of(long long pos, long long share) {
     return pos < (1LL << 31) && share < (1LL << 31) ? (int)((uint32_t)pos / (uint32_t)share) : (int)(pos / share);
 }
+// x * 2^e for e <= 0, also where 2^e alone is no float32: sums hold pages of zeros, whose p are up to 2^80 times the weights'.
+__device__ __forceinline__ float fade(float x, float e) { return x * ex2(fmaxf(e, -100.f)) * ex2(fminf(e + 100.f, 0.f)); }
 // A column's partial result: Mu, the sum, 128 channels divided by it.
 struct PartColumn { const float *mu, *sum, *o; };
 __device__ __forceinline__ PartColumn SlotColumn(const float *slot, int qc, int c) { return {slot + c, slot + qc + c, slot + 2 * qc + (size_t)c * kHeadDim}; }
@@ -175,13 +182,13 @@ __device__ __forceinline__ void gather_parts(Part part, int n, int lane, float4 
                 m = *p.mu;
                 l = *p.sum;
             }
-            const float top = fmaxf(mu[k], warp_max(m)), back = ex2(mu[k] - top);
-            w[k] = l * ex2(m - top);
+            const float top = fmaxf(mu[k], warp_max(m)), back = mu[k] - top;
+            w[k] = fade(l, m - top);
             float all = w[k];
 #pragma unroll
             for (int s = 16; s; s >>= 1) all += __shfl_xor_sync(0xffffffffu, all, s);
-            sum[k] = sum[k] * back + all;
-            o[k] = make_float4(o[k].x * back, o[k].y * back, o[k].z * back, o[k].w * back);
+            sum[k] = fade(sum[k], back) + all;
+            o[k] = make_float4(fade(o[k].x, back), fade(o[k].y, back), fade(o[k].z, back), fade(o[k].w, back));
             mu[k] = top;
         }
         for (int i = 0; i < here; i += 8) {
@@ -444,14 +451,14 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     // tiles two before them are done with
                     float *sc = ring + (it & (kRowsRing - 1)) * 40;
                     const float v_max = warp_max(mine ? fabsf(vs) : 0.f);
-                    if (v_max > v_ref * kScaleRange) {
+                    if (v_max > v_ref * kRowsScaleUp) {
                         v_ref = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
                         v_inv = __fdiv_rn(1.f, v_ref);
                         v_lg = __log2f(v_ref);
                     }
-                    // a page's weights are 2^(y + lr) * c: lr is the logarithm of v_scale / Vref, at least -20 (p of a page of tiny values stays in
-                    // reach), and c what that leaves, 1 for all but such pages; p is the weight times 2^-lr
-                    const float lr = id >= 0 ? fmaxf(__log2f(fmaxf(fabsf(vs), 1.17549435e-38f)) - v_lg, -20.f) : 0.f, inv_r = ex2(-lr), c = id >= 0 ? vs * v_inv * inv_r : 1.f;
+                    // a page's weights are 2^(y + lr) * c: lr is the logarithm of v_scale / Vref, at least -80 (p of a page of zeros stays in
+                    // reach), and c what that leaves, 1 for all but such pages and negative scales; p is the weight times 2^-lr
+                    const float lr = id >= 0 ? fmaxf(__log2f(fmaxf(fabsf(vs), 1.17549435e-38f)) - v_lg, kRowsScaleDown) : 0.f, inv_r = ex2(-lr), c = id >= 0 ? vs * v_inv * inv_r : 1.f;
                     const uint32_t odd = __ballot_sync(0xffffffffu, mine && !(c > 0.9999f));
                     if (mine) {
                         sc[k] = ks;
@@ -841,13 +848,13 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         const bool seen = need && top > -INFINITY;
                         const float d = !seen ? 0.f : set ? fmaxf(ceilf(top) - kLag, 0.f) : ceilf(top) - kLag;
                         const float f = seen && set ? (d > 120.f ? 0.f : ex2(-d)) : 1.f;
+                        l = make_float2(set && seen ? fade(l.x, -d) : l.x, set && seen ? fade(l.y, -d) : l.y);
                         mu += d;
                         set |= seen;
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
                             for (int p = 0; p < 8; ++p) y[k][p] = make_float2(y[k][p].x - d, y[k][p].y - d);
-                        l = make_float2(l.x * f, l.y * f);
                         if (q > 0 && __any_sync(0xffffffffu, f != 1.f)) rescale(f);
                     }
                     l = add2(l, l_half);
@@ -871,7 +878,7 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 tc_fence_after();
                 const float4 x0 = exch[row], x1 = exch[128 + row];
                 mu = fmaxf(x0.y == 0.f ? kMuNone : x0.x, x1.y == 0.f ? kMuNone : x1.x);
-                const float l0 = x0.y == 0.f ? 0.f : x0.y * ex2(x0.x - mu), l1 = x1.y == 0.f ? 0.f : x1.y * ex2(x1.x - mu);
+                const float l0 = x0.y == 0.f ? 0.f : fade(x0.y, x0.x - mu), l1 = x1.y == 0.f ? 0.f : fade(x1.y, x1.x - mu);
                 sum = l0 + l1;
                 const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
                 f[0] = x0.y == 0.f ? 0.f : ex2(x0.x - mu) * inv * x0.z;
