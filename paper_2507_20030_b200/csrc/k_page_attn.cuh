@@ -22,9 +22,10 @@
 // follows the column's largest weight lazily: it is raised (and O, l rescaled) only when some weight exceeds 2^15 or so, and then
 // to 2^-6 or 2^-8 of the largest, so weights stay in their format's range and most tiles exchange one vote instead of a maximum per
 // column.  It follows the weights and not p, so a page of large values that hardly counts takes no bits from the others.  Vref is
-// the power of two above the first tile's largest v_scale; only a scale 2^20 beyond it moves it, which rescales O alone: p, and
-// with it l, stays within 2^20 of the weights, in float32's reach (pages of zeros have the smallest scale, and their tokens
-// count in l all the same).  O stays in TMEM over all tiles of a segment.
+// the power of two above the first tile's largest v_scale (2^-66 at least), and stays: p is the weight over v_scale / Vref, from 2^-60 to 2^40, and float32 holds it
+// and l (pages of zeros have the smallest scale, and their tokens count in l all the same).  Only a scale beyond 2^40 of Vref moves it, and rescales
+// O.  From the first page on that lies beyond 2^20 of it (a segment `far`), Mu is settled before every tile's weights are taken, since p of a tile taken
+// again would pass float32.  O stays in TMEM over all tiles of a segment.
 //
 // Measured: a decode step over 16 x 16384 tokens of 8 kv heads 89 us (6.0 TB/s of codes), over 131072 tokens 54 us (39 us of
 // it in the tiles); 2048 new tokens over 18432 962 us (608 TFLOP/s), bound by the softmax warps (an instruction issued in 53 %
@@ -46,7 +47,11 @@ namespace pages {
 
 constexpr int kTile = 128;                                // tokens of a tile
 constexpr uint32_t kTileBytes = kTile * kHeadDim;         // 16 KB: K or V codes of a tile
-constexpr float kScaleRange = 1048576.f;                  // of v_scale about Vref
+// of v_scale about Vref: within `near` weights are taken before Mu is known to hold them; beyond `up` Vref moves; below `down` (a logarithm) p is cut off
+constexpr float kScaleNear = 0x1p20f, kScaleUp = 0x1p40f, kScaleDown = -60.f;
+// Vref for a largest v_scale of v_max: the power of two above it, no less than `least`, 2^-126 of pages of zeros over the factor `down`: their p then stand so
+// far above their weights that what follows finds Mu low.
+__device__ __forceinline__ float scale_ref(float v_max, float least) { return __uint_as_float((__float_as_uint(fmaxf(v_max, least)) + 0x7fffffu) & 0xff800000u); }
 constexpr float kMuNone = -3e38f;                         // a part that saw no token
 constexpr int kMaxBlocks = 1024;                          // blocks of new tokens that MODE 1 takes
 constexpr unsigned int kErrAttnTma = 0x41, kErrAttnMma = 0x42, kErrAttnSoftmax = 0x43;
@@ -134,6 +139,8 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// x * 2^e for e <= 0, also where 2^e alone is no float32: sums hold pages of zeros, whose p are up to 2^80 times the weights'.
+__device__ __forceinline__ float fade(float x, float e) { return x * ex2(fmaxf(e, -100.f)) * ex2(fminf(e + 100.f, 0.f)); }
 __device__ __forceinline__ float warp_max(float v) {
     float r;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -497,7 +504,7 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     int *col_lim = reinterpret_cast<int *>(col_f + QC);                      // [QC] tokens that the column sees
     int *col_set = col_lim + QC;                                             // [QC] Mu stands for a maximum
     float *red = reinterpret_cast<float *>(col_set + QC);                    // [4][QC]
-    float *stage_ks = red + 4 * QC;                                          // [KST][32]: 8 k_scale, 8 v_scale, the largest |v_scale|, at 24 the pages that are there
+    float *stage_ks = red + 4 * QC;                                          // [KST][32]: 8 k_scale, 8 v_scale, Vref, at 24 the pages that are there and, as the sign, whether the segment is far
     uint64_t *bars = reinterpret_cast<uint64_t *>(stage_ks + KST * 32);
     const uint32_t bar0 = smem_u32(bars);
     constexpr int kBars = 2 * (KST + VST);
@@ -667,7 +674,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
             };
             int id, id_next;
-            float ks, vs, ks_next, vs_next;
+            float ks, vs, ks_next, vs_next, v_ref = 0.f;
+            bool far = false;
             fetch(s.t0, id, ks, vs);
             for (int tb = s.t0; tb < s.t1; tb += tiles_batch) {
                 fetch(tb + tiles_batch, id_next, ks_next, vs_next);
@@ -691,14 +699,19 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     // softmax warps are done with the tile that had it (wide: they gave its V's room, which the tile before this
                     // one has taken, so KST is at most VST + 1)
                     float *sc = stage_ks + st * 32;
-                    const float v_max = warp_max(mine ? fabsf(vs) : 0.f);
+                    const float v_abs = fabsf(vs), v_max = warp_max(mine ? v_abs : 0.f);
+                    if (v_ref == 0.f || v_max > v_ref * kScaleUp) {
+                        far |= v_ref > 0.f;
+                        v_ref = scale_ref(v_max, 0x1p-66f);
+                    }
+                    far |= __any_sync(0xffffffffu, mine && id >= 0 && !(v_abs >= v_ref * (1.f / kScaleNear) && v_abs <= v_ref * kScaleNear));
                     if (mine) {
                         sc[k] = ks;
                         sc[8 + k] = vs;
                     }
                     if (lane == 0) {
-                        sc[16] = v_max;
-                        reinterpret_cast<uint32_t *>(sc)[24] = have;
+                        sc[16] = v_ref;
+                        reinterpret_cast<uint32_t *>(sc)[24] = have | (far ? 0x80000000u : 0u);
                     }
                     __syncwarp();
                     if (lane == 0) {
@@ -911,10 +924,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 tc_fence_after();
                 const float *sc = stage_ks + st * 32;
                 const int pg = row >> a.page_shift;
-                const float ks = sc[pg], vs = sc[8 + pg], v_max = sc[16];
+                const float ks = sc[pg], vs = sc[8 + pg], v_now = sc[16];
                 const uint32_t have = reinterpret_cast<const uint32_t *>(sc)[24];
                 const int tok = t * kTile + row;
-                // columns may see a different number of this tile's tokens, or pages may be missing
+                // columns may see a different number of this tile's tokens, pages may be missing, or the segment is far
                 const bool masked = (t + 1) * kTile > s.see0 || have != (1u << (kTile >> a.page_shift)) - 1u;
                 const bool valid = tok < s.live && ((have >> pg) & 1u);
                 const uint32_t ts = tmem_s + (it & 1) * NS + lane_addr + c_wg;
@@ -947,14 +960,13 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 const bool own = C::WIDE && !masked && !common;            // each column's factor is still to come
                 if (own) kf = ks;
                 const float2 ks2 = make_float2(kf, kf);
-                // a column without a maximum: Mu is settled before the weights are taken; a v_scale far beyond those before: Vref
-                bool raise = unset_any;
+                // a column without a maximum, v_scales far apart: Mu is settled before the weights are taken
+                bool raise = unset_any || (int32_t)have < 0;
                 float o_factor = 1.f;
-                if (v_max > v_ref * kScaleRange) {
-                    const float up = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
-                    if (v_ref > 0.f) o_factor = v_ref / up;
-                    v_ref = up;
-                    v_inv = __fdiv_rn(1.f, up);
+                if (v_now != v_ref) {
+                    if (v_ref > 0.f) o_factor = v_ref / v_now;
+                    v_ref = v_now;
+                    v_inv = __fdiv_rn(1.f, v_now);
                 }
                 const float2 r2 = make_float2(vs * v_inv, vs * v_inv);
                 // y of the columns c_wg + c0 .. from their raw scores
@@ -1051,9 +1063,10 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 bool again = false;
                 for (;;) {
                     if (raise) {
+                        const bool far = (int32_t)have < 0;
                         // Mu to kLagTo below the column maxima, and what has been summed rescaled
                         if (t > s.t0) wait(pdone((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, kErrAttnSoftmax);
-                        const float lift = __log2f(fmaxf(fabsf(r2.x), 1.f / kScaleRange));
+                        const float lift = fmaxf(__log2f(fabsf(r2.x)), kScaleDown);
 #pragma unroll 1
                         for (int c0 = 0; c0 < QW; c0 += kPart) {
                             float raw[kLoad];
@@ -1073,11 +1086,13 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                             const int c = c_wg + row;
                             const float m = fmaxf(fmaxf(red[c], red[QC + c]), fmaxf(red[2 * QC + c], red[3 * QC + c])) - C::kLagTo;
                             const bool first = col_set[c] == 0, seen = m > -INFINITY;
-                            const float d = seen && (first || m > 0.f) ? m : 0.f;
+                            const float d = !seen || !(first || m > 0.f) ? 0.f : far ? 2.f * ceilf(0.5f * m) : m;
                             mu_at(c) -= d;
                             // 1: nothing has been summed yet; 0: what has been is beyond float32's reach, or was summed as infinity
-                            // (p of a tile that is taken again reaches 2^(d + kLagTo + 20))
-                            col_f[c] = first ? 1.f : d > 96.f ? 0.f : ex2(-d);
+                            // (p of a tile that is taken again reaches 2^(d + kLagTo + 20)).  Far: no tile is, but sums reach 2^75 and more, which
+                            // factors down to float32's least subnormal, powers of two, bring to where new weights leave them nothing
+                            const float root = ex2(-0.5f * d);
+                            col_f[c] = first ? 1.f : far ? __fmul_rn(root, root) : d > 96.f ? 0.f : ex2(-d);
                             if (seen) col_set[c] = 1;
                             unset = first && !seen;
                         }
@@ -1106,9 +1121,8 @@ k_page_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                         raise = false;
                     }
                     const float excess = again ? weights(std::true_type{}) : weights(std::false_type{});
-                    // a weight beyond its format's range (or, beside a far smaller scale, p beyond l's): raise Mu, and the weights
-                    // once more
-                    if (done_max || !softmax_any(ex2(excess) * fmaxf(fabsf(r2.x), 1.f / kScaleRange) > C::kMostWeight, 2 + wg, 128)) break;
+                    // a weight beyond its format's range: raise Mu, and the weights once more
+                    if (done_max || !softmax_any(ex2(excess) * fabsf(r2.x) > C::kMostWeight, 2 + wg, 128)) break;
                     raise = again = true;
                 }
                 uint8_t *vtile = gbase + C::kOffV + (uint32_t)sv * kTileBytes;
@@ -1338,7 +1352,7 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
                 const int c = c0 + kJoinGroups * k;
                 if (c < c_end) {
                     const float *p = slot(i);
-                    const float l = p[qc + c] * ex2(p[c] - mu[k]);             // a part's output is divided by its sum already
+                    const float l = fade(p[qc + c], p[c] - mu[k]);             // a part's output is divided by its sum already
                     sum[k] += l;
                     o[k] = fmaf(p[2 * qc + (size_t)c * kHeadDim + d], l, o[k]);
                 }
@@ -1367,17 +1381,17 @@ __global__ void __launch_bounds__(kHeadDim *kJoinGroups) k_page_attn_join(const 
                 }
                 __syncthreads();
                 const float top = fmaxf(mu, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
-                const float back = ex2(mu - top);
+                const float back = mu - top;
                 if (grp == 0) {
-                    l *= ex2(m - top);
+                    l = fade(l, m - top);
                     f_s[d] = l;
 #pragma unroll
                     for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
                     if ((d & 31) == 0) red_s[1][d >> 5] = l;
                 }
                 __syncthreads();
-                sum = sum * back + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
-                o *= back;
+                sum = fade(sum, back) + (red_s[1][0] + red_s[1][1]) + (red_s[1][2] + red_s[1][3]);
+                o = fade(o, back);
                 mu = top;
 #pragma unroll 8
                 for (int i = grp; i < k; i += kJoinGroups) o = fmaf(slot(i0 + i)[2 * qc + (size_t)c * kHeadDim + d], f_s[i], o);

@@ -10,7 +10,7 @@
 // Softmax in base 2: y = s * (k_scale * q_scale * scale * log2 e) - Mu, p = 2^y, l += p, w = p * (v_scale / Vref).  Mu follows the row's largest weight
 // lazily: when the weights of half a tile sum up to more than 2^15.5 it is raised by a whole number that puts the largest at 2^6 .. 2^7, what was summed (l and O) is
 // multiplied by a power of two, and they are taken once more.  No maximum is formed otherwise.  Weights w therefore keep 2^-11 of themselves and 2^-31 of the
-// row's largest.  Vref is the power of two above the first tile's largest v_scale.  It stays, so that a page of other values changes nothing for those
+// row's largest.  Vref is the power of two above the first tile's largest v_scale (2^-46 at least).  It stays, so that a page of other values changes nothing for those
 // that follow: y has the logarithm of v_scale / Vref in it, from 2^-80 to 2^60, and p is 2^y times the inverse, which float32 holds with a sum of a
 // billion tokens (with Vref raised for pages beyond 2^20 and lower ones held to 2^-20, ordinary pages behind one 2^26 times as loud lost their weights'
 // bits, behind one 2^31 times all of them).  Only a v_scale beyond 2^60 of it moves Vref, and O with it.
@@ -158,8 +158,6 @@ template <int MODE> struct RowsWork {
 __device__ __forceinline__ int cta_of(long long pos, long long share) {
     return pos < (1LL << 31) && share < (1LL << 31) ? (int)((uint32_t)pos / (uint32_t)share) : (int)(pos / share);
 }
-// x * 2^e for e <= 0, also where 2^e alone is no float32: sums hold pages of zeros, whose p are up to 2^80 times the weights'.
-__device__ __forceinline__ float fade(float x, float e) { return x * ex2(fmaxf(e, -100.f)) * ex2(fminf(e + 100.f, 0.f)); }
 // A column's partial result: Mu, the sum, 128 channels divided by it.
 struct PartColumn { const float *mu, *sum, *o; };
 __device__ __forceinline__ PartColumn SlotColumn(const float *slot, int qc, int c) { return {slot + c, slot + qc + c, slot + 2 * qc + (size_t)c * kHeadDim}; }
@@ -451,8 +449,8 @@ k_page_rows(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                     // tiles two before them are done with
                     float *sc = ring + (it & (kRowsRing - 1)) * 40;
                     const float v_max = warp_max(mine ? fabsf(vs) : 0.f);
-                    if (v_max > v_ref * kRowsScaleUp) {
-                        v_ref = __uint_as_float((__float_as_uint(fmaxf(v_max, 1.17549435e-38f)) + 0x7fffffu) & 0xff800000u);
+                    if (v_ref == 0.f || v_max > v_ref * kRowsScaleUp) {
+                        v_ref = scale_ref(v_max, 0x1p-46f);
                         v_inv = __fdiv_rn(1.f, v_ref);
                         v_lg = __log2f(v_ref);
                     }

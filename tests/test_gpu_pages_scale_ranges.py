@@ -84,6 +84,7 @@ CASES = {
     "later26": loud([0.5], 26), "later40": loud([0.5], 40), "later55": loud([0.5], 55), "first26": loud([0.0], 26), "first40": loud([0.0], 40),
     "first55": loud([0.0], 55), "first75": loud([0.0], 75), "both50": loud([0.0, 0.3, 0.6, 0.95], 50), "heavy40": loud([0.4], 40, weight=8),
     "zeros_first": zeros([0.0], 3), "zeros_later": zeros([0.3, 0.7], 12), "zeros_and_loud": lambda *a: (zeros([0.2], 5)(*a), loud([0.6], 45)(*a)),
+    "zeros_then_loud": lambda *a: (zeros([0.0], 5)(*a), loud([0.5], 45)(*a)), "tiny": lambda n, cache, row, scale: cache[3].fill(2.0 ** -117),
     "quiet": loud([0.1, 0.5, 0.9], -30, weight=-20), "signs": signs, "no_values": no_values,
 }
 
@@ -140,7 +141,14 @@ def run(fk, call, dtype, page, H, G, lens, edit, new=None, shared=0, width=1, se
     pg.close()
 
 
+# What the calls promise, in every form: scales within 2^40 of one another, and pages of zeros; the form with rows reaches further.
+NEAR = {k: v for k, v in CASES.items() if not k[-2:].isdigit() or int(k[-2:]) <= 40} | {
+    "later38": loud([0.5], 38), "first38": loud([0.0], 38), "both38": loud([0.0, 0.3, 0.6, 0.95], 38), "heavy38": loud([0.4], 38, weight=8),
+    "zeros_and_loud": lambda *a: (zeros([0.2], 5)(*a), loud([0.6], 38)(*a)), "zeros_then_loud": lambda *a: (zeros([0.0], 5)(*a), loud([0.5], 38)(*a)),
+    "zeros_then_very_loud": lambda *a: (zeros([0.0], 0)(*a), loud([0.5], 17 + 7, weight=17 + 7)(*a)),
+    "quiet": loud([0.1, 0.5, 0.9], -38, weight=-20)}
 EVERY = pytest.mark.parametrize("edit", list(CASES))
+EVERY_NEAR = pytest.mark.parametrize("edit", list(NEAR))
 
 
 @EVERY
@@ -153,3 +161,35 @@ def test_shared_columns_as_rows(fk, edit, page, G, shared, rows):
 @pytest.mark.parametrize("page,G,lens,new", [(16, 4, [2000], [40]), (64, 2, [1500, 700], [20, 70]), (128, 1, [3000], [50])])
 def test_differential_prompts_as_rows(fk, edit, page, G, lens, new):
     run(fk, "attn_diff", torch.bfloat16, page, 2, G, lens, CASES[edit], new, width=60000)
+
+
+BOTH = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+
+
+@EVERY_NEAR
+@BOTH
+@pytest.mark.parametrize("call", ["attn", "attn_diff"])
+@pytest.mark.parametrize("page,G,lens", [(16, 4, [2000, 130]), (128, 1, [3000])])
+def test_decode_steps(fk, edit, dtype, call, page, G, lens):
+    run(fk, call, dtype, page, 2, G, lens, NEAR[edit])
+
+
+@EVERY_NEAR
+@BOTH
+@pytest.mark.parametrize("page,G,shared,rows", [(16, 8, 1600, 3), (128, 2, 384, 2)])
+def test_shared_columns_in_eights(fk, edit, dtype, page, G, shared, rows):
+    run(fk, "attn_shared", dtype, page, 2, G, [shared + 1 + i % 5 for i in range(rows)], NEAR[edit], shared=shared)
+
+
+@EVERY_NEAR
+@BOTH
+@pytest.mark.parametrize("call", ["attn", "attn_diff"])
+@pytest.mark.parametrize("page,G,lens,new", [(16, 2, [900, 40, 300], [2, 1, 1])])
+def test_new_tokens_in_eights(fk, edit, dtype, call, page, G, lens, new):
+    run(fk, call, dtype, page, 2, G, lens, NEAR[edit], new)
+
+
+@EVERY_NEAR
+@pytest.mark.parametrize("page,G,lens,new", [(16, 8, [900, 1300], [40, 7]), (128, 1, [700, 140], [200, 1])])
+def test_prompts_of_many_columns(fk, edit, page, G, lens, new):
+    run(fk, "attn", torch.bfloat16, page, 2, G, lens, NEAR[edit], new)
