@@ -13,9 +13,13 @@ AttnPlan plan_diff(const faedkv_pages *pg, int batch, int n_tokens) {
     const double tiles = ((double)n_tokens * gq / 8 + batch) * (double)p.max_tiles * pg->cfg.n_kv_heads;
     return tiles * 3.1 > 20000.0 ? plan_rows(pg, gq, batch, n_tokens) : plan_attn(pg, gq, batch, n_tokens, false);
 }
-size_t maps_at(const faedkv_pages *pg, int batch, int n_tokens) {   // where the maps' results lie in the workspace
+// The workspace: parts of split units, then the maps' results of whole ones, float32 by token and head.  The form with rows (more tokens than sequences, so
+// never a decode step) has none of those: it finishes whole units where they are attended.
+struct DiffBytes { size_t parts, maps; };
+DiffBytes diff_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
     const AttnPlan p = plan_diff(pg, batch, n_tokens), q = plan_attn(pg, 2 * pg->gq, batch, n_tokens);
-    return ((n_tokens == batch && q.bytes0 > p.bytes1 ? q.bytes0 : p.bytes1) + 15) / 16 * 16;
+    return {((n_tokens == batch && q.bytes0 > p.bytes1 ? q.bytes0 : p.bytes1) + 15) / 16 * 16,
+            p.wide ? 0 : sizeof(float) * 2 * kHeadDim * (size_t)n_tokens * pg->cfg.n_q_heads};
 }
 
 }  // namespace
@@ -25,7 +29,8 @@ extern "C" {
 size_t faedkv_pages_attn_diff_bytes(const faedkv_pages *pg, int batch, int n_tokens) {
     if (pg == nullptr || pg->gq > 4 || batch < 1 || batch > pg->cfg.max_batch || n_tokens < 0) return 0;
     if ((long long)n_tokens + batch > (1LL << 30)) return 0;
-    return maps_at(pg, batch, n_tokens) + sizeof(float) * 2 * kHeadDim * (size_t)n_tokens * pg->cfg.n_q_heads;
+    const DiffBytes b = diff_bytes(pg, batch, n_tokens);
+    return b.parts + b.maps;
 }
 
 int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *q_start, int n_tokens, int batch,
@@ -60,7 +65,8 @@ int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, cons
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const int gq = 2 * pg->gq;
     const AttnPlan p = q_start == nullptr ? plan_attn(pg, gq, batch, n_tokens) : plan_diff(pg, batch, n_tokens);
-    float *maps = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + maps_at(pg, batch, n_tokens));
+    const DiffBytes b = diff_bytes(pg, batch, n_tokens);
+    float *maps = b.maps == 0 ? nullptr : reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + b.parts);
     const pages::AttnArgs a{q, maps, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, gq, c.max_pages,
                             c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)gq + 1u, scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};

@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(256) k_page_diff_join(const AttnArgs a, const 
     if (!FAEDKV_IN_BOUNDS(kTagPageAttn, cta0 >= 0 && cta1 < ctas && tok >= 0 && tok < a.n_tokens && h >= 0 && h < a.H)) return;
     const size_t row = ((size_t)tok * a.H + h) * heads + g;
     float4 a1, a2;
-    if (cta0 == cta1) {                                    // one CTA had it all
+    if (MODE == 0 && cta0 == cta1) {                       // one CTA had it all
         const float *x = diff.maps + row * 2 * kHeadDim + 4 * lane;
         a1 = load4(x);
         a2 = load4(x + kHeadDim);

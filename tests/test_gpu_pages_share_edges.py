@@ -5,7 +5,8 @@ import pytest
 import torch
 
 import pages_ref as ref
-from test_gpu_pages_diff import expect
+from helpers import Guarded
+from test_gpu_pages_diff import case as diff_case, expect
 from test_gpu_pages_shared import case as shared_case
 
 pytestmark = pytest.mark.gpu
@@ -113,3 +114,26 @@ def test_the_norm_of_heads_whose_squares_are_beyond_float32(fk, dtype, exponent,
     if dtype == torch.bfloat16:
         diff_call(fk, dtype, 64, 2, 2, [700, 300], [100, 20], edit, True, eps, width=60000)    # columns as rows, two row tiles and one
         diff_call(fk, dtype, 64, 1, 4, [5000], [10], edit, True, eps, width=20000)             # split, one row tile
+
+
+def test_workspace_of_a_long_differential_prompt(fk):
+    """The form with rows keeps no maps: its workspace does not grow with the tokens, and no byte behind it is touched."""
+    pg = fk.Pages(n_kv_heads=8, n_q_heads=32, page_size=64, n_pages=4096, max_pages=2048, max_batch=4)
+    parts = 148 * 2 * 256 * 130 * 4                            # two partial results of 256 columns a CTA
+    assert all(0 < pg.attn_diff_bytes(b, n) <= parts + (1 << 20) for b in (1, 4) for n in (100, 1000, 32768, 131072))
+    for b, n in ((4, 4), (4, 2), (1, 1)):                      # eight columns at a time: a float32 row for each token, head and map
+        assert pg.attn_diff_bytes(b, n) >= n * 32 * 2 * 128 * 4
+
+
+@pytest.mark.parametrize("dtype,lens,new,width", [
+    (torch.bfloat16, [700, 300], [100, 20], 60000), (torch.bfloat16, [9, 30], [7, 9], 1), (torch.bfloat16, [1200] * 30, [40] * 30, 60000),
+    (torch.float32, [700, 300], [100, 20], 1), (torch.bfloat16, [700, 300], None, 1),
+])
+def test_differential_calls_stay_within_their_workspace(fk, dtype, lens, new, width):
+    pg, args, kw, out = diff_case(fk, dtype, 16, 1, 2, lens, new, width=width)
+    ws = Guarded((pg.attn_diff_bytes(len(lens), out.shape[0]),), torch.uint8, 255)
+    want = out.clone()
+    out.fill_(7.0)
+    pg.attn_diff(*args, **kw, ws=ws.t)
+    ws.check("the workspace")
+    assert torch.equal(out, want) and pg.device_status() == 0
