@@ -563,6 +563,10 @@ int faedkv_pages_reset_device_status(faedkv_pages *pg, void *stream);
  * output of such a call is invalid. */
 int faedkv_pages_test_hooks(faedkv_pages *pg, unsigned long long wait_limit_ns, int withhold_tile);
 
+/* Test hook of release and compact: most = 8 lets them use clusters of at most eight CTAs, as they do by themselves where the device (a
+ * partition of one) has no room for sixteen; 0 = ask the device again. */
+int faedkv_pages_test_cluster(faedkv_pages *pg, int most);
+
 /* faedkv_debug_word() for the kernels of the paged cache. */
 long long faedkv_pages_debug_word(faedkv_pages *pg, void *stream);
 

@@ -39,7 +39,7 @@ EXPORTS = [
     "faedkv_pages_compact", "faedkv_pages_store", "faedkv_pages_attn_bytes", "faedkv_pages_attn", "faedkv_pages_attn_diff_bytes", "faedkv_pages_attn_diff",
     "faedkv_pages_attn_shared_bytes", "faedkv_pages_attn_shared",
     "faedkv_pages_load", "faedkv_pages_device_status",
-    "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_debug_word",
+    "faedkv_pages_reset_device_status", "faedkv_pages_launch_count", "faedkv_pages_test_hooks", "faedkv_pages_test_cluster", "faedkv_pages_debug_word",
 ]
 
 STATIC_SCRATCH_BYTES = 8 << 20
@@ -188,6 +188,8 @@ def load() -> ctypes.CDLL:
     lib.faedkv_pages_reset_device_status.restype = _int
     lib.faedkv_pages_test_hooks.argtypes = [_vp, ctypes.c_ulonglong, _int]
     lib.faedkv_pages_test_hooks.restype = _int
+    lib.faedkv_pages_test_cluster.argtypes = [_vp, _int]
+    lib.faedkv_pages_test_cluster.restype = _int
     lib.faedkv_pages_debug_word.argtypes = [_vp, _vp]
     lib.faedkv_pages_debug_word.restype = _ll
     lib.faedkv_pages_launch_count.argtypes = [_vp]
@@ -727,6 +729,10 @@ class Pages:
     def test_hooks(self, wait_limit_ns: int = 0, withhold_tile: int = 0):
         """faedkv_pages_test_hooks: wait limit of the attention's bounded waits and the withheld-signal test."""
         self._check(self._lib.faedkv_pages_test_hooks(self._h, int(wait_limit_ns), int(withhold_tile)))
+
+    def test_cluster(self, most: int = 0):
+        """faedkv_pages_test_cluster: release and compact with clusters of eight CTAs."""
+        self._check(self._lib.faedkv_pages_test_cluster(self._h, int(most)))
 
     def debug_word(self, stream=None) -> int:
         return int(self._lib.faedkv_pages_debug_word(self._h, self._on(stream)))

@@ -33,6 +33,33 @@ int launch_cluster(faedkv_pages *pg, const char *what, void (*kernel)(Args...), 
     return launch_check(pg, what);
 }
 
+// CTAs of the largest cluster that the device can hold: a partition of one may have no sixteen SMs that reach one another.  Asked once a handle.
+int cluster_most(faedkv_pages *pg) {
+    if (pg->cluster_most == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(pages::kCluster);
+        cfg.blockDim = dim3(pages::kPlanThreads);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = pages::kCluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        pg->cluster_most = pages::kCluster;
+        auto room_for = [&](auto kernel) {
+            int n = 0;
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                   cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
+        };
+        if (!room_for(pages::k_page_release<pages::kCluster>) || !room_for(pages::k_page_release_short<4>) ||
+            !room_for(pages::k_page_compact_plan<pages::kCluster>)) {
+            cudaGetLastError();                            // an answer, not an error of the call
+            pg->cluster_most = pages::kClusterAnywhere;
+        }
+    }
+    return pg->cluster_most;
+}
+
 // Up to this many forks and rows the CTAs that copy find out for themselves what comes before them: the marks fit shared memory.
 bool forks_alone(int batch, int n_forks) { return n_forks <= pages::kForkSmall && batch <= pages::kForkRows; }
 
@@ -101,10 +128,12 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     const pages::ReleaseArgs a{t_len, n_new, table, n_free, free_pages, kv_len, n_free_out, static_cast<int32_t *>(ws), batch,
                                pg->cfg.max_pages, pg->cfg.n_pages, pg->page_shift, pg->dev_status};
     // parts of a row, a warp each: more than one where there are fewer rows than warps, or where that makes them short enough for registers
-    const int warps = pages::kPlanThreads / 32, most = pages::kCluster * warps;
-    int parts = 1, ctas = pages::kCluster;
+    const int warps = pages::kPlanThreads / 32, widest = cluster_most(pg), most = widest * warps;
+    int parts = 1, ctas = widest;
     while (parts < 32 && pg->cfg.max_pages > 256 * parts) parts *= 2;
-    const bool in_registers = pg->cfg.max_pages <= 256 * parts && parts * batch <= 4 * most && pg->cfg.n_pages <= pages::kReleaseShort;
+    // (two and four runs a warp by the full cluster only)
+    const bool in_registers = pg->cfg.max_pages <= 256 * parts && parts * batch <= (widest == pages::kCluster ? 4 * most : most) &&
+                              pg->cfg.n_pages <= pages::kReleaseShort;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (in_registers)                                      // as few CTAs as have the warps: a larger cluster takes longer to begin and to meet
         while (ctas > 1 && parts * batch <= ctas / 2 * warps) ctas /= 2;
@@ -115,7 +144,8 @@ int faedkv_pages_release(faedkv_pages *pg, const int32_t *t_len, const int32_t *
     return each == 1   ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<1>, 22, ctas, st, a, parts)
            : each == 2 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<2>, 23, ctas, st, a, parts)
            : each == 4 ? launch_cluster(pg, "k_page_release_short", pages::k_page_release_short<4>, 24, ctas, st, a, parts)
-                       : launch_cluster(pg, "k_page_release", pages::k_page_release, 25, ctas, st, a, parts);
+           : widest == pages::kCluster ? launch_cluster(pg, "k_page_release", pages::k_page_release<pages::kCluster>, 25, ctas, st, a, parts)
+                                       : launch_cluster(pg, "k_page_release", pages::k_page_release<pages::kClusterAnywhere>, 27, ctas, st, a, parts);
 }
 
 size_t faedkv_pages_compact_bytes(const faedkv_pages *pg) {
@@ -142,7 +172,9 @@ int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, con
     if (c.n_pages <= pages::kCompactShort && (long long)batch * c.max_pages <= 16 * pages::kCompactShort) {
         pages::k_page_compact_short<<<1, pages::kPlanThreads, 0, st>>>(a);
         if (int r = launch_check(pg, "k_page_compact_short")) return r;
-    } else if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan, 26, pages::kCluster, st, a)) {
+    } else if (cluster_most(pg) == pages::kCluster) {
+        if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan<pages::kCluster>, 26, pages::kCluster, st, a)) return r;
+    } else if (int r = launch_cluster(pg, "k_page_compact_plan", pages::k_page_compact_plan<pages::kClusterAnywhere>, 28, pages::kClusterAnywhere, st, a)) {
         return r;
     }
     CUDA_TRY(pg, launch_pdl(pages::k_page_move, dim3(pg->n_sm * 8), dim3(256), 0, st, a));
@@ -150,6 +182,12 @@ int faedkv_pages_compact(faedkv_pages *pg, const int32_t *kv_len, int batch, con
 }
 
 }  // extern "C"
+
+extern "C" int faedkv_pages_test_cluster(faedkv_pages *pg, int most) {
+    if (pg == nullptr || (most != 0 && most != pages::kClusterAnywhere)) return FAEDKV_ERR_INVALID_ARG;
+    pg->cluster_most = most;
+    return FAEDKV_OK;
+}
 
 // The checked build's word of this file's kernels (each translation unit has one).
 long long pages_share_debug_word(faedkv_pages *pg) { return debug_word_here(pg); }

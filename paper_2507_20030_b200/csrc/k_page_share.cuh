@@ -12,7 +12,8 @@ namespace faedkv {
 namespace pages {
 
 constexpr unsigned int kBadRow = 0x106;                   // a row of the block table that there is not, or that may not be written
-constexpr int kCluster = 16;                              // CTAs that meet in one launch: the most there are
+constexpr int kCluster = 16;                              // CTAs that meet in one launch: the most there are,
+constexpr int kClusterAnywhere = 8;                       // and what every GPU or part of one has room for
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -356,12 +357,11 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release_short(cons
     if (tid == 0 && rank == 0) *a.n_free_out = (int)min(all, (long long)a.n_pages);   // (n_free_out may be n_free: all have read it)
 }
 
-constexpr int kReleaseItems = 65536 / kCluster;           // items of a CTA: one warp's part of a row
-
-// Any number of rows and pages: the runs are read again in every phase.
+// Any number of rows and pages, by a cluster of CTAS: the runs are read again in every phase.
+template <int CTAS>
 static __global__ void __launch_bounds__(kPlanThreads) k_page_release(const ReleaseArgs a, const int parts) {
     __shared__ long long warp_sums[32];
-    __shared__ int32_t count[kReleaseItems];
+    __shared__ int32_t count[65536 / CTAS];                // items of a CTA: one warp's part of a row
     constexpr int kWarps = kPlanThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
     const long long cap = (long long)a.W << a.page_shift;
@@ -369,7 +369,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release(const Rele
     const int height = height_of(a.n_free, a.n_pages, a.status, tid == 0 && rank == 0);
     int32_t *totals = a.ws + a.n_pages;
     // items of this CTA: consecutive, so that the pages it pushes are too
-    const int n_items = a.B * parts, each = (n_items + kCluster - 1) / kCluster;
+    const int n_items = a.B * parts, each = (n_items + CTAS - 1) / CTAS;
     const int item0 = min(n_items, rank * each), item1 = min(n_items, item0 + each);
     // f(entry, page) for the pages of an item
     auto entries = [&](int item, auto f) {
@@ -436,7 +436,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release(const Rele
     if (tid == 0) totals[rank] = base;
     cluster_sync();
     long long at0 = height, all = height;
-    for (int r = 0; r < kCluster; ++r) {
+    for (int r = 0; r < CTAS; ++r) {
         const int n = __ldcg(totals + r);
         if (r < rank) at0 += n;
         all += n;
@@ -461,7 +461,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_release(const Rele
         });
     }
     cluster_sync();                                       // kv_len may be t_len, n_free_out may be n_free
-    for (int b = rank * kPlanThreads + tid; b < a.B; b += kCluster * kPlanThreads) a.kv_len[b] = a.n_new[b] < 0 ? 0 : a.t_len[b];
+    for (int b = rank * kPlanThreads + tid; b < a.B; b += CTAS * kPlanThreads) a.kv_len[b] = a.n_new[b] < 0 ? 0 : a.t_len[b];
     if (tid == 0 && rank == 0) *a.n_free_out = (int)min(all, (long long)a.n_pages);
 }
 
@@ -479,11 +479,12 @@ constexpr int kCompactHead = 64;                          // counts: live pages 
 
 // One cluster: which pages are in use, and where each goes.  With n of them, the pages in use from n on go to the pages below n
 // that are not, both in ascending order: the fewest moves, and no page is read and written.
+template <int CTAS>
 static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_plan(const CompactArgs a) {
     __shared__ long long warp_sums[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster_rank();
     const long long cap = (long long)a.W << a.page_shift;
-    const int page = 1 << a.page_shift, all = kCluster * kPlanThreads, me = rank * kPlanThreads + tid;
+    const int page = 1 << a.page_shift, all = CTAS * kPlanThreads, me = rank * kPlanThreads + tid;
     int32_t *holes = a.ws + kCompactHead, *moves = holes + a.n_pages / 2;
     for (int p = me; p < a.n_pages; p += all) a.new_id[p] = -1;
     cluster_sync();
@@ -505,7 +506,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_plan(const
     }
     cluster_sync();
     // consecutive pages of a CTA, of a thread
-    const int each = ((a.n_pages + kCluster - 1) / kCluster + kPlanThreads - 1) / kPlanThreads;
+    const int each = ((a.n_pages + CTAS - 1) / CTAS + kPlanThreads - 1) / kPlanThreads;
     const long long lo = (long long)me * each;
     const int p0 = (int)min(lo, (long long)a.n_pages), p1 = (int)min(lo + each, (long long)a.n_pages);
     int live = 0;
@@ -515,7 +516,7 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_plan(const
     if (tid == 0) a.ws[rank] = (int)total;
     cluster_sync();
     int n = 0;
-    for (int r = 0; r < kCluster; ++r) n += __ldcg(a.ws + r);
+    for (int r = 0; r < CTAS; ++r) n += __ldcg(a.ws + r);
     long long mine = 0;                                   // holes, and pages that move in the upper half
     for (int p = p0; p < p1; ++p) {
         const bool used = __ldcg(a.new_id + p) == 0;
@@ -524,15 +525,15 @@ static __global__ void __launch_bounds__(kPlanThreads) k_page_compact_plan(const
     }
     const long long upto = block_scan(mine, warp_sums, &total);
     if (tid == 0) {
-        a.ws[kCluster + rank] = (int)(total & 0xffffffffLL);
-        a.ws[2 * kCluster + rank] = (int)(total >> 32);
+        a.ws[CTAS + rank] = (int)(total & 0xffffffffLL);
+        a.ws[2 * CTAS + rank] = (int)(total >> 32);
     }
     cluster_sync();
     long long at = upto - mine;
     int n_moves = 0;
-    for (int r = 0; r < kCluster; ++r) {
-        const int m = __ldcg(a.ws + 2 * kCluster + r);
-        if (r < rank) at += (long long)__ldcg(a.ws + kCluster + r) + ((long long)m << 32);
+    for (int r = 0; r < CTAS; ++r) {
+        const int m = __ldcg(a.ws + 2 * CTAS + r);
+        if (r < rank) at += (long long)__ldcg(a.ws + CTAS + r) + ((long long)m << 32);
         n_moves += m;
     }
     for (int p = p0; p < p1; ++p) {

@@ -23,6 +23,7 @@ struct faedkv_pages {
     unsigned long long launches = 0;
     unsigned long long wait_limit_ns = umma::kWaitLimitNs;   // faedkv_pages_test_hooks
     int withhold_tile = 0;
+    int cluster_most = 0;                      // CTAs of the largest cluster there is room for; 0: not asked yet
     char err[512] = {0};
 };
 

@@ -1,10 +1,13 @@
 """Shared pages and differential attention at the edges of what their calls accept: starts that are any int32, steps without
 forks, every wrong table entry."""
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
 
 import pages_ref as ref
+import test_gpu_pages_share as share_tests
 from helpers import Guarded
 from test_gpu_pages_diff import case as diff_case, expect
 from test_gpu_pages_shared import case as shared_case
@@ -137,3 +140,42 @@ def test_differential_calls_stay_within_their_workspace(fk, dtype, lens, new, wi
     pg.attn_diff(*args, **kw, ws=ws.t)
     ws.check("the workspace")
     assert torch.equal(out, want) and pg.device_status() == 0
+
+
+@pytest.fixture()
+def partition(fk):
+    """Handles as on a part of a GPU that has no room for clusters of sixteen CTAs."""
+    def pages(**kw):
+        pg = fk.Pages(**kw)
+        pg.test_cluster(8)
+        return pg
+    return SimpleNamespace(Pages=pages, BF16=fk.BF16, F32=fk.F32)
+
+
+@pytest.mark.parametrize("page,W,B,n_pages", [(16, 30, 7, 200), (64, 9, 300, 1500), (64, 2, 256, 700), (64, 2, 257, 700), (16, 257, 200, 20000), (16, 2, 20000, 30000),
+                                              (16, 6000, 40, 9000), (16, 9, 30, 65537)])
+def test_release_by_clusters_of_eight(partition, page, W, B, n_pages):
+    share_tests.test_release(partition, page, W, B, n_pages)
+
+
+@pytest.mark.parametrize("H,page,W,B,n_pages", [(1, 16, 9, 6, 100), (1, 16, 50, 1500, 66000)])
+def test_compact_by_clusters_of_eight(partition, H, page, W, B, n_pages):
+    share_tests.test_compact(partition, H, page, W, B, n_pages)
+
+
+def test_what_room_a_gpu_has_is_asked_for_under_capture_too(fk):
+    pg = share_tests.make(fk, n_pages=70000, W=9, B=3)                 # the first call of the handle is a captured one
+    cache = pg.alloc()
+    t, n_new, table = ref.ints([20, 40, 3]), ref.ints([1, -1, 0]), ref.ints(np.arange(27).reshape(3, 9) + 60000)
+    free, nf, new_id = ref.ints(np.zeros(70000)), ref.ints([5]), ref.ints(np.zeros(70000))
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (pg._bytes("faedkv_pages_release_bytes"), pg._bytes("faedkv_pages_compact_bytes"))]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pg.release(t, n_new, table, free, nf, t, nf, ws=ws[0])
+        pg.compact(t, table, table, free, nf, new_id, *cache, ws=ws[1])
+    assert nf.tolist() == [5]
+    graph.replay()
+    assert nf.tolist() == [70000 - 3] and t.tolist() == [20, 0, 3] and table[0, :2].tolist() == [0, 1] and table[2, 0].item() == 2
+    for bad in (-1, 1, 7, 9, 16):
+        with pytest.raises(fk.FaedkvError):
+            pg.test_cluster(bad)
