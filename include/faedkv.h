@@ -478,8 +478,10 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
  * pages, as faedkv_pages_fork() leaves them; of those, whole pages count.  They are read once for a block of the group's query heads, through
  * the table row of the first row of the block that has them all; what a row holds behind them is read for itself.  A row that holds less
  * than its group shares is attended alone, as is the only row of a group and one that stands in no group or in one whose bounds
- * are not rows of the batch (status 0x105).  q, out, scale and results as faedkv_pages_attn(), rounding as there (bf16: a softmax weight
- * is held to 2^-11 of itself and 2^-31 of its row's largest); the tables are not searched for other shared pages.
+ * are not rows of the batch (status 0x105).  q, out, scale and results as faedkv_pages_attn().  Rounding as there, but that a weight
+ * of a bf16 call, times its page's v_scale, is held to 2^-11 of itself and 2^-31 of its row's largest, as for many query columns there: which blocks
+ * take the form for many goes by the batch, the groups and the width of the table (in the other one they keep 2^-12 and 2^-34).  The tables
+ * are not searched for other shared pages.  One new token a row; steps of several go to faedkv_pages_attn(), which reads what rows share once for each.
  * ws: faedkv_pages_attn_shared_bytes() (0 for arguments that the call would refuse), 16-byte aligned, overwritten. */
 size_t faedkv_pages_attn_shared_bytes(const faedkv_pages *pg, int batch, int n_groups);
 int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, const int32_t *group_start, const int32_t *shared_len,

@@ -172,7 +172,7 @@ int faedkv_pages_attn(faedkv_pages *pg, const void *q, long long ld_q, const int
     const AttnPlan p = plan_attn(pg, pg->gq, batch, n_tokens);
     const pages::AttnArgs a{q, out, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, pg->gq,
                             c.max_pages, c.n_pages, pg->page_shift, p.blocks,
-                            65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
+                            pages::inverse_g(pg->gq), scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
     return dispatch_attn<0>(pg, mk, mv, a, p, 0, st);
 }

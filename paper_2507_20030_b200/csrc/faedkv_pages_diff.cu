@@ -68,7 +68,7 @@ int faedkv_pages_attn_diff(faedkv_pages *pg, const void *q, long long ld_q, cons
     const DiffBytes b = diff_bytes(pg, batch, n_tokens);
     float *maps = b.maps == 0 ? nullptr : reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + b.parts);
     const pages::AttnArgs a{q, maps, q_start, kv_len, table, k_scale, v_scale, ld_q, n_tokens, batch, c.n_kv_heads, gq, c.max_pages,
-                            c.n_pages, pg->page_shift, p.blocks, 65536u / (unsigned)gq + 1u, scale * 1.44269504088896341f,
+                            c.n_pages, pg->page_shift, p.blocks, pages::inverse_g(gq), scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile};
     const pages::DiffArgs d{maps, lam, gain, out, q_start, n_tokens, batch, c.n_q_heads, eps};
     if (p.wide && q_start != nullptr) {                    // whole units are finished where they are attended

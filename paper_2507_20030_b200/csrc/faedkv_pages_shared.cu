@@ -23,7 +23,7 @@ SharedPlan plan_shared(const faedkv_pages *pg, int batch, int n_groups) {
     // 10 us once.  (8 kv heads x 4 query heads, 60 tokens behind, us in eights and with rows: one group of 16 rows over 8192 tokens 31 and 35, over 16384 43
     // and 39; of 32 rows over 2048 28 and 33, over 4096 35.5 and 34.4; of 64 rows over 1024 36 and 40, over 2048 44 and 42, over 32768 218 and 81; four groups
     // of 8 rows over 8192 48 and 52, of 16 79 and 60.)  The host knows the tables' width, not the lengths: where they are far apart the second launch is
-    // taken too early, which costs those 10 us at most.
+    // taken too early, which costs those 10 us at most (8 rows behind 2048 tokens, their table as wide or for 131072: 16.8 and 23.3 us).
     const long long max_tiles = ((long long)c.max_pages * c.page_size + pages::kTile - 1) / pages::kTile;
     const double cols = (double)batch * pg->gq / n_groups, group_tiles = (double)max_tiles * c.n_kv_heads * n_groups;
     const double saved = group_tiles * (0.39 * cols - (cols <= 128 ? 10.7 : 0.086 * cols));
@@ -118,7 +118,7 @@ int faedkv_pages_attn_shared(faedkv_pages *pg, const void *q, long long ld_q, co
     if (int r = make_map(pg, &mv, v_pages)) return r;
     const SharedPlan p = plan_shared(pg, batch, n_groups);
     const pages::AttnArgs a{q, out, nullptr, kv_len, table, k_scale, v_scale, ld_q, batch, batch, c.n_kv_heads, pg->gq, c.max_pages,
-                            c.n_pages, pg->page_shift, 0, 65536u / (unsigned)pg->gq + 1u, scale * 1.44269504088896341f,
+                            c.n_pages, pg->page_shift, 0, pages::inverse_g(pg->gq), scale * 1.44269504088896341f,
                             static_cast<unsigned char *>(ws), pg->dev_status, pg->wait_limit_ns, pg->withhold_tile, group_start, shared_len,
                             n_groups, 0, nullptr, nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -100,7 +100,7 @@ struct AttnArgs {
     const float *ks, *vs;
     long long ld_q;
     int n_tokens, B, H, G, W, n_pages, page_shift, blocks;
-    uint32_t inv_g;                                       // c * inv_g >> 16 = c / G for the columns c < 128
+    uint32_t inv_g;                                       // c * inv_g >> 16 = c / G for the columns c < 256, G <= 8
     float scale_log2;                                     // scale * log2(e)
     unsigned char *ws;
     unsigned int *status;
@@ -112,6 +112,15 @@ struct AttnArgs {
     int n_groups, which;
     float *whole, *slots;
 };
+
+constexpr uint32_t inverse_g(int g) { return 65536u / (unsigned)g + 1u; }
+constexpr bool divides_columns() {
+    for (int g = 1; g <= 8; ++g)
+        for (uint32_t c = 0; c < 256; ++c)
+            if ((c * inverse_g(g) >> 16) != c / (unsigned)g) return false;
+    return true;
+}
+static_assert(divides_columns(), "inv_g");
 
 // Workspace of MODE 0 and 1: header, records, two partial results per CTA (of the unit it goes on with, of the one it leaves).
 struct UnitMeta { long long first; int tiles, pad; };                             // MODE 0, by unit

@@ -5,7 +5,7 @@
 // norm(o) = o * gain / sqrt(mean(o^2) + eps) over the head's 128 channels, or o itself without a gain.  k_page_attn and k_page_rows compute the a_m as
 // columns (rows) of one pass over the cache: the codes of K and V are read once for both maps of all heads, and a map's query is zero in the other's
 // channels, so that one product over 128 channels gives either score; half of its multiplications are with zero, which costs a decode step nothing (16 x
-// 16384 tokens, 8 kv heads: 89 us, the bytes alone 82) and a prompt a quarter of its products.
+// 16384 tokens, 8 kv heads: 89 to 93 us, the bytes alone 82) and a prompt a quarter of its products.
 #pragma once
 #include "k_page_rows.cuh"
 

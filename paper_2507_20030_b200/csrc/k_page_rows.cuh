@@ -21,9 +21,9 @@
 // warpgroup, and the two results meet as parts of a softmax do.  Four warps convert V; a TMA warp; one warp issues the first product and one
 // the second, since what an issuer waits for between products would leave the tensor cores idle.
 //
-// What bounds it is the two softmax warps of a scheduler: a half tile of both takes them some 2500 cycles, of which the exponentials are 1024 and the
+// What bounds it is the two softmax warps of a scheduler: a half tile of both takes them some 2200 cycles, of which the exponentials are 1024 and the
 // tensor cores' products as many; the rest is what a warp waits for between its steps (loads from tensor memory, its turn, stores), and registers leave
-// no room for a third.  1024 + 1 + 333 new tokens over 9216 + 4001 + 333, 8 kv x 16 differential heads: 190 us, 0.35 of the tensor cores' measured rate
+// no room for a third.  1024 + 1 + 333 new tokens over 9216 + 4001 + 333, 8 kv x 16 differential heads: 190 to 195 us, 0.35 of the tensor cores' measured rate
 // (303 in k_page_attn's form with 128 columns).
 #pragma once
 #include "k_page_attn.cuh"

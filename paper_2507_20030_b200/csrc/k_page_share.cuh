@@ -48,7 +48,7 @@ struct ForkArgs {
     unsigned int *status;
 };
 
-// Tokens that fork i takes: none where it is refused (valid becomes false).
+// Tokens that fork i takes from row s: the row's length, cut to what the table holds and to len[i].  (Whether a fork is refused is its callers' to say.)
 __device__ __forceinline__ int fork_length(const ForkArgs &a, int i, int s, bool report) {
     const long long cap = (long long)a.W << a.page_shift;
     const int t = a.kv_len[s];
@@ -241,7 +241,7 @@ struct ReleaseArgs {
 // Short: every warp has K runs of up to 256 pages at most and keeps them in registers from the first load to the last store, and the pages that running
 // requests name are bits in shared memory, each CTA's own first, then all of them.  What bounds it is the chain: lengths, entries, three meetings of the
 // cluster, the stack.  (512 requests of up to 256 pages: 34 us with each row read in every phase and eight CTAs; 25 with the entries in registers and the
-// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  32 rows: 8.6 us with sixteen CTAs, 5.4
+// running requests' pages as atomics to global memory, 22 as bits, 18 with sixteen CTAs.  32 rows: 8.6 us with sixteen CTAs, 6.5
 // with one.)
 constexpr int kReleaseShort = 65536;                      // pages
 __device__ __forceinline__ uint32_t load_of_cta(const uint32_t *p, int cta) {        // what p is in another CTA of the cluster

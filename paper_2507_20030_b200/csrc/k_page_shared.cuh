@@ -4,8 +4,8 @@
 // shared page once, and k_page_attn each row alone over the tokens behind.  The two results of a query row, each in parts where it was split over
 // CTAs, meet here as parts of any softmax do: out = sum_i l_i 2^(m_i - m) o_i / sum_i l_i 2^(m_i - m), m the largest m_i.
 //
-// Measured, 8 kv x 32 query heads: 64 rows behind 32768 common tokens and 512 of their own 88 us (read by each row for itself they are 64 times the bytes;
-// the shared pages, the tails and the products each take 20 us at full rate), 8 rows behind 2048 16.5 us, mostly start, join and its launch.
+// Measured, 8 kv x 32 query heads: 64 rows behind 32768 common tokens and up to 512 of their own 87 us (409 read by each row for itself; at full rate the
+// shared pages take 10 us, the tails 5 and the products 20), 8 rows behind 2048 16.8 us (17.8), mostly start, join and its launch.
 #pragma once
 #include "k_page_rows.cuh"
 
